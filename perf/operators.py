@@ -93,12 +93,13 @@ def _blocks(n):
 
 
 def _quantize(x, nc):
-    """x: binary32 (..., n) -> codes (nc, ..., 16 G), scales (nc, ..., G).  The scale of a
-    block is 2^(floor(log2 of its largest magnitude) - 2), at least 2^-127; the elements are
-    rounded to nearest, ties to even, at most 6."""
-    n = x.shape[-1]
-    groups = _blocks(n)
-    r = torch.nn.functional.pad(x, (0, groups * BLOCK - n)).reshape(*x.shape[:-1], groups, BLOCK)
+    """x: binary32 (rows, n) -> codes (nc, rows, 64 G), scales (nc, G, rows, 4), G groups of
+    four blocks covering a row, zeros past its end.  The scale of a block is 2^(floor(log2 of
+    its largest magnitude) - 2), at least 2^-127; the elements are rounded to nearest, ties
+    to even, at most 6."""
+    rows, n = x.shape
+    groups = (n + 4 * BLOCK - 1) // (4 * BLOCK)
+    r = torch.nn.functional.pad(x, (0, groups * 4 * BLOCK - n)).reshape(rows, groups * 4, BLOCK)
     codes, scales = [], []
     for _ in range(nc):
         _, e = torch.frexp(r.abs().amax(-1, keepdim=True))
@@ -108,8 +109,8 @@ def _quantize(x, nc):
         code = ((a > 0.25).int() + (a >= 0.75).int() + (a > 1.25).int() + (a >= 1.75).int() + (a > 2.5).int()
                 + (a >= 3.5).int() + (a > 5.0).int()) + 8 * (y < 0).int()
         pairs = code.reshape(*code.shape[:-1], BLOCK // 2, 2)
-        codes.append((pairs[..., 0] + 16 * pairs[..., 1]).to(torch.uint8).flatten(-2))
-        scales.append((top + 127).to(torch.uint8).squeeze(-1))
+        codes.append((pairs[..., 0] + 16 * pairs[..., 1]).to(torch.uint8).reshape(rows, 64 * groups))
+        scales.append((top + 127).to(torch.uint8).reshape(rows, groups, 4).transpose(0, 1).contiguous())
         r = r - _values(code) * _power(top)
     return torch.stack(codes), torch.stack(scales)
 
@@ -125,12 +126,12 @@ def _values(code):
 
 
 def _dequantize(codes, scales, n):
-    """Binary32 values (..., n): the sum of the components, the smallest first."""
+    """Binary32 values (rows, n): the sum of the components, the smallest first."""
     total = None
     for c, s in zip(reversed(codes.unbind(0)), reversed(scales.unbind(0))):
-        c = c.int()
+        c, s = c.int(), s.transpose(0, 1).int()
         v = _values(torch.stack((c & 15, c >> 4), -1).flatten(-2).reshape(*s.shape, BLOCK))
-        v = (v * _power(s.int() - 127).unsqueeze(-1)).flatten(-2)[..., :n]
+        v = (v * _power(s - 127).unsqueeze(-1)).flatten(1)[:, :n]
         total = v if total is None else total + v
     return total
 
@@ -317,7 +318,8 @@ def _decode64(codes, scales, n):
     expo, mant = (nibble % 8) // 2, (nibble % 2).double()
     mag = torch.where(expo == 0, 0.5 * mant, (1.0 + 0.5 * mant) * 2.0 ** (expo - 1).double())
     mag = torch.where(nibble >= 8, -mag, mag)
-    return (mag * (2.0 ** (scales.double() - 127.0)).repeat_interleave(BLOCK, -1)).sum(0)[..., :n]
+    unit = (2.0 ** (scales.permute(0, 2, 1, 3).double() - 127.0)).flatten(2).repeat_interleave(BLOCK, -1)
+    return (mag * unit).sum(0)[:, :n]
 
 
 def _round64(x, nc):
