@@ -12,8 +12,8 @@
  *   allocates nothing per call and keeps no state besides two static per-device
  *   arrays: a binary16 exponential table (128 KiB, built on the first mc_exp call on
  *   a device) and the 8 MiB scratch of mc_matmul_splitk_noalloc.  Calls that need
- *   scratch memory (mc_matmul_splitk, mc_matmul_exact, mc_linreg_gd_step) take a
- *   caller-owned workspace.
+ *   scratch memory (mc_matmul_splitk, mc_matmul_exact, mc_linreg_gd_step, the MXFP4
+ *   products, the distillation loss) take a caller-owned workspace.
  * Layout.  Dense, component-major ("planar"): component c of element i of an MC
  *   array of n elements is at element offset c*n + i.  A plain tensor is one plane.
  *   Matrices are row-major inside each plane.  The paper's interleaved layout
@@ -70,7 +70,9 @@
 extern "C" {
 #endif
 
-typedef enum { MCF_F16 = 0, MCF_F32 = 1, MCF_F64 = 2, MCF_F16S = 3 } mcf_dtype;
+/* MCF_BF16 (bfloat16) is taken by the mc_mx4_* and mc_distill_* calls alone; those take
+ * MCF_F16, MCF_BF16 and MCF_F32. */
+typedef enum { MCF_F16 = 0, MCF_F32 = 1, MCF_F64 = 2, MCF_F16S = 3, MCF_BF16 = 4 } mcf_dtype;
 
 typedef enum {
   MCF_OK = 0,
@@ -369,6 +371,107 @@ int mc_linreg_gd_step(int dtype, int nc, int64_t n, int64_t d, const void *X, co
 /* Workspace bytes mc_linreg_gd_step needs, or a negative mcf_status for arguments it
  * would reject. */
 int64_t mc_linreg_workspace(int dtype, int nc, int64_t n, int64_t d);
+
+/* ---------------------------------------------------------------------------------
+ * Microscaled 4-bit (MXFP4) tensors
+ *
+ * An MXFP4 number is an E2M1 element (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives)
+ * times the power of two of its block: 32 elements along a row share one E8M0 scale
+ * (byte s stands for 2^(s - 127), 255 for NaN).  An MXFP4 tensor of nc components is the
+ * sum of nc of them, each the rounding of what the components before it leave -- an MC
+ * value (Section 2) whose component format has 4 bits.  1 <= nc <= 4.
+ * Layout of a tensor of `rows` rows of n elements, G = ceil(n / 128) groups of four blocks:
+ *   codes:  [nc][rows][64 G] bytes, element i of a row in byte i / 2, the low half for even
+ *           i; zeros past n; 16-byte aligned.
+ *   scales: [nc][G][rows][4] bytes, block b of group q of row r at byte 4 (q rows + r) + b of
+ *           its component; zeros for blocks wholly past n; 4-byte aligned.
+ * Sums of the products are held in binary32; results are rounded once to the call's format.
+ * Non-finite inputs propagate by IEEE rules through the products of the single components
+ * and of the pieces an input is split into, so an infinite factor may give NaN where the
+ * product of the whole numbers would be infinite.
+ * Workspaces: device memory of at least the matching ..._workspace(...) bytes, 16-byte
+ * aligned, owned by the caller, not overlapping the other arguments; may be NULL when that
+ * size is 0; contents on entry do not matter; calls sharing one must not overlap in time.
+ * Too small or misaligned: MCF_E_ARG; NULL when needed: MCF_E_NULL.
+ */
+
+/* Quantisation.  The exact value v of an element (with nc_in > 1 the sum of its planes, in
+ * binary64 where binary32 does not hold it) is split into nc components: with a the largest
+ * magnitude of its block and X = max(floor(log2 a) - 2, -127), the component is v 2^-X
+ * rounded to nearest E2M1, ties to even, at most 6, times 2^X, and v minus it is the next
+ * component's value.  A block with an infinity or NaN gets the scale 255 and zero codes in
+ * every component.
+ * x: [nc_in][rows][n]; codes and scales as above.  rows ceil(n / 128) at most 2^34. */
+int mc_mx4_quantize(int dtype, int nc_in, int nc, int64_t rows, int64_t n, const void *x, void *codes, void *scales,
+                    void *stream);
+
+/* Reading back: out = the sum of the components in binary32, the last one first, rounded to
+ * the format.  out: [rows][n]. */
+int mc_mx4_dequantize(int dtype, int nc, int64_t rows, int64_t n, const void *codes, const void *scales, void *out,
+                      void *stream);
+
+/* C = A B^T of two MXFP4 tensors (a_nc and b_nc components) on the scaled matrix
+ * instructions.  A: M rows of K, B: N rows of K, C: [M][N] in the call's format.
+ * M <= 2^20, N <= 2^24, K <= 2^22. */
+int mc_mx4_matmul(int dtype, int64_t M, int64_t N, int64_t K, const void *a_codes, const void *a_scales, int a_nc,
+                  const void *b_codes, const void *b_scales, int b_nc, void *workspace, int64_t workspace_bytes,
+                  void *C, void *stream);
+int64_t mc_mx4_matmul_workspace(int dtype, int64_t M, int64_t N, int64_t K, int a_nc, int b_nc);
+
+/* Linear layer of a plain input with an MXFP4 weight: y = x W^T (+ b).
+ * x: [batch][in]; codes, scales: W, `out` rows of `in`, nc components; b: [out] or NULL;
+ * y: [batch][out].  batch <= 2^20, in <= 2^22, out <= 2^24. */
+int mc_mx4_linear_fwd(int dtype, int nc, int64_t batch, int64_t in, int64_t out, const void *x, const void *codes,
+                      const void *scales, const void *b, void *workspace, int64_t workspace_bytes, void *y,
+                      void *stream);
+int64_t mc_mx4_linear_fwd_workspace(int dtype, int nc, int64_t batch, int64_t in, int64_t out);
+
+/* Its gradients, given that of the loss with respect to y:
+ *   dX = dY W      [batch][in]
+ *   dW = dY^T x    [out][in]   the gradient with respect to the numbers W stands for, which
+ *                              a straight-through rule hands to the weight it was made from
+ *   db = sum_t dY  [out]
+ * dX, dW and db may each be NULL (not computed); codes and scales are needed for dX only, x
+ * for dW only.  dY: [batch][out].  batch, in, out <= 2^20. */
+int mc_mx4_linear_bwd(int dtype, int nc, int64_t batch, int64_t in, int64_t out, const void *x, const void *codes,
+                      const void *scales, const void *dY, void *dX, void *dW, void *db, void *workspace,
+                      int64_t workspace_bytes, void *stream);
+int64_t mc_mx4_linear_bwd_workspace(int dtype, int nc, int64_t batch, int64_t in, int64_t out);
+
+/* ---------------------------------------------------------------------------------
+ * Distillation from a teacher's top logits
+ *
+ * A row has the student's logits z_j, j < vocab, and up to k teacher entries (ids_i, t_i),
+ * in any order.  With p the softmax over the row's used entries of t_i / T and q the softmax
+ * over the row of z_j / T:
+ *   loss  = T^2 sum_i p_i (log p_i - log q_{ids_i})
+ *   dz_j  = g T (q_j - sum of the p_i with ids_i = j)       (g: the row's upstream gradient)
+ * An entry with ids_i outside [0, vocab) is unused; a row with no used entry, or with none
+ * above -inf, has loss 0 and gradient 0.  A logit of -inf has q_j = 0; a teacher entry with
+ * p_i > 0 there makes the loss +inf.  Statistics and sums are binary32.
+ * z: plain [rows][vocab], or (nc > 1) an MC value [nc][rows][vocab] whose planes are summed
+ *   in binary32, the last one first; its gradient is plain, that of the sum (Section 2.1).
+ * ids: int32 [rows][k]; t: [rows][k] in z's format; 0 <= k <= 1024 (may be NULL for k = 0).
+ * temperature: positive and finite.  loss: binary32 [rows].
+ * stats: binary32 [rows][2], the row's largest logit m and sum_j exp((z_j - m) / T).
+ * g: binary32 [rows], or NULL for ones.  dz: [rows][vocab] in z's format.
+ * No output may overlap an input or another output.  rows < 2^31, 1 <= vocab <= 2^30. */
+
+/* loss, and stats for the backward call (stats may be NULL).  workspace: at least
+ * mc_distill_workspace(rows, vocab) bytes, under the rules above. */
+int mc_distill_fwd(int dtype, int nc, int64_t rows, int64_t vocab, int64_t k, const void *z, const void *ids,
+                   const void *t, double temperature, void *workspace, int64_t workspace_bytes, void *loss,
+                   void *stats, void *stream);
+
+/* dz from the forward call's stats. */
+int mc_distill_bwd(int dtype, int nc, int64_t rows, int64_t vocab, int64_t k, const void *z, const void *ids,
+                   const void *t, double temperature, const void *stats, const void *g, void *dz, void *stream);
+
+/* Both in one pass over z, for a g that is known beforehand (1 / rows for a mean). */
+int mc_distill_fwd_bwd(int dtype, int nc, int64_t rows, int64_t vocab, int64_t k, const void *z, const void *ids,
+                       const void *t, double temperature, const void *g, void *workspace, int64_t workspace_bytes,
+                       void *loss, void *dz, void *stream);
+int64_t mc_distill_workspace(int64_t rows, int64_t vocab);
 
 /* Human-readable name of a status code (static storage). */
 const char *mc_status_str(int status);

@@ -24,12 +24,15 @@ __all__ = [
     "mc_matmul_batched", "mc_bmm", "mc_addmm", "matmul_mcn", "mc_mul_slow", "mc_square", "mc_matmul_pruned",
     "mc_matmul_exact", "mc_matmul_exact_workspace", "mc_linreg_workspace", "mc_linreg_gd_step",
     "mc_linear_fwd_exact", "mc_linear_bwd", "mc_linear_bwd_workspace", "lib", "LIB_PATH", "MCFError",
+    "mc_mx4_quantize", "mc_mx4_dequantize", "mc_mx4_matmul", "mc_mx4_matmul_workspace", "mc_mx4_linear_fwd",
+    "mc_mx4_linear_fwd_workspace", "mc_mx4_linear_bwd", "mc_mx4_linear_bwd_workspace", "mc_distill_fwd",
+    "mc_distill_bwd", "mc_distill_fwd_bwd", "mc_distill_workspace",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmcf.so")
 _lib = None
 
-MCF_F16, MCF_F32, MCF_F64, MCF_F16S = 0, 1, 2, 3
+MCF_F16, MCF_F32, MCF_F64, MCF_F16S, MCF_BF16 = 0, 1, 2, 3, 4
 
 
 class MCFError(RuntimeError):
@@ -91,6 +94,23 @@ def lib() -> ctypes.CDLL:
         L.mc_linear_bwd_workspace.argtypes = [ci, ci, i64, i64, i64]
         L.mc_linear_fwd.restype = ci
         L.mc_linear_fwd.argtypes = [ci, ci, i64, i64, i64, vp, vp, vp, vp, vp]
+        cd = ctypes.c_double
+        for name, args, res in (
+            ("mc_mx4_quantize", [ci, ci, ci, i64, i64, vp, vp, vp, vp], ci),
+            ("mc_mx4_dequantize", [ci, ci, i64, i64, vp, vp, vp, vp], ci),
+            ("mc_mx4_matmul", [ci, i64, i64, i64, vp, vp, ci, vp, vp, ci, vp, i64, vp, vp], ci),
+            ("mc_mx4_matmul_workspace", [ci, i64, i64, i64, ci, ci], i64),
+            ("mc_mx4_linear_fwd", [ci, ci, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp, vp], ci),
+            ("mc_mx4_linear_fwd_workspace", [ci, ci, i64, i64, i64], i64),
+            ("mc_mx4_linear_bwd", [ci, ci, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, i64, vp], ci),
+            ("mc_mx4_linear_bwd_workspace", [ci, ci, i64, i64, i64], i64),
+            ("mc_distill_fwd", [ci, ci, i64, i64, i64, vp, vp, vp, cd, vp, i64, vp, vp, vp], ci),
+            ("mc_distill_bwd", [ci, ci, i64, i64, i64, vp, vp, vp, cd, vp, vp, vp, vp], ci),
+            ("mc_distill_fwd_bwd", [ci, ci, i64, i64, i64, vp, vp, vp, cd, vp, vp, i64, vp, vp, vp], ci),
+            ("mc_distill_workspace", [i64, i64], i64),
+        ):
+            f = getattr(L, name)
+            f.argtypes, f.restype = args, res
         L.mc_status_str.restype = ctypes.c_char_p
         L.mc_status_str.argtypes = [ci]
         _lib = L
@@ -115,6 +135,7 @@ def _check(status: int, what: str):
 # and the current stream's handle is read without building a Stream object (a 7850-element
 # MC-SGD update, two calls: 21 -> 15 us).
 _DTYPE_CODES = {}
+_PLAIN_CODES = {}  # the formats of the mc_mx4_* and mc_distill_* calls
 _torch_module = None
 _raw_stream = None
 _plain_tensor = None
@@ -126,6 +147,7 @@ def _torch():
         import torch
 
         _DTYPE_CODES.update({torch.float16: MCF_F16, torch.float32: MCF_F32, torch.float64: MCF_F64})
+        _PLAIN_CODES.update({torch.float16: MCF_F16, torch.bfloat16: MCF_BF16, torch.float32: MCF_F32})
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
         _plain_tensor = torch.Tensor
         _torch_module = torch
@@ -613,3 +635,254 @@ def matmul_mcn(x, y, *, nc: int, x_mc: bool = True, y_mc: bool = False):
     if ry == 1:
         out = out.squeeze(-1)
     return out
+
+
+# MXFP4 tensors are pairs (codes, scales) of uint8 tensors: for a tensor of shape (*S, n) in nc
+# components, G = ceil(n / 128), codes (nc, *S, 64 G) and scales (nc, G, *S, 4).  The layout is
+# in include/mcf.h.
+
+
+def _plain_code(dtype) -> int:
+    code = _PLAIN_CODES.get(dtype)
+    if code is None:
+        _torch()
+        code = _PLAIN_CODES.get(dtype)
+        if code is None:
+            raise TypeError(f"dtype must be float16, bfloat16 or float32, got {dtype}")
+    return code
+
+
+def _mx4(pair, n, name):
+    """(nc, S, codes pointer, scales pointer) of an MXFP4 tensor of row length n."""
+    codes, scales = pair
+    torch = _torch()
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+        raise TypeError(f"{name}: codes and scales must be uint8")
+    if codes.get_device() != scales.get_device():
+        raise ValueError(f"{name}: codes and scales must be on one device")
+    groups = (n + 127) // 128
+    cs, ss = codes.shape, scales.shape
+    if n < 0 or len(cs) < 2 or cs[-1] != 64 * groups or len(ss) != len(cs) + 1 \
+            or ss[0] != cs[0] or ss[1] != groups or ss[2:-1] != cs[1:-1] or ss[-1] != 4:
+        raise ValueError(f"{name}: codes {tuple(cs)} and scales {tuple(ss)} are not an MXFP4 tensor of rows of {n}")
+    return cs[0], cs[1:-1], _dev(codes, name), _dev(scales, name)
+
+
+def _device(t, other, name):
+    if t.get_device() != other.get_device():
+        raise ValueError(f"{name} must be on the other operands' device")
+
+
+def _out(out, like, shape, dtype):
+    if out is None:
+        return _torch().empty(shape, dtype=dtype, device=like.device)
+    if tuple(out.shape) != tuple(shape) or out.dtype != dtype or out.get_device() != like.get_device():
+        raise ValueError("out has the wrong shape, dtype or device")
+    return out
+
+
+def _space(workspace, needed, like):
+    """(tensor to keep, pointer, bytes) of a workspace, allocated here when needed and not given."""
+    if workspace is None:
+        if needed <= 0:
+            return None, None, 0
+        workspace = _torch().empty(needed, dtype=_torch().uint8, device=like.device)
+    _device(workspace, like, "workspace")
+    return workspace, _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
+
+
+def _bytes(needed, what) -> int:
+    _check(int(needed) if needed < 0 else 0, what)
+    return int(needed)
+
+
+def mc_mx4_quantize(x, *, nc: int = 1, x_mc: bool = False, out=None):
+    """x (*S, n), or with x_mc an MC value (planes, *S, n) -> its MXFP4 tensor (codes, scales)
+    of nc components: each block of 32 along a row scaled by a power of two and rounded to
+    E2M1, each component the rounding of what the ones before it leave."""
+    torch = _torch()
+    code = _plain_code(x.dtype)
+    if x.dim() < (2 if x_mc else 1):
+        raise ValueError("x must be (*S, n), or (planes, *S, n) with x_mc")
+    nc_in = x.shape[0] if x_mc else 1
+    shape = tuple(x.shape[1:] if x_mc else x.shape)
+    n, rows = shape[-1], math.prod(shape[:-1])
+    groups = (n + 127) // 128
+    want = (nc,) + shape[:-1] + (64 * groups,), (nc, groups) + shape[:-1] + (4,)
+    if nc < 1:
+        raise ValueError("nc must be positive")
+    codes, scales = (_out(o, x, w, torch.uint8) for o, w in zip(out or (None, None), want))
+    st = (_lib or lib()).mc_mx4_quantize(code, nc_in, nc, rows, n, _dev(x, "x"), _dev(codes, "codes"),
+                                         _dev(scales, "scales"), _stream(x))
+    _check(st, "mc_mx4_quantize")
+    return codes, scales
+
+
+def mc_mx4_dequantize(codes, scales, n: int, *, dtype, out=None):
+    """The numbers (*S, n) an MXFP4 tensor stands for, in `dtype`."""
+    nc, shape, cp, sp = _mx4((codes, scales), n, "codes and scales")
+    out = _out(out, codes, tuple(shape) + (n,), dtype)
+    st = (_lib or lib()).mc_mx4_dequantize(_plain_code(dtype), nc, math.prod(shape), n, cp, sp, _dev(out, "out"),
+                                           _stream(codes))
+    _check(st, "mc_mx4_dequantize")
+    return out
+
+
+def mc_mx4_matmul_workspace(dtype, M: int, N: int, K: int, a_nc: int, b_nc: int) -> int:
+    """Workspace bytes of mc_mx4_matmul."""
+    return _bytes((_lib or lib()).mc_mx4_matmul_workspace(_plain_code(dtype), M, N, K, a_nc, b_nc),
+                  "mc_mx4_matmul_workspace")
+
+
+def mc_mx4_matmul(a, b, K: int, *, dtype, out=None, workspace=None):
+    """a b^T of two MXFP4 tensors (codes, scales) with M and N rows of K -> (M, N) of `dtype`.
+    `workspace`: an optional device byte tensor; one is allocated here when needed and not given."""
+    a_nc, sa, ac, asc = _mx4(a, K, "a")
+    b_nc, sb, bc, bsc = _mx4(b, K, "b")
+    _device(b[0], a[0], "b")
+    if len(sa) != 1 or len(sb) != 1:
+        raise ValueError("a and b must be MXFP4 tensors of matrices")
+    M, N = sa[0], sb[0]
+    out = _out(out, a[0], (M, N), dtype)
+    keep, wp, wn = _space(workspace, mc_mx4_matmul_workspace(dtype, M, N, K, a_nc, b_nc), a[0])
+    st = (_lib or lib()).mc_mx4_matmul(_plain_code(dtype), M, N, K, ac, asc, a_nc, bc, bsc, b_nc, wp, wn,
+                                       _dev(out, "out"), _stream(a[0]))
+    _check(st, "mc_mx4_matmul")
+    return out
+
+
+def mc_mx4_linear_fwd_workspace(dtype, nc: int, batch: int, in_: int, out: int) -> int:
+    """Workspace bytes of mc_mx4_linear_fwd."""
+    return _bytes((_lib or lib()).mc_mx4_linear_fwd_workspace(_plain_code(dtype), nc, batch, in_, out),
+                  "mc_mx4_linear_fwd_workspace")
+
+
+def mc_mx4_linear_fwd(x, W, b=None, *, out=None, workspace=None):
+    """y = x W^T + b.  x: (batch, in) plain, W: the MXFP4 tensor (codes, scales) of an (out, in)
+    weight, b: (out,) of x's dtype or None -> (batch, out).  `workspace`: an optional device byte
+    tensor; one is allocated here when needed and not given."""
+    if x.dim() != 2:
+        raise ValueError("x must be (batch, in)")
+    T, I = x.shape
+    nc, s, wc, wsc = _mx4(W, I, "W")
+    _device(W[0], x, "W")
+    if len(s) != 1:
+        raise ValueError("W must be the MXFP4 tensor of a matrix")
+    O = s[0]
+    if b is not None:
+        _device(b, x, "b")
+        if b.dtype != x.dtype or tuple(b.shape) != (O,):
+            raise ValueError("dtype or bias shape mismatch")
+    code = _plain_code(x.dtype)
+    out = _out(out, x, (T, O), x.dtype)
+    keep, wp, wn = _space(workspace, _bytes((_lib or lib()).mc_mx4_linear_fwd_workspace(code, nc, T, I, O),
+                                            "mc_mx4_linear_fwd"), x)
+    st = _lib.mc_mx4_linear_fwd(code, nc, T, I, O, _dev(x, "x"), wc, wsc, None if b is None else _dev(b, "b"), wp, wn,
+                                _dev(out, "out"), _stream(x))
+    _check(st, "mc_mx4_linear_fwd")
+    return out
+
+
+def mc_mx4_linear_bwd_workspace(dtype, nc: int, batch: int, in_: int, out: int) -> int:
+    """Workspace bytes of mc_mx4_linear_bwd with every gradient."""
+    return _bytes((_lib or lib()).mc_mx4_linear_bwd_workspace(_plain_code(dtype), nc, batch, in_, out),
+                  "mc_mx4_linear_bwd_workspace")
+
+
+def mc_mx4_linear_bwd(x, W, dY, *, dx: bool = True, dw: bool = True, db: bool = True, workspace=None):
+    """The gradients of mc_mx4_linear_fwd: dX = dY W (batch, in), dW = dY^T x (out, in), the
+    gradient of the numbers W stands for, and db = column sums of dY (out,); None for those not
+    requested.  `workspace`: an optional device byte tensor; one is allocated here when not given."""
+    if x.dim() != 2:
+        raise ValueError("x must be (batch, in)")
+    T, I = x.shape
+    nc, s, wc, wsc = _mx4(W, I, "W")
+    _device(W[0], x, "W")
+    _device(dY, x, "dY")
+    if len(s) != 1:
+        raise ValueError("W must be the MXFP4 tensor of a matrix")
+    O = s[0]
+    if tuple(dY.shape) != (T, O) or dY.dtype != x.dtype:
+        raise ValueError(f"dY must be {(T, O)} of x's dtype, got {tuple(dY.shape)} of {dY.dtype}")
+    code = _plain_code(x.dtype)
+    outs = [_empty(x, (T, I)) if dx else None, _empty(x, (O, I)) if dw else None, _empty(x, (O,)) if db else None]
+    keep, wp, wn = _space(workspace, _bytes((_lib or lib()).mc_mx4_linear_bwd_workspace(code, nc, T, I, O),
+                                            "mc_mx4_linear_bwd"), x)
+    st = _lib.mc_mx4_linear_bwd(code, nc, T, I, O, _dev(x, "x"), wc, wsc, _dev(dY, "dY"),
+                                *(None if o is None else o.data_ptr() for o in outs), wp, wn, _stream(x))
+    _check(st, "mc_mx4_linear_bwd")
+    return tuple(outs)
+
+
+def _distill_args(z, ids, t, g):
+    """(code, nc, rows, vocab, k) of a distillation call's tensors."""
+    torch = _torch()
+    nc = 1
+    if z.dim() == 3:
+        nc, rows, vocab = z.shape
+    elif z.dim() == 2:
+        rows, vocab = z.shape
+    else:
+        raise ValueError("z must be (rows, vocab), or (nc, rows, vocab) of an MC value")
+    if ids.dtype != torch.int32:
+        raise TypeError(f"ids must be int32, got {ids.dtype}")
+    if ids.dim() != 2 or ids.shape[0] != rows or t.shape != ids.shape or t.dtype != z.dtype:
+        raise ValueError("ids and t must be (rows, k), t of z's dtype")
+    _device(ids, z, "ids")
+    _device(t, z, "t")
+    if g is not None:
+        if g.dtype != torch.float32 or tuple(g.shape) != (rows,):
+            raise ValueError("g must be (rows,) float32")
+        _device(g, z, "g")
+    return _plain_code(z.dtype), nc, rows, vocab, ids.shape[1]
+
+
+def mc_distill_workspace(rows: int, vocab: int) -> int:
+    """Workspace bytes of mc_distill_fwd and mc_distill_fwd_bwd."""
+    return _bytes((_lib or lib()).mc_distill_workspace(rows, vocab), "mc_distill_workspace")
+
+
+def mc_distill_fwd(z, ids, t, *, temperature: float = 1.0, workspace=None):
+    """Distillation from a teacher's top logits (see include/mcf.h): the loss of every row,
+    T^2 KL(softmax of the k teacher logits t at ids || softmax of z), at temperature T.  z: (rows,
+    vocab) plain or (nc, rows, vocab) MC; ids: (rows, k) int32, an id outside the vocabulary is an
+    unused entry; t: (rows, k).  Returns (loss (rows,), stats (rows, 2)), both float32; stats are
+    for mc_distill_bwd."""
+    torch = _torch()
+    code, nc, rows, vocab, k = _distill_args(z, ids, t, None)
+    loss = torch.empty(rows, dtype=torch.float32, device=z.device)
+    stats = torch.empty((rows, 2), dtype=torch.float32, device=z.device)
+    keep, wp, wn = _space(workspace, mc_distill_workspace(rows, vocab), z)
+    st = _lib.mc_distill_fwd(code, nc, rows, vocab, k, _dev(z, "z"), _dev(ids, "ids"), _dev(t, "t"),
+                             float(temperature), wp, wn, loss.data_ptr(), stats.data_ptr(), _stream(z))
+    _check(st, "mc_distill_fwd")
+    return loss, stats
+
+
+def mc_distill_bwd(z, ids, t, stats, g=None, *, temperature: float = 1.0, out=None):
+    """The gradient (rows, vocab) of sum_r g_r loss_r with respect to z (of the planes' sum for
+    an MC z) from mc_distill_fwd's stats.  g: (rows,) float32, or None for ones."""
+    code, nc, rows, vocab, k = _distill_args(z, ids, t, g)
+    if stats.dtype != _torch().float32 or tuple(stats.shape) != (rows, 2):
+        raise ValueError("stats must be (rows, 2) float32")
+    _device(stats, z, "stats")
+    out = _out(out, z, (rows, vocab), z.dtype)
+    st = (_lib or lib()).mc_distill_bwd(code, nc, rows, vocab, k, _dev(z, "z"), _dev(ids, "ids"), _dev(t, "t"),
+                                        float(temperature), _dev(stats, "stats"), None if g is None else _dev(g, "g"),
+                                        _dev(out, "out"), _stream(z))
+    _check(st, "mc_distill_bwd")
+    return out
+
+
+def mc_distill_fwd_bwd(z, ids, t, g=None, *, temperature: float = 1.0, out=None, workspace=None):
+    """(loss, gradient) of mc_distill_fwd and mc_distill_bwd in one pass over z."""
+    torch = _torch()
+    code, nc, rows, vocab, k = _distill_args(z, ids, t, g)
+    loss = torch.empty(rows, dtype=torch.float32, device=z.device)
+    out = _out(out, z, (rows, vocab), z.dtype)
+    keep, wp, wn = _space(workspace, mc_distill_workspace(rows, vocab), z)
+    st = _lib.mc_distill_fwd_bwd(code, nc, rows, vocab, k, _dev(z, "z"), _dev(ids, "ids"), _dev(t, "t"),
+                                 float(temperature), None if g is None else _dev(g, "g"), wp, wn, loss.data_ptr(),
+                                 _dev(out, "out"), _stream(z))
+    _check(st, "mc_distill_fwd_bwd")
+    return loss, out

@@ -122,4 +122,37 @@ int64_t linreg_workspace_bytes(int dtype, int nc, int64_t n, int64_t d);
 hipError_t launch_linreg_step(int dtype, int nc, int64_t n, int64_t d, const void *X, const void *y_neg, void *W,
                               double s2n, double s1n, double neg_lr, void *ws, void *loss, hipStream_t stream);
 
+// Formats of the calls on MXFP4 tensors and of the distillation loss.
+constexpr int LM_F16 = 0, LM_F32 = 1, LM_BF16 = 4;
+
+// Quantisation into nc MXFP4 components and reading back (mx4_quant.hip); layouts in mx4.hpp.
+hipError_t launch_mx4_quantize(int dtype, int nc_in, int nc, int64_t rows, int64_t n, const void *x, void *codes,
+                               void *scales, hipStream_t stream);
+hipError_t launch_mx4_dequantize(int dtype, int nc, int64_t rows, int64_t n, const void *codes, const void *scales,
+                                 void *out, hipStream_t stream);
+
+// C [M][N] = A B^T of two MXFP4 tensors, and the linear layer of a plain x with an MXFP4 weight
+// (mx4_matmul.hip).  ws holds the bytes of the matching workspace function.
+int64_t mx4_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int a_nc, int b_nc);
+hipError_t launch_mx4_matmul(int dtype, int64_t M, int64_t N, int64_t K, const void *a_codes, const void *a_scales,
+                             int a_nc, const void *b_codes, const void *b_scales, int b_nc, void *ws, void *C,
+                             hipStream_t stream);
+int64_t mx4_linear_workspace_bytes(int dtype, int nc, int64_t batch, int64_t in, int64_t out);
+hipError_t launch_mx4_linear(int dtype, int nc, int64_t batch, int64_t in, int64_t out, const void *x,
+                             const void *codes, const void *scales, const void *bias, void *ws, void *y,
+                             hipStream_t stream);
+// Its gradients (mx4_backward.hip); dX, dW and db may each be null.
+int64_t mx4_linear_bwd_workspace_bytes(int dtype, int nc, int64_t batch, int64_t in, int64_t out, int dx, int dw,
+                                       int db);
+hipError_t launch_mx4_linear_bwd(int dtype, int nc, int64_t batch, int64_t in, int64_t out, const void *x,
+                                 const void *codes, const void *scales, const void *dY, void *dX, void *dW, void *db,
+                                 void *ws, hipStream_t stream);
+
+// Distillation from a teacher's top logits (distill.hip).  stats_in null: loss and stats from z
+// (dz too where it is not null); else dz alone from the given stats.
+int64_t distill_workspace_bytes(int64_t rows, int64_t vocab);
+hipError_t launch_distill(int dtype, int nc, int64_t rows, int64_t vocab, int64_t k, const void *z, const void *ids,
+                          const void *t, double temperature, const void *stats_in, const void *g, void *ws, void *loss,
+                          void *stats, void *dz, hipStream_t stream);
+
 }  // namespace mcf

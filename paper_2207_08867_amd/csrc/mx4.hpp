@@ -1,0 +1,120 @@
+// mx4.hpp -- what the kernels on microscaled 4-bit (MXFP4) tensors share: the element
+// conversions of gfx950, 8-element loads and stores of plain tensors, and the splitting of
+// wider formats into bfloat16 pieces.
+//
+// A block is 32 elements along a row.  An element is E2M1 (sign, 2 exponent bits, 1 mantissa
+// bit: 0, 0.5, 1, 1.5, 2, 3, 4, 6), the block's scale E8M0 (byte s stands for 2^(s - 127), 255
+// for NaN).  Four blocks form a group of 128 elements: 64 bytes of codes (element 2i in the low
+// half of byte i) and one 32-bit word of scales.  Codes are [nc][rows][64 G] bytes, scales
+// [nc][G][rows] words, G = ceil(n / 128): the words of neighbouring rows lie side by side, as the
+// product kernels read them, and the zero padding of a row's last group spares them a K tail.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace mcf {
+
+constexpr int MX_GROUP = 128;
+inline __host__ __device__ int64_t mx_groups(int64_t n) { return (n + MX_GROUP - 1) / MX_GROUP; }
+
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// Eight elements of a plain tensor.  The address is aligned to the element only: rows of odd
+// length start anywhere, and gfx950 loads 16 bytes from any address.
+template <typename T>
+struct Raw8 {
+  T v[8];
+};
+
+template <typename T>
+__device__ inline Raw8<T> load8(const T *p) {
+  Raw8<T> r;
+  __builtin_memcpy(&r, p, sizeof(r));
+  return r;
+}
+
+// Eight elements from p, of which those at or past `left` are read as zero.
+template <typename T>
+__device__ inline Raw8<T> load8_tail(const T *p, int64_t left) {
+  if (left >= 8) return load8(p);
+  Raw8<T> r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r.v[i] = i < left ? p[i] : (T)0.0f;
+  return r;
+}
+
+template <typename T>
+__device__ inline void store8_tail(T *p, const Raw8<T> &r, int64_t left) {
+  if (left >= 8) {
+    __builtin_memcpy(p, &r, sizeof(r));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < left) p[i] = r.v[i];
+  }
+}
+
+// Eight E2M1 codes (one word) of a block as bfloat16 values.  scale: the binary32 number whose
+// exponent field is the block's scale byte (byte << 23; the conversion reads that field alone, 0
+// standing for 2^-127 and 255 for NaN).  Exact but for a value past bfloat16's range (inf).
+__device__ inline bf16x8 mx_bf16(uint32_t w, float scale) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+  bf16x8 r = {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  return r;
+}
+
+__device__ inline void mx_f32(uint32_t w, float scale, float v[8]) {
+  const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0);
+  const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);
+  const f32x2 c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 2);
+  const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 3);
+  v[0] = a[0], v[1] = a[1], v[2] = b[0], v[3] = b[1], v[4] = c[0], v[5] = c[1], v[6] = d[0], v[7] = d[1];
+}
+
+__device__ inline float mx_scale(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+
+// The number of bfloat16 pieces that hold a value of T exactly (8 significant bits each; the
+// last of a binary32 value below 2^-100 may lose bits under bfloat16's smallest number).
+template <typename T>
+constexpr int mx_pieces() {
+  return sizeof(T) == 4 ? 3 : (__is_same(T, __bf16) ? 1 : 2);
+}
+
+// The leading piece of v: v rounded to bfloat16, cut off instead where rounding would pass the
+// largest finite number (and for infinities and NaN, which keep their kind).
+__device__ inline __bf16 mx_lead(float v) {
+  uint32_t u = __builtin_bit_cast(uint32_t, v);
+  const uint32_t a = u & 0x7fffffffu;
+  if (a < 0x7f7f8000u) return (__bf16)v;
+  if (a > 0x7f800000u) u |= 0x00400000u;
+  return __builtin_bit_cast(__bf16, (uint16_t)(u >> 16));
+}
+
+// v = p[0] + p[1] + ...; an infinity or NaN is its first piece, the others zero.
+template <int P>
+__device__ inline void mx_split(float v, __bf16 p[P]) {
+  p[0] = mx_lead(v);
+  if constexpr (P > 1) {
+    const bool finite = (__builtin_bit_cast(uint32_t, v) & 0x7f800000u) != 0x7f800000u;
+    float r = finite ? v - (float)p[0] : 0.0f;
+#pragma unroll
+    for (int i = 1; i < P; ++i) {
+      p[i] = (__bf16)r;
+      r -= (float)p[i];
+    }
+  }
+}
+
+}  // namespace mcf

@@ -1,0 +1,240 @@
+// mx4_quant.hip -- quantisation into MXFP4 components and reading back.
+//
+// Quantisation of a block v_0 .. v_31: X = max(floor(log2 max|v_i|) - 2, -127), the element i
+// is v_i 2^-X rounded to nearest E2M1, ties to even, at most 6; what is left, v_i minus the
+// number the element stands for, is the next component's input.  The remainder is exact in
+// binary32: it is a multiple of v_i's last place and no larger than v_i, or within 2^(X-2) of
+// zero.  Both directions stream: 2 to 4 bytes read and 17/32 of a byte written per element and
+// component (or back), so HBM bounds them.  A lane takes 8 elements and four lanes a block, so
+// a wavefront reads 1 KiB of binary16 in one instruction and writes 256 bytes of codes; the
+// block's maximum is two DPP steps inside a quad.
+#include "mcf_internal.hpp"
+#include "mx4.hpp"
+
+namespace mcf {
+namespace {
+
+template <int CTRL>
+__device__ inline uint32_t quad_max(uint32_t m) {
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)m, CTRL, 0xf, 0xf, true);
+  return o > m ? o : m;
+}
+
+// The largest value of a quad of lanes.
+__device__ inline uint32_t block_max(uint32_t m) { return quad_max<0x4e>(quad_max<0xb1>(m)); }
+
+struct QuantArgs {
+  const void *x;
+  uint8_t *codes, *scales;
+  int64_t rows, n, groups, chunks;  // chunks: 8-element pieces, 16 a group, of all rows
+  int nc;
+};
+
+__device__ inline uint32_t pack8(const float v[8], float scale) {
+  uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[0], v[1], scale, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], scale, 1);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], scale, 3);
+}
+
+// d as binary32 with its inexactness kept in the last bit (rounding to odd), so that a later
+// rounding to E2M1 equals one rounding of d.
+__device__ inline float round_odd(double d) {
+  const float f = (float)d;
+  const uint32_t u = __builtin_bit_cast(uint32_t, f);
+  const double back = (double)f;
+  if (back == d || !(u & 0x7f800000u)) return f;  // exact, or far below every rounding boundary
+  const uint32_t cut = (fabs(back) > fabs(d) ? u - 1 : u) | 1u;
+  return __builtin_bit_cast(float, cut);
+}
+
+struct BlockAt {
+  int64_t row, group;
+  int in;  // the lane's piece of the group, 0 .. 15
+};
+
+__device__ inline void put(const QuantArgs &a, const BlockAt &b, int c, uint32_t word, uint32_t byte) {
+  uint8_t *codes = a.codes + ((int64_t)c * a.rows + b.row) * (a.groups * 64) + b.group * 64 + b.in * 4;
+  *reinterpret_cast<uint32_t *>(codes) = word;
+  if ((b.in & 3) == 0) a.scales[(((int64_t)c * a.groups + b.group) * a.rows + b.row) * 4 + (b.in >> 2)] = (uint8_t)byte;
+}
+
+// Components of binary32 values.  A block with an infinity or NaN gets the scale 255 (NaN) and
+// zero codes in every component.
+__device__ inline void quantize32(const QuantArgs &a, const BlockAt &b, float v[8]) {
+  for (int c = 0; c < a.nc; ++c) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t u = __builtin_bit_cast(uint32_t, v[i]) & 0x7fffffffu;
+      m = u > m ? u : m;
+    }
+    const uint32_t e = block_max(m) >> 23;
+    const uint32_t byte = e == 255 ? 255 : (e > 2 ? e - 2 : 0);
+    const float scale = mx_scale(byte == 255 ? 127 : byte);
+    const uint32_t word = byte == 255 ? 0 : pack8(v, scale);
+    put(a, b, c, word, byte);
+    if (c + 1 < a.nc && byte != 255) {
+      float q[8];
+      mx_f32(word, scale, q);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] -= q[i];
+    }
+  }
+}
+
+// The same from binary64 values, for sums of planes that binary32 does not hold.
+__device__ inline void quantize64(const QuantArgs &a, const BlockAt &b, double v[8]) {
+  for (int c = 0; c < a.nc; ++c) {
+    uint32_t m = 0;  // the largest biased binary64 exponent
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t e = (uint32_t)(__builtin_bit_cast(uint64_t, v[i]) >> 52) & 0x7ffu;
+      m = e > m ? e : m;
+    }
+    m = block_max(m);
+    const int X = (int)m - 1023 - 2;
+    const uint32_t byte = m == 0x7ff ? 255 : (X < -127 ? 0 : (X > 127 ? 254 : X + 127));
+    const int E = (int)byte - 127;
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = round_odd(ldexp(v[i], -E));
+    const uint32_t word = byte == 255 ? 0 : pack8(y, 1.0f);
+    put(a, b, c, word, byte);
+    if (c + 1 < a.nc && byte != 255) {
+      float q[8];
+      mx_f32(word, 1.0f, q);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] -= ldexp((double)q[i], E);
+    }
+  }
+}
+
+template <typename T, int NIN>
+__global__ __launch_bounds__(256) void mx_quant_kernel(QuantArgs a) {
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  // whole quads leave together: chunks is a multiple of 16
+  if (id >= a.chunks) return;
+  BlockAt b;
+  const int64_t gid = id >> 4;
+  b.in = (int)(id & 15);
+  if (gid <= 0xffffffffll && a.groups <= 0xffffffffll) {
+    b.row = (uint32_t)gid / (uint32_t)a.groups;
+  } else {
+    b.row = gid / a.groups;
+  }
+  b.group = gid - b.row * a.groups;
+  const int64_t col = b.group * MX_GROUP + b.in * 8;
+  const T *x = reinterpret_cast<const T *>(a.x) + b.row * a.n + col;
+  float v[8];
+  if constexpr (NIN == 1) {
+    const Raw8<T> r = load8_tail(x, a.n - col);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (float)r.v[i];
+    quantize32(a, b, v);
+  } else {
+    // the planes' sum, the last plane first, with the error of every addition (Two-Sum): where
+    // all errors are zero the binary32 sum is exact
+    Raw8<T> r[NIN];
+#pragma unroll
+    for (int p = 0; p < NIN; ++p) r[p] = load8_tail(x + p * a.rows * a.n, a.n - col);
+    bool exact = true;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float s = (float)r[NIN - 1].v[i];
+#pragma unroll
+      for (int p = NIN - 2; p >= 0; --p) {
+        const float y = (float)r[p].v[i], t = y + s, z = t - y;
+        exact = exact && ((y - (t - z)) + (s - z)) == 0.0f;
+        s = t;
+      }
+      v[i] = s;
+    }
+    if (__all(exact)) {
+      quantize32(a, b, v);
+    } else {
+      // binary16 and bfloat16 planes of one value sum exactly in 53 bits; binary32 planes that
+      // span more round there
+      double d[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        d[i] = (double)(float)r[NIN - 1].v[i];
+#pragma unroll
+        for (int p = NIN - 2; p >= 0; --p) d[i] += (double)(float)r[p].v[i];
+      }
+      quantize64(a, b, d);
+    }
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void mx_dequant_kernel(const uint8_t *codes, const uint8_t *scales, T *out, int nc,
+                                                         int64_t rows, int64_t n, int64_t groups, int64_t per_row,
+                                                         int64_t chunks) {
+  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= chunks) return;
+  const int64_t row = (id <= 0xffffffffll && per_row <= 0xffffffffll) ? (int64_t)((uint32_t)id / (uint32_t)per_row)
+                                                                      : id / per_row;
+  const int64_t piece = id - row * per_row;
+  float v[8] = {};
+  for (int c = nc - 1; c >= 0; --c) {  // the smallest component first
+    const int64_t plane = (int64_t)c * rows;
+    const uint32_t word =
+        *reinterpret_cast<const uint32_t *>(codes + (plane + row) * (groups * 64) + piece * 4);
+    const uint32_t byte = scales[((plane * groups) + (piece >> 4) * rows + row) * 4 + ((piece >> 2) & 3)];
+    float q[8];
+    mx_f32(word, mx_scale(byte), q);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = c == nc - 1 ? q[i] : v[i] + q[i];
+  }
+  Raw8<T> r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r.v[i] = (T)v[i];
+  store8_tail(out + row * n + piece * 8, r, n - piece * 8);
+}
+
+template <typename T>
+hipError_t quantize(int nc_in, const QuantArgs &a, hipStream_t stream) {
+  const dim3 grid((unsigned)((a.chunks + 255) / 256));
+  switch (nc_in) {
+    case 1: mx_quant_kernel<T, 1><<<grid, 256, 0, stream>>>(a); break;
+    case 2: mx_quant_kernel<T, 2><<<grid, 256, 0, stream>>>(a); break;
+    case 3: mx_quant_kernel<T, 3><<<grid, 256, 0, stream>>>(a); break;
+    default: mx_quant_kernel<T, 4><<<grid, 256, 0, stream>>>(a); break;
+  }
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_mx4_quantize(int dtype, int nc_in, int nc, int64_t rows, int64_t n, const void *x, void *codes,
+                               void *scales, hipStream_t stream) {
+  QuantArgs a;
+  a.x = x;
+  a.codes = (uint8_t *)codes;
+  a.scales = (uint8_t *)scales;
+  a.rows = rows;
+  a.n = n;
+  a.groups = mx_groups(n);
+  a.chunks = rows * a.groups * 16;
+  a.nc = nc;
+  if (dtype == LM_F16) return quantize<_Float16>(nc_in, a, stream);
+  if (dtype == LM_BF16) return quantize<__bf16>(nc_in, a, stream);
+  return quantize<float>(nc_in, a, stream);
+}
+
+hipError_t launch_mx4_dequantize(int dtype, int nc, int64_t rows, int64_t n, const void *codes, const void *scales,
+                                 void *out, hipStream_t stream) {
+  const int64_t per_row = (n + 7) / 8, chunks = rows * per_row, groups = mx_groups(n);
+  const dim3 grid((unsigned)((chunks + 255) / 256));
+  const uint8_t *c = (const uint8_t *)codes, *s = (const uint8_t *)scales;
+  if (dtype == LM_F16)
+    mx_dequant_kernel<_Float16><<<grid, 256, 0, stream>>>(c, s, (_Float16 *)out, nc, rows, n, groups, per_row, chunks);
+  else if (dtype == LM_BF16)
+    mx_dequant_kernel<__bf16><<<grid, 256, 0, stream>>>(c, s, (__bf16 *)out, nc, rows, n, groups, per_row, chunks);
+  else
+    mx_dequant_kernel<float><<<grid, 256, 0, stream>>>(c, s, (float *)out, nc, rows, n, groups, per_row, chunks);
+  return hipGetLastError();
+}
+
+}  // namespace mcf
