@@ -8,49 +8,10 @@
 // products A B^T of staged tensors, summed over pairs of pieces in binary32.
 #include "mcf_internal.hpp"
 #include "mx4.hpp"
+#include "mx4_gemm.hpp"
 
 namespace mcf {
 namespace {
-
-__device__ inline uint16_t bits(__bf16 v) { return __builtin_bit_cast(uint16_t, v); }
-__device__ inline uint16_t bits(_Float16 v) { return __builtin_bit_cast(uint16_t, v); }
-
-// Staged pieces of one element of T: bfloat16 pieces, or the binary16 number itself.
-template <typename T, bool HALF>
-struct Pieces {
-  static constexpr int P = HALF ? 1 : mx_pieces<T>();
-  static __device__ inline void of(T v, uint16_t p[P]) {
-    if constexpr (HALF) {
-      p[0] = bits((_Float16)v);
-    } else {
-      __bf16 q[P];
-      mx_split<P>((float)v, q);
-#pragma unroll
-      for (int i = 0; i < P; ++i) p[i] = bits(q[i]);
-    }
-  }
-};
-
-// src [rows][cols] -> dst [P][rows][ld], zeros from cols to ld.
-template <typename T>
-__global__ __launch_bounds__(256) void mx_stage_kernel(const T *src, uint16_t *dst, int64_t rows, int64_t cols,
-                                                       int64_t ld) {
-  using S = Pieces<T, false>;
-  const int64_t per_row = ld / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (id >= rows * per_row) return;
-  const int64_t row = id / per_row, col = (id - row * per_row) * 8;
-  const Raw8<T> r = load8_tail(src + row * cols + col, cols - col);
-  uint16_t out[S::P][8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    uint16_t p[S::P];
-    S::of(r.v[i], p);
-#pragma unroll
-    for (int k = 0; k < S::P; ++k) out[k][i] = p[k];
-  }
-#pragma unroll
-  for (int k = 0; k < S::P; ++k) __builtin_memcpy(dst + ((int64_t)k * rows + row) * ld + col, out[k], 16);
-}
 
 // src [rows][cols] -> dst [P][cols][ld], the transpose, zeros from rows to ld (a multiple of 64).
 template <typename T, bool HALF>
@@ -90,7 +51,7 @@ __global__ __launch_bounds__(256) void mx_unpack_t_kernel(const uint8_t *codes, 
     }
     const bf16x8 v = mx_bf16(word, mx_scale(byte));
 #pragma unroll
-    for (int k = 0; k < 8; ++k) tile[piece * 8 + k][r] = bits((__bf16)v[k]);
+    for (int k = 0; k < 8; ++k) tile[piece * 8 + k][r] = __builtin_bit_cast(uint16_t, (__bf16)v[k]);
   }
   __syncthreads();
   for (int i = threadIdx.x; i < 128 * 64; i += 256) {
@@ -99,40 +60,34 @@ __global__ __launch_bounds__(256) void mx_unpack_t_kernel(const uint8_t *codes, 
   }
 }
 
-struct StagedArgs {
-  const uint16_t *a, *b;  // [pieces][M][ld], [pieces][N][ld]
-  void *c;                // [M][N]
-  int64_t M, N, ld;
-  int pa, pb;
-};
-
-// C = sum over piece pairs (i, j) of A_i B_j^T; with three pieces a side the pairs i + j > 2 are
-// left out: each is within 2^-26 of |A||B|, less than one rounding of the sum.
-template <typename T, bool HALF>
-__global__ __launch_bounds__(64) void mx_staged_kernel(StagedArgs a) {
-  const int lane = threadIdx.x, r = lane & 31, g = lane >> 5;
-  const int64_t m0 = (int64_t)blockIdx.y * 32, n0 = (int64_t)blockIdx.x * 32;
-  const int64_t ra = m0 + r < a.M ? m0 + r : a.M - 1, rb = n0 + r < a.N ? n0 + r : a.N - 1;
-  f32x16 acc = {};
-  for (int i = 0; i < a.pa; ++i)
-    for (int j = 0; j < a.pb; ++j) {
-      if (a.pa == 3 && a.pb == 3 && i + j > 2) continue;
-      const uint16_t *pa = a.a + ((int64_t)i * a.M + ra) * a.ld + g * 8;
-      const uint16_t *pb = a.b + ((int64_t)j * a.N + rb) * a.ld + g * 8;
-      for (int64_t k = 0; k < a.ld; k += 16) {
-        const u32x4 x = *reinterpret_cast<const u32x4 *>(pa + k), y = *reinterpret_cast<const u32x4 *>(pb + k);
-        if constexpr (HALF)
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), acc, 0, 0, 0);
-        else
-          acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
-      }
+// The pairs (i, j) of pieces with i + j < `below`.
+void set_pairs(GemmArgs &a, int na, int nb, int below) {
+  a.pairs = 0;
+  for (int i = 0; i < na; ++i)
+    for (int j = 0; j < nb; ++j) {
+      if (i + j >= below) continue;
+      a.pa[a.pairs] = (uint8_t)i;
+      a.pb[a.pairs++] = (uint8_t)j;
     }
-  T *c = reinterpret_cast<T *>(a.c);
-#pragma unroll
-  for (int i = 0; i < 16; ++i) {
-    const int64_t m = m0 + (i >> 2) * 8 + g * 4 + (i & 3), n = n0 + r;
-    if (m < a.M && n < a.N) c[m * a.N + n] = (T)acc[i];
-  }
+}
+
+// C [M][N] from staged a [na][M][ld] and b [nb][N][ld], pairs i + j < below.
+template <typename T, bool HALF>
+hipError_t staged(const uint16_t *a, int na, const uint16_t *b, int nb, int64_t M, int64_t N, int64_t ld, int below,
+                  void *c, void *partial, hipStream_t stream) {
+  GemmArgs g = {};
+  g.a = (const char *)a;
+  g.b = (const char *)b;
+  g.a_plane = M * ld * 2;
+  g.b_plane = N * ld * 2;
+  g.a_ld = g.b_ld = ld * 2;
+  g.c = c;
+  g.partial = (float *)partial;
+  g.M = M;
+  g.N = N;
+  g.steps = (int)(ld / 64);
+  set_pairs(g, na, nb, below);
+  return gemm<HALF ? GEMM_F16 : GEMM_BF16, T>(g, stream);
 }
 
 // db: a workgroup sums 64 columns, its four wavefronts every fourth row.
@@ -156,7 +111,8 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 struct Plan {
   int p, pw;        // pieces of a plain element: for dX, for dW
   int64_t op, tp;   // padded reductions
-  int64_t dy, wt, dyt, xt;  // bytes
+  int64_t dy, wt, dyt, xt;  // bytes of the staged operands
+  int64_t partx, partw;     // of the products' partial sums
 };
 
 Plan plan(int dtype, int nc, int64_t T, int64_t I, int64_t O) {
@@ -169,6 +125,8 @@ Plan plan(int dtype, int nc, int64_t T, int64_t I, int64_t O) {
   s.wt = up(nc * I * s.op * 2, 256);
   s.dyt = up(s.pw * O * s.tp * 2, 256);
   s.xt = up(s.pw * I * s.tp * 2, 256);
+  s.partx = gemm_partial_bytes(T, I, s.op / 64 * s.p * nc);
+  s.partw = gemm_partial_bytes(O, I, s.tp / 64 * (s.pw == 3 ? 6 : 1));
   return s;
 }
 
@@ -184,8 +142,8 @@ hipError_t backward(int nc, int64_t rows, int64_t in, int64_t out, const T *x, c
       mx_unpack_t_kernel<<<dim3((unsigned)mx_groups(in), blocks(s.op, 64), (unsigned)nc), 256, 0, stream>>>(
           codes, scales, wt, out, in, mx_groups(in), s.op);
     }
-    StagedArgs a = {dy, wt, dX, rows, in, s.op, s.p, nc};
-    mx_staged_kernel<T, false><<<dim3(blocks(in, 32), blocks(rows, 32)), 64, 0, stream>>>(a);
+    const hipError_t e = staged<T, false>(dy, s.p, wt, nc, rows, in, s.op, s.p + nc, dX, ws + s.dy + s.wt, stream);
+    if (e != hipSuccess) return e;
   }
   if (dW) {
     uint16_t *dyt = (uint16_t *)ws, *xt = (uint16_t *)(ws + s.dyt);
@@ -193,8 +151,10 @@ hipError_t backward(int nc, int64_t rows, int64_t in, int64_t out, const T *x, c
       mx_stage_t_kernel<T, HALF><<<dim3(blocks(out, 64), blocks(s.tp, 64)), 256, 0, stream>>>(dY, dyt, rows, out, s.tp);
       mx_stage_t_kernel<T, HALF><<<dim3(blocks(in, 64), blocks(s.tp, 64)), 256, 0, stream>>>(x, xt, rows, in, s.tp);
     }
-    StagedArgs a = {dyt, xt, dW, out, in, s.tp, s.pw, s.pw};
-    mx_staged_kernel<T, HALF><<<dim3(blocks(in, 32), blocks(out, 32)), 64, 0, stream>>>(a);
+    // of two values in three pieces the pairs past i + j = 2 are left out: each is within 2^-26 of
+    // |dY||x|, less than one rounding of the sum
+    const hipError_t e = staged<T, HALF>(dyt, s.pw, xt, s.pw, out, in, s.tp, 3, dW, ws + s.dyt + s.xt, stream);
+    if (e != hipSuccess) return e;
   }
   if (db) mx_colsum_kernel<T><<<blocks(out, 64), 256, 0, stream>>>(dY, db, rows, out);
   return hipGetLastError();
@@ -205,7 +165,7 @@ hipError_t backward(int nc, int64_t rows, int64_t in, int64_t out, const T *x, c
 int64_t mx4_linear_bwd_workspace_bytes(int dtype, int nc, int64_t batch, int64_t in, int64_t out, int dx, int dw,
                                        int db) {
   const Plan s = plan(dtype, nc, batch, in, out);
-  const int64_t a = dx ? s.dy + s.wt : 0, b = dw ? s.dyt + s.xt : 0;
+  const int64_t a = dx ? s.dy + s.wt + s.partx : 0, b = dw ? s.dyt + s.xt + s.partw : 0;
   return a > b ? a : b;
 }
 

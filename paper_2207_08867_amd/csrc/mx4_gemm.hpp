@@ -1,0 +1,361 @@
+// mx4_gemm.hpp -- the large products C = sum over pairs (i, j) of A_i B_j^T behind the MXFP4 calls,
+// one kernel for three kinds of operands, all rows of the reduction:
+//   GEMM_FP4   both sides MXFP4 codes with their scales (32 x 32 x 64 scaled products);
+//   GEMM_BF16, GEMM_F16   both sides 16-bit numbers (32 x 32 x 16 products);
+//   GEMM_MIX   A bfloat16, B MXFP4 codes, turned into bfloat16 in registers.
+// The operands of one instruction are 16 bytes a lane in every kind, and it takes as long (32
+// cycles of a SIMD at the full rate), so the kinds share tiles, staging and schedule.
+//
+// A workgroup computes BM x BN outputs, WM x WN wavefronts TM x TN tiles of 32 x 32 each.  A step
+// brings 128 bytes of every row of A (256 codes or 64 16-bit numbers) and as much of the reduction
+// of B into LDS by direct loads (no registers in between) while the step before is multiplied: two
+// buffers, one barrier a step.  Chunk c (16 bytes) of row r lies at position c ^ (r mod 8) of its
+// row, so the eight lanes that LDS serves together read eight different groups of four banks.
+//
+// What bounds it: the matrix instructions.  A wavefront tile of 128 x 128 reads 8 x 1 KiB of LDS
+// for 16 instructions, half of LDS's rate; the tile's 64 KiB a step are fetched over the L2 at 32
+// bytes a cycle and CU.
+#pragma once
+
+#include "mcf_internal.hpp"
+#include "mx4.hpp"
+
+namespace mcf {
+
+enum GemmKind { GEMM_FP4 = 0, GEMM_BF16 = 1, GEMM_F16 = 2, GEMM_MIX = 3 };
+
+struct GemmArgs {
+  const char *a, *b;              // pieces' planes of rows
+  int64_t a_plane, b_plane;       // bytes from plane to plane
+  int64_t a_ld, b_ld;             // bytes of a row
+  const uint32_t *as, *bs;        // scales [plane][groups][rows]
+  int64_t groups;
+  void *c;                        // [M][N]
+  const void *bias;               // [N] or null
+  float *partial;                 // [slices][M][N], with more than one slice
+  int64_t M, N;
+  int steps, total, slices;       // steps of a pair, of all pairs; slices of the reduction
+  int pairs;
+  uint8_t pa[16], pb[16];
+};
+
+// 16 (4) bytes a lane from base + off straight into LDS at `to` + 16 (4) lane.  The loads are
+// asm so that the compiler does not wait for them in front of every LDS read; gemm_wait does.
+// m0 holds the LDS address, and a load that reads it follows its write by a wait state.
+__device__ inline void lds_load16(uint32_t to, uint32_t off, const void *base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base) : "memory");
+}
+__device__ inline void lds_load4(uint32_t to, uint32_t off, const void *base) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base) : "memory");
+}
+__device__ inline const char *uniform(const void *p) {
+  const uint64_t u = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+  return (const char *)((uint64_t)hi << 32 | lo);
+}
+__device__ inline void gemm_wait() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+__device__ inline uint32_t lds_address(const void *p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
+}
+
+// Workgroup id -> tile.  Ids go to the 8 XCDs in turn; each XCD takes a contiguous run of tiles, and
+// a run walks 8 rows of tiles column by column, so that the tiles an XCD works on share operands
+// in its L2.
+__device__ inline void gemm_tile(uint32_t id, uint32_t gm, uint32_t gn, uint32_t *tm, uint32_t *tn) {
+  const uint32_t n = gm * gn, q = n / 8, rest = n % 8, x = id % 8, l = id / 8;
+  const uint32_t t = x < rest ? x * (q + 1) + l : rest * (q + 1) + (x - rest) * q + l;
+  const uint32_t band = t / (8 * gn), first = band * 8, rows = gm - first < 8 ? gm - first : 8, in = t - first * gn;
+  *tm = first + in % rows;
+  *tn = in / rows;
+}
+
+template <GemmKind KIND, typename T, int WM, int WN, int TM, int TN>
+__global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
+  constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NW = WM * WN;
+  constexpr int BB = KIND == GEMM_MIX ? 32 : 128;  // bytes of a row of B in a step
+  constexpr bool SCALED_A = KIND == GEMM_FP4, SCALED_B = KIND == GEMM_FP4 || KIND == GEMM_MIX;
+  constexpr int SG = KIND == GEMM_FP4 ? 2 : 1;     // words of scales of a row in a step
+  struct Stage {
+    char a[BM * 128];
+    char b[BN * BB];
+    uint32_t as[SCALED_A ? SG * BM : 1], bs[SCALED_B ? SG * BN : 1];
+  };
+  __shared__ __attribute__((aligned(128))) Stage st[2];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t tm, tn;
+  gemm_tile(blockIdx.x, (uint32_t)((a.M + BM - 1) / BM), (uint32_t)((a.N + BN - 1) / BN), &tm, &tn);
+  const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+  const int slice = blockIdx.y;
+  const int s_begin = (int)((int64_t)a.total * slice / a.slices), s_end = (int)((int64_t)a.total * (slice + 1) / a.slices);
+
+  // what this lane loads in a step: rows past the end repeat the last one
+  constexpr int LA = BM / 8 / NW, LB = BN * BB / 1024 / NW;
+  static_assert(BM % (8 * NW) == 0 && (BN * BB) % (1024 * NW) == 0, "whole loads a wavefront");
+  uint32_t offa[LA], offb[LB];
+  const int64_t la = a.M - m0, lb = a.N - n0;  // rows left
+#pragma unroll
+  for (int i = 0; i < LA; ++i) {
+    const int r = (wave * LA + i) * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
+    offa[i] = (uint32_t)((r < la ? r : la - 1) * a.a_ld) + c * 16;
+  }
+#pragma unroll
+  for (int i = 0; i < LB; ++i) {
+    int r, c;
+    if constexpr (BB == 128) {
+      r = (wave * LB + i) * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
+    } else {
+      r = (wave * LB + i) * 32 + (lane >> 1), c = lane & 1;
+    }
+    offb[i] = (uint32_t)((r < lb ? r : lb - 1) * a.b_ld) + c * 16;
+  }
+
+  const uint32_t upper = (((lane & 7) ^ (lane >> 3)) & 4) * 16;  // 64 where this lane loads a row's upper half
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(&st[0]));
+  const auto load = [&](int buf, int step) {
+    const int pair = a.pairs == 1 ? 0 : step / a.steps, k = step - pair * a.steps;
+    const uint32_t to = lds0 + buf * (uint32_t)sizeof(Stage);
+    const char *pa = uniform(a.a + a.pa[pair] * a.a_plane + m0 * a.a_ld + (int64_t)k * 128);
+    const char *pb = uniform(a.b + a.pb[pair] * a.b_plane + n0 * a.b_ld + (int64_t)k * BB);
+    if constexpr (KIND == GEMM_FP4) {
+      // an odd group count: the last step's upper half re-reads the lower one and counts for
+      // nothing (its scales are taken as 0 on both sides, and 2^-254 times 36 is 0)
+      const uint32_t back = 2 * k + 1 < a.groups ? 0 : upper;
+#pragma unroll
+      for (int i = 0; i < LA; ++i)
+        lds_load16(to + offsetof(Stage, a) + (wave * LA + i) * 1024, offa[i] - back, pa);
+#pragma unroll
+      for (int i = 0; i < LB; ++i)
+        lds_load16(to + offsetof(Stage, b) + (wave * LB + i) * 1024, offb[i] - back, pb);
+    } else {
+#pragma unroll
+      for (int i = 0; i < LA; ++i) lds_load16(to + offsetof(Stage, a) + (wave * LA + i) * 1024, offa[i], pa);
+#pragma unroll
+      for (int i = 0; i < LB; ++i) lds_load16(to + offsetof(Stage, b) + (wave * LB + i) * 1024, offb[i], pb);
+    }
+    if constexpr (SCALED_A) {
+#pragma unroll
+      for (int i = wave; i < SG * BM / 64; i += NW) {
+        const int e = i * 64, g = e / BM, r = e % BM + lane;
+        const int64_t grp = 2 * k + g < a.groups ? 2 * k + g : a.groups - 1;
+        lds_load4(to + offsetof(Stage, as) + e * 4, (uint32_t)(r < la ? r : la - 1) * 4,
+                  uniform(a.as + (a.pa[pair] * a.groups + grp) * a.M + m0));
+      }
+    }
+    if constexpr (SCALED_B) {
+#pragma unroll
+      for (int i = wave; i < SG * BN / 64; i += NW) {
+        const int e = i * 64, g = e / BN, r = e % BN + lane;
+        int64_t grp = KIND == GEMM_FP4 ? 2 * k + g : k >> 1;
+        if (grp >= a.groups) grp = a.groups - 1;
+        lds_load4(to + offsetof(Stage, bs) + e * 4, (uint32_t)(r < lb ? r : lb - 1) * 4,
+                  uniform(a.bs + (a.pb[pair] * a.groups + grp) * a.N + n0));
+      }
+    }
+  };
+
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+
+  const int r = lane & 31, g = lane >> 5, wm = (wave / WN) * TM * 32, wn = (wave % WN) * TN * 32;
+  if (s_begin < s_end) {
+    load(0, s_begin);
+    gemm_wait();
+  }
+  for (int step = s_begin; step < s_end; ++step) {
+    const int buf = (step - s_begin) & 1;
+    if (step + 1 < s_end) load(buf ^ 1, step + 1);
+    const Stage &S = st[buf];
+    const char *ra = S.a + (wm + r) * 128, *rb = S.b + (wn + r) * BB;
+    if constexpr (KIND == GEMM_FP4) {
+      const int k = a.pairs == 1 ? step : step % a.steps;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t keep = h == 0 || 2 * k + 1 < a.groups ? 0xffffffffu : 0u;
+        int sa[TM], sb[TN];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) sa[i] = (int)((S.as[h * BM + wm + i * 32 + r] & keep) >> (8 * g));
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sb[j] = (int)((S.bs[h * BN + wn + j * 32 + r] & keep) >> (8 * g));
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          const int c = ((4 * h + 2 * q + g) ^ (r & 7)) * 16;
+          i32x8 fa[TM] = {}, fb[TN] = {};
+#pragma unroll
+          for (int i = 0; i < TM; ++i) {
+            const i32x4 v = *reinterpret_cast<const i32x4 *>(ra + i * 32 * 128 + c);
+            fa[i] = __builtin_shufflevector(v, v, 0, 1, 2, 3, -1, -1, -1, -1);
+          }
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            const i32x4 v = *reinterpret_cast<const i32x4 *>(rb + j * 32 * 128 + c);
+            fb[j] = __builtin_shufflevector(v, v, 0, 1, 2, 3, -1, -1, -1, -1);
+          }
+#pragma unroll
+          for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+              if (q == 0)
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa[i], fb[j], acc[i][j], 4, 4, 0, sa[i], 0, sb[j]);
+              else
+                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa[i], fb[j], acc[i][j], 4, 4, 2, sa[i], 2, sb[j]);
+            }
+        }
+      }
+    } else {
+      u32x4 codes[KIND == GEMM_MIX ? TN : 1];
+      float scale[KIND == GEMM_MIX ? TN : 1];
+      if constexpr (KIND == GEMM_MIX) {
+        // lane group g takes block g of the step's two: the reduction runs over them side by side
+        const int k = a.pairs == 1 ? step : step % a.steps, shift = 8 * (2 * (k & 1) + g);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          codes[j] = *reinterpret_cast<const u32x4 *>(rb + j * 32 * BB + g * 16);
+          scale[j] = mx_scale((S.bs[wn + j * 32 + r] >> shift) & 255u);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int c = ((4 * g + q) ^ (r & 7)) * 16;
+        u32x4 fa[TM], fb[TN];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) fa[i] = *reinterpret_cast<const u32x4 *>(ra + i * 32 * 128 + c);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          if constexpr (KIND == GEMM_MIX)
+            fb[j] = __builtin_bit_cast(u32x4, mx_bf16(codes[j][q], scale[j]));
+          else
+            fb[j] = *reinterpret_cast<const u32x4 *>(rb + j * 32 * 128 + c);
+        }
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) {
+            if constexpr (KIND == GEMM_F16)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, fa[i]), __builtin_bit_cast(f16x8, fb[j]), acc[i][j], 0, 0, 0);
+            else
+              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[i]), __builtin_bit_cast(bf16x8, fb[j]), acc[i][j], 0, 0, 0);
+          }
+      }
+    }
+    gemm_wait();  // the next step has landed and this buffer is free
+  }
+
+  // lane (r, g): column r of a tile, rows 8 (e / 4) + 4 g + e mod 4
+  const bool parts = a.slices > 1;
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    const int64_t n = n0 + wn + j * 32 + r;
+    if (n >= a.N) continue;
+    const float add = !parts && a.bias ? (float)reinterpret_cast<const T *>(a.bias)[n] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int64_t m = m0 + wm + i * 32 + (e >> 2) * 8 + g * 4 + (e & 3);
+        if (m >= a.M) continue;
+        if (parts)
+          a.partial[((int64_t)slice * a.M + m) * a.N + n] = acc[i][j][e];
+        else
+          reinterpret_cast<T *>(a.c)[m * a.N + n] = (T)(a.bias ? acc[i][j][e] + add : acc[i][j][e]);
+      }
+  }
+}
+
+// The slices' sums, in the slices' order.
+template <typename T>
+__global__ __launch_bounds__(256) void mx_gemm_sum_kernel(GemmArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = a.M * a.N;
+  if (i >= n) return;
+  float v = a.partial[i];
+  for (int s = 1; s < a.slices; ++s) v += a.partial[s * n + i];
+  if (a.bias) v += (float)reinterpret_cast<const T *>(a.bias)[i % a.N];
+  reinterpret_cast<T *>(a.c)[i] = (T)v;
+}
+
+// Staged pieces of one element of T: bfloat16 pieces, or the binary16 number itself.
+template <typename T, bool HALF>
+struct Pieces {
+  static constexpr int P = HALF ? 1 : mx_pieces<T>();
+  static __device__ inline void of(T v, uint16_t p[P]) {
+    if constexpr (HALF) {
+      p[0] = __builtin_bit_cast(uint16_t, (_Float16)v);
+    } else {
+      __bf16 q[P];
+      mx_split<P>((float)v, q);
+#pragma unroll
+      for (int i = 0; i < P; ++i) p[i] = __builtin_bit_cast(uint16_t, q[i]);
+    }
+  }
+};
+
+// src [rows][cols] -> dst [P][rows][ld], zeros from cols to ld.
+template <typename T>
+__global__ __launch_bounds__(256) void mx_stage_kernel(const T *src, uint16_t *dst, int64_t rows, int64_t cols,
+                                                       int64_t ld) {
+  using S = Pieces<T, false>;
+  const int64_t per_row = ld / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (id >= rows * per_row) return;
+  const int64_t row = id <= 0xffffffffll ? (int64_t)((uint32_t)id / (uint32_t)per_row) : id / per_row;
+  const int64_t col = (id - row * per_row) * 8;
+  const Raw8<T> r = load8_tail(src + row * cols + col, cols - col);
+  uint16_t out[S::P][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    uint16_t p[S::P];
+    S::of(r.v[i], p);
+#pragma unroll
+    for (int k = 0; k < S::P; ++k) out[k][i] = p[k];
+  }
+#pragma unroll
+  for (int k = 0; k < S::P; ++k) __builtin_memcpy(dst + ((int64_t)k * rows + row) * ld + col, out[k], 16);
+}
+
+struct GemmPlan {
+  int tile;    // 256, 128 or 64: outputs a side of a workgroup
+  int slices;
+};
+
+// Tile and slices of the reduction for an M x N product of `total` steps, a function of the sizes
+// alone.
+inline GemmPlan gemm_plan(int64_t M, int64_t N, int64_t total) {
+  const auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
+  GemmPlan p;
+  p.tile = tiles(256) >= 192 ? 256 : (tiles(128) >= 128 ? 128 : 64);
+  const int64_t n = tiles(p.tile);
+  int64_t s = n >= 192 || n == 0 ? 1 : 512 / n;
+  if (s > total / 4) s = total / 4;
+  if (s > 16) s = 16;
+  p.slices = s < 1 ? 1 : (int)s;
+  return p;
+}
+
+inline int64_t gemm_partial_bytes(int64_t M, int64_t N, int64_t total) {
+  const GemmPlan p = gemm_plan(M, N, total);
+  return p.slices > 1 ? p.slices * M * N * 4 : 0;
+}
+
+template <GemmKind KIND, typename T>
+hipError_t gemm(GemmArgs &a, hipStream_t stream) {
+  a.total = a.steps * a.pairs;
+  const GemmPlan p = gemm_plan(a.M, a.N, a.total);
+  a.slices = p.slices;
+  const dim3 grid((unsigned)(((a.M + p.tile - 1) / p.tile) * ((a.N + p.tile - 1) / p.tile)), (unsigned)p.slices);
+  if (p.tile == 256)
+    mx_gemm_kernel<KIND, T, 2, 2, 4, 4><<<grid, 256, 0, stream>>>(a);
+  else if (p.tile == 128)
+    mx_gemm_kernel<KIND, T, 2, 2, 2, 2><<<grid, 256, 0, stream>>>(a);
+  else
+    mx_gemm_kernel<KIND, T, 2, 1, 1, 2><<<grid, 128, 0, stream>>>(a);
+  if (p.slices > 1)
+    mx_gemm_sum_kernel<T><<<(unsigned)((a.M * a.N + 255) / 256), 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace mcf

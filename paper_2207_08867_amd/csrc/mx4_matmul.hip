@@ -8,6 +8,7 @@
 // the result's.
 #include "mcf_internal.hpp"
 #include "mx4.hpp"
+#include "mx4_gemm.hpp"
 
 namespace mcf {
 namespace {
@@ -165,24 +166,112 @@ hipError_t thin_any(int dtype, const ThinArgs &a, hipStream_t stream) {
 
 }  // namespace
 
-int64_t mx4_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int a_nc, int b_nc) { return 0; }
+// Up to THIN rows of x the weight is read straight into registers; above, tiles go through LDS.
+constexpr int64_t THIN = 64;
+
+namespace {
+
+int pieces_of(int dtype) { return dtype == LM_F32 ? 3 : (dtype == LM_F16 ? 2 : 1); }
+
+// A bfloat16 x whose rows are whole groups at 16-byte addresses is multiplied where it lies; any
+// other is staged as bfloat16 pieces of padded rows.
+bool in_place(int dtype, int64_t in, const void *x) {
+  return dtype == LM_BF16 && in % MX_GROUP == 0 && (uintptr_t)x % 16 == 0;
+}
+
+int64_t stage_bytes(int dtype, int64_t batch, int64_t in) {
+  return pieces_of(dtype) * batch * mx_groups(in) * MX_GROUP * 2;
+}
+
+template <typename T>
+hipError_t mix_gemm(GemmArgs &g, int dtype, const void *x, int64_t in, void *ws, hipStream_t stream) {
+  const int64_t ld = g.groups * MX_GROUP;
+  g.a = (const char *)x;
+  if (!in_place(dtype, in, x)) {
+    mx_stage_kernel<T><<<(unsigned)((g.M * (ld / 8) + 255) / 256), 256, 0, stream>>>((const T *)x, (uint16_t *)ws, g.M,
+                                                                                     in, ld);
+    g.a = (const char *)ws;
+    g.partial = (float *)((char *)ws + stage_bytes(dtype, g.M, in));
+  }
+  g.a_ld = ld * 2;
+  g.a_plane = g.M * g.a_ld;
+  return gemm<GEMM_MIX, T>(g, stream);
+}
+
+void set_pairs(GemmArgs &g, int na, int nb) {
+  g.pairs = 0;
+  for (int j = 0; j < nb; ++j)
+    for (int i = 0; i < na; ++i) {
+      g.pa[g.pairs] = (uint8_t)i;
+      g.pb[g.pairs++] = (uint8_t)j;
+    }
+}
+
+}  // namespace
+
+int64_t mx4_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int a_nc, int b_nc) {
+  if (M <= THIN) return 0;
+  return gemm_partial_bytes(M, N, (mx_groups(K) + 1) / 2 * a_nc * b_nc);
+}
 
 hipError_t launch_mx4_matmul(int dtype, int64_t M, int64_t N, int64_t K, const void *a_codes, const void *a_scales,
                              int a_nc, const void *b_codes, const void *b_scales, int b_nc, void *ws, void *C,
                              hipStream_t stream) {
-  ThinArgs a = {a_codes, (const uint32_t *)a_scales, (const uint8_t *)b_codes, (const uint32_t *)b_scales, nullptr, C,
-                M, N, K, mx_groups(K), a_nc, b_nc};
-  return thin_any<true>(dtype, a, stream);
+  const int64_t G = mx_groups(K);
+  if (M <= THIN) {
+    ThinArgs a = {a_codes, (const uint32_t *)a_scales, (const uint8_t *)b_codes, (const uint32_t *)b_scales, nullptr, C,
+                  M, N, K, G, a_nc, b_nc};
+    return thin_any<true>(dtype, a, stream);
+  }
+  GemmArgs g = {};
+  g.a = (const char *)a_codes;
+  g.b = (const char *)b_codes;
+  g.a_ld = g.b_ld = G * 64;
+  g.a_plane = M * g.a_ld;
+  g.b_plane = N * g.b_ld;
+  g.as = (const uint32_t *)a_scales;
+  g.bs = (const uint32_t *)b_scales;
+  g.groups = G;
+  g.c = C;
+  g.partial = (float *)ws;
+  g.M = M;
+  g.N = N;
+  g.steps = (int)((G + 1) / 2);
+  set_pairs(g, a_nc, b_nc);
+  if (dtype == LM_F16) return gemm<GEMM_FP4, _Float16>(g, stream);
+  if (dtype == LM_BF16) return gemm<GEMM_FP4, __bf16>(g, stream);
+  return gemm<GEMM_FP4, float>(g, stream);
 }
 
-int64_t mx4_linear_workspace_bytes(int dtype, int nc, int64_t batch, int64_t in, int64_t out) { return 0; }
+int64_t mx4_linear_workspace_bytes(int dtype, int nc, int64_t batch, int64_t in, int64_t out) {
+  if (batch <= THIN) return 0;
+  return stage_bytes(dtype, batch, in) + gemm_partial_bytes(batch, out, mx_groups(in) * 2 * nc * pieces_of(dtype));
+}
 
 hipError_t launch_mx4_linear(int dtype, int nc, int64_t batch, int64_t in, int64_t out, const void *x,
                              const void *codes, const void *scales, const void *bias, void *ws, void *y,
                              hipStream_t stream) {
-  ThinArgs a = {x, nullptr, (const uint8_t *)codes, (const uint32_t *)scales, bias, y, batch, out, in, mx_groups(in),
-                1, nc};
-  return thin_any<false>(dtype, a, stream);
+  const int64_t G = mx_groups(in);
+  if (batch <= THIN) {
+    ThinArgs a = {x, nullptr, (const uint8_t *)codes, (const uint32_t *)scales, bias, y, batch, out, in, G, 1, nc};
+    return thin_any<false>(dtype, a, stream);
+  }
+  GemmArgs g = {};
+  g.b = (const char *)codes;
+  g.b_ld = G * 64;
+  g.b_plane = out * g.b_ld;
+  g.bs = (const uint32_t *)scales;
+  g.groups = G;
+  g.c = y;
+  g.bias = bias;
+  g.partial = (float *)ws;
+  g.M = batch;
+  g.N = out;
+  g.steps = (int)(G * 2);
+  set_pairs(g, pieces_of(dtype), nc);
+  if (dtype == LM_F16) return mix_gemm<_Float16>(g, dtype, x, in, ws, stream);
+  if (dtype == LM_BF16) return mix_gemm<__bf16>(g, dtype, x, in, ws, stream);
+  return mix_gemm<float>(g, dtype, x, in, ws, stream);
 }
 
 }  // namespace mcf

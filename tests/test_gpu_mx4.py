@@ -253,7 +253,7 @@ def test_linear_nonfinite_rows_stay_apart(mcf):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("nc", [1, 2])
+@pytest.mark.parametrize("nc", [1, 2, 3])
 @pytest.mark.parametrize("T, O, I", [(1, 1, 1), (1, 64, 128), (7, 33, 70), (64, 50, 129), (100, 99, 784), (130, 260, 300),
                                      (513, 40, 31), (300, 300, 257)])
 def test_backward(mcf, dtype, nc, T, O, I):

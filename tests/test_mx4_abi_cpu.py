@@ -92,6 +92,21 @@ def test_linear_bwd(L):
     assert f(F32, 2, 100, 784, 99, x, c, s, dy, dx, dw, db, dy, need, None) == E_ALIAS
 
 
+def test_workspace_sizes(L):
+    """Every size gives a size, empty ones included; results of nothing need none."""
+    for dtype in (F16, BF16, F32):
+        for T in (0, 1, 17, 65, 1000, 1 << 20):
+            for I in (0, 1, 128, 1000):
+                for O in (0, 1, 300, 5000):
+                    assert L.mc_mx4_matmul_workspace(dtype, T, O, I, 1, 2) >= 0
+                    assert L.mc_mx4_linear_fwd_workspace(dtype, 3, T, I, O) >= 0
+                    assert L.mc_mx4_linear_bwd_workspace(dtype, 4, T, I, O) >= 0
+    assert L.mc_mx4_linear_bwd_workspace(F32, 1, 0, 0, 0) == 0
+    assert L.mc_mx4_linear_fwd_workspace(F32, 5, 1, 1, 1) == E_NC
+    assert L.mc_mx4_linear_bwd_workspace(F32, 1, 1, 1, (1 << 20) + 1) == E_SHAPE
+    assert L.mc_distill_workspace(-1, 5) == E_SHAPE and L.mc_distill_workspace(0, 5) == 0
+
+
 def test_distill(L):
     z, ids, t, g, w, loss, stats, dz = (P(i << 26) for i in range(1, 9))
     fwd, bwd, both = L.mc_distill_fwd, L.mc_distill_bwd, L.mc_distill_fwd_bwd
