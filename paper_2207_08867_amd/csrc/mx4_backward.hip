@@ -62,13 +62,9 @@ __global__ __launch_bounds__(256) void mx_unpack_t_kernel(const uint8_t *codes, 
 
 // The pairs (i, j) of pieces with i + j < `below`.
 void set_pairs(GemmArgs &a, int na, int nb, int below) {
-  a.pairs = 0;
   for (int i = 0; i < na; ++i)
-    for (int j = 0; j < nb; ++j) {
-      if (i + j >= below) continue;
-      a.pa[a.pairs] = (uint8_t)i;
-      a.pb[a.pairs++] = (uint8_t)j;
-    }
+    for (int j = 0; j < nb; ++j)
+      if (i + j < below) gemm_pair(a, i, j);
 }
 
 // C [M][N] from staged a [na][M][ld] and b [nb][N][ld], pairs i + j < below.

@@ -35,8 +35,8 @@ struct GemmArgs {
   float *partial;                 // [slices][M][N], with more than one slice
   int64_t M, N;
   int steps, total, slices;       // steps of a pair, of all pairs; slices of the reduction
-  int pairs;
-  uint8_t pa[16], pb[16];
+  int pairs;                      // at most 16
+  uint64_t pa, pb;                // the planes of pair p, 4 bits each
 };
 
 // 16 (4) bytes a lane from base + off straight into LDS at `to` + 16 (4) lane.  The loads are
@@ -68,6 +68,21 @@ __device__ inline void gemm_tile(uint32_t id, uint32_t gm, uint32_t gn, uint32_t
   const uint32_t band = t / (8 * gn), first = band * 8, rows = gm - first < 8 ? gm - first : 8, in = t - first * gn;
   *tm = first + in % rows;
   *tn = in / rows;
+}
+
+template <GemmKind KIND, int TM, int TN>
+struct Operands {
+  u32x4 a[TM], b[KIND == GEMM_MIX ? 1 : TN];
+};
+template <GemmKind KIND, int TM, int TN>
+struct Scales {
+  uint32_t a[KIND == GEMM_FP4 ? 2 : 1][TM], b[KIND == GEMM_FP4 ? 2 : 1][TN];
+  u32x4 codes[KIND == GEMM_MIX ? TN : 1];
+  float scale[TN];
+};
+__device__ inline i32x8 widen(u32x4 v) {
+  const i32x4 w = __builtin_bit_cast(i32x4, v);
+  return __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1);
 }
 
 template <GemmKind KIND, typename T, int WM, int WN, int TM, int TN>
@@ -113,11 +128,19 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
 
   const uint32_t upper = (((lane & 7) ^ (lane >> 3)) & 4) * 16;  // 64 where this lane loads a row's upper half
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(&st[0]));
-  const auto load = [&](int buf, int step) {
-    const int pair = a.pairs == 1 ? 0 : step / a.steps, k = step - pair * a.steps;
+  // A step is step k of a pair.
+  struct At {
+    int pair, k;
+  };
+  const auto next = [&](At s, bool go) {
+    const bool wrap = s.k + 1 == a.steps;
+    return At{go && wrap ? s.pair + 1 : s.pair, go ? (wrap ? 0 : s.k + 1) : s.k};
+  };
+  const auto load = [&](int buf, At s) {
+    const int k = s.k, ia = (int)(a.pa >> (4 * s.pair)) & 15, ib = (int)(a.pb >> (4 * s.pair)) & 15;
     const uint32_t to = lds0 + buf * (uint32_t)sizeof(Stage);
-    const char *pa = uniform(a.a + a.pa[pair] * a.a_plane + m0 * a.a_ld + (int64_t)k * 128);
-    const char *pb = uniform(a.b + a.pb[pair] * a.b_plane + n0 * a.b_ld + (int64_t)k * BB);
+    const char *pa = uniform(a.a + ia * a.a_plane + m0 * a.a_ld + (int64_t)k * 128);
+    const char *pb = uniform(a.b + ib * a.b_plane + n0 * a.b_ld + (int64_t)k * BB);
     if constexpr (KIND == GEMM_FP4) {
       // an odd group count: the last step's upper half re-reads the lower one and counts for
       // nothing (its scales are taken as 0 on both sides, and 2^-254 times 36 is 0)
@@ -134,23 +157,26 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
 #pragma unroll
       for (int i = 0; i < LB; ++i) lds_load16(to + offsetof(Stage, b) + (wave * LB + i) * 1024, offb[i], pb);
     }
+    // Words of scales, 64 a load; a wavefront past the last one repeats a load, with the same data.
     if constexpr (SCALED_A) {
+      constexpr int N = SG * BM / 64;
 #pragma unroll
-      for (int i = wave; i < SG * BM / 64; i += NW) {
-        const int e = i * 64, g = e / BM, r = e % BM + lane;
+      for (int i = 0; i < (N + NW - 1) / NW; ++i) {
+        const int e = (wave + i * NW) % N * 64, g = e / BM, r = e % BM + lane;
         const int64_t grp = 2 * k + g < a.groups ? 2 * k + g : a.groups - 1;
         lds_load4(to + offsetof(Stage, as) + e * 4, (uint32_t)(r < la ? r : la - 1) * 4,
-                  uniform(a.as + (a.pa[pair] * a.groups + grp) * a.M + m0));
+                  uniform(a.as + (ia * a.groups + grp) * a.M + m0));
       }
     }
     if constexpr (SCALED_B) {
+      constexpr int N = SG * BN / 64;
 #pragma unroll
-      for (int i = wave; i < SG * BN / 64; i += NW) {
-        const int e = i * 64, g = e / BN, r = e % BN + lane;
+      for (int i = 0; i < (N + NW - 1) / NW; ++i) {
+        const int e = (wave + i * NW) % N * 64, g = e / BN, r = e % BN + lane;
         int64_t grp = KIND == GEMM_FP4 ? 2 * k + g : k >> 1;
         if (grp >= a.groups) grp = a.groups - 1;
         lds_load4(to + offsetof(Stage, bs) + e * 4, (uint32_t)(r < lb ? r : lb - 1) * 4,
-                  uniform(a.bs + (a.pb[pair] * a.groups + grp) * a.N + n0));
+                  uniform(a.bs + (ib * a.groups + grp) * a.N + n0));
       }
     }
   };
@@ -164,87 +190,112 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
 
   const int r = lane & 31, g = lane >> 5, wm = (wave / WN) * TM * 32, wn = (wave % WN) * TN * 32;
-  if (s_begin < s_end) {
-    load(0, s_begin);
-    gemm_wait();
-  }
-  for (int step = s_begin; step < s_end; ++step) {
-    const int buf = (step - s_begin) & 1;
-    if (step + 1 < s_end) load(buf ^ 1, step + 1);
+  // The operands of quarter q of a step, of which a lane holds chunk 4 g + q (16-bit kinds) or
+  // 2 q + g (FP4) of its rows, and what multiplies them.
+  Operands<KIND, TM, TN> op[2];
+  Scales<KIND, TM, TN> sc;
+  const auto read = [&](int buf, int q, Operands<KIND, TM, TN> &o) {
     const Stage &S = st[buf];
-    const char *ra = S.a + (wm + r) * 128, *rb = S.b + (wn + r) * BB;
+    const int c = ((KIND == GEMM_FP4 ? 2 * q + g : 4 * g + q) ^ (r & 7)) * 16;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) o.a[i] = *reinterpret_cast<const u32x4 *>(S.a + (wm + r + i * 32) * 128 + c);
+    if constexpr (KIND != GEMM_MIX) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) o.b[j] = *reinterpret_cast<const u32x4 *>(S.b + (wn + r + j * 32) * 128 + c);
+    }
+  };
+  const auto read_scales = [&](int buf, int k) {
+    const Stage &S = st[buf];
     if constexpr (KIND == GEMM_FP4) {
-      const int k = a.pairs == 1 ? step : step % a.steps;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint32_t keep = h == 0 || 2 * k + 1 < a.groups ? 0xffffffffu : 0u;
-        int sa[TM], sb[TN];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) sa[i] = (int)((S.as[h * BM + wm + i * 32 + r] & keep) >> (8 * g));
+        for (int i = 0; i < TM; ++i) sc.a[h][i] = (S.as[h * BM + wm + i * 32 + r] & keep) >> (8 * g);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) sb[j] = (int)((S.bs[h * BN + wn + j * 32 + r] & keep) >> (8 * g));
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const int c = ((4 * h + 2 * q + g) ^ (r & 7)) * 16;
-          i32x8 fa[TM] = {}, fb[TN] = {};
-#pragma unroll
-          for (int i = 0; i < TM; ++i) {
-            const i32x4 v = *reinterpret_cast<const i32x4 *>(ra + i * 32 * 128 + c);
-            fa[i] = __builtin_shufflevector(v, v, 0, 1, 2, 3, -1, -1, -1, -1);
-          }
-#pragma unroll
-          for (int j = 0; j < TN; ++j) {
-            const i32x4 v = *reinterpret_cast<const i32x4 *>(rb + j * 32 * 128 + c);
-            fb[j] = __builtin_shufflevector(v, v, 0, 1, 2, 3, -1, -1, -1, -1);
-          }
-#pragma unroll
-          for (int i = 0; i < TM; ++i)
-#pragma unroll
-            for (int j = 0; j < TN; ++j) {
-              if (q == 0)
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa[i], fb[j], acc[i][j], 4, 4, 0, sa[i], 0, sb[j]);
-              else
-                acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(fa[i], fb[j], acc[i][j], 4, 4, 2, sa[i], 2, sb[j]);
-            }
-        }
-      }
-    } else {
-      u32x4 codes[KIND == GEMM_MIX ? TN : 1];
-      float scale[KIND == GEMM_MIX ? TN : 1];
-      if constexpr (KIND == GEMM_MIX) {
-        // lane group g takes block g of the step's two: the reduction runs over them side by side
-        const int k = a.pairs == 1 ? step : step % a.steps, shift = 8 * (2 * (k & 1) + g);
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          codes[j] = *reinterpret_cast<const u32x4 *>(rb + j * 32 * BB + g * 16);
-          scale[j] = mx_scale((S.bs[wn + j * 32 + r] >> shift) & 255u);
-        }
-      }
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c = ((4 * g + q) ^ (r & 7)) * 16;
-        u32x4 fa[TM], fb[TN];
-#pragma unroll
-        for (int i = 0; i < TM; ++i) fa[i] = *reinterpret_cast<const u32x4 *>(ra + i * 32 * 128 + c);
-#pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          if constexpr (KIND == GEMM_MIX)
-            fb[j] = __builtin_bit_cast(u32x4, mx_bf16(codes[j][q], scale[j]));
-          else
-            fb[j] = *reinterpret_cast<const u32x4 *>(rb + j * 32 * 128 + c);
-        }
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-          for (int j = 0; j < TN; ++j) {
-            if constexpr (KIND == GEMM_F16)
-              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, fa[i]), __builtin_bit_cast(f16x8, fb[j]), acc[i][j], 0, 0, 0);
-            else
-              acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[i]), __builtin_bit_cast(bf16x8, fb[j]), acc[i][j], 0, 0, 0);
-          }
+        for (int j = 0; j < TN; ++j) sc.b[h][j] = (S.bs[h * BN + wn + j * 32 + r] & keep) >> (8 * g);
       }
     }
-    gemm_wait();  // the next step has landed and this buffer is free
+    if constexpr (KIND == GEMM_MIX) {
+      // lane group g takes block g of the step's two: the reduction runs over them side by side
+      const int shift = 8 * (2 * (k & 1) + g);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        sc.codes[j] = *reinterpret_cast<const u32x4 *>(S.b + (wn + r + j * 32) * BB + g * 16);
+        sc.scale[j] = mx_scale((S.bs[wn + j * 32 + r] >> shift) & 255u);
+      }
+    }
+  };
+  const auto multiply = [&](int q, const Operands<KIND, TM, TN> &o) {
+    u32x4 fb[TN];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      if constexpr (KIND == GEMM_MIX)
+        fb[j] = __builtin_bit_cast(u32x4, mx_bf16(sc.codes[j][q], sc.scale[j]));
+      else
+        fb[j] = o.b[j];
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        f32x16 &c = acc[i][j];
+        if constexpr (KIND == GEMM_FP4) {
+          const i32x8 x = widen(o.a[i]), y = widen(fb[j]);
+          const int sa = (int)sc.a[q >> 1][i], sb = (int)sc.b[q >> 1][j];
+          if ((q & 1) == 0)
+            c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 0, sa, 0, sb);
+          else
+            c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 2, sa, 2, sb);
+        } else if constexpr (KIND == GEMM_F16) {
+          c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, o.a[i]), __builtin_bit_cast(f16x8, fb[j]), c, 0, 0, 0);
+        } else {
+          c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, o.a[i]), __builtin_bit_cast(bf16x8, fb[j]), c, 0, 0, 0);
+        }
+      }
+  };
+  // Reads of the next quarter between the products of this one.
+  const auto weave = [&]() {
+    constexpr int READS = TM + (KIND == GEMM_MIX ? 0 : TN), EACH = TM * TN / READS > 0 ? TM * TN / READS : 1;
+#pragma unroll
+    for (int i = 0; i < READS; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+    }
+  };
+
+  if (s_begin < s_end) {
+    const int last = s_end - 1;
+    At here = {s_begin / a.steps, s_begin % a.steps}, ahead = next(here, s_begin < last);
+    load(0, here);
+    gemm_wait();
+    load(1, ahead);
+    read_scales(0, here.k);
+    read(0, 0, op[0]);
+    for (int step = s_begin; step < s_end; ++step) {
+      const int buf = (step - s_begin) & 1;
+      read(buf, 1, op[1]);
+      multiply(0, op[0]);
+      weave();
+      read(buf, 2, op[0]);
+      multiply(1, op[1]);
+      weave();
+      read(buf, 3, op[1]);
+      multiply(2, op[0]);
+      weave();
+      // Every read of this buffer is out.  Once all wavefronts are here the next step's buffer has
+      // landed and this one is free; the last quarter's products cover the first reads.  Past the
+      // end the last step is loaded and read again, and not multiplied.
+      gemm_wait();
+      here = ahead;
+      ahead = next(ahead, step + 2 <= last);
+      load(buf, ahead);
+      read(buf ^ 1, 0, op[0]);
+      multiply(3, op[1]);
+      weave();
+      read_scales(buf ^ 1, here.k);
+    }
+    gemm_wait();  // no load may land after the workgroup has left
   }
 
   // lane (r, g): column r of a tile, rows 8 (e / 4) + 4 g + e mod 4
@@ -321,6 +372,11 @@ struct GemmPlan {
   int tile;    // 256, 128 or 64: outputs a side of a workgroup
   int slices;
 };
+
+inline void gemm_pair(GemmArgs &a, int i, int j) {
+  a.pa |= (uint64_t)i << (4 * a.pairs);
+  a.pb |= (uint64_t)j << (4 * a.pairs++);
+}
 
 // Tile and slices of the reduction for an M x N product of `total` steps, a function of the sizes
 // alone.

@@ -199,12 +199,8 @@ hipError_t mix_gemm(GemmArgs &g, int dtype, const void *x, int64_t in, void *ws,
 }
 
 void set_pairs(GemmArgs &g, int na, int nb) {
-  g.pairs = 0;
   for (int j = 0; j < nb; ++j)
-    for (int i = 0; i < na; ++i) {
-      g.pa[g.pairs] = (uint8_t)i;
-      g.pb[g.pairs++] = (uint8_t)j;
-    }
+    for (int i = 0; i < na; ++i) gemm_pair(g, i, j);
 }
 
 }  // namespace
