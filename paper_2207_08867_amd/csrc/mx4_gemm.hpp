@@ -70,6 +70,37 @@ __device__ inline void gemm_tile(uint32_t id, uint32_t gm, uint32_t gn, uint32_t
   *tn = in / rows;
 }
 
+// A wavefront's tiles to `to`, its first element in the M x N result; `rows` and `cols` are what is
+// left of the result there.  Lane (r, g) holds column r of a tile, rows 8 (e / 4) + 4 g + e mod 4.
+// A row's start is scalar arithmetic, the lane's part a 32-bit offset.
+template <typename T, int TM, int TN>
+__device__ inline void gemm_store(const f32x16 (&acc)[TM][TN], T *to, const T *bias, int64_t ld, int rows, int cols) {
+  const int lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5;
+  const uint32_t off = (uint32_t)(4 * g * ld + r);
+  if (rows >= 32 * TM && cols >= 32 * TN) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        T *row = to + (i * 32 + (e >> 2) * 8 + (e & 3)) * ld;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) row[off + j * 32] = (T)(bias ? acc[i][j][e] + (float)bias[j * 32 + r] : acc[i][j][e]);
+      }
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int m = i * 32 + (e >> 2) * 8 + (e & 3);
+      T *row = to + m * ld;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        if (m + 4 * g < rows && j * 32 + r < cols)
+          row[off + j * 32] = (T)(bias ? acc[i][j][e] + (float)bias[j * 32 + r] : acc[i][j][e]);
+    }
+}
+
 template <GemmKind KIND, int TM, int TN>
 struct Operands {
   u32x4 a[TM], b[KIND == GEMM_MIX ? 1 : TN];
@@ -91,12 +122,12 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
   constexpr int BB = KIND == GEMM_MIX ? 32 : 128;  // bytes of a row of B in a step
   constexpr bool SCALED_A = KIND == GEMM_FP4, SCALED_B = KIND == GEMM_FP4 || KIND == GEMM_MIX;
   constexpr int SG = KIND == GEMM_FP4 ? 2 : 1;     // words of scales of a row in a step
-  struct Stage {
+  struct alignas(128) Stage {
     char a[BM * 128];
     char b[BN * BB];
     uint32_t as[SCALED_A ? SG * BM : 1], bs[SCALED_B ? SG * BN : 1];
   };
-  __shared__ __attribute__((aligned(128))) Stage st[2];
+  __shared__ Stage st[2];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t tm, tn;
@@ -109,7 +140,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
   constexpr int LA = BM / 8 / NW, LB = BN * BB / 1024 / NW;
   static_assert(BM % (8 * NW) == 0 && (BN * BB) % (1024 * NW) == 0, "whole loads a wavefront");
   uint32_t offa[LA], offb[LB];
-  const int64_t la = a.M - m0, lb = a.N - n0;  // rows left
+  const int64_t la = a.M - m0 < BM ? a.M - m0 : BM, lb = a.N - n0 < BN ? a.N - n0 : BN;  // rows left
 #pragma unroll
   for (int i = 0; i < LA; ++i) {
     const int r = (wave * LA + i) * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
@@ -298,25 +329,13 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
     gemm_wait();  // no load may land after the workgroup has left
   }
 
-  // lane (r, g): column r of a tile, rows 8 (e / 4) + 4 g + e mod 4
-  const bool parts = a.slices > 1;
-#pragma unroll
-  for (int j = 0; j < TN; ++j) {
-    const int64_t n = n0 + wn + j * 32 + r;
-    if (n >= a.N) continue;
-    const float add = !parts && a.bias ? (float)reinterpret_cast<const T *>(a.bias)[n] : 0.0f;
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int64_t m = m0 + wm + i * 32 + (e >> 2) * 8 + g * 4 + (e & 3);
-        if (m >= a.M) continue;
-        if (parts)
-          a.partial[((int64_t)slice * a.M + m) * a.N + n] = acc[i][j][e];
-        else
-          reinterpret_cast<T *>(a.c)[m * a.N + n] = (T)(a.bias ? acc[i][j][e] + add : acc[i][j][e]);
-      }
-  }
+  const int64_t at = (m0 + wm) * a.N + n0 + wn;
+  if (a.slices > 1)
+    gemm_store<float, TM, TN>(acc, a.partial + slice * a.M * a.N + at, nullptr, a.N, (int)la - wm, (int)lb - wn);
+  else
+    gemm_store<T, TM, TN>(acc, reinterpret_cast<T *>(a.c) + at,
+                          a.bias ? reinterpret_cast<const T *>(a.bias) + n0 + wn : nullptr, a.N, (int)la - wm,
+                          (int)lb - wn);
 }
 
 // The slices' sums, in the slices' order.
