@@ -9,8 +9,8 @@
 // A workgroup computes BM x BN outputs, WM x WN wavefronts TM x TN tiles of 32 x 32 each.  A step
 // brings 128 bytes of every row of A (256 codes or 64 16-bit numbers) and as much of the reduction
 // of B into LDS by direct loads (no registers in between) while the step before is multiplied: two
-// buffers, one barrier a step.  Chunk c (16 bytes) of row r lies at position c ^ (r mod 8) of its
-// row, so the eight lanes that LDS serves together read eight different groups of four banks.
+// buffers, one barrier a step.  Chunk c (16 bytes) of row r lies at position c ^ (r / 2 mod 8) of
+// its row: 16 neighbouring rows' chunks c lie in 16 different groups of four of the 64 banks.
 //
 // What bounds it: the matrix instructions.  A wavefront tile of 128 x 128 reads 8 x 1 KiB of LDS
 // for 16 instructions, half of LDS's rate; the tile's 64 KiB a step are fetched over the L2 at 32
@@ -138,26 +138,28 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
 
   // what this lane loads in a step: rows past the end repeat the last one
   constexpr int LA = BM / 8 / NW, LB = BN * BB / 1024 / NW;
+  static_assert(LA % 2 == 0 && (BB != 128 || LB % 2 == 0), "rows of a load start at a multiple of 16 or 8 past one");
   static_assert(BM % (8 * NW) == 0 && (BN * BB) % (1024 * NW) == 0, "whole loads a wavefront");
   uint32_t offa[LA], offb[LB];
   const int64_t la = a.M - m0 < BM ? a.M - m0 : BM, lb = a.N - n0 < BN ? a.N - n0 : BN;  // rows left
 #pragma unroll
   for (int i = 0; i < LA; ++i) {
-    const int r = (wave * LA + i) * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
+    const int r = (wave * LA + i) * 8 + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
     offa[i] = (uint32_t)((r < la ? r : la - 1) * a.a_ld) + c * 16;
   }
 #pragma unroll
   for (int i = 0; i < LB; ++i) {
     int r, c;
     if constexpr (BB == 128) {
-      r = (wave * LB + i) * 8 + (lane >> 3), c = (lane & 7) ^ (r & 7);
+      r = (wave * LB + i) * 8 + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
     } else {
       r = (wave * LB + i) * 32 + (lane >> 1), c = lane & 1;
     }
     offb[i] = (uint32_t)((r < lb ? r : lb - 1) * a.b_ld) + c * 16;
   }
 
-  const uint32_t upper = (((lane & 7) ^ (lane >> 3)) & 4) * 16;  // 64 where this lane loads a row's upper half
+  // 64 where this lane's even-numbered (odd-numbered) loads are of a row's upper half
+  const uint32_t upper[2] = {((uint32_t)lane & 4) * 16, (~(uint32_t)lane & 4) * 16};
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_address(&st[0]));
   // A step is step k of a pair.
   struct At {
@@ -175,13 +177,14 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
     if constexpr (KIND == GEMM_FP4) {
       // an odd group count: the last step's upper half re-reads the lower one and counts for
       // nothing (its scales are taken as 0 on both sides, and 2^-254 times 36 is 0)
-      const uint32_t back = 2 * k + 1 < a.groups ? 0 : upper;
+      const bool whole = 2 * k + 1 < a.groups;
+      const uint32_t back[2] = {whole ? 0 : upper[0], whole ? 0 : upper[1]};
 #pragma unroll
       for (int i = 0; i < LA; ++i)
-        lds_load16(to + offsetof(Stage, a) + (wave * LA + i) * 1024, offa[i] - back, pa);
+        lds_load16(to + offsetof(Stage, a) + (wave * LA + i) * 1024, offa[i] - back[i & 1], pa);
 #pragma unroll
       for (int i = 0; i < LB; ++i)
-        lds_load16(to + offsetof(Stage, b) + (wave * LB + i) * 1024, offb[i] - back, pb);
+        lds_load16(to + offsetof(Stage, b) + (wave * LB + i) * 1024, offb[i] - back[i & 1], pb);
     } else {
 #pragma unroll
       for (int i = 0; i < LA; ++i) lds_load16(to + offsetof(Stage, a) + (wave * LA + i) * 1024, offa[i], pa);
@@ -227,7 +230,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
   Scales<KIND, TM, TN> sc;
   const auto read = [&](int buf, int q, Operands<KIND, TM, TN> &o) {
     const Stage &S = st[buf];
-    const int c = ((KIND == GEMM_FP4 ? 2 * q + g : 4 * g + q) ^ (r & 7)) * 16;
+    const int c = ((KIND == GEMM_FP4 ? 2 * q + g : 4 * g + q) ^ ((r >> 1) & 7)) * 16;
 #pragma unroll
     for (int i = 0; i < TM; ++i) o.a[i] = *reinterpret_cast<const u32x4 *>(S.a + (wm + r + i * 32) * 128 + c);
     if constexpr (KIND != GEMM_MIX) {
@@ -423,7 +426,7 @@ hipError_t gemm(GemmArgs &a, hipStream_t stream) {
   a.slices = p.slices;
   const dim3 grid((unsigned)(((a.M + p.tile - 1) / p.tile) * ((a.N + p.tile - 1) / p.tile)), (unsigned)p.slices);
   if (p.tile == 256)
-    mx_gemm_kernel<KIND, T, 2, 2, 4, 4><<<grid, 256, 0, stream>>>(a);
+    mx_gemm_kernel<KIND, T, 2, 4, 4, 2><<<grid, 512, 0, stream>>>(a);
   else if (p.tile == 128)
     mx_gemm_kernel<KIND, T, 2, 2, 2, 2><<<grid, 256, 0, stream>>>(a);
   else
