@@ -7,9 +7,9 @@
 // cycles of a SIMD at the full rate), so the kinds share tiles, staging and schedule.
 //
 // A workgroup computes BM x BN outputs, WM x WN wavefronts TM x TN tiles of 32 x 32 each.  A step
-// brings 128 bytes of every row of A (256 codes or 64 16-bit numbers) and as much of the reduction
-// of B into LDS by direct loads (no registers in between) while the step before is multiplied: two
-// buffers, one barrier a step.  Chunk c (16 bytes) of row r lies at position c ^ (r / 2 mod 8) of
+// is 128 bytes of every row of A (256 codes or 64 16-bit numbers) and as much of the reduction of
+// B.  Steps go into a ring of S LDS buffers by direct loads (no registers in between), S - 1 steps
+// ahead of the products; one barrier a step.  Chunk c (16 bytes) of row r lies at position c ^ (r / 2 mod 8) of
 // its row: 16 neighbouring rows' chunks c lie in 16 different groups of four of the 64 banks.
 //
 // What bounds it: the matrix instructions.  A wavefront tile of 128 x 128 reads 8 x 1 KiB of LDS
@@ -53,7 +53,12 @@ __device__ inline const char *uniform(const void *p) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
   return (const char *)((uint64_t)hi << 32 | lo);
 }
-__device__ inline void gemm_wait() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+// All but the youngest LEFT loads of this wavefront have landed and its LDS reads are done; then
+// the workgroup's barrier.
+template <int LEFT>
+__device__ inline void gemm_wait() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+}
 
 __device__ inline uint32_t lds_address(const void *p) {
   return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p;
@@ -116,7 +121,7 @@ __device__ inline i32x8 widen(u32x4 v) {
   return __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1);
 }
 
-template <GemmKind KIND, typename T, int WM, int WN, int TM, int TN>
+template <GemmKind KIND, typename T, int WM, int WN, int TM, int TN, int S>
 __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NW = WM * WN;
   constexpr int BB = KIND == GEMM_MIX ? 32 : 128;  // bytes of a row of B in a step
@@ -127,7 +132,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
     char b[BN * BB];
     uint32_t as[SCALED_A ? SG * BM : 1], bs[SCALED_B ? SG * BN : 1];
   };
-  __shared__ Stage st[2];
+  __shared__ Stage st[S];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t tm, tn;
@@ -137,9 +142,11 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
   const int s_begin = (int)((int64_t)a.total * slice / a.slices), s_end = (int)((int64_t)a.total * (slice + 1) / a.slices);
 
   // what this lane loads in a step: rows past the end repeat the last one
-  constexpr int LA = BM / 8 / NW, LB = BN * BB / 1024 / NW;
+  constexpr int NB = BN * BB / 1024, LA = BM / 8 / NW, LB = (NB + NW - 1) / NW;
+  constexpr int LOADS = LA + LB + (SCALED_A ? (SG * BM / 64 + NW - 1) / NW : 0) + (SCALED_B ? (SG * BN / 64 + NW - 1) / NW : 0);
+  static_assert(LOADS * (S - 1) < 64, "vmcnt counts to 63");
   static_assert(LA % 2 == 0 && (BB != 128 || LB % 2 == 0), "rows of a load start at a multiple of 16 or 8 past one");
-  static_assert(BM % (8 * NW) == 0 && (BN * BB) % (1024 * NW) == 0, "whole loads a wavefront");
+  static_assert(BM % (8 * NW) == 0 && (BB != 128 || NB % NW == 0), "whole loads a wavefront");
   uint32_t offa[LA], offb[LB];
   const int64_t la = a.M - m0 < BM ? a.M - m0 : BM, lb = a.N - n0 < BN ? a.N - n0 : BN;  // rows left
 #pragma unroll
@@ -153,7 +160,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
     if constexpr (BB == 128) {
       r = (wave * LB + i) * 8 + (lane >> 3), c = (lane & 7) ^ ((r >> 1) & 7);
     } else {
-      r = (wave * LB + i) * 32 + (lane >> 1), c = lane & 1;
+      r = (wave * LB + i) % NB * 32 + (lane >> 1), c = lane & 1;  // past the last one: again
     }
     offb[i] = (uint32_t)((r < lb ? r : lb - 1) * a.b_ld) + c * 16;
   }
@@ -189,7 +196,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
 #pragma unroll
       for (int i = 0; i < LA; ++i) lds_load16(to + offsetof(Stage, a) + (wave * LA + i) * 1024, offa[i], pa);
 #pragma unroll
-      for (int i = 0; i < LB; ++i) lds_load16(to + offsetof(Stage, b) + (wave * LB + i) * 1024, offb[i], pb);
+      for (int i = 0; i < LB; ++i) lds_load16(to + offsetof(Stage, b) + (wave * LB + i) % NB * 1024, offb[i], pb);
     }
     // Words of scales, 64 a load; a wavefront past the last one repeats a load, with the same data.
     if constexpr (SCALED_A) {
@@ -229,25 +236,25 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
   Operands<KIND, TM, TN> op[2];
   Scales<KIND, TM, TN> sc;
   const auto read = [&](int buf, int q, Operands<KIND, TM, TN> &o) {
-    const Stage &S = st[buf];
+    const Stage &B = st[buf];
     const int c = ((KIND == GEMM_FP4 ? 2 * q + g : 4 * g + q) ^ ((r >> 1) & 7)) * 16;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) o.a[i] = *reinterpret_cast<const u32x4 *>(S.a + (wm + r + i * 32) * 128 + c);
+    for (int i = 0; i < TM; ++i) o.a[i] = *reinterpret_cast<const u32x4 *>(B.a + (wm + r + i * 32) * 128 + c);
     if constexpr (KIND != GEMM_MIX) {
 #pragma unroll
-      for (int j = 0; j < TN; ++j) o.b[j] = *reinterpret_cast<const u32x4 *>(S.b + (wn + r + j * 32) * 128 + c);
+      for (int j = 0; j < TN; ++j) o.b[j] = *reinterpret_cast<const u32x4 *>(B.b + (wn + r + j * 32) * 128 + c);
     }
   };
   const auto read_scales = [&](int buf, int k) {
-    const Stage &S = st[buf];
+    const Stage &B = st[buf];
     if constexpr (KIND == GEMM_FP4) {
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         const uint32_t keep = h == 0 || 2 * k + 1 < a.groups ? 0xffffffffu : 0u;
 #pragma unroll
-        for (int i = 0; i < TM; ++i) sc.a[h][i] = (S.as[h * BM + wm + i * 32 + r] & keep) >> (8 * g);
+        for (int i = 0; i < TM; ++i) sc.a[h][i] = (B.as[h * BM + wm + i * 32 + r] & keep) >> (8 * g);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) sc.b[h][j] = (S.bs[h * BN + wn + j * 32 + r] & keep) >> (8 * g);
+        for (int j = 0; j < TN; ++j) sc.b[h][j] = (B.bs[h * BN + wn + j * 32 + r] & keep) >> (8 * g);
       }
     }
     if constexpr (KIND == GEMM_MIX) {
@@ -255,8 +262,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
       const int shift = 8 * (2 * (k & 1) + g);
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        sc.codes[j] = *reinterpret_cast<const u32x4 *>(S.b + (wn + r + j * 32) * BB + g * 16);
-        sc.scale[j] = mx_scale((S.bs[wn + j * 32 + r] >> shift) & 255u);
+        sc.codes[j] = *reinterpret_cast<const u32x4 *>(B.b + (wn + r + j * 32) * BB + g * 16);
+        sc.scale[j] = mx_scale((B.bs[wn + j * 32 + r] >> shift) & 255u);
       }
     }
   };
@@ -300,14 +307,18 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
 
   if (s_begin < s_end) {
     const int last = s_end - 1;
-    At here = {s_begin / a.steps, s_begin % a.steps}, ahead = next(here, s_begin < last);
-    load(0, here);
-    gemm_wait();
-    load(1, ahead);
-    read_scales(0, here.k);
+    At here = {s_begin / a.steps, s_begin % a.steps}, ahead = here;
+    int k = here.k, buf = 0;
+#pragma unroll
+    for (int i = 0; i < S; ++i) {
+      load(i, ahead);
+      ahead = next(ahead, s_begin + i < last);
+    }
+    gemm_wait<LOADS * (S - 1)>();
+    read_scales(0, k);
     read(0, 0, op[0]);
     for (int step = s_begin; step < s_end; ++step) {
-      const int buf = (step - s_begin) & 1;
+      const int then = buf + 1 == S ? 0 : buf + 1;
       read(buf, 1, op[1]);
       multiply(0, op[0]);
       weave();
@@ -320,16 +331,17 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
       // Every read of this buffer is out.  Once all wavefronts are here the next step's buffer has
       // landed and this one is free; the last quarter's products cover the first reads.  Past the
       // end the last step is loaded and read again, and not multiplied.
-      gemm_wait();
-      here = ahead;
-      ahead = next(ahead, step + 2 <= last);
+      gemm_wait<LOADS * (S - 2)>();
       load(buf, ahead);
-      read(buf ^ 1, 0, op[0]);
+      ahead = next(ahead, step + S < last);
+      read(then, 0, op[0]);
       multiply(3, op[1]);
       weave();
-      read_scales(buf ^ 1, here.k);
+      if (step < last) k = k + 1 == a.steps ? 0 : k + 1;
+      read_scales(then, k);
+      buf = then;
     }
-    gemm_wait();  // no load may land after the workgroup has left
+    gemm_wait<0>();  // no load may land after the workgroup has left
   }
 
   const int64_t at = (m0 + wm) * a.N + n0 + wn;
@@ -390,28 +402,45 @@ __global__ __launch_bounds__(256) void mx_stage_kernel(const T *src, uint16_t *d
   for (int k = 0; k < S::P; ++k) __builtin_memcpy(dst + ((int64_t)k * rows + row) * ld + col, out[k], 16);
 }
 
-struct GemmPlan {
-  int tile;    // 256, 128 or 64: outputs a side of a workgroup
-  int slices;
-};
-
 inline void gemm_pair(GemmArgs &a, int i, int j) {
   a.pa |= (uint64_t)i << (4 * a.pairs);
   a.pb |= (uint64_t)j << (4 * a.pairs++);
 }
 
-// Tile and slices of the reduction for an M x N product of `total` steps, a function of the sizes
-// alone.
+struct GemmPlan {
+  int tile;    // 256, 128 or 64: outputs a side of a workgroup
+  int slices;  // of the reduction
+};
+
+// Tile and slices for an M x N product of `total` steps: the least time by this model, a function of
+// the sizes alone.  Measured (us): a step of a grid of 256 workgroups, and of one of 512, which two
+// of the smaller tiles' workgroups a CU share; and what a launch costs besides its steps.  The
+// kinds differ by up to a fifth, mostly alike.
 inline GemmPlan gemm_plan(int64_t M, int64_t N, int64_t total) {
-  const auto tiles = [&](int64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
-  GemmPlan p;
-  p.tile = tiles(256) >= 192 ? 256 : (tiles(128) >= 128 ? 128 : 64);
-  const int64_t n = tiles(p.tile);
-  int64_t s = n >= 192 || n == 0 ? 1 : 512 / n;
-  if (s > total / 4) s = total / 4;
-  if (s > 16) s = 16;
-  p.slices = s < 1 ? 1 : (int)s;
-  return p;
+  struct Row {
+    int tile;
+    double step1, step2, fixed;
+  };
+  constexpr Row rows[3] = {{256, 1.7, 3.4, 9.0}, {128, 0.6, 1.0, 5.0}, {64, 0.33, 0.45, 3.0}};
+  GemmPlan best = {64, 1};
+  double least = 1e300;
+  for (const Row &r : rows) {
+    const int64_t tiles = ((M + r.tile - 1) / r.tile) * ((N + r.tile - 1) / r.tile);
+    for (int slices : {1, 2, 3, 4, 6, 8, 12, 16}) {
+      // a slice keeps four steps or more; the partial sums stay below 2^28 bytes
+      if (slices > 1 && (total < 4 * slices || (double)M * (double)N * slices > 67108864.0)) break;
+      const int64_t n = tiles * slices, full = n / 512, rest = n % 512;
+      const double steps = (double)((total + slices - 1) / slices);
+      double t = r.fixed + steps * ((double)full * r.step2 + (rest > 256 ? r.step2 : (rest > 0 ? r.step1 : 0.0)));
+      // the slices' sum: a launch, and its reads and writes at 4 TB/s
+      if (slices > 1) t += 3.0 + (double)M * (double)N * (4.0 * slices + 4.0) / 4e6;
+      if (t < least) {
+        least = t;
+        best = {r.tile, slices};
+      }
+    }
+  }
+  return best;
 }
 
 inline int64_t gemm_partial_bytes(int64_t M, int64_t N, int64_t total) {
@@ -426,11 +455,11 @@ hipError_t gemm(GemmArgs &a, hipStream_t stream) {
   a.slices = p.slices;
   const dim3 grid((unsigned)(((a.M + p.tile - 1) / p.tile) * ((a.N + p.tile - 1) / p.tile)), (unsigned)p.slices);
   if (p.tile == 256)
-    mx_gemm_kernel<KIND, T, 2, 4, 4, 2><<<grid, 512, 0, stream>>>(a);
+    mx_gemm_kernel<KIND, T, 2, 4, 4, 2, 2><<<grid, 512, 0, stream>>>(a);
   else if (p.tile == 128)
-    mx_gemm_kernel<KIND, T, 2, 2, 2, 2><<<grid, 256, 0, stream>>>(a);
+    mx_gemm_kernel<KIND, T, 2, 2, 2, 2, 2><<<grid, 256, 0, stream>>>(a);
   else
-    mx_gemm_kernel<KIND, T, 2, 1, 1, 2><<<grid, 128, 0, stream>>>(a);
+    mx_gemm_kernel<KIND, T, 2, 2, 1, 1, 4><<<grid, 256, 0, stream>>>(a);
   if (p.slices > 1)
     mx_gemm_sum_kernel<T><<<(unsigned)((a.M * a.N + 255) / 256), 256, 0, stream>>>(a);
   return hipGetLastError();
