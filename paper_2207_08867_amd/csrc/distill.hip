@@ -98,7 +98,7 @@ __device__ inline float logit(const DistillArgs &a, const T *z, int64_t col) {
   return v;
 }
 
-// Joins over the workgroup in a fixed order; every thread gets the result.  `lds`: NT / 64 slots.
+// Joins over the workgroup in a fixed order; every thread gets the result.
 template <typename T, int NT>
 __device__ inline MaxSum block_join(const DistillArgs &a, MaxSum r, MaxSum *lds) {
 #pragma unroll
@@ -109,207 +109,282 @@ __device__ inline MaxSum block_join(const DistillArgs &a, MaxSum r, MaxSum *lds)
     // both sides join in the lower lane's order, so the lanes agree
     r = (threadIdx.x & d) ? join<T>(a, o, r) : join<T>(a, r, o);
   }
-  if constexpr (NT > 64) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = r;
-    __syncthreads();
-    r = lds[0];
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = r;
+  __syncthreads();
+  r = lds[0];
 #pragma unroll
-    for (int w = 1; w < NT / 64; ++w) r = join<T>(a, r, lds[w]);
-  }
+  for (int w = 1; w < NT / 64; ++w) r = join<T>(a, r, lds[w]);
   return r;
 }
 
-__device__ inline float combine(float a, float b) { return fmaxf(a, b); }
-__device__ inline double combine(double a, double b) { return a + b; }
-
-// The maximum of binary32 values, the sum of binary64 ones.
-template <int NT, typename V>
-__device__ inline V block_reduce(V v, V *lds) {
+__device__ inline float wave_max(float v) {
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v = combine(v, __shfl_xor(v, d));
-  if constexpr (NT > 64) {
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = lds[0];
+  for (int d = 1; d < 64; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+__device__ inline double wave_sum(double v) {
 #pragma unroll
-    for (int w = 1; w < NT / 64; ++w) v = combine(v, lds[w]);
-  }
+  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
   return v;
 }
 
+// A row's teacher entries, worked out by the first wavefront while the row is on its way:
+// e = exp((t - top) / T), 0 where unused; all = the sum of the e of every entry with this id; the
+// teacher's softmax is p = e / sum.  The k entries' sums and the loss are binary64: they are few, the
+// divergence is a small difference of large logarithms, and where a mask of the type's lowest value
+// meets a teacher's entry the terms come up to binary32's largest number.
 template <int NT>
 struct Shared {
   MaxSum join[NT / 64];
-  float top[NT / 64];
-  double sum[NT / 64];
-  int id[1024];
-  float e[1024];
+  double sum;  // of the used entries' e; 0: none counts
+  float top;   // the largest used t
 };
+// The entries' arrays, 16 k bytes of LDS.
+extern __shared__ float entry_space[];
+#define ENTRIES                                                       \
+  [[maybe_unused]] int *const eid = (int *)entry_space;               \
+  [[maybe_unused]] float *const ee = entry_space + a.k;               \
+  [[maybe_unused]] float *const eall = ee + a.k, *const ez = eall + a.k
 
-struct Teacher {
-  float top;    // the largest used t
-  double sum;   // of the used entries' exp((t - top) / T)
-  float inv;    // 1 / sum; 0: no entry counts
+// What lanes of a wavefront wrote to LDS is there for its other lanes.
+__device__ inline void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// The sum of the e of the entries with this id, in the entries' order.
+__device__ inline float same_id(const DistillArgs &a, int id) {
+  ENTRIES;
+  float all = 0.0f;
+  int j = 0;
+  for (; j + 8 <= a.k; j += 8) {
+    int other[8];
+    float e[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) other[i] = eid[j + i], e[i] = ee[j + i];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) all += other[i] == id ? e[i] : 0.0f;
+  }
+  for (; j < a.k; ++j) all += eid[j] == id ? ee[j] : 0.0f;
+  return all;
+}
+
+// The first entry of a lane, loaded ahead of the row so that it does not wait for it.
+template <typename T>
+struct First {
+  int id;
+  T t;
 };
-
-// The teacher's softmax: p = e / sum; e and id of every entry into LDS (e = 0, id = -1 where
-// unused).  The k entries' sums and the loss are binary64: they are few, the divergence is a
-// small difference of large logarithms, and where a mask of the type's lowest value meets a
-// teacher's entry the terms come up to binary32's largest number.
-template <typename T, int NT>
-__device__ inline Teacher teacher(const DistillArgs &a, int64_t row, Shared<NT> &sh) {
-  const T *t = reinterpret_cast<const T *>(a.t) + row * a.k;
-  const int32_t *ids = a.ids + row * a.k;
-  float top = -FLT_MAX;
-  for (int i = threadIdx.x; i < a.k; i += NT) {
-    const int id = ids[i];
-    const bool used = id >= 0 && id < a.vocab;
-    const float v = used ? (float)t[i] : -INFINITY;
-    sh.id[i] = used ? id : -1;
-    sh.e[i] = v;
-    top = fmaxf(top, v);
+template <typename T>
+__device__ inline First<T> first_entry(const DistillArgs &a, int64_t row) {
+  First<T> f = {-1, (T)0.0f};
+  if ((int)threadIdx.x < a.k && threadIdx.x < 64) {
+    f.id = a.ids[row * a.k + threadIdx.x];
+    f.t = reinterpret_cast<const T *>(a.t)[row * a.k + threadIdx.x];
   }
-  top = block_reduce<NT>(top, sh.top);
-  double sum = 0.0;
-  for (int i = threadIdx.x; i < a.k; i += NT) {
-    const float e = expz<float>(a, sh.e[i] - top);
-    sh.e[i] = e;
-    sum += (double)e;
-  }
-  __syncthreads();
-  Teacher r;
-  r.top = top;
-  r.sum = block_reduce<NT>(sum, sh.sum);
-  r.inv = r.sum == 0.0 ? 0.0f : (float)(1.0 / r.sum);  // a NaN stays one
-  return r;
+  return f;
 }
 
 template <typename T, bool ONE, int NT>
-__device__ inline float row_loss(const DistillArgs &a, int64_t row, const T *z, const Teacher &te, const MaxSum &st,
-                                 Shared<NT> &sh) {
+__device__ inline void teacher(const DistillArgs &a, int64_t row, const T *z, const First<T> &f, Shared<NT> &sh) {
+  ENTRIES;
+  if (threadIdx.x < 64) {
+    float top = -FLT_MAX;
+    for (int i = threadIdx.x; i < a.k; i += 64) {
+      const int id = i < 64 ? f.id : a.ids[row * a.k + i];
+      const T t = i < 64 ? f.t : reinterpret_cast<const T *>(a.t)[row * a.k + i];
+      const bool used = id >= 0 && id < a.vocab;
+      const float v = used ? (float)t : -INFINITY;
+      eid[i] = used ? id : -1;
+      ee[i] = v;
+      top = fmaxf(top, v);
+    }
+    top = wave_max(top);
+    double sum = 0.0;
+    for (int i = threadIdx.x; i < a.k; i += 64) {
+      const float e = expz<float>(a, ee[i] - top);
+      ee[i] = e;
+      sum += (double)e;
+    }
+    sum = wave_sum(sum);
+    if (threadIdx.x == 0) sh.top = top, sh.sum = sum;
+  }
+  // the logits at the entries and the sums of equal ids: up to 64 entries by the one wavefront that
+  // wrote them, more by all
+  if (a.k > 64)
+    __syncthreads();
+  else
+    wave_sync();
+  const int n = a.k > 64 ? NT : 64;
+  if ((int)threadIdx.x < n)
+    for (int i = threadIdx.x; i < a.k; i += n) {
+      const int id = eid[i];
+      ez[i] = id >= 0 ? logit<T, ONE>(a, z, id) : 0.0f;
+      eall[i] = same_id(a, id);
+    }
+  // read by others only behind block_join's barrier
+}
+
+// The row's loss, by the first wavefront.
+template <typename T, int NT>
+__device__ inline void row_loss(const DistillArgs &a, int64_t row, const MaxSum &st, const Shared<NT> &sh) {
   const T *t = reinterpret_cast<const T *>(a.t) + row * a.k;
-  const float log_s = logf(st.s), log_sum = logf((float)te.sum);
-  const double inv = te.sum == 0.0 ? 0.0 : 1.0 / te.sum;
+  ENTRIES;
+  const float log_s = logf(st.s), log_sum = logf((float)sh.sum);
+  const double inv = sh.sum == 0.0 ? 0.0 : 1.0 / sh.sum;
   double sum = 0.0;
-  for (int i = threadIdx.x; i < a.k; i += NT) {
-    const double p = (double)sh.e[i] * inv;
+  for (int i = threadIdx.x; i < a.k; i += 64) {
+    const double p = (double)ee[i] * inv;
     if (p == 0.0) continue;
-    const int id = sh.id[i];
-    if (id < 0) {  // the entries' sum is not a number: so is the loss
+    if (eid[i] < 0) {  // the entries' sum is not a number: so is the loss
       sum += p;
       continue;
     }
-    const float zi = logit<T, ONE>(a, z, id);
-    const float log_p = ((float)t[i] - te.top) / a.temperature - log_sum;
+    const float zi = ez[i];
+    const float log_p = ((float)t[i] - sh.top) / a.temperature - log_sum;
     const float log_q = zi == -INFINITY ? -INFINITY : (zi - st.m) / a.temperature - log_s;
     sum += p * ((double)log_p - (double)log_q);
   }
-  sum = block_reduce<NT>(sum, sh.sum);
-  return (float)((double)a.temperature * (double)a.temperature * sum);
+  sum = wave_sum(sum);
+  if (threadIdx.x == 0) a.loss[row] = (float)((double)a.temperature * (double)a.temperature * sum);
 }
 
-// The teacher's entries of columns [lo, hi): written over what the pass over the row left there.
-template <typename T, bool ONE, int NT>
-__device__ inline void entries(const DistillArgs &a, const T *z, T *dz, const MaxSum &st, float inv_s, float inv_p,
-                               float coef, int lo, int hi, const Shared<NT> &sh) {
+// The gradient at the teacher's entries of columns [lo, hi): written over what the pass over the row
+// left there.
+template <typename T, int NT>
+__device__ inline void entries(const DistillArgs &a, T *dz, const MaxSum &st, float inv_s, float inv_p, float coef, int lo,
+                               int hi) {
+  ENTRIES;
   for (int i = threadIdx.x; i < a.k; i += NT) {
-    const int id = sh.id[i];
+    const int id = eid[i];
     if (id < lo || id >= hi) continue;
-    float p = 0.0f;  // every entry of this id, in the entries' order
-    for (int j = 0; j < a.k; ++j) p += sh.id[j] == id ? sh.e[j] : 0.0f;
-    const float q = expz<T>(a, logit<T, ONE>(a, z, id) - st.m) * inv_s;
-    dz[id] = (T)(coef * (q - p * inv_p));
+    const float q = expz<T>(a, ez[i] - st.m) * inv_s;
+    dz[id] = (T)(coef * (q - eall[i] * inv_p));
   }
 }
 
 template <typename T>
-__device__ inline void grad8(const DistillArgs &a, const float v[8], T *dz, int64_t col, float m, float f) {
+__device__ inline Raw8<T> grad8(const DistillArgs &a, const float v[8], float m, float f) {
   Raw8<T> r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r.v[i] = (T)(expz<T>(a, v[i] - m) * f);
-  store8_tail(dz + col, r, a.vocab - col);
+  return r;
 }
 
 template <typename T>
-__device__ inline void zero8(const DistillArgs &a, T *dz, int64_t col) {
+__device__ inline Raw8<T> zero8() {
   Raw8<T> r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r.v[i] = (T)0.0f;
-  store8_tail(dz + col, r, a.vocab - col);
+  return r;
 }
 
-// One workgroup a row.  CH > 0: the row fits CH pieces of 8 elements a thread and is kept in
-// registers for the gradient; CH = 0: it is read again.
-template <typename T, bool ONE, int NT, int CH, bool GRAD>
-__global__ __launch_bounds__(NT) void distill_row_kernel(DistillArgs a) {
+// The kept elements as a new value, so that the compiler converts 16-bit ones again in the next
+// pass instead of holding them in 32 bits.
+template <typename T>
+__device__ inline void renew(Raw8<T> &r) {
+  if constexpr (sizeof(T) == 2) {
+    u32x4 u = __builtin_bit_cast(u32x4, r);
+    asm("" : "+v"(u));
+    r = __builtin_bit_cast(Raw8<T>, u);
+  }
+}
+
+// One workgroup a row.  CH > 0: the row, of 8 elements or more, fits CH pieces of 8 elements a
+// thread and is kept in registers between the sum and the gradient; CH = 0: it is read again.  A
+// piece past the row's last whole one is the row's last eight elements, of which those that belong to
+// its neighbour do not count in the sum and get the same gradient twice.  With given (m, s) the
+// gradient alone.  OCC: wavefronts a SIMD, bought with registers: rows' phases overlap.
+template <typename T, bool ONE, int NT, int CH, bool GRAD, int OCC>
+__global__ __launch_bounds__(NT, OCC) void distill_row_kernel(DistillArgs a) {
+  constexpr int FLY = ONE ? 4 : 2;  // pieces in flight where the row is read again
   __shared__ Shared<NT> sh;
   const int64_t row = blockIdx.x;
   const T *z = reinterpret_cast<const T *>(a.z) + row * a.vocab;
   MaxSum st = {-FLT_MAX, 0.0f};
   Raw8<T> keep[CH > 0 ? CH : 1];
+  const auto column = [&](int c) { return (c * NT + (int)threadIdx.x) * 8; };
+  const auto begin = [&](int c) { return column(c) < a.vocab - 8 ? column(c) : a.vocab - 8; };
+  const First<T> first = first_entry<T>(a, row);
   if constexpr (CH > 0) {
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int64_t col = ((int64_t)c * NT + threadIdx.x) * 8, left = a.vocab - col;
-      keep[c] = load8_tail(z + col, left);
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i >= left) keep[c].v[i] = (T)-INFINITY;
-    }
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      float v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = (float)keep[c].v[i];
-      add8<T>(a, st, v);
-    }
-  } else {
-    for (int64_t col = threadIdx.x * 8; col < a.vocab; col += NT * 8) {
-      float v[8];
-      logits8<T, ONE>(a, z, col, v);
-      add8<T>(a, st, v);
-    }
+    for (int c = 0; c < CH; ++c)
+      if (column(c) < a.vocab) keep[c] = load8(z + begin(c));
   }
-  st = block_join<T, NT>(a, st, sh.join);
-  const Teacher te = teacher<T, NT>(a, row, sh);
-  const float loss = row_loss<T, ONE, NT>(a, row, z, te, st, sh);
-  if (threadIdx.x == 0) {
-    if (a.loss) a.loss[row] = loss;
-    if (a.stats) a.stats[2 * row] = st.m, a.stats[2 * row + 1] = st.s;
+  teacher<T, ONE, NT>(a, row, z, first, sh);
+  if (a.stats_in) {
+    st.m = a.stats_in[2 * row], st.s = a.stats_in[2 * row + 1];
+    __syncthreads();
+  } else {
+    if constexpr (CH > 0) {
+      // the thread's maximum first (a neighbour's elements do no harm there), then its sum
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+        if (column(c) < a.vocab) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) st.m = fmaxf(st.m, (float)keep[c].v[i]);
+        }
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        renew(keep[c]);
+        if ((c + 1) * NT * 8 <= a.vocab) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) st.s += expz<T>(a, (float)keep[c].v[i] - st.m);
+        } else if (column(c) < a.vocab) {
+          const int skip = column(c) - begin(c);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) st.s += i < skip ? 0.0f : expz<T>(a, (float)keep[c].v[i] - st.m);
+        }
+      }
+    } else {
+      for (int64_t col = threadIdx.x * 8; col < a.vocab; col += NT * 8 * FLY) {
+        float v[FLY][8];
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) logits8<T, ONE>(a, z, col + u * NT * 8, v[u]);
+#pragma unroll
+        for (int u = 0; u < FLY; ++u) add8<T>(a, st, v[u]);
+      }
+    }
+    st = block_join<T, NT>(a, st, sh.join);
   }
   if constexpr (GRAD) {
     T *dz = reinterpret_cast<T *>(a.dz) + row * a.vocab;
     const float coef = (a.g ? a.g[row] : 1.0f) * a.temperature;
     const float inv_s = st.s == 0.0f ? 0.0f : 1.0f / st.s;
-    const bool none = te.inv == 0.0f;
-    if constexpr (CH > 0) {
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        const int64_t col = ((int64_t)c * NT + threadIdx.x) * 8;
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (float)keep[c].v[i];
-        if (none)
-          zero8(a, dz, col);
-        else
-          grad8<T>(a, v, dz, col, st.m, coef * inv_s);
-      }
+    if (sh.sum == 0.0) {  // no entry counts
+      for (int64_t col = threadIdx.x * 8; col < a.vocab; col += NT * 8) store8_tail(dz + col, zero8<T>(), a.vocab - col);
     } else {
-      for (int64_t col = threadIdx.x * 8; col < a.vocab; col += NT * 8) {
-        if (none) {
-          zero8(a, dz, col);
-          continue;
+      if constexpr (CH > 0) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+          if (column(c) < a.vocab) {
+            renew(keep[c]);
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = (float)keep[c].v[i];
+            const Raw8<T> r = grad8<T>(a, v, st.m, coef * inv_s);
+            __builtin_memcpy(dz + begin(c), &r, sizeof(r));
+          }
+      } else {
+        for (int64_t col = threadIdx.x * 8; col < a.vocab; col += NT * 8 * FLY) {
+          float v[FLY][8];
+#pragma unroll
+          for (int u = 0; u < FLY; ++u) logits8<T, ONE>(a, z, col + u * NT * 8, v[u]);
+#pragma unroll
+          for (int u = 0; u < FLY; ++u) {
+            const int64_t at = col + u * NT * 8;
+            store8_tail(dz + at, grad8<T>(a, v[u], st.m, coef * inv_s), a.vocab - at);
+          }
         }
-        float v[8];
-        logits8<T, ONE>(a, z, col, v);
-        grad8<T>(a, v, dz, col, st.m, coef * inv_s);
       }
+      __syncthreads();  // the pass's stores come before the entries'
+      entries<T, NT>(a, dz, st, inv_s, (float)(1.0 / sh.sum), coef, 0, a.vocab);
     }
-    if (none) return;
-    __syncthreads();  // the pass's stores come before the entries'
-    entries<T, ONE, NT>(a, z, dz, st, inv_s, te.inv, coef, 0, a.vocab, sh);
+  }
+  if (threadIdx.x < 64) {
+    if (a.loss) row_loss<T, NT>(a, row, st, sh);
+    if (a.stats && threadIdx.x == 0) a.stats[2 * row] = st.m, a.stats[2 * row + 1] = st.s;
   }
 }
 
@@ -339,8 +414,10 @@ __global__ __launch_bounds__(256) void distill_finish_kernel(DistillArgs a) {
   const int64_t row = blockIdx.y;
   const T *z = reinterpret_cast<const T *>(a.z) + row * a.vocab;
   MaxSum st = {-FLT_MAX, 0.0f};
+  teacher<T, ONE, 256>(a, row, z, first_entry<T>(a, row), sh);
   if (a.stats_in) {
     st.m = a.stats_in[2 * row], st.s = a.stats_in[2 * row + 1];
+    __syncthreads();
   } else {
     for (int c = threadIdx.x; c < a.chunks; c += 256) {
       const f32x2 p = a.partial[row * a.chunks + c];
@@ -348,34 +425,32 @@ __global__ __launch_bounds__(256) void distill_finish_kernel(DistillArgs a) {
     }
     st = block_join<T, 256>(a, st, sh.join);
   }
-  const Teacher te = teacher<T, 256>(a, row, sh);
-  if (blockIdx.x == 0) {
-    if (a.loss) {
-      const float loss = row_loss<T, ONE, 256>(a, row, z, te, st, sh);
-      if (threadIdx.x == 0) a.loss[row] = loss;
-    }
-    if (a.stats && threadIdx.x == 0) a.stats[2 * row] = st.m, a.stats[2 * row + 1] = st.s;
-  }
   if constexpr (GRAD) {
     T *dz = reinterpret_cast<T *>(a.dz) + row * a.vocab;
     const float coef = (a.g ? a.g[row] : 1.0f) * a.temperature;
     const float inv_s = st.s == 0.0f ? 0.0f : 1.0f / st.s;
-    const bool none = te.inv == 0.0f;
+    const bool none = sh.sum == 0.0;
     const int64_t lo = (int64_t)blockIdx.x * CHUNK;
+#pragma unroll
     for (int c = 0; c < CHUNK / 2048; ++c) {
       const int64_t col = lo + c * 2048 + threadIdx.x * 8;
-      if (none) {
-        zero8(a, dz, col);
-      } else {
+      Raw8<T> r = zero8<T>();
+      if (!none) {
         float v[8];
         logits8<T, ONE>(a, z, col, v);
-        grad8<T>(a, v, dz, col, st.m, coef * inv_s);
+        r = grad8<T>(a, v, st.m, coef * inv_s);
       }
+      store8_tail(dz + col, r, a.vocab - col);
     }
-    if (none) return;
-    __syncthreads();
-    const int64_t hi = lo + CHUNK < a.vocab ? lo + CHUNK : a.vocab;
-    entries<T, ONE, 256>(a, z, dz, st, inv_s, te.inv, coef, (int)lo, (int)hi, sh);
+    if (!none) {
+      __syncthreads();
+      const int64_t hi = lo + CHUNK < a.vocab ? lo + CHUNK : a.vocab;
+      entries<T, 256>(a, dz, st, inv_s, (float)(1.0 / sh.sum), coef, (int)lo, (int)hi);
+    }
+  }
+  if (blockIdx.x == 0 && threadIdx.x < 64) {
+    if (a.loss) row_loss<T, 256>(a, row, st, sh);
+    if (a.stats && threadIdx.x == 0) a.stats[2 * row] = st.m, a.stats[2 * row + 1] = st.s;
   }
 }
 
@@ -383,47 +458,40 @@ __global__ __launch_bounds__(256) void distill_finish_kernel(DistillArgs a) {
 bool several(int64_t rows, int64_t vocab) { return rows < 256 && vocab > 2 * CHUNK; }
 
 template <typename T, bool ONE, bool GRAD>
-hipError_t forward(const DistillArgs &a, hipStream_t stream) {
+hipError_t run(const DistillArgs &a, hipStream_t stream) {
   if (several(a.rows, a.vocab)) {
     const dim3 grid((unsigned)a.chunks, (unsigned)a.rows);
-    distill_partial_kernel<T, ONE><<<grid, 256, 0, stream>>>(a);
-    distill_finish_kernel<T, ONE, GRAD><<<GRAD ? grid : dim3(1, (unsigned)a.rows), 256, 0, stream>>>(a);
+    if (!a.stats_in) distill_partial_kernel<T, ONE><<<grid, 256, 0, stream>>>(a);
+    distill_finish_kernel<T, ONE, GRAD><<<GRAD ? grid : dim3(1, (unsigned)a.rows), 256, 16 * a.k, stream>>>(a);
     return hipGetLastError();
   }
+  // The row in registers where it fits 64 of them a thread, read again where it does not (MC
+  // logits, rows below one piece, long rows).
   const dim3 grid((unsigned)a.rows);
-  if (a.vocab <= 512)
-    distill_row_kernel<T, ONE, 64, ONE ? 1 : 0, GRAD><<<grid, 64, 0, stream>>>(a);
-  else if (a.vocab <= 8192)
-    distill_row_kernel<T, ONE, 256, ONE ? 4 : 0, GRAD><<<grid, 256, 0, stream>>>(a);
-  else if (a.vocab <= 32768)
-    distill_row_kernel<T, ONE, 512, ONE ? 8 : 0, GRAD><<<grid, 512, 0, stream>>>(a);
-  else
-    distill_row_kernel<T, ONE, 1024, 0, GRAD><<<grid, 1024, 0, stream>>>(a);
-  return hipGetLastError();
-}
-
-template <typename T, bool ONE>
-hipError_t backward(const DistillArgs &a, hipStream_t stream) {
-  // the grid's second dimension holds 65535 rows a launch
-  DistillArgs b = a;
-  for (int64_t r = 0; r < a.rows; r += 65535) {
-    b.rows = a.rows - r < 65535 ? a.rows - r : 65535;
-    b.z = (const T *)a.z + r * a.vocab;
-    b.dz = (T *)a.dz + r * a.vocab;
-    b.t = (const T *)a.t + r * a.k;
-    b.ids = a.ids + r * a.k;
-    b.stats_in = a.stats_in + 2 * r;
-    b.g = a.g ? a.g + r : nullptr;
-    distill_finish_kernel<T, ONE, true>
-        <<<dim3((unsigned)a.chunks, (unsigned)b.rows), 256, 0, stream>>>(b);
+#define ROW(NT, CH, OCC) distill_row_kernel<T, ONE, NT, CH, GRAD, OCC><<<grid, NT, 16 * a.k, stream>>>(a)
+  if constexpr (ONE) {
+    constexpr bool SHORT = sizeof(T) == 2;
+    if (a.vocab >= 8) {
+      if (a.vocab <= 512) return ROW(64, 1, 8), hipGetLastError();
+      if (a.vocab <= 1024) return ROW(64, 2, 8), hipGetLastError();
+      if (a.vocab <= 2048) return ROW(64, 4, 8), hipGetLastError();
+      if (a.vocab <= 4096) return ROW(256, 2, 8), hipGetLastError();
+      if (a.vocab <= 8192) return ROW(256, 4, SHORT ? 8 : 6), hipGetLastError();
+      if (a.vocab <= 16384) return ROW(512, 4, SHORT ? 8 : 6), hipGetLastError();
+      if (a.vocab <= 32768) return ROW(512, 8, SHORT ? 8 : 4), hipGetLastError();
+      if (a.vocab <= 65536) return ROW(1024, 8, 4), hipGetLastError();
+      if constexpr (SHORT)
+        if (a.vocab <= 131072) return ROW(1024, 16, 4), hipGetLastError();
+    }
   }
+  if (a.vocab <= 2048)
+    ROW(64, 0, 4);
+  else if (a.vocab <= 32768)
+    ROW(256, 0, 4);
+  else
+    ROW(1024, 0, 4);
+#undef ROW
   return hipGetLastError();
-}
-
-template <typename T, bool ONE>
-hipError_t run(const DistillArgs &a, hipStream_t stream) {
-  if (a.stats_in) return backward<T, ONE>(a, stream);
-  return a.dz ? forward<T, ONE, true>(a, stream) : forward<T, ONE, false>(a, stream);
 }
 
 }  // namespace
@@ -456,9 +524,14 @@ hipError_t launch_distill(int dtype, int nc, int64_t rows, int64_t vocab, int64_
   a.c_hi = (float)c;
   if ((double)a.c_hi > c) a.c_hi = nextafterf(a.c_hi, 0.0f);
   a.c_lo = fmaxf((float)(c - (double)a.c_hi), FLT_MIN);
-  if (dtype == LM_F16) return nc == 1 ? run<_Float16, true>(a, stream) : run<_Float16, false>(a, stream);
-  if (dtype == LM_BF16) return nc == 1 ? run<__bf16, true>(a, stream) : run<__bf16, false>(a, stream);
-  return nc == 1 ? run<float, true>(a, stream) : run<float, false>(a, stream);
+  const auto go = [&](auto zero) {
+    using T = decltype(zero);
+    if (nc == 1) return dz ? run<T, true, true>(a, stream) : run<T, true, false>(a, stream);
+    return dz ? run<T, false, true>(a, stream) : run<T, false, false>(a, stream);
+  };
+  if (dtype == LM_F16) return go((_Float16)0.0f);
+  if (dtype == LM_BF16) return go((__bf16)0.0f);
+  return go(0.0f);
 }
 
 }  // namespace mcf
