@@ -15,6 +15,7 @@ Tensor conventions (component-major):
 from __future__ import annotations
 
 import ctypes
+import functools
 import math
 import os
 
@@ -655,15 +656,14 @@ def _plain_code(dtype) -> int:
 def _mx4(pair, n, name):
     """(nc, S, codes pointer, scales pointer) of an MXFP4 tensor of row length n."""
     codes, scales = pair
-    torch = _torch()
-    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8:
+    u8 = (_torch_module or _torch()).uint8
+    if codes.dtype is not u8 or scales.dtype is not u8:
         raise TypeError(f"{name}: codes and scales must be uint8")
     if codes.get_device() != scales.get_device():
         raise ValueError(f"{name}: codes and scales must be on one device")
     groups = (n + 127) // 128
     cs, ss = codes.shape, scales.shape
-    if n < 0 or len(cs) < 2 or cs[-1] != 64 * groups or len(ss) != len(cs) + 1 \
-            or ss[0] != cs[0] or ss[1] != groups or ss[2:-1] != cs[1:-1] or ss[-1] != 4:
+    if n < 0 or len(cs) < 2 or cs[-1] != 64 * groups or ss != (cs[0], groups, *cs[1:-1], 4):
         raise ValueError(f"{name}: codes {tuple(cs)} and scales {tuple(ss)} are not an MXFP4 tensor of rows of {n}")
     return cs[0], cs[1:-1], _dev(codes, name), _dev(scales, name)
 
@@ -675,7 +675,8 @@ def _device(t, other, name):
 
 def _out(out, like, shape, dtype):
     if out is None:
-        return _torch().empty(shape, dtype=dtype, device=like.device)
+        return like.new_empty(shape, dtype=dtype) if type(like) is _plain_tensor else \
+            _torch().empty(shape, dtype=dtype, device=like.device)
     if tuple(out.shape) != tuple(shape) or out.dtype != dtype or out.get_device() != like.get_device():
         raise ValueError("out has the wrong shape, dtype or device")
     return out
@@ -686,33 +687,40 @@ def _space(workspace, needed, like):
     if workspace is None:
         if needed <= 0:
             return None, None, 0
-        workspace = _torch().empty(needed, dtype=_torch().uint8, device=like.device)
+        workspace = _out(None, like, (needed,), _torch_module.uint8)
+        return workspace, workspace.data_ptr(), needed
     _device(workspace, like, "workspace")
     return workspace, _dev(workspace, "workspace"), workspace.numel() * workspace.element_size()
 
 
-def _bytes(needed, what) -> int:
-    _check(int(needed) if needed < 0 else 0, what)
-    return int(needed)
+@functools.lru_cache(maxsize=4096)
+def _bytes(name, *sizes) -> int:
+    """Workspace bytes of a call, a function of its sizes alone."""
+    needed = int(getattr(_lib or lib(), name)(*sizes))
+    _check(needed if needed < 0 else 0, name)
+    return needed
 
 
 def mc_mx4_quantize(x, *, nc: int = 1, x_mc: bool = False, out=None):
     """x (*S, n), or with x_mc an MC value (planes, *S, n) -> its MXFP4 tensor (codes, scales)
     of nc components: each block of 32 along a row scaled by a power of two and rounded to
     E2M1, each component the rounding of what the ones before it leave."""
-    torch = _torch()
     code = _plain_code(x.dtype)
-    if x.dim() < (2 if x_mc else 1):
+    shape = x.shape
+    nc_in = 1
+    if len(shape) < (2 if x_mc else 1):
         raise ValueError("x must be (*S, n), or (planes, *S, n) with x_mc")
-    nc_in = x.shape[0] if x_mc else 1
-    shape = tuple(x.shape[1:] if x_mc else x.shape)
-    n, rows = shape[-1], math.prod(shape[:-1])
-    groups = (n + 127) // 128
-    want = (nc,) + shape[:-1] + (64 * groups,), (nc, groups) + shape[:-1] + (4,)
     if nc < 1:
         raise ValueError("nc must be positive")
-    codes, scales = (_out(o, x, w, torch.uint8) for o, w in zip(out or (None, None), want))
-    st = (_lib or lib()).mc_mx4_quantize(code, nc_in, nc, rows, n, _dev(x, "x"), _dev(codes, "codes"),
+    if x_mc:
+        nc_in, shape = shape[0], shape[1:]
+    n, lead = shape[-1], shape[:-1]
+    groups = (n + 127) // 128
+    codes, scales = out or (None, None)
+    u8 = _torch_module.uint8
+    codes = _out(codes, x, (nc, *lead, 64 * groups), u8)
+    scales = _out(scales, x, (nc, groups, *lead, 4), u8)
+    st = (_lib or lib()).mc_mx4_quantize(code, nc_in, nc, math.prod(lead), n, _dev(x, "x"), _dev(codes, "codes"),
                                          _dev(scales, "scales"), _stream(x))
     _check(st, "mc_mx4_quantize")
     return codes, scales
@@ -721,7 +729,7 @@ def mc_mx4_quantize(x, *, nc: int = 1, x_mc: bool = False, out=None):
 def mc_mx4_dequantize(codes, scales, n: int, *, dtype, out=None):
     """The numbers (*S, n) an MXFP4 tensor stands for, in `dtype`."""
     nc, shape, cp, sp = _mx4((codes, scales), n, "codes and scales")
-    out = _out(out, codes, tuple(shape) + (n,), dtype)
+    out = _out(out, codes, (*shape, n), dtype)
     st = (_lib or lib()).mc_mx4_dequantize(_plain_code(dtype), nc, math.prod(shape), n, cp, sp, _dev(out, "out"),
                                            _stream(codes))
     _check(st, "mc_mx4_dequantize")
@@ -730,8 +738,7 @@ def mc_mx4_dequantize(codes, scales, n: int, *, dtype, out=None):
 
 def mc_mx4_matmul_workspace(dtype, M: int, N: int, K: int, a_nc: int, b_nc: int) -> int:
     """Workspace bytes of mc_mx4_matmul."""
-    return _bytes((_lib or lib()).mc_mx4_matmul_workspace(_plain_code(dtype), M, N, K, a_nc, b_nc),
-                  "mc_mx4_matmul_workspace")
+    return _bytes("mc_mx4_matmul_workspace", _plain_code(dtype), M, N, K, a_nc, b_nc)
 
 
 def mc_mx4_matmul(a, b, K: int, *, dtype, out=None, workspace=None):
@@ -753,8 +760,7 @@ def mc_mx4_matmul(a, b, K: int, *, dtype, out=None, workspace=None):
 
 def mc_mx4_linear_fwd_workspace(dtype, nc: int, batch: int, in_: int, out: int) -> int:
     """Workspace bytes of mc_mx4_linear_fwd."""
-    return _bytes((_lib or lib()).mc_mx4_linear_fwd_workspace(_plain_code(dtype), nc, batch, in_, out),
-                  "mc_mx4_linear_fwd_workspace")
+    return _bytes("mc_mx4_linear_fwd_workspace", _plain_code(dtype), nc, batch, in_, out)
 
 
 def mc_mx4_linear_fwd(x, W, b=None, *, out=None, workspace=None):
@@ -775,9 +781,8 @@ def mc_mx4_linear_fwd(x, W, b=None, *, out=None, workspace=None):
             raise ValueError("dtype or bias shape mismatch")
     code = _plain_code(x.dtype)
     out = _out(out, x, (T, O), x.dtype)
-    keep, wp, wn = _space(workspace, _bytes((_lib or lib()).mc_mx4_linear_fwd_workspace(code, nc, T, I, O),
-                                            "mc_mx4_linear_fwd"), x)
-    st = _lib.mc_mx4_linear_fwd(code, nc, T, I, O, _dev(x, "x"), wc, wsc, None if b is None else _dev(b, "b"), wp, wn,
+    keep, wp, wn = _space(workspace, _bytes("mc_mx4_linear_fwd_workspace", code, nc, T, I, O), x)
+    st = (_lib or lib()).mc_mx4_linear_fwd(code, nc, T, I, O, _dev(x, "x"), wc, wsc, None if b is None else _dev(b, "b"), wp, wn,
                                 _dev(out, "out"), _stream(x))
     _check(st, "mc_mx4_linear_fwd")
     return out
@@ -785,8 +790,7 @@ def mc_mx4_linear_fwd(x, W, b=None, *, out=None, workspace=None):
 
 def mc_mx4_linear_bwd_workspace(dtype, nc: int, batch: int, in_: int, out: int) -> int:
     """Workspace bytes of mc_mx4_linear_bwd with every gradient."""
-    return _bytes((_lib or lib()).mc_mx4_linear_bwd_workspace(_plain_code(dtype), nc, batch, in_, out),
-                  "mc_mx4_linear_bwd_workspace")
+    return _bytes("mc_mx4_linear_bwd_workspace", _plain_code(dtype), nc, batch, in_, out)
 
 
 def mc_mx4_linear_bwd(x, W, dY, *, dx: bool = True, dw: bool = True, db: bool = True, workspace=None):
@@ -806,9 +810,8 @@ def mc_mx4_linear_bwd(x, W, dY, *, dx: bool = True, dw: bool = True, db: bool = 
         raise ValueError(f"dY must be {(T, O)} of x's dtype, got {tuple(dY.shape)} of {dY.dtype}")
     code = _plain_code(x.dtype)
     outs = [_empty(x, (T, I)) if dx else None, _empty(x, (O, I)) if dw else None, _empty(x, (O,)) if db else None]
-    keep, wp, wn = _space(workspace, _bytes((_lib or lib()).mc_mx4_linear_bwd_workspace(code, nc, T, I, O),
-                                            "mc_mx4_linear_bwd"), x)
-    st = _lib.mc_mx4_linear_bwd(code, nc, T, I, O, _dev(x, "x"), wc, wsc, _dev(dY, "dY"),
+    keep, wp, wn = _space(workspace, _bytes("mc_mx4_linear_bwd_workspace", code, nc, T, I, O), x)
+    st = (_lib or lib()).mc_mx4_linear_bwd(code, nc, T, I, O, _dev(x, "x"), wc, wsc, _dev(dY, "dY"),
                                 *(None if o is None else o.data_ptr() for o in outs), wp, wn, _stream(x))
     _check(st, "mc_mx4_linear_bwd")
     return tuple(outs)
@@ -816,30 +819,32 @@ def mc_mx4_linear_bwd(x, W, dY, *, dx: bool = True, dw: bool = True, db: bool = 
 
 def _distill_args(z, ids, t, g):
     """(code, nc, rows, vocab, k) of a distillation call's tensors."""
-    torch = _torch()
+    torch = _torch_module or _torch()
     nc = 1
-    if z.dim() == 3:
-        nc, rows, vocab = z.shape
-    elif z.dim() == 2:
-        rows, vocab = z.shape
+    shape = z.shape
+    if len(shape) == 2:
+        rows, vocab = shape
+    elif len(shape) == 3:
+        nc, rows, vocab = shape
     else:
         raise ValueError("z must be (rows, vocab), or (nc, rows, vocab) of an MC value")
-    if ids.dtype != torch.int32:
+    if ids.dtype is not torch.int32:
         raise TypeError(f"ids must be int32, got {ids.dtype}")
-    if ids.dim() != 2 or ids.shape[0] != rows or t.shape != ids.shape or t.dtype != z.dtype:
+    shape = ids.shape
+    if len(shape) != 2 or shape[0] != rows or t.shape != shape or t.dtype is not z.dtype:
         raise ValueError("ids and t must be (rows, k), t of z's dtype")
     _device(ids, z, "ids")
     _device(t, z, "t")
     if g is not None:
-        if g.dtype != torch.float32 or tuple(g.shape) != (rows,):
+        if g.dtype is not torch.float32 or g.shape != (rows,):
             raise ValueError("g must be (rows,) float32")
         _device(g, z, "g")
-    return _plain_code(z.dtype), nc, rows, vocab, ids.shape[1]
+    return _plain_code(z.dtype), nc, rows, vocab, shape[1]
 
 
 def mc_distill_workspace(rows: int, vocab: int) -> int:
     """Workspace bytes of mc_distill_fwd and mc_distill_fwd_bwd."""
-    return _bytes((_lib or lib()).mc_distill_workspace(rows, vocab), "mc_distill_workspace")
+    return _bytes("mc_distill_workspace", rows, vocab)
 
 
 def mc_distill_fwd(z, ids, t, *, temperature: float = 1.0, workspace=None):
@@ -850,10 +855,10 @@ def mc_distill_fwd(z, ids, t, *, temperature: float = 1.0, workspace=None):
     for mc_distill_bwd."""
     torch = _torch()
     code, nc, rows, vocab, k = _distill_args(z, ids, t, None)
-    loss = torch.empty(rows, dtype=torch.float32, device=z.device)
-    stats = torch.empty((rows, 2), dtype=torch.float32, device=z.device)
-    keep, wp, wn = _space(workspace, mc_distill_workspace(rows, vocab), z)
-    st = _lib.mc_distill_fwd(code, nc, rows, vocab, k, _dev(z, "z"), _dev(ids, "ids"), _dev(t, "t"),
+    loss = _out(None, z, (rows,), torch.float32)
+    stats = _out(None, z, (rows, 2), torch.float32)
+    keep, wp, wn = _space(workspace, _bytes("mc_distill_workspace", rows, vocab), z)
+    st = (_lib or lib()).mc_distill_fwd(code, nc, rows, vocab, k, _dev(z, "z"), _dev(ids, "ids"), _dev(t, "t"),
                              float(temperature), wp, wn, loss.data_ptr(), stats.data_ptr(), _stream(z))
     _check(st, "mc_distill_fwd")
     return loss, stats
@@ -878,10 +883,10 @@ def mc_distill_fwd_bwd(z, ids, t, g=None, *, temperature: float = 1.0, out=None,
     """(loss, gradient) of mc_distill_fwd and mc_distill_bwd in one pass over z."""
     torch = _torch()
     code, nc, rows, vocab, k = _distill_args(z, ids, t, g)
-    loss = torch.empty(rows, dtype=torch.float32, device=z.device)
+    loss = _out(None, z, (rows,), torch.float32)
     out = _out(out, z, (rows, vocab), z.dtype)
-    keep, wp, wn = _space(workspace, mc_distill_workspace(rows, vocab), z)
-    st = _lib.mc_distill_fwd_bwd(code, nc, rows, vocab, k, _dev(z, "z"), _dev(ids, "ids"), _dev(t, "t"),
+    keep, wp, wn = _space(workspace, _bytes("mc_distill_workspace", rows, vocab), z)
+    st = (_lib or lib()).mc_distill_fwd_bwd(code, nc, rows, vocab, k, _dev(z, "z"), _dev(ids, "ids"), _dev(t, "t"),
                                  float(temperature), None if g is None else _dev(g, "g"), wp, wn, loss.data_ptr(),
                                  _dev(out, "out"), _stream(z))
     _check(st, "mc_distill_fwd_bwd")

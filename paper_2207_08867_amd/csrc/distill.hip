@@ -146,13 +146,6 @@ extern __shared__ float entry_space[];
   [[maybe_unused]] float *const ee = entry_space + a.k;               \
   [[maybe_unused]] float *const eall = ee + a.k, *const ez = eall + a.k
 
-// What lanes of a wavefront wrote to LDS is there for its other lanes.
-__device__ inline void wave_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-}
-
 // The sum of the e of the entries with this id, in the entries' order.
 __device__ inline float same_id(const DistillArgs &a, int id) {
   ENTRIES;

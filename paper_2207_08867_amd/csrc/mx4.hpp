@@ -92,29 +92,45 @@ constexpr int mx_pieces() {
   return sizeof(T) == 4 ? 3 : (__is_same(T, __bf16) ? 1 : 2);
 }
 
-// The leading piece of v: v rounded to bfloat16, cut off instead where rounding would pass the
-// largest finite number (and for infinities and NaN, which keep their kind).
-__device__ inline __bf16 mx_lead(float v) {
-  uint32_t u = __builtin_bit_cast(uint32_t, v);
-  const uint32_t a = u & 0x7fffffffu;
-  if (a < 0x7f7f8000u) return (__bf16)v;
-  if (a > 0x7f800000u) u |= 0x00400000u;
-  return __builtin_bit_cast(__bf16, (uint16_t)(u >> 16));
+// v = p[0] + p[1] + ...: each piece what is left rounded to bfloat16.  T: the format v comes from.
+// A binary32 value that would round past bfloat16's largest number is cut off instead.  An infinity
+// or NaN makes the later pieces NaN.
+template <typename T, int P>
+__device__ inline void mx_split(float v, __bf16 p[P]) {
+  p[0] = (__bf16)v;
+  if constexpr (sizeof(T) == 4) {
+    const uint32_t u = __builtin_bit_cast(uint32_t, v), a = u & 0x7fffffffu;
+    if (a >= 0x7f7f8000u && a < 0x7f800000u) p[0] = __builtin_bit_cast(__bf16, (uint16_t)(u >> 16));
+  }
+  float r = v;
+#pragma unroll
+  for (int i = 1; i < P; ++i) {
+    r -= (float)p[i - 1];
+    p[i] = (__bf16)r;
+  }
 }
 
-// v = p[0] + p[1] + ...; an infinity or NaN is its first piece, the others zero.
-template <int P>
-__device__ inline void mx_split(float v, __bf16 p[P]) {
-  p[0] = mx_lead(v);
-  if constexpr (P > 1) {
-    const bool finite = (__builtin_bit_cast(uint32_t, v) & 0x7f800000u) != 0x7f800000u;
-    float r = finite ? v - (float)p[0] : 0.0f;
+// Eight values into P registers of eight pieces.
+template <typename T, int P>
+__device__ inline void mx_split8(const Raw8<T> &x, bf16x8 f[P]) {
+  if constexpr (P == 1) {
+    f[0] = __builtin_bit_cast(bf16x8, x);
+  } else {
 #pragma unroll
-    for (int i = 1; i < P; ++i) {
-      p[i] = (__bf16)r;
-      r -= (float)p[i];
+    for (int i = 0; i < 8; ++i) {
+      __bf16 q[P];
+      mx_split<T, P>((float)x.v[i], q);
+#pragma unroll
+      for (int p = 0; p < P; ++p) f[p][i] = q[p];
     }
   }
+}
+
+// What lanes of a wavefront wrote to LDS is there for its other lanes.
+__device__ inline void wave_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 }  // namespace mcf

@@ -373,7 +373,7 @@ struct Pieces {
       p[0] = __builtin_bit_cast(uint16_t, (_Float16)v);
     } else {
       __bf16 q[P];
-      mx_split<P>((float)v, q);
+      mx_split<T, P>((float)v, q);
 #pragma unroll
       for (int i = 0; i < P; ++i) p[i] = __builtin_bit_cast(uint16_t, q[i]);
     }

@@ -13,6 +13,11 @@
 namespace mcf {
 namespace {
 
+template <int N>
+struct Count {
+  static constexpr int value = N;
+};
+
 struct ThinArgs {
   const void *x;             // plain [M][K], or codes [x_nc][M][64 G]
   const uint32_t *x_scales;  // [x_nc][G][M]
@@ -24,18 +29,46 @@ struct ThinArgs {
   int x_nc, w_nc;
 };
 
+// The 32 elements of a plain x that lane group g needs of a group of 128, as loaded.
+template <typename T>
+struct XRow {
+  Raw8<T> v[4];
+};
+
+// acc += W x over one group: lane (r, g) holds codes of block g of weight row r and the elements of
+// that block of x row r, and takes the reduction in the order that lays the blocks' eight numbers j
+// side by side.
+template <typename T>
+__device__ inline f32x4 thin_group(f32x4 acc, u32x4 code, float scale, const XRow<T> &x) {
+  constexpr int P = mx_pieces<T>();
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const bf16x8 wf = mx_bf16(code[j], scale);
+    bf16x8 xf[P];
+    mx_split8<T, P>(x.v[j], xf);
+#pragma unroll
+    for (int p = 0; p < P; ++p) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf[p], acc, 0, 0, 0);
+  }
+  return acc;
+}
+
+__device__ inline f32x4 thin_group(f32x4 acc, u32x4 code, uint32_t scale, u32x4 x, uint32_t x_scale) {
+  i32x8 av = {}, bv = {};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) av[i] = (int)code[i], bv[i] = (int)x[i];
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, acc, 4, 4, 0, (int)scale, 0, (int)x_scale);
+}
+
 // Few rows of x.  A workgroup owns 16 rows of the weight and 16 MT rows of x, and its NW
 // wavefronts share the reduction, group by group; their sums are joined through LDS in the
-// wavefronts' order.  A group is 128 long: lane (r, g) of the wavefront holds block g of weight row
-// r, 16 bytes of codes, which is the operand of one 16 x 16 x 128 scaled product, or of four
-// 16 x 16 x 32 bfloat16 products that take the reduction in the order that lays block g's eight
-// numbers j before lane group g.  The weight is read once and straight into registers; U groups
-// are in flight per wavefront.
+// wavefronts' order.  A lane's 16 bytes of codes, one block, are the operand of one 16 x 16 x 128
+// scaled product, or of four 16 x 16 x 32 bfloat16 products.  The weight is read once, straight
+// into registers.  What bounds it is the latency of its loads: U groups of a wavefront are asked for
+// before the first is used, so with 4096 columns (NW = 8, U = 4) the whole weight is in flight.
 template <typename T, bool PACKED, int MT, int NW, int U>
 __global__ __launch_bounds__(64 * NW) void mx_thin_kernel(ThinArgs a) {
-  constexpr int P = PACKED ? 1 : mx_pieces<T>();
   __shared__ f32x4 part[NW][MT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int64_t n0 = (int64_t)blockIdx.x * 16, m0 = (int64_t)blockIdx.y * (16 * MT);
   const int64_t wrow = n0 + r < a.N ? n0 + r : a.N - 1;
   int64_t xrow[MT];
@@ -44,80 +77,73 @@ __global__ __launch_bounds__(64 * NW) void mx_thin_kernel(ThinArgs a) {
   f32x4 acc[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) acc[t] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int64_t whole = PACKED ? a.G : a.K / MX_GROUP;  // groups that need no tail check
 
   for (int cw = 0; cw < a.w_nc; ++cw) {
     const uint8_t *w = a.w + ((int64_t)cw * a.N + wrow) * (a.G * 64) + g * 16;
     const uint32_t *ws = a.w_scales + (int64_t)cw * a.G * a.N + wrow;
-    for (int cx = 0; cx < a.x_nc; ++cx) {
-      for (int64_t s0 = wave; s0 < a.G; s0 += NW * U) {
-        u32x4 code[U];
-        uint32_t scale[U];
+    const auto codes_at = [&](int64_t s) { return *reinterpret_cast<const u32x4 *>(w + s * 64); };
+    const auto scale_at = [&](int64_t s) { return (ws[s * a.N] >> (8 * g)) & 255u; };
+    if constexpr (PACKED) {
+      for (int cx = 0; cx < a.x_nc; ++cx) {
+        const uint8_t *x = reinterpret_cast<const uint8_t *>(a.x) + (int64_t)cx * a.M * (a.G * 64) + g * 16;
+        const uint32_t *xs = a.x_scales + (int64_t)cx * a.G * a.M;
+        const auto run = [&](int64_t s0, auto count) {
+          constexpr int C = decltype(count)::value;
+          u32x4 code[C], xc[MT][C];
+          uint32_t scale[C], sc[MT][C];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int64_t s = s0 + u * NW;
-          code[u] = u32x4{0, 0, 0, 0};
-          scale[u] = 0;
-          if (s < a.G) {
-            code[u] = *reinterpret_cast<const u32x4 *>(w + s * 64);
-            scale[u] = (ws[s * a.N] >> (8 * g)) & 255u;
-          }
+          for (int u = 0; u < C; ++u) code[u] = codes_at(s0 + u * NW), scale[u] = scale_at(s0 + u * NW);
+#pragma unroll
+          for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int u = 0; u < C; ++u) {
+              xc[t][u] = *reinterpret_cast<const u32x4 *>(x + xrow[t] * (a.G * 64) + (s0 + u * NW) * 64);
+              sc[t][u] = (xs[(s0 + u * NW) * a.M + xrow[t]] >> (8 * g)) & 255u;
+            }
+#pragma unroll
+          for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int u = 0; u < C; ++u) acc[t] = thin_group(acc[t], code[u], scale[u], xc[t][u], sc[t][u]);
+        };
+        int64_t s = wave;
+        for (; s + (U - 1) * NW < whole; s += U * NW) run(s, Count<U>());
+        for (; s < whole; s += NW) run(s, Count<1>());
+      }
+    } else {
+      const T *x = reinterpret_cast<const T *>(a.x) + g * 32;
+      const auto run = [&](int64_t s0, auto count) {
+        constexpr int C = decltype(count)::value;
+        u32x4 code[C];
+        uint32_t scale[C];
+#pragma unroll
+        for (int u = 0; u < C; ++u) code[u] = codes_at(s0 + u * NW), scale[u] = scale_at(s0 + u * NW);
+        XRow<T> xr[C];
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+#pragma unroll
+          for (int u = 0; u < C; ++u)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) xr[u].v[j] = load8(x + xrow[t] * a.K + (s0 + u * NW) * MX_GROUP + j * 8);
+#pragma unroll
+          for (int u = 0; u < C; ++u) acc[t] = thin_group<T>(acc[t], code[u], mx_scale(scale[u]), xr[u]);
         }
-        if constexpr (PACKED) {
-          const uint8_t *x = reinterpret_cast<const uint8_t *>(a.x);
+      };
+      int64_t s = wave;
+      for (; s + (U - 1) * NW < whole; s += U * NW) run(s, Count<U>());
+      for (; s < whole; s += NW) run(s, Count<1>());
+      if (s < a.G) {  // the ragged last group: zeros past the row
+        const u32x4 code = codes_at(s);
+        const float scale = mx_scale(scale_at(s));
 #pragma unroll
-          for (int t = 0; t < MT; ++t) {
-            u32x4 xc[U];
-            uint32_t xs[U];
+        for (int t = 0; t < MT; ++t) {
+          XRow<T> xr;
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-              const int64_t s = s0 + u * NW;
-              xc[u] = u32x4{0, 0, 0, 0};
-              xs[u] = 0;
-              if (s < a.G) {
-                xc[u] = *reinterpret_cast<const u32x4 *>(x + ((int64_t)cx * a.M + xrow[t]) * (a.G * 64) + s * 64 + g * 16);
-                xs[u] = (a.x_scales[((int64_t)cx * a.G + s) * a.M + xrow[t]] >> (8 * g)) & 255u;
-              }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-              i32x8 av = {}, bv = {};
-#pragma unroll
-              for (int i = 0; i < 4; ++i) av[i] = (int)code[u][i], bv[i] = (int)xc[u][i];
-              acc[t] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(av, bv, acc[t], 4, 4, 0, (int)scale[u], 0,
-                                                                        (int)xs[u]);
-            }
+          for (int j = 0; j < 4; ++j) {
+            const int64_t k = s * MX_GROUP + j * 8;
+            xr.v[j] = load8_tail(x + xrow[t] * a.K + k, a.K - k - g * 32);
           }
-        } else {
-          const T *x = reinterpret_cast<const T *>(a.x);
-#pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int64_t k = (s0 + u * NW) * 128 + g * 32;
-            const float sc = mx_scale(scale[u]);
-#pragma unroll
-            for (int t = 0; t < MT; ++t) {
-              Raw8<T> xr[4];
-#pragma unroll
-              for (int j = 0; j < 4; ++j) xr[j] = load8_tail(x + xrow[t] * a.K + k + j * 8, a.K - (k + j * 8));
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                const bf16x8 wf = mx_bf16(code[u][j], sc);
-                if constexpr (P == 1) {
-                  acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, __builtin_bit_cast(bf16x8, xr[j]), acc[t], 0, 0, 0);
-                } else {
-                  bf16x8 xf[P];
-#pragma unroll
-                  for (int i = 0; i < 8; ++i) {
-                    __bf16 q[P];
-                    mx_split<P>((float)xr[j].v[i], q);
-#pragma unroll
-                    for (int p = 0; p < P; ++p) xf[p][i] = q[p];
-                  }
-#pragma unroll
-                  for (int p = 0; p < P; ++p) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf[p], acc[t], 0, 0, 0);
-                }
-              }
-            }
-          }
+          acc[t] = thin_group<T>(acc[t], code, scale, xr);
         }
       }
     }
@@ -141,20 +167,115 @@ __global__ __launch_bounds__(64 * NW) void mx_thin_kernel(ThinArgs a) {
   }
 }
 
+// One to XT rows of a binary16 or binary32 x.  As above, but the pieces of x are made once: a lane
+// splits 8 elements of each row, of the four groups that its wavefront holds, and the wavefront
+// reads them back from LDS as operands.  Splitting in the operands' layout instead repeats it in all
+// 16 lanes of a block, most of them for rows that x does not have: 4096 x 4096, one row of
+// binary16: 12.4 us a call so, 9 us in this kernel.
+template <typename T, int XT, int NW>
+__global__ __launch_bounds__(64 * NW) void mx_token_kernel(ThinArgs a) {
+  constexpr int P = mx_pieces<T>(), U = 4;
+  __shared__ bf16x8 pieces[NW][XT][P][U][16];  // [piece of 8 elements] of a group
+  __shared__ f32x4 part[NW][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const int64_t wrow = n0 + r < a.N ? n0 + r : a.N - 1;
+  const int rows = (int)a.M, xr = r < rows ? r : 0;
+  const T *x = reinterpret_cast<const T *>(a.x);
+  f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  for (int64_t s0 = wave; s0 < a.G; s0 += NW * U) {
+    // this lane's 8 elements: piece r of group g of the four
+    const int64_t k = (s0 + g * NW) * MX_GROUP + r * 8;
+    Raw8<T> raw[XT];
+#pragma unroll
+    for (int t = 0; t < XT; ++t) raw[t] = load8_tail(x + (t < rows ? t : 0) * a.K + k, a.K - k);
+    for (int cw = 0; cw < a.w_nc; ++cw) {
+      const uint8_t *w = a.w + ((int64_t)cw * a.N + wrow) * (a.G * 64) + g * 16;
+      const uint32_t *ws = a.w_scales + (int64_t)cw * a.G * a.N + wrow;
+      u32x4 code[U];
+      uint32_t scale[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t s = s0 + u * NW < a.G ? s0 + u * NW : a.G - 1;  // past the end: x is zero there
+        code[u] = *reinterpret_cast<const u32x4 *>(w + s * 64);
+        scale[u] = (ws[s * a.N] >> (8 * g)) & 255u;
+      }
+      if (cw == 0) {
+#pragma unroll
+        for (int t = 0; t < XT; ++t) {
+          bf16x8 f[P];
+          mx_split8<T, P>(raw[t], f);
+#pragma unroll
+          for (int p = 0; p < P; ++p) pieces[wave][t][p][g][r] = f[p];
+        }
+        wave_sync();
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool in = s0 + u * NW < a.G;
+        const float sc = mx_scale(in ? scale[u] : 0);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const bf16x8 wf = mx_bf16(code[u][j], sc);
+#pragma unroll
+          for (int p = 0; p < P; ++p)
+            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, pieces[wave][XT == 1 ? 0 : xr][p][u][g * 4 + j], acc, 0, 0, 0);
+        }
+      }
+    }
+    wave_sync();  // the pieces are read before the next ones are written
+  }
+  part[wave][lane] = acc;
+  __syncthreads();
+  if (wave > 0 || r >= rows) return;
+  f32x4 v = part[0][lane];
+#pragma unroll
+  for (int w = 1; w < NW; ++w) v += part[w][lane];
+  T *y = reinterpret_cast<T *>(a.y) + r * a.N;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t n = n0 + 4 * g + i;
+    if (n < a.N) y[n] = (T)(a.bias ? v[i] + (float)reinterpret_cast<const T *>(a.bias)[n] : v[i]);
+  }
+}
+
 template <typename T, bool PACKED, int MT>
 hipError_t thin_mt(const ThinArgs &a, hipStream_t stream) {
   const dim3 grid((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
-  if (a.G <= 8)
-    mx_thin_kernel<T, PACKED, MT, 4, 2><<<grid, 256, 0, stream>>>(a);
+  // about four groups a wavefront
+  constexpr int U = MT == 1 ? (sizeof(T) == 4 && !PACKED ? 2 : 4) : 2;
+  if (a.G <= 4)
+    mx_thin_kernel<T, PACKED, MT, 2, U><<<grid, 128, 0, stream>>>(a);
+  else if (a.G <= 16)
+    mx_thin_kernel<T, PACKED, MT, 4, U><<<grid, 256, 0, stream>>>(a);
   else
-    mx_thin_kernel<T, PACKED, MT, 8, 2><<<grid, 512, 0, stream>>>(a);
+    mx_thin_kernel<T, PACKED, MT, 8, U><<<grid, 512, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <typename T, int XT>
+hipError_t token(const ThinArgs &a, hipStream_t stream) {
+  const dim3 grid((unsigned)((a.N + 15) / 16));
+  if (a.G <= 4)
+    mx_token_kernel<T, XT, 2><<<grid, 128, 0, stream>>>(a);
+  else if (a.G <= 16)
+    mx_token_kernel<T, XT, 4><<<grid, 256, 0, stream>>>(a);
+  else
+    mx_token_kernel<T, XT, 8><<<grid, 512, 0, stream>>>(a);
   return hipGetLastError();
 }
 
 template <typename T, bool PACKED>
 hipError_t thin(const ThinArgs &a, hipStream_t stream) {
-  if (a.M <= 16) return thin_mt<T, PACKED, 1>(a, stream);
-  return thin_mt<T, PACKED, 4>(a, stream);
+  if constexpr (!PACKED && mx_pieces<T>() > 1) {
+    if (a.M == 1) return token<T, 1>(a, stream);
+    if (a.M <= 4) return token<T, 4>(a, stream);
+    return thin_mt<T, PACKED, 1>(a, stream);
+  } else {
+    if (a.M <= 16) return thin_mt<T, PACKED, 1>(a, stream);
+    if constexpr (!PACKED) return thin_mt<T, PACKED, 2>(a, stream);
+    else return a.M <= 32 ? thin_mt<T, PACKED, 2>(a, stream) : thin_mt<T, PACKED, 4>(a, stream);
+  }
 }
 
 template <bool PACKED>
@@ -166,8 +287,11 @@ hipError_t thin_any(int dtype, const ThinArgs &a, hipStream_t stream) {
 
 }  // namespace
 
-// Up to THIN rows of x the weight is read straight into registers; above, tiles go through LDS.
-constexpr int64_t THIN = 64;
+// Up to so many rows of x the weight is read straight into registers; above, tiles go through LDS
+// (4096 x 4096, us: 64 and 65 rows of MXFP4 8.9 and 11.4; 32 and 64 rows of bfloat16 by registers 11.0
+// and 22.2, 65 by tiles 16.4; 16 and 64 rows of binary16 13.7 and 35.5, 65 by tiles 25.4).
+constexpr int64_t THIN_PACKED = 64;
+int64_t thin_rows(int dtype) { return dtype == LM_BF16 ? 32 : 16; }
 
 namespace {
 
@@ -206,7 +330,7 @@ void set_pairs(GemmArgs &g, int na, int nb) {
 }  // namespace
 
 int64_t mx4_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K, int a_nc, int b_nc) {
-  if (M <= THIN) return 0;
+  if (M <= THIN_PACKED) return 0;
   return gemm_partial_bytes(M, N, (mx_groups(K) + 1) / 2 * a_nc * b_nc);
 }
 
@@ -214,7 +338,7 @@ hipError_t launch_mx4_matmul(int dtype, int64_t M, int64_t N, int64_t K, const v
                              int a_nc, const void *b_codes, const void *b_scales, int b_nc, void *ws, void *C,
                              hipStream_t stream) {
   const int64_t G = mx_groups(K);
-  if (M <= THIN) {
+  if (M <= THIN_PACKED) {
     ThinArgs a = {a_codes, (const uint32_t *)a_scales, (const uint8_t *)b_codes, (const uint32_t *)b_scales, nullptr, C,
                   M, N, K, G, a_nc, b_nc};
     return thin_any<true>(dtype, a, stream);
@@ -240,7 +364,7 @@ hipError_t launch_mx4_matmul(int dtype, int64_t M, int64_t N, int64_t K, const v
 }
 
 int64_t mx4_linear_workspace_bytes(int dtype, int nc, int64_t batch, int64_t in, int64_t out) {
-  if (batch <= THIN) return 0;
+  if (batch <= thin_rows(dtype)) return 0;
   return stage_bytes(dtype, batch, in) + gemm_partial_bytes(batch, out, mx_groups(in) * 2 * nc * pieces_of(dtype));
 }
 
@@ -248,7 +372,7 @@ hipError_t launch_mx4_linear(int dtype, int nc, int64_t batch, int64_t in, int64
                              const void *codes, const void *scales, const void *bias, void *ws, void *y,
                              hipStream_t stream) {
   const int64_t G = mx_groups(in);
-  if (batch <= THIN) {
+  if (batch <= thin_rows(dtype)) {
     ThinArgs a = {x, nullptr, (const uint8_t *)codes, (const uint32_t *)scales, bias, y, batch, out, in, G, 1, nc};
     return thin_any<false>(dtype, a, stream);
   }
