@@ -13,29 +13,31 @@
 namespace mcf {
 namespace {
 
-// Sums over a workgroup's 32 groups of lanes of 64 columns, 8 a lane.
-__device__ inline void join_columns(const float part[8], float (*f)[64], float *sums, int64_t cols) {
-#pragma unroll
-  for (int k = 0; k < 8; ++k) f[threadIdx.x >> 3][(threadIdx.x & 7) * 8 + k] = part[k];
-  __syncthreads();
-  if (threadIdx.x < 64 && threadIdx.x < cols) {
-    float s = 0.0f;
-    for (int i = 0; i < 32; ++i) s += f[i][threadIdx.x];
-    sums[threadIdx.x] = s;
-  }
-}
+// What is staged for the two products, all of it in one launch: workgroups [0, n_dy) take tiles of dY,
+// the next n_x tiles of x, the last n_w tiles of W.
+struct StageArgs {
+  const void *dY, *x;            // [T][O], [T][I]
+  const uint8_t *codes;          // W, [nc][O][64 groups] and its scales
+  const uint32_t *scales;
+  uint16_t *dy, *dyt, *xt, *wt;  // [P][T][op], [P'][O][tp], [P'][I][tp], [nc][I][op]; dy or dyt may be null
+  float *sums;                   // [tp / 128][O] column sums of dY's tiles, or null
+  void *db;                      // with a single row of tiles their sums are db itself
+  int64_t T, O, I, op, tp, groups, n_dy, n_x;
+};
 
-// src [rows][cols] -> dst [P][cols][ld], the transpose, zeros from rows to ld (a multiple of 128).
-// A workgroup turns 128 rows x 64 columns through LDS: a wavefront reads 8 rows of 64 columns in one
-// instruction (16-bit formats) and writes 16 bytes a lane, 8 rows of one column.  SUM: the columns'
-// sums of the 128 rows go to sums [tiles of rows][cols], for db.
-template <typename T, bool HALF, bool SUM>
-__global__ __launch_bounds__(256) void mx_stage_t_kernel(const T *src, uint16_t *dst, float *sums, int64_t rows,
-                                                         int64_t cols, int64_t ld) {
+constexpr int TILE_ROW = 66;  // halfwords: the rows of one column lie in different banks
+
+// A tile of 128 rows x 64 columns of src [rows][cols]: its pieces as they lie to plain [P][rows][pld]
+// (zeros up to pld), transposed to dst [P'][cols][ld] (zeros up to ld), its columns' sums to sums
+// [tiles of rows][cols].  A wavefront reads 8 rows of 64 columns in one instruction (16-bit
+// formats) and writes 16 bytes a lane, 8 rows of one column.
+template <typename T, bool HALF>
+__device__ inline void stage_tile(const T *src, uint16_t *plain, uint16_t *dst, float *sums, T *whole, int64_t rows,
+                                  int64_t cols, int64_t pld, int64_t ld, int64_t row_tile, int64_t col_tile, char *lds) {
   using S = Pieces<T, HALF>;
-  // [row][column]: 66 halfwords a row, so the rows of one column lie in different banks
-  __shared__ uint16_t tile[S::P][128][66];
-  const int64_t c0 = (int64_t)blockIdx.x * 64, r0 = (int64_t)blockIdx.y * 128;
+  using R = Pieces<T, false>;
+  uint16_t(*tile)[128][TILE_ROW] = reinterpret_cast<uint16_t(*)[128][TILE_ROW]>(lds);
+  const int64_t c0 = col_tile * 64, r0 = row_tile * 128;
   float part[8] = {};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -44,46 +46,65 @@ __global__ __launch_bounds__(256) void mx_stage_t_kernel(const T *src, uint16_t 
 #pragma unroll
     for (int k = 0; k < 8; ++k) v.v[k] = (T)0.0f;
     if (r0 + r < rows) v = load8_tail(src + (r0 + r) * cols + c0 + c, cols - c0 - c);
+    if (plain && r0 + r < rows) {
+      bf16x8 f[R::P];
+      mx_split8<T, R::P>(v, f);
+#pragma unroll
+      for (int q = 0; q < R::P; ++q)
+        *reinterpret_cast<bf16x8 *>(plain + ((int64_t)q * rows + r0 + r) * pld + c0 + c) = f[q];
+    }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       uint16_t p[S::P];
       S::of(v.v[k], p);
 #pragma unroll
       for (int q = 0; q < S::P; ++q) tile[q][r][c + k] = p[q];
-      if constexpr (SUM) part[k] += (float)v.v[k];
+      part[k] += (float)v.v[k];
     }
   }
   __syncthreads();
+  if (dst) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int c = i * 16 + (threadIdx.x >> 4), r = (threadIdx.x & 15) * 8;
-    if (c0 + c < cols) {
+    for (int i = 0; i < 4; ++i) {
+      const int c = i * 16 + (threadIdx.x >> 4), r = (threadIdx.x & 15) * 8;
+      if (c0 + c < cols) {
 #pragma unroll
-      for (int q = 0; q < S::P; ++q) {
-        uint16_t out[8];
+        for (int q = 0; q < S::P; ++q) {
+          uint16_t out[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) out[k] = tile[q][r + k][c];
-        __builtin_memcpy(dst + ((int64_t)q * cols + c0 + c) * ld + r0 + r, out, 16);
+          for (int k = 0; k < 8; ++k) out[k] = tile[q][r + k][c];
+          __builtin_memcpy(dst + ((int64_t)q * cols + c0 + c) * ld + r0 + r, out, 16);
+        }
       }
     }
   }
-  if constexpr (SUM) {
+  if (sums || whole) {
     __syncthreads();
-    join_columns(part, reinterpret_cast<float(*)[64]>(tile), sums + blockIdx.y * cols + c0, cols - c0);
+    float(*f)[64] = reinterpret_cast<float(*)[64]>(lds);  // 32 groups of lanes, 64 columns
+#pragma unroll
+    for (int k = 0; k < 8; ++k) f[threadIdx.x >> 3][(threadIdx.x & 7) * 8 + k] = part[k];
+    __syncthreads();
+    if (threadIdx.x < 64 && c0 + threadIdx.x < cols) {
+      float t = 0.0f;
+      for (int i = 0; i < 32; ++i) t += f[i][threadIdx.x];
+      if (whole)
+        whole[c0 + threadIdx.x] = (T)t;
+      else
+        sums[row_tile * cols + c0 + threadIdx.x] = t;
+    }
   }
 }
 
-// The numbers of an MXFP4 weight [nc][out][in], transposed: dst [nc][in][ld], ld >= out.
-__global__ __launch_bounds__(256) void mx_unpack_t_kernel(const uint8_t *codes, const uint32_t *scales, uint16_t *dst,
-                                                          int64_t out, int64_t in, int64_t groups, int64_t ld) {
-  __shared__ __attribute__((aligned(16))) uint16_t tile[128][72];  // [element][row], rows 16 bytes aligned
-  const int64_t grp = blockIdx.x, r0 = (int64_t)blockIdx.y * 64, c = blockIdx.z;
+// The numbers of one group of 128 columns of 64 rows of W, transposed into wt [nc][in][op].
+__device__ inline void unpack_tile(const StageArgs &a, int64_t grp, int64_t row_tile, int64_t c, char *lds) {
+  uint16_t(*tile)[72] = reinterpret_cast<uint16_t(*)[72]>(lds);  // [element][row], rows 16 bytes aligned
+  const int64_t r0 = row_tile * 64;
   for (int i = threadIdx.x; i < 1024; i += 256) {  // 64 rows x 16 pieces of 8 elements
     const int r = i >> 4, piece = i & 15;
     uint32_t word = 0, byte = 0;
-    if (r0 + r < out) {
-      word = *reinterpret_cast<const uint32_t *>(codes + (c * out + r0 + r) * (groups * 64) + grp * 64 + piece * 4);
-      byte = (scales[(c * groups + grp) * out + r0 + r] >> (8 * (piece >> 2))) & 255u;
+    if (r0 + r < a.O) {
+      word = *reinterpret_cast<const uint32_t *>(a.codes + (c * a.O + r0 + r) * (a.groups * 64) + grp * 64 + piece * 4);
+      byte = (a.scales[(c * a.groups + grp) * a.O + r0 + r] >> (8 * (piece >> 2))) & 255u;
     }
     const bf16x8 v = mx_bf16(word, mx_scale(byte));
 #pragma unroll
@@ -92,8 +113,30 @@ __global__ __launch_bounds__(256) void mx_unpack_t_kernel(const uint8_t *codes, 
   __syncthreads();
   for (int i = threadIdx.x; i < 128 * 8; i += 256) {
     const int k = i >> 3, r = (i & 7) * 8;
-    if (grp * 128 + k < in)
-      *reinterpret_cast<u32x4 *>(dst + (c * in + grp * 128 + k) * ld + r0 + r) = *reinterpret_cast<const u32x4 *>(&tile[k][r]);
+    if (grp * 128 + k < a.I)
+      *reinterpret_cast<u32x4 *>(a.wt + (c * a.I + grp * 128 + k) * a.op + r0 + r) =
+          *reinterpret_cast<const u32x4 *>(&tile[k][r]);
+  }
+}
+
+template <typename T, bool HALF>
+__global__ __launch_bounds__(256) void mx_stage_all_kernel(StageArgs a) {
+  constexpr int P = Pieces<T, HALF>::P, BYTES = P * 128 * TILE_ROW * 2;
+  __shared__ __attribute__((aligned(16))) char lds[BYTES > 128 * 144 ? BYTES : 128 * 144];
+  int64_t id = blockIdx.x;
+  if (id < a.n_dy) {
+    const int64_t across = a.op / 64;
+    stage_tile<T, HALF>(reinterpret_cast<const T *>(a.dY), a.dy, a.dyt, a.sums, reinterpret_cast<T *>(a.db), a.T, a.O,
+                        a.op, a.tp, id / across, id % across, lds);
+  } else if (id < a.n_dy + a.n_x) {
+    id -= a.n_dy;
+    const int64_t across = (a.I + 63) / 64;
+    stage_tile<T, HALF>(reinterpret_cast<const T *>(a.x), nullptr, a.xt, nullptr, nullptr, a.T, a.I, 0, a.tp, id / across,
+                        id % across, lds);
+  } else {
+    id -= a.n_dy + a.n_x;
+    const int64_t grp = id % a.groups, row_tile = id / a.groups % (a.op / 64);
+    unpack_tile(a, grp, row_tile, id / (a.groups * (a.op / 64)), lds);
   }
 }
 
@@ -123,25 +166,6 @@ hipError_t staged(const uint16_t *a, int na, const uint16_t *b, int nb, int64_t 
   return gemm<HALF ? GEMM_F16 : GEMM_BF16, T>(g, stream);
 }
 
-// Those sums alone, in the same order.
-template <typename T>
-__global__ __launch_bounds__(256) void mx_colsum_kernel(const T *dy, float *sums, int64_t rows, int64_t cols) {
-  __shared__ float f[32][64];
-  const int64_t c0 = (int64_t)blockIdx.x * 64, r0 = (int64_t)blockIdx.y * 128;
-  float part[8] = {};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = i * 32 + (threadIdx.x >> 3), c = (threadIdx.x & 7) * 8;
-    Raw8<T> v;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v.v[k] = (T)0.0f;
-    if (r0 + r < rows) v = load8_tail(dy + (r0 + r) * cols + c0 + c, cols - c0 - c);
-#pragma unroll
-    for (int k = 0; k < 8; ++k) part[k] += (float)v.v[k];
-  }
-  join_columns(part, f, sums + blockIdx.y * cols + c0, cols - c0);
-}
-
 // db from the tiles' sums: a workgroup takes 64 columns, its wavefronts a quarter of the tiles each.
 template <typename T>
 __global__ __launch_bounds__(256) void mx_db_kernel(const float *sums, T *db, int64_t tiles, int64_t cols) {
@@ -160,28 +184,28 @@ __global__ __launch_bounds__(256) void mx_db_kernel(const float *sums, T *db, in
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 
 // Workspace: dX needs dY [P][T][Op] and W^T [nc][I][Op]; dW needs dY^T [P'][O][Tp] and x^T
-// [P'][I][Tp], Op and Tp whole groups; both share one area, used one after the other.
+// [P'][I][Tp], Op and Tp whole groups; db the column sums of dY's tiles.
 struct Plan {
-  int p, pw;        // pieces of a plain element: for dX, for dW
-  int64_t op, tp;   // padded reductions
+  int p, pw;                // pieces of a plain element: for dX, for dW
+  int64_t op, tp;           // padded reductions
   int64_t dy, wt, dyt, xt;  // bytes of the staged operands
   int64_t partx, partw;     // of the products' partial sums
-  int64_t sums;             // of the column sums' parts
+  int64_t sums;             // of the column sums
 };
 
-Plan plan(int dtype, int nc, int64_t T, int64_t I, int64_t O) {
+Plan plan(int dtype, int nc, int64_t T, int64_t I, int64_t O, bool dx, bool dw, bool db) {
   Plan s;
   s.p = dtype == LM_F32 ? 3 : (dtype == LM_F16 ? 2 : 1);
   s.pw = dtype == LM_F32 ? 3 : 1;
   s.op = up(O, MX_GROUP);
   s.tp = up(T, MX_GROUP);
-  s.dy = up(s.p * T * s.op * 2, 256);
-  s.wt = up(nc * I * s.op * 2, 256);
-  s.dyt = up(s.pw * O * s.tp * 2, 256);
-  s.xt = up(s.pw * I * s.tp * 2, 256);
-  s.partx = gemm_partial_bytes(T, I, s.op / 64 * s.p * nc);
-  s.sums = up((T + 127) / 128 * O * 4, 256);
-  s.partw = gemm_partial_bytes(O, I, s.tp / 64 * (s.pw == 3 ? 6 : 1));
+  s.dy = dx ? up(s.p * T * s.op * 2, 256) : 0;
+  s.wt = dx ? up(nc * I * s.op * 2, 256) : 0;
+  s.partx = dx ? up(gemm_partial_bytes(T, I, s.op / 64 * s.p * nc), 256) : 0;
+  s.dyt = dw ? up(s.pw * O * s.tp * 2, 256) : 0;
+  s.xt = dw ? up(s.pw * I * s.tp * 2, 256) : 0;
+  s.partw = dw ? up(gemm_partial_bytes(O, I, s.tp / 64 * (s.pw == 3 ? 6 : 1)), 256) : 0;
+  s.sums = db ? up(s.tp / 128 * O * 4, 256) : 0;
   return s;
 }
 
@@ -189,43 +213,59 @@ template <typename T, bool HALF>
 hipError_t backward(int nc, int64_t rows, int64_t in, int64_t out, const T *x, const uint8_t *codes,
                     const uint32_t *scales, const T *dY, T *dX, T *dW, T *db, const Plan &s, char *ws,
                     hipStream_t stream) {
-  const auto blocks = [](int64_t n, int64_t per) { return (unsigned)((n + per - 1) / per); };
-  // the column sums' parts come first in the workspace and stay; the products' staged operands
-  // follow, one product's after the other's
-  float *sums = (float *)ws;
-  if (db) ws += s.sums;
-  if (dX) {
-    uint16_t *dy = (uint16_t *)ws, *wt = (uint16_t *)(ws + s.dy);
-    if (out > 0) {  // else a reduction of nothing: zeros
-      mx_stage_kernel<T><<<blocks(rows * s.op / 8, 256), 256, 0, stream>>>(dY, dy, rows, out, s.op);
-      mx_unpack_t_kernel<<<dim3((unsigned)mx_groups(in), blocks(s.op, 64), (unsigned)nc), 256, 0, stream>>>(
-          codes, scales, wt, out, in, mx_groups(in), s.op);
+  const auto take = [&](int64_t bytes) {
+    char *p = ws;
+    ws += bytes;
+    return p;
+  };
+  StageArgs a = {};
+  a.dY = dY;
+  a.x = x;
+  a.codes = codes;
+  a.scales = scales;
+  a.T = rows;
+  a.O = out;
+  a.I = in;
+  a.op = s.op;
+  a.tp = s.tp;
+  a.groups = mx_groups(in);
+  uint16_t *dy = (uint16_t *)take(s.dy), *wt = (uint16_t *)take(s.wt);
+  char *partx = take(s.partx);
+  uint16_t *dyt = (uint16_t *)take(s.dyt), *xt = (uint16_t *)take(s.xt);
+  char *partw = take(s.partw);
+  float *sums = (float *)take(s.sums);
+  const int64_t row_tiles = s.tp / 128;
+  int64_t n_w = 0;
+  if (rows > 0 && out > 0) {
+    a.n_dy = row_tiles * (s.op / 64);
+    if (dX) {
+      a.dy = dy;
+      a.wt = wt;
+      n_w = a.groups * (s.op / 64) * nc;
     }
-    const hipError_t e = staged<T, false>(dy, s.p, wt, nc, rows, in, s.op, s.p + nc, dX, ws + s.dy + s.wt, stream);
+    if (dW) {
+      a.dyt = dyt;
+      a.xt = xt;
+      a.n_x = row_tiles * ((in + 63) / 64);
+    }
+    if (db) {
+      a.sums = sums;
+      if (row_tiles == 1) a.db = db;
+    }
+    mx_stage_all_kernel<T, HALF><<<(unsigned)(a.n_dy + a.n_x + n_w), 256, 0, stream>>>(a);
+  }
+  // reductions of nothing give zeros
+  if (dX) {
+    const hipError_t e = staged<T, false>(dy, s.p, wt, nc, rows, in, s.op, s.p + nc, dX, partx, stream);
     if (e != hipSuccess) return e;
   }
   if (dW) {
-    uint16_t *dyt = (uint16_t *)ws, *xt = (uint16_t *)(ws + s.dyt);
-    if (rows > 0) {
-      const dim3 grid(blocks(out, 64), blocks(s.tp, 128));
-      if (db)
-        mx_stage_t_kernel<T, HALF, true><<<grid, 256, 0, stream>>>(dY, dyt, sums, rows, out, s.tp);
-      else
-        mx_stage_t_kernel<T, HALF, false><<<grid, 256, 0, stream>>>(dY, dyt, nullptr, rows, out, s.tp);
-      mx_stage_t_kernel<T, HALF, false>
-          <<<dim3(blocks(in, 64), blocks(s.tp, 128)), 256, 0, stream>>>(x, xt, nullptr, rows, in, s.tp);
-    }
     // of two values in three pieces the pairs past i + j = 2 are left out: each is within 2^-26 of
     // |dY||x|, less than one rounding of the sum
-    const hipError_t e = staged<T, HALF>(dyt, s.pw, xt, s.pw, out, in, s.tp, 3, dW, ws + s.dyt + s.xt, stream);
+    const hipError_t e = staged<T, HALF>(dyt, s.pw, xt, s.pw, out, in, s.tp, 3, dW, partw, stream);
     if (e != hipSuccess) return e;
   }
-  if (db) {
-    const int64_t tiles = s.tp / 128;
-    if (!dW && tiles > 0)
-      mx_colsum_kernel<T><<<dim3(blocks(out, 64), (unsigned)tiles), 256, 0, stream>>>(dY, sums, rows, out);
-    mx_db_kernel<T><<<blocks(out, 64), 256, 0, stream>>>(sums, db, tiles, out);
-  }
+  if (db && row_tiles != 1) mx_db_kernel<T><<<(unsigned)((out + 63) / 64), 256, 0, stream>>>(sums, db, row_tiles, out);
   return hipGetLastError();
 }
 
@@ -233,15 +273,14 @@ hipError_t backward(int nc, int64_t rows, int64_t in, int64_t out, const T *x, c
 
 int64_t mx4_linear_bwd_workspace_bytes(int dtype, int nc, int64_t batch, int64_t in, int64_t out, int dx, int dw,
                                        int db) {
-  const Plan s = plan(dtype, nc, batch, in, out);
-  const int64_t a = dx ? s.dy + s.wt + s.partx : 0, b = dw ? s.dyt + s.xt + s.partw : 0;
-  return (a > b ? a : b) + (db ? s.sums : 0);
+  const Plan s = plan(dtype, nc, batch, in, out, dx, dw, db);
+  return s.dy + s.wt + s.partx + s.dyt + s.xt + s.partw + s.sums;
 }
 
 hipError_t launch_mx4_linear_bwd(int dtype, int nc, int64_t batch, int64_t in, int64_t out, const void *x,
                                  const void *codes, const void *scales, const void *dY, void *dX, void *dW, void *db,
                                  void *ws, hipStream_t stream) {
-  const Plan s = plan(dtype, nc, batch, in, out);
+  const Plan s = plan(dtype, nc, batch, in, out, dX != nullptr, dW != nullptr, db != nullptr);
   const uint8_t *c = (const uint8_t *)codes;
   const uint32_t *sc = (const uint32_t *)scales;
   if (dtype == LM_F16)
