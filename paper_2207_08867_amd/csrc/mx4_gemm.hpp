@@ -143,7 +143,8 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
 
   // what this lane loads in a step: rows past the end repeat the last one
   constexpr int NB = BN * BB / 1024, LA = BM / 8 / NW, LB = (NB + NW - 1) / NW;
-  constexpr int LOADS = LA + LB + (SCALED_A ? (SG * BM / 64 + NW - 1) / NW : 0) + (SCALED_B ? (SG * BN / 64 + NW - 1) / NW : 0);
+  constexpr int LOADS_A = LA + (SCALED_A ? (SG * BM / 64 + NW - 1) / NW : 0);
+  constexpr int LOADS = LOADS_A + LB + (SCALED_B ? (SG * BN / 64 + NW - 1) / NW : 0);
   static_assert(LOADS * (S - 1) < 64, "vmcnt counts to 63");
   static_assert(LA % 2 == 0 && (BB != 128 || LB % 2 == 0), "rows of a load start at a multiple of 16 or 8 past one");
   static_assert(BM % (8 * NW) == 0 && (BB != 128 || NB % NW == 0), "whole loads a wavefront");
@@ -176,28 +177,18 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
     const bool wrap = s.k + 1 == a.steps;
     return At{go && wrap ? s.pair + 1 : s.pair, go ? (wrap ? 0 : s.k + 1) : s.k};
   };
-  const auto load = [&](int buf, At s) {
-    const int k = s.k, ia = (int)(a.pa >> (4 * s.pair)) & 15, ib = (int)(a.pb >> (4 * s.pair)) & 15;
+  // The loads of a step of A, and of B, each with its scales.
+  const auto load_a = [&](int buf, At s) {
+    const int k = s.k, ia = (int)(a.pa >> (4 * s.pair)) & 15;
     const uint32_t to = lds0 + buf * (uint32_t)sizeof(Stage);
     const char *pa = uniform(a.a + ia * a.a_plane + m0 * a.a_ld + (int64_t)k * 128);
-    const char *pb = uniform(a.b + ib * a.b_plane + n0 * a.b_ld + (int64_t)k * BB);
-    if constexpr (KIND == GEMM_FP4) {
-      // an odd group count: the last step's upper half re-reads the lower one and counts for
-      // nothing (its scales are taken as 0 on both sides, and 2^-254 times 36 is 0)
-      const bool whole = 2 * k + 1 < a.groups;
-      const uint32_t back[2] = {whole ? 0 : upper[0], whole ? 0 : upper[1]};
+    // FP4, an odd group count: the last step's upper half re-reads the lower one and counts for
+    // nothing (its scales are taken as 0 on both sides, and 2^-254 times 36 is 0)
+    const bool whole = KIND != GEMM_FP4 || 2 * k + 1 < a.groups;
+    const uint32_t back[2] = {whole ? 0 : upper[0], whole ? 0 : upper[1]};
 #pragma unroll
-      for (int i = 0; i < LA; ++i)
-        lds_load16(to + offsetof(Stage, a) + (wave * LA + i) * 1024, offa[i] - back[i & 1], pa);
-#pragma unroll
-      for (int i = 0; i < LB; ++i)
-        lds_load16(to + offsetof(Stage, b) + (wave * LB + i) * 1024, offb[i] - back[i & 1], pb);
-    } else {
-#pragma unroll
-      for (int i = 0; i < LA; ++i) lds_load16(to + offsetof(Stage, a) + (wave * LA + i) * 1024, offa[i], pa);
-#pragma unroll
-      for (int i = 0; i < LB; ++i) lds_load16(to + offsetof(Stage, b) + (wave * LB + i) % NB * 1024, offb[i], pb);
-    }
+    for (int i = 0; i < LA; ++i)
+      lds_load16(to + offsetof(Stage, a) + (wave * LA + i) * 1024, KIND == GEMM_FP4 ? offa[i] - back[i & 1] : offa[i], pa);
     // Words of scales, 64 a load; a wavefront past the last one repeats a load, with the same data.
     if constexpr (SCALED_A) {
       constexpr int N = SG * BM / 64;
@@ -209,6 +200,16 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
                   uniform(a.as + (ia * a.groups + grp) * a.M + m0));
       }
     }
+  };
+  const auto load_b = [&](int buf, At s) {
+    const int k = s.k, ib = (int)(a.pb >> (4 * s.pair)) & 15;
+    const uint32_t to = lds0 + buf * (uint32_t)sizeof(Stage);
+    const char *pb = uniform(a.b + ib * a.b_plane + n0 * a.b_ld + (int64_t)k * BB);
+    const bool whole = KIND != GEMM_FP4 || 2 * k + 1 < a.groups;
+    const uint32_t back[2] = {whole ? 0 : upper[0], whole ? 0 : upper[1]};
+#pragma unroll
+    for (int i = 0; i < LB; ++i)
+      lds_load16(to + offsetof(Stage, b) + (wave * LB + i) % NB * 1024, KIND == GEMM_FP4 ? offb[i] - back[i & 1] : offb[i], pb);
     if constexpr (SCALED_B) {
       constexpr int N = SG * BN / 64;
 #pragma unroll
@@ -234,7 +235,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
   // The operands of quarter q of a step, of which a lane holds chunk 4 g + q (16-bit kinds) or
   // 2 q + g (FP4) of its rows, and what multiplies them.
   Operands<KIND, TM, TN> op[2];
-  Scales<KIND, TM, TN> sc;
+  Scales<KIND, TM, TN> sc, sc_next;
   const auto read = [&](int buf, int q, Operands<KIND, TM, TN> &o) {
     const Stage &B = st[buf];
     const int c = ((KIND == GEMM_FP4 ? 2 * q + g : 4 * g + q) ^ ((r >> 1) & 7)) * 16;
@@ -245,7 +246,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
       for (int j = 0; j < TN; ++j) o.b[j] = *reinterpret_cast<const u32x4 *>(B.b + (wn + r + j * 32) * 128 + c);
     }
   };
-  const auto read_scales = [&](int buf, int k) {
+  const auto read_scales = [&](int buf, int k, Scales<KIND, TM, TN> &sc) {
     const Stage &B = st[buf];
     if constexpr (KIND == GEMM_FP4) {
 #pragma unroll
@@ -311,15 +312,22 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
     int k = here.k, buf = 0;
 #pragma unroll
     for (int i = 0; i < S; ++i) {
-      load(i, ahead);
+      load_a(i, ahead);
+      if (i + 1 == S) break;  // its B comes with the first step's products
+      load_b(i, ahead);
       ahead = next(ahead, s_begin + i < last);
     }
-    gemm_wait<LOADS * (S - 1)>();
-    read_scales(0, k);
+    gemm_wait<LOADS * (S - 2) + LOADS_A>();
+    read_scales(0, k, sc);
     read(0, 0, op[0]);
     for (int step = s_begin; step < s_end; ++step) {
-      const int then = buf + 1 == S ? 0 : buf + 1;
+      const int then = buf + 1 == S ? 0 : buf + 1, before = buf == 0 ? S - 1 : buf - 1;
+      load_b(before, ahead);
+      ahead = next(ahead, step + S - 1 < last);
       read(buf, 1, op[1]);
+      // a wavefront in its products goes before one at its loads (2 to 4% of the 16-bit kinds; the
+      // scaled products lose 1%)
+      if constexpr (KIND != GEMM_FP4) __builtin_amdgcn_s_setprio(1);
       multiply(0, op[0]);
       weave();
       read(buf, 2, op[0]);
@@ -328,17 +336,18 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
       read(buf, 3, op[1]);
       multiply(2, op[0]);
       weave();
+      if constexpr (KIND != GEMM_FP4) __builtin_amdgcn_s_setprio(0);
       // Every read of this buffer is out.  Once all wavefronts are here the next step's buffer has
       // landed and this one is free; the last quarter's products cover the first reads.  Past the
       // end the last step is loaded and read again, and not multiplied.
       gemm_wait<LOADS * (S - 2)>();
-      load(buf, ahead);
-      ahead = next(ahead, step + S < last);
+      load_a(buf, ahead);
+      if (step < last) k = k + 1 == a.steps ? 0 : k + 1;
+      read_scales(then, k, sc_next);
       read(then, 0, op[0]);
       multiply(3, op[1]);
       weave();
-      if (step < last) k = k + 1 == a.steps ? 0 : k + 1;
-      read_scales(then, k);
+      sc = sc_next;
       buf = then;
     }
     gemm_wait<0>();  // no load may land after the workgroup has left
@@ -353,14 +362,21 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
                           (int)lb - wn);
 }
 
-// The slices' sums, in the slices' order.
+// The slices' sums, in the slices' order; eight slices are asked for at a time.
 template <typename T>
 __global__ __launch_bounds__(256) void mx_gemm_sum_kernel(GemmArgs a) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = a.M * a.N;
   if (i >= n) return;
-  float v = a.partial[i];
-  for (int s = 1; s < a.slices; ++s) v += a.partial[s * n + i];
-  if (a.bias) v += (float)reinterpret_cast<const T *>(a.bias)[i % a.N];
+  float v = 0.0f;
+  for (int s0 = 0; s0 < a.slices; s0 += 8) {
+    float p[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) p[u] = s0 + u < a.slices ? a.partial[(s0 + u) * n + i] : 0.0f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v += p[u];
+  }
+  // n stays below 2^26 with more than one slice
+  if (a.bias) v += (float)reinterpret_cast<const T *>(a.bias)[(uint32_t)i % (uint32_t)a.N];
   reinterpret_cast<T *>(a.c)[i] = (T)v;
 }
 
