@@ -380,3 +380,47 @@ def test_many_elements(mcf):
     alone = mcf.mc_mx4_quantize(x[pick].contiguous())
     assert torch.equal(codes[:, pick], alone[0]) and torch.equal(scales[:, :, pick], alone[1])
     assert torch.equal(back[pick], mcf.mc_mx4_dequantize(*alone, n, dtype=torch.float16))
+
+
+def values64(W, n):
+    """The numbers of an MXFP4 tensor on the GPU, summed over its components, in binary64."""
+    import torch
+
+    codes, scales = W[0].long(), W[1].permute(0, 2, 1, 3).double()
+    nib = torch.stack((codes & 15, codes >> 4), -1).reshape(codes.shape[0], codes.shape[1], -1, 32)
+    mag = torch.tensor(ref.MAGNITUDES, device="cuda")[nib & 7] * (1.0 - 2.0 * (nib >> 3))
+    return (mag * torch.exp2(scales - 127.0).flatten(2).unsqueeze(-1)).flatten(2).sum(0)[:, :n]
+
+
+@pytest.mark.parametrize("M, N, K", [(4099, 4100, 4224), (2100, 8200, 2049), (520, 5000, 8192), (8200, 70, 1000)])
+def test_large_products_exact_sums(mcf, M, N, K):
+    """The largest tiles, their ragged edges and the products in slices: integer operands whose every
+    partial sum binary32 holds (36 K < 2^22 quarters), so all orders give the same."""
+    import torch
+
+    g = np.random.default_rng(M + K)
+    A, B = (tuple(map(dev, random_mx4(g, 1, r, K, 127, 128))) for r in (M, N))
+    a, b = values64(A, K), values64(B, K)
+    assert torch.equal(mcf.mc_mx4_matmul(A, B, K, dtype=torch.float32).double(), a @ b.t())
+    x = torch.from_numpy(g.integers(-4, 5, (M, K)).astype(np.float32)).cuda()
+    want = x.double() @ b.t()
+    for dtype in (torch.float16, torch.bfloat16, torch.float32):
+        assert torch.equal(mcf.mc_mx4_linear_fwd(x.to(dtype), B).double(), want.to(dtype).double()), dtype
+    dY = torch.from_numpy(g.integers(-2, 3, (M, N)).astype(np.float32)).cuda()
+    for dtype in (torch.float16, torch.bfloat16, torch.float32):
+        dX, dW, db = mcf.mc_mx4_linear_bwd(x.to(dtype), B, dY.to(dtype))
+        assert torch.equal(dX.double(), (dY.double() @ b).to(dtype).double()), dtype
+        assert torch.equal(dW.double(), (dY.double().t() @ x.double()).to(dtype).double()), dtype
+        assert torch.equal(db.double(), dY.double().sum(0).to(dtype).double()), dtype
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_results_repeat(mcf, dtype):
+    """The same bits from one call to the next."""
+    import torch
+
+    W = mcf.mc_mx4_quantize(torch.randn(300, 1000, device="cuda"), nc=2)
+    x = torch.randn(500, 1000, device="cuda").to(getattr(torch, dtype))
+    first = mcf.mc_mx4_linear_fwd(x, W)
+    for _ in range(3):
+        assert torch.equal(mcf.mc_mx4_linear_fwd(x, W), first)
