@@ -75,6 +75,17 @@ __device__ inline bf16x8 mx_bf16(uint32_t w, float scale) {
   return r;
 }
 
+// The same as binary16; exact where the scale is between 2^-23 and 2^13.
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+__device__ inline f16x8 mx_f16(uint32_t w, float scale) {
+  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0);
+  const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1);
+  const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2);
+  const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3);
+  f16x8 r = {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  return r;
+}
+
 __device__ inline void mx_f32(uint32_t w, float scale, float v[8]) {
   const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 0);
   const f32x2 b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, scale, 1);

@@ -2,7 +2,12 @@
 // one kernel for three kinds of operands, all rows of the reduction:
 //   GEMM_FP4   both sides MXFP4 codes with their scales (32 x 32 x 64 scaled products);
 //   GEMM_BF16, GEMM_F16   both sides 16-bit numbers (32 x 32 x 16 products);
-//   GEMM_MIX   A bfloat16, B MXFP4 codes, turned into bfloat16 in registers.
+//   GEMM_MIX   A bfloat16, B MXFP4 codes, turned into bfloat16 in registers;
+//   GEMM_MIXH  A binary16, B MXFP4 codes, turned into binary16 in registers: a row of B is taken
+//              relative to its largest scale, the power of two goes to the result's column.  36
+//              binades below that scale are exact in binary16; a tile with a number further down
+//              (which the rows' pass over the scales finds) splits A into two bfloat16 pieces
+//              instead, in registers, at half the rate.
 // The operands of one instruction are 16 bytes a lane in every kind, and it takes as long (32
 // cycles of a SIMD at the full rate), so the kinds share tiles, staging and schedule.
 //
@@ -22,7 +27,7 @@
 
 namespace mcf {
 
-enum GemmKind { GEMM_FP4 = 0, GEMM_BF16 = 1, GEMM_F16 = 2, GEMM_MIX = 3 };
+enum GemmKind { GEMM_FP4 = 0, GEMM_BF16 = 1, GEMM_F16 = 2, GEMM_MIX = 3, GEMM_MIXH = 4 };
 
 struct GemmArgs {
   const char *a, *b;              // pieces' planes of rows
@@ -30,6 +35,8 @@ struct GemmArgs {
   int64_t a_ld, b_ld;             // bytes of a row
   const uint32_t *as, *bs;        // scales [plane][groups][rows]
   int64_t groups;
+  const uint8_t *top, *wide;      // MIXH: the largest scale of each row of B, and for every 64 rows
+                                  // whether a number lies too far below it
   void *c;                        // [M][N]
   const void *bias;               // [N] or null
   float *partial;                 // [slices][M][N], with more than one slice
@@ -77,22 +84,14 @@ __device__ inline void gemm_tile(uint32_t id, uint32_t gm, uint32_t gn, uint32_t
 
 // A wavefront's tiles to `to`, its first element in the M x N result; `rows` and `cols` are what is
 // left of the result there.  Lane (r, g) holds column r of a tile, rows 8 (e / 4) + 4 g + e mod 4.
-// A row's start is scalar arithmetic, the lane's part a 32-bit offset.
-template <typename T, int TM, int TN>
-__device__ inline void gemm_store(const f32x16 (&acc)[TM][TN], T *to, const T *bias, int64_t ld, int rows, int cols) {
+// A row's start is scalar arithmetic, the lane's part a 32-bit offset.  SHIFT: the columns' powers
+// of two.
+template <typename T, bool SHIFT, int TM, int TN>
+__device__ inline void gemm_store(const f32x16 (&acc)[TM][TN], T *to, const T *bias, const int (&shift)[TN], int64_t ld,
+                                  int rows, int cols) {
   const int lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5;
   const uint32_t off = (uint32_t)(4 * g * ld + r);
-  if (rows >= 32 * TM && cols >= 32 * TN) {
-#pragma unroll
-    for (int i = 0; i < TM; ++i)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        T *row = to + (i * 32 + (e >> 2) * 8 + (e & 3)) * ld;
-#pragma unroll
-        for (int j = 0; j < TN; ++j) row[off + j * 32] = (T)(bias ? acc[i][j][e] + (float)bias[j * 32 + r] : acc[i][j][e]);
-      }
-    return;
-  }
+  const bool whole = rows >= 32 * TM && cols >= 32 * TN;
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -101,19 +100,28 @@ __device__ inline void gemm_store(const f32x16 (&acc)[TM][TN], T *to, const T *b
       T *row = to + m * ld;
 #pragma unroll
       for (int j = 0; j < TN; ++j)
-        if (m + 4 * g < rows && j * 32 + r < cols)
-          row[off + j * 32] = (T)(bias ? acc[i][j][e] + (float)bias[j * 32 + r] : acc[i][j][e]);
+        if (whole || (m + 4 * g < rows && j * 32 + r < cols)) {
+          float v = acc[i][j][e];
+          if constexpr (SHIFT) v = ldexpf(v, shift[j]);
+          row[off + j * 32] = (T)(bias ? v + (float)bias[j * 32 + r] : v);
+        }
     }
 }
 
+template <bool B>
+struct Flag {
+  static constexpr bool value = B;
+};
+constexpr bool gemm_mixed(GemmKind k) { return k == GEMM_MIX || k == GEMM_MIXH; }
+
 template <GemmKind KIND, int TM, int TN>
 struct Operands {
-  u32x4 a[TM], b[KIND == GEMM_MIX ? 1 : TN];
+  u32x4 a[TM], b[gemm_mixed(KIND) ? 1 : TN];
 };
 template <GemmKind KIND, int TM, int TN>
 struct Scales {
   uint32_t a[KIND == GEMM_FP4 ? 2 : 1][TM], b[KIND == GEMM_FP4 ? 2 : 1][TN];
-  u32x4 codes[KIND == GEMM_MIX ? TN : 1];
+  u32x4 codes[gemm_mixed(KIND) ? TN : 1];
   float scale[TN];
 };
 __device__ inline i32x8 widen(u32x4 v) {
@@ -124,8 +132,9 @@ __device__ inline i32x8 widen(u32x4 v) {
 template <GemmKind KIND, typename T, int WM, int WN, int TM, int TN, int S>
 __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NW = WM * WN;
-  constexpr int BB = KIND == GEMM_MIX ? 32 : 128;  // bytes of a row of B in a step
-  constexpr bool SCALED_A = KIND == GEMM_FP4, SCALED_B = KIND == GEMM_FP4 || KIND == GEMM_MIX;
+  constexpr bool MIX = gemm_mixed(KIND);
+  constexpr int BB = MIX ? 32 : 128;  // bytes of a row of B in a step
+  constexpr bool SCALED_A = KIND == GEMM_FP4, SCALED_B = KIND == GEMM_FP4 || MIX;
   constexpr int SG = KIND == GEMM_FP4 ? 2 : 1;     // words of scales of a row in a step
   struct alignas(128) Stage {
     char a[BM * 128];
@@ -236,17 +245,31 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
   // 2 q + g (FP4) of its rows, and what multiplies them.
   Operands<KIND, TM, TN> op[2];
   Scales<KIND, TM, TN> sc, sc_next;
+  // MIXH: a column's power of two, and whether this tile needs the wide form
+  int shift_of[TN];
+  bool any_wide = false;
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    shift_of[j] = 0;
+    if constexpr (KIND == GEMM_MIXH) {
+      const int64_t n = n0 + wn + j * 32 + r;
+      shift_of[j] = (int)a.top[n < a.N ? n : a.N - 1] - 140;
+    }
+  }
+  if constexpr (KIND == GEMM_MIXH) {
+    for (int64_t n = n0; n < n0 + lb; n += 64) any_wide = any_wide || a.wide[n / 64] != 0;
+  }
   const auto read = [&](int buf, int q, Operands<KIND, TM, TN> &o) {
     const Stage &B = st[buf];
     const int c = ((KIND == GEMM_FP4 ? 2 * q + g : 4 * g + q) ^ ((r >> 1) & 7)) * 16;
 #pragma unroll
     for (int i = 0; i < TM; ++i) o.a[i] = *reinterpret_cast<const u32x4 *>(B.a + (wm + r + i * 32) * 128 + c);
-    if constexpr (KIND != GEMM_MIX) {
+    if constexpr (!MIX) {
 #pragma unroll
       for (int j = 0; j < TN; ++j) o.b[j] = *reinterpret_cast<const u32x4 *>(B.b + (wn + r + j * 32) * 128 + c);
     }
   };
-  const auto read_scales = [&](int buf, int k, Scales<KIND, TM, TN> &sc) {
+  const auto read_scales = [&](int buf, int k, Scales<KIND, TM, TN> &sc, auto wide) {
     const Stage &B = st[buf];
     if constexpr (KIND == GEMM_FP4) {
 #pragma unroll
@@ -258,27 +281,38 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
         for (int j = 0; j < TN; ++j) sc.b[h][j] = (B.bs[h * BN + wn + j * 32 + r] & keep) >> (8 * g);
       }
     }
-    if constexpr (KIND == GEMM_MIX) {
+    if constexpr (MIX) {
       // lane group g takes block g of the step's two: the reduction runs over them side by side
       const int shift = 8 * (2 * (k & 1) + g);
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
         sc.codes[j] = *reinterpret_cast<const u32x4 *>(B.b + (wn + r + j * 32) * BB + g * 16);
-        sc.scale[j] = mx_scale((B.bs[wn + j * 32 + r] >> shift) & 255u);
+        uint32_t byte = (B.bs[wn + j * 32 + r] >> shift) & 255u;
+        if constexpr (KIND == GEMM_MIXH && !decltype(wide)::value) {
+          // relative to the row's largest scale, which becomes 2^13: 6 2^13 is below binary16's end
+          const int rel = (int)byte - shift_of[j];
+          byte = byte == 255 ? 255 : (rel > 0 ? rel : 0);
+        }
+        sc.scale[j] = mx_scale(byte);
       }
     }
   };
-  const auto multiply = [&](int q, const Operands<KIND, TM, TN> &o) {
+  const auto multiply = [&](int q, const Operands<KIND, TM, TN> &o, auto wide) {
     u32x4 fb[TN];
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
-      if constexpr (KIND == GEMM_MIX)
+      if constexpr (KIND == GEMM_MIXH && !decltype(wide)::value)
+        fb[j] = __builtin_bit_cast(u32x4, mx_f16(sc.codes[j][q], sc.scale[j]));
+      else if constexpr (MIX)
         fb[j] = __builtin_bit_cast(u32x4, mx_bf16(sc.codes[j][q], sc.scale[j]));
       else
         fb[j] = o.b[j];
     }
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < TM; ++i) {
+      bf16x8 piece[2];
+      if constexpr (KIND == GEMM_MIXH && decltype(wide)::value)
+        mx_split8<_Float16, 2>(__builtin_bit_cast(Raw8<_Float16>, o.a[i]), piece);
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
         f32x16 &c = acc[i][j];
@@ -289,16 +323,21 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
             c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 0, sa, 0, sb);
           else
             c = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 2, sa, 2, sb);
-        } else if constexpr (KIND == GEMM_F16) {
+        } else if constexpr (KIND == GEMM_MIXH && decltype(wide)::value) {
+#pragma unroll
+          for (int p = 0; p < 2; ++p)
+            c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(piece[p], __builtin_bit_cast(bf16x8, fb[j]), c, 0, 0, 0);
+        } else if constexpr (KIND == GEMM_F16 || KIND == GEMM_MIXH) {
           c = __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, o.a[i]), __builtin_bit_cast(f16x8, fb[j]), c, 0, 0, 0);
         } else {
           c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, o.a[i]), __builtin_bit_cast(bf16x8, fb[j]), c, 0, 0, 0);
         }
       }
+    }
   };
   // Reads of the next quarter between the products of this one.
   const auto weave = [&]() {
-    constexpr int READS = TM + (KIND == GEMM_MIX ? 0 : TN), EACH = TM * TN / READS > 0 ? TM * TN / READS : 1;
+    constexpr int READS = TM + (MIX ? 0 : TN), EACH = TM * TN / READS > 0 ? TM * TN / READS : 1;
 #pragma unroll
     for (int i = 0; i < READS; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
@@ -306,7 +345,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
     }
   };
 
-  if (s_begin < s_end) {
+  const auto run = [&](auto wide) {
     const int last = s_end - 1;
     At here = {s_begin / a.steps, s_begin % a.steps}, ahead = here;
     int k = here.k, buf = 0;
@@ -318,7 +357,7 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
       ahead = next(ahead, s_begin + i < last);
     }
     gemm_wait<LOADS * (S - 2) + LOADS_A>();
-    read_scales(0, k, sc);
+    read_scales(0, k, sc, wide);
     read(0, 0, op[0]);
     for (int step = s_begin; step < s_end; ++step) {
       const int then = buf + 1 == S ? 0 : buf + 1, before = buf == 0 ? S - 1 : buf - 1;
@@ -328,13 +367,13 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
       // a wavefront in its products goes before one at its loads (2 to 4% of the 16-bit kinds; the
       // scaled products lose 1%)
       if constexpr (KIND != GEMM_FP4) __builtin_amdgcn_s_setprio(1);
-      multiply(0, op[0]);
+      multiply(0, op[0], wide);
       weave();
       read(buf, 2, op[0]);
-      multiply(1, op[1]);
+      multiply(1, op[1], wide);
       weave();
       read(buf, 3, op[1]);
-      multiply(2, op[0]);
+      multiply(2, op[0], wide);
       weave();
       if constexpr (KIND != GEMM_FP4) __builtin_amdgcn_s_setprio(0);
       // Every read of this buffer is out.  Once all wavefronts are here the next step's buffer has
@@ -343,23 +382,35 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
       gemm_wait<LOADS * (S - 2)>();
       load_a(buf, ahead);
       if (step < last) k = k + 1 == a.steps ? 0 : k + 1;
-      read_scales(then, k, sc_next);
+      read_scales(then, k, sc_next, wide);
       read(then, 0, op[0]);
-      multiply(3, op[1]);
+      multiply(3, op[1], wide);
       weave();
       sc = sc_next;
       buf = then;
     }
     gemm_wait<0>();  // no load may land after the workgroup has left
+  };
+  if (s_begin < s_end) {
+    if (KIND == GEMM_MIXH && any_wide)
+      run(Flag<KIND == GEMM_MIXH>());
+    else
+      run(Flag<false>());
   }
 
   const int64_t at = (m0 + wm) * a.N + n0 + wn;
+  constexpr bool SHIFT = KIND == GEMM_MIXH;
+  if (any_wide) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j) shift_of[j] = 0;
+  }
   if (a.slices > 1)
-    gemm_store<float, TM, TN>(acc, a.partial + slice * a.M * a.N + at, nullptr, a.N, (int)la - wm, (int)lb - wn);
+    gemm_store<float, SHIFT, TM, TN>(acc, a.partial + slice * a.M * a.N + at, nullptr, shift_of, a.N, (int)la - wm,
+                                     (int)lb - wn);
   else
-    gemm_store<T, TM, TN>(acc, reinterpret_cast<T *>(a.c) + at,
-                          a.bias ? reinterpret_cast<const T *>(a.bias) + n0 + wn : nullptr, a.N, (int)la - wm,
-                          (int)lb - wn);
+    gemm_store<T, SHIFT, TM, TN>(acc, reinterpret_cast<T *>(a.c) + at,
+                                 a.bias ? reinterpret_cast<const T *>(a.bias) + n0 + wn : nullptr, shift_of, a.N,
+                                 (int)la - wm, (int)lb - wn);
 }
 
 // The slices' sums, in the slices' order; eight slices are asked for at a time.
@@ -397,10 +448,10 @@ struct Pieces {
 };
 
 // src [rows][cols] -> dst [P][rows][ld], zeros from cols to ld.
-template <typename T>
+template <typename T, bool HALF>
 __global__ __launch_bounds__(256) void mx_stage_kernel(const T *src, uint16_t *dst, int64_t rows, int64_t cols,
                                                        int64_t ld) {
-  using S = Pieces<T, false>;
+  using S = Pieces<T, HALF>;
   const int64_t per_row = ld / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (id >= rows * per_row) return;
   const int64_t row = id <= 0xffffffffll ? (int64_t)((uint32_t)id / (uint32_t)per_row) : id / per_row;

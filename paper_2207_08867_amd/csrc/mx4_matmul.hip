@@ -295,31 +295,88 @@ int64_t thin_rows(int dtype) { return dtype == LM_BF16 ? 32 : 16; }
 
 namespace {
 
-int pieces_of(int dtype) { return dtype == LM_F32 ? 3 : (dtype == LM_F16 ? 2 : 1); }
+// MIXH's pass over B's scales [nc][groups][N] and codes [nc][N][64 groups]: the largest scale of
+// each row (NaN blocks aside), and for 64 rows whether a block with a number in it lies more than 36
+// binades below its row's.  A workgroup takes 64 rows, its wavefronts a quarter of the groups each.
+__global__ __launch_bounds__(256) void mx_top_kernel(const uint32_t *scales, const uint8_t *codes, uint8_t *top,
+                                                            uint8_t *wide, int nc, int64_t groups, int64_t N) {
+  __shared__ int part[4][64];
+  __shared__ int far[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t row = (int64_t)blockIdx.x * 64 + lane, n = row < N ? row : N - 1;
+  const int64_t total = nc * groups, from = total * wave / 4, to = total * (wave + 1) / 4;
+  int m = 0;
+#pragma unroll 4
+  for (int64_t i = from; i < to; ++i) {
+    const uint32_t w = scales[i * N + n];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const int s = (int)(w >> (8 * b)) & 255;
+      m = s != 255 && s > m ? s : m;
+    }
+  }
+  part[wave][lane] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < 4; ++w) m = part[w][lane] > m ? part[w][lane] : m;
+  bool out = false;
+  for (int64_t i = from; i < to; ++i) {
+    const uint32_t w = scales[i * N + n];
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      if ((int)((w >> (8 * b)) & 255u) >= m - 36) continue;
+      // component i / groups, group i mod groups
+      const u32x4 c = *reinterpret_cast<const u32x4 *>(codes + ((i / groups) * N + n) * (groups * 64) + (i % groups) * 64 + b * 16);
+      out = out || (((c[0] | c[1]) | (c[2] | c[3])) & 0x77777777u) != 0;
+    }
+  }
+  const bool any = __any(out);
+  if (lane == 0) far[wave] = any;
+  __syncthreads();
+  if (wave == 0) {
+    if (row < N) top[row] = (uint8_t)m;
+    if (lane == 0) wide[blockIdx.x] = (far[0] | far[1] | far[2] | far[3]) != 0;
+  }
+}
 
-// A bfloat16 x whose rows are whole groups at 16-byte addresses is multiplied where it lies; any
-// other is staged as bfloat16 pieces of padded rows.
+// Staged planes of a plain x: bfloat16 pieces of binary32, the 16-bit formats as they are.
+int planes_of(int dtype) { return dtype == LM_F32 ? 3 : 1; }
+
+// A 16-bit x whose rows are whole groups at 16-byte addresses is multiplied where it lies; any other
+// is staged in padded rows.
 bool in_place(int dtype, int64_t in, const void *x) {
-  return dtype == LM_BF16 && in % MX_GROUP == 0 && (uintptr_t)x % 16 == 0;
+  return dtype != LM_F32 && in % MX_GROUP == 0 && (uintptr_t)x % 16 == 0;
 }
 
+int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 int64_t stage_bytes(int dtype, int64_t batch, int64_t in) {
-  return pieces_of(dtype) * batch * mx_groups(in) * MX_GROUP * 2;
+  return planes_of(dtype) * batch * mx_groups(in) * MX_GROUP * 2;
 }
+// The rows' largest scales and the flags of 64 rows each.
+int64_t top_bytes(int dtype, int64_t out) { return dtype == LM_F16 ? up16(out) + up16((out + 63) / 64) : 0; }
 
 template <typename T>
-hipError_t mix_gemm(GemmArgs &g, int dtype, const void *x, int64_t in, void *ws, hipStream_t stream) {
+hipError_t mix_gemm(GemmArgs &g, int dtype, int nc, const void *x, int64_t in, char *ws, hipStream_t stream) {
+  constexpr bool HALF = __is_same(T, _Float16);
   const int64_t ld = g.groups * MX_GROUP;
   g.a = (const char *)x;
   if (!in_place(dtype, in, x)) {
-    mx_stage_kernel<T><<<(unsigned)((g.M * (ld / 8) + 255) / 256), 256, 0, stream>>>((const T *)x, (uint16_t *)ws, g.M,
-                                                                                     in, ld);
-    g.a = (const char *)ws;
-    g.partial = (float *)((char *)ws + stage_bytes(dtype, g.M, in));
+    mx_stage_kernel<T, HALF><<<(unsigned)((g.M * (ld / 8) + 255) / 256), 256, 0, stream>>>((const T *)x, (uint16_t *)ws,
+                                                                                          g.M, in, ld);
+    g.a = ws;
   }
+  ws += stage_bytes(dtype, g.M, in);
+  if constexpr (HALF) {
+    g.top = (const uint8_t *)ws;
+    g.wide = g.top + up16(g.N);
+    mx_top_kernel<<<(unsigned)((g.N + 63) / 64), 256, 0, stream>>>(g.bs, (const uint8_t *)g.b, (uint8_t *)g.top,
+                                                                  (uint8_t *)g.wide, nc, g.groups, g.N);
+    ws += top_bytes(dtype, g.N);
+  }
+  g.partial = (float *)ws;
   g.a_ld = ld * 2;
   g.a_plane = g.M * g.a_ld;
-  return gemm<GEMM_MIX, T>(g, stream);
+  return gemm<HALF ? GEMM_MIXH : GEMM_MIX, T>(g, stream);
 }
 
 void set_pairs(GemmArgs &g, int na, int nb) {
@@ -365,7 +422,8 @@ hipError_t launch_mx4_matmul(int dtype, int64_t M, int64_t N, int64_t K, const v
 
 int64_t mx4_linear_workspace_bytes(int dtype, int nc, int64_t batch, int64_t in, int64_t out) {
   if (batch <= thin_rows(dtype)) return 0;
-  return stage_bytes(dtype, batch, in) + gemm_partial_bytes(batch, out, mx_groups(in) * 2 * nc * pieces_of(dtype));
+  return stage_bytes(dtype, batch, in) + top_bytes(dtype, out) +
+         gemm_partial_bytes(batch, out, mx_groups(in) * 2 * nc * planes_of(dtype));
 }
 
 hipError_t launch_mx4_linear(int dtype, int nc, int64_t batch, int64_t in, int64_t out, const void *x,
@@ -384,14 +442,13 @@ hipError_t launch_mx4_linear(int dtype, int nc, int64_t batch, int64_t in, int64
   g.groups = G;
   g.c = y;
   g.bias = bias;
-  g.partial = (float *)ws;
   g.M = batch;
   g.N = out;
   g.steps = (int)(G * 2);
-  set_pairs(g, pieces_of(dtype), nc);
-  if (dtype == LM_F16) return mix_gemm<_Float16>(g, dtype, x, in, ws, stream);
-  if (dtype == LM_BF16) return mix_gemm<__bf16>(g, dtype, x, in, ws, stream);
-  return mix_gemm<float>(g, dtype, x, in, ws, stream);
+  set_pairs(g, planes_of(dtype), nc);
+  if (dtype == LM_F16) return mix_gemm<_Float16>(g, dtype, nc, x, in, (char *)ws, stream);
+  if (dtype == LM_BF16) return mix_gemm<__bf16>(g, dtype, nc, x, in, (char *)ws, stream);
+  return mix_gemm<float>(g, dtype, nc, x, in, (char *)ws, stream);
 }
 
 }  // namespace mcf

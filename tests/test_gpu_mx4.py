@@ -424,3 +424,41 @@ def test_results_repeat(mcf, dtype):
     first = mcf.mc_mx4_linear_fwd(x, W)
     for _ in range(3):
         assert torch.equal(mcf.mc_mx4_linear_fwd(x, W), first)
+
+
+@pytest.mark.parametrize("below", [0, 35, 36, 37, 60, 120])
+@pytest.mark.parametrize("T, O, I", [(70, 130, 256), (300, 520, 640)])
+def test_binary16_layer_of_wide_rows(mcf, below, T, O, I):
+    """Blocks far below the largest one of their weight row, where x is zero at the large ones: the
+    small ones alone make the result, exactly, whatever lies between them."""
+    import torch
+
+    g = np.random.default_rng(below)
+    codes, scales = random_mx4(g, 1, O, I, 117, 118)
+    small = 117
+    big = np.arange(0, I // 128) % 2 == 0  # every second group is large in all four blocks
+    scales[:, big] = min(small + below, 254)
+    scales[:, ~big, O // 2] = 0  # a row whose small blocks are the least there is, with no numbers in them
+    codes.reshape(1, O, I // 128, 64)[:, O // 2, ~big] = 0
+    x = g.integers(-4, 5, (T, I)).astype(np.float64)
+    x.reshape(T, I // 128, 128)[:, big] = 0.0
+    W = dev(codes), dev(scales)
+    got = mcf.mc_mx4_linear_fwd(dev(x, "float16"), W)
+    want = torch.from_numpy(x).cuda() @ values64(W, I).t()
+    assert torch.equal(got.double(), want.half().double())
+    b = torch.randn(O, device="cuda").half()
+    got = mcf.mc_mx4_linear_fwd(dev(x, "float16"), W, b)
+    assert (got.double() - (want + b.double())).abs().max() <= 2.0 ** -11 * (want.abs().max() + 8)
+
+
+def test_binary16_layer_keeps_nan_blocks(mcf):
+    """A weight block that stands for NaN makes its column NaN and no other."""
+    import torch
+
+    x = torch.randn(100, 300, device="cuda").half()
+    w = torch.randn(90, 300, device="cuda")
+    w[7, 40] = float("nan")
+    y = mcf.mc_mx4_linear_fwd(x, mcf.mc_mx4_quantize(w))
+    assert torch.isnan(y[:, 7]).all()
+    keep = torch.arange(90, device="cuda") != 7
+    assert torch.isfinite(y[:, keep]).all()
