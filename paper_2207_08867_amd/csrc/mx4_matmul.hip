@@ -297,14 +297,15 @@ namespace {
 
 // MIXH's pass over B's scales [nc][groups][N] and codes [nc][N][64 groups]: the largest scale of
 // each row (NaN blocks aside), and for 64 rows whether a block with a number in it lies more than 36
-// binades below its row's.  A workgroup takes 64 rows, its wavefronts a quarter of the groups each.
-__global__ __launch_bounds__(256) void mx_top_kernel(const uint32_t *scales, const uint8_t *codes, uint8_t *top,
+// binades below its row's.  A workgroup takes 64 rows, its 16
+// wavefronts a part of the groups each.
+__global__ __launch_bounds__(1024) void mx_top_kernel(const uint32_t *scales, const uint8_t *codes, uint8_t *top,
                                                             uint8_t *wide, int nc, int64_t groups, int64_t N) {
-  __shared__ int part[4][64];
-  __shared__ int far[4];
+  __shared__ int part[16][64];
+  __shared__ int far[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t row = (int64_t)blockIdx.x * 64 + lane, n = row < N ? row : N - 1;
-  const int64_t total = nc * groups, from = total * wave / 4, to = total * (wave + 1) / 4;
+  const int64_t total = nc * groups, from = total * wave / 16, to = total * (wave + 1) / 16;
   int m = 0;
 #pragma unroll 4
   for (int64_t i = from; i < to; ++i) {
@@ -318,7 +319,7 @@ __global__ __launch_bounds__(256) void mx_top_kernel(const uint32_t *scales, con
   part[wave][lane] = m;
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < 4; ++w) m = part[w][lane] > m ? part[w][lane] : m;
+  for (int w = 0; w < 16; ++w) m = part[w][lane] > m ? part[w][lane] : m;
   bool out = false;
   for (int64_t i = from; i < to; ++i) {
     const uint32_t w = scales[i * N + n];
@@ -335,7 +336,8 @@ __global__ __launch_bounds__(256) void mx_top_kernel(const uint32_t *scales, con
   __syncthreads();
   if (wave == 0) {
     if (row < N) top[row] = (uint8_t)m;
-    if (lane == 0) wide[blockIdx.x] = (far[0] | far[1] | far[2] | far[3]) != 0;
+    const bool all = __any(lane < 16 && far[lane & 15] != 0);
+    if (lane == 0) wide[blockIdx.x] = all;
   }
 }
 
@@ -369,7 +371,7 @@ hipError_t mix_gemm(GemmArgs &g, int dtype, int nc, const void *x, int64_t in, c
   if constexpr (HALF) {
     g.top = (const uint8_t *)ws;
     g.wide = g.top + up16(g.N);
-    mx_top_kernel<<<(unsigned)((g.N + 63) / 64), 256, 0, stream>>>(g.bs, (const uint8_t *)g.b, (uint8_t *)g.top,
+    mx_top_kernel<<<(unsigned)((g.N + 63) / 64), 1024, 0, stream>>>(g.bs, (const uint8_t *)g.b, (uint8_t *)g.top,
                                                                   (uint8_t *)g.wide, nc, g.groups, g.N);
     ws += top_bytes(dtype, g.N);
   }
