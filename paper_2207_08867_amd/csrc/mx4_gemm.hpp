@@ -495,7 +495,7 @@ inline GemmPlan gemm_plan(int64_t M, int64_t N, int64_t total) {
     int tile;
     double step1, step2, fixed;
   };
-  constexpr Row rows[3] = {{256, 1.7, 3.4, 9.0}, {128, 0.6, 1.0, 5.0}, {64, 0.33, 0.45, 3.0}};
+  constexpr Row rows[3] = {{256, 1.7, 3.4, 9.0}, {128, 0.6, 1.0, 5.0}, {64, 0.36, 0.52, 3.0}};
   GemmPlan best = {64, 1};
   double least = 1e300;
   for (const Row &r : rows) {
