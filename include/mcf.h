@@ -401,7 +401,8 @@ int64_t mc_linreg_workspace(int dtype, int nc, int64_t n, int64_t d);
  * rounded to nearest E2M1, ties to even, at most 6, times 2^X, and v minus it is the next
  * component's value.  A block with an infinity or NaN gets the scale 255 and zero codes in
  * every component.
- * x: [nc_in][rows][n]; codes and scales as above.  rows ceil(n / 128) at most 2^34. */
+ * x: [nc_in][rows][n]; codes and scales as above.  ceil(rows / 16) ceil(n / 128)
+ * below 2^31. */
 int mc_mx4_quantize(int dtype, int nc_in, int nc, int64_t rows, int64_t n, const void *x, void *codes, void *scales,
                     void *stream);
 

@@ -5,8 +5,7 @@
 // number the element stands for, is the next component's input.  The remainder is exact in
 // binary32: it is a multiple of v_i's last place and no larger than v_i, or within 2^(X-2) of
 // zero.  Both directions stream: 2 to 4 bytes read and 17/32 of a byte written per element and
-// component (or back), so HBM bounds them.  A lane takes 8 elements and four lanes a block, so
-// a wavefront reads 1 KiB of binary16 in one instruction and writes 256 bytes of codes; the
+// component (or back), so HBM bounds them.  A lane takes 8 elements and four lanes a block; the
 // block's maximum is two DPP steps inside a quad.
 #include "mcf_internal.hpp"
 #include "mx4.hpp"
@@ -26,7 +25,7 @@ __device__ inline uint32_t block_max(uint32_t m) { return quad_max<0x4e>(quad_ma
 struct QuantArgs {
   const void *x;
   uint8_t *codes, *scales;
-  int64_t rows, n, groups, chunks;  // chunks: 8-element pieces, 16 a group, of all rows
+  int64_t rows, n, groups;
   int nc;
 };
 
@@ -46,6 +45,16 @@ __device__ inline float round_odd(double d) {
   if (back == d || !(u & 0x7f800000u)) return f;  // exact, or far below every rounding boundary
   const uint32_t cut = (fabs(back) > fabs(d) ? u - 1 : u) | 1u;
   return __builtin_bit_cast(float, cut);
+}
+
+// A workgroup covers one group of TILE_ROWS rows: 256 bytes of binary16 side by side in each row, and
+// the scales of neighbouring rows, 64 bytes, in one line.  Measured (us, quantising and reading back):
+// 100000 x 100 binary16 7.3 and 10.3, against 37.9 and 35.4 with the 16 groups along one row; 8192 x
+// 8192 bfloat16 28 and 37 (6.1 and 4.6 TB/s), alike for every shape.
+constexpr int TILE_ROWS = 16;
+
+__device__ inline int64_t divide(int64_t a, int64_t b) {
+  return (a | b) <= 0xffffffffll ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
 struct BlockAt {
@@ -112,18 +121,12 @@ __device__ inline void quantize64(const QuantArgs &a, const BlockAt &b, double v
 
 template <typename T, int NIN>
 __global__ __launch_bounds__(256) void mx_quant_kernel(QuantArgs a) {
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  // whole quads leave together: chunks is a multiple of 16
-  if (id >= a.chunks) return;
   BlockAt b;
-  const int64_t gid = id >> 4;
-  b.in = (int)(id & 15);
-  if (gid <= 0xffffffffll && a.groups <= 0xffffffffll) {
-    b.row = (uint32_t)gid / (uint32_t)a.groups;
-  } else {
-    b.row = gid / a.groups;
-  }
-  b.group = gid - b.row * a.groups;
+  const int64_t tile = divide(blockIdx.x, a.groups);
+  b.in = (int)(threadIdx.x & 15);
+  b.row = tile * TILE_ROWS + (threadIdx.x >> 4);
+  b.group = blockIdx.x - tile * a.groups;
+  if (b.row >= a.rows) return;  // whole quads leave together
   const int64_t col = b.group * MX_GROUP + b.in * 8;
   const T *x = reinterpret_cast<const T *>(a.x) + b.row * a.n + col;
   float v[8];
@@ -169,19 +172,17 @@ __global__ __launch_bounds__(256) void mx_quant_kernel(QuantArgs a) {
 
 template <typename T>
 __global__ __launch_bounds__(256) void mx_dequant_kernel(const uint8_t *codes, const uint8_t *scales, T *out, int nc,
-                                                         int64_t rows, int64_t n, int64_t groups, int64_t per_row,
-                                                         int64_t chunks) {
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (id >= chunks) return;
-  const int64_t row = (id <= 0xffffffffll && per_row <= 0xffffffffll) ? (int64_t)((uint32_t)id / (uint32_t)per_row)
-                                                                      : id / per_row;
-  const int64_t piece = id - row * per_row;
+                                                         int64_t rows, int64_t n, int64_t groups) {
+  const int64_t tile = divide(blockIdx.x, groups), group = blockIdx.x - tile * groups;
+  const int in = (int)(threadIdx.x & 15);
+  const int64_t row = tile * TILE_ROWS + (threadIdx.x >> 4);
+  const int64_t col = group * MX_GROUP + in * 8;
+  if (row >= rows || col >= n) return;
   float v[8] = {};
   for (int c = nc - 1; c >= 0; --c) {  // the smallest component first
     const int64_t plane = (int64_t)c * rows;
-    const uint32_t word =
-        *reinterpret_cast<const uint32_t *>(codes + (plane + row) * (groups * 64) + piece * 4);
-    const uint32_t byte = scales[((plane * groups) + (piece >> 4) * rows + row) * 4 + ((piece >> 2) & 3)];
+    const uint32_t word = *reinterpret_cast<const uint32_t *>(codes + (plane + row) * (groups * 64) + group * 64 + in * 4);
+    const uint32_t byte = scales[((int64_t)c * groups * rows + group * rows + row) * 4 + (in >> 2)];
     float q[8];
     mx_f32(word, mx_scale(byte), q);
 #pragma unroll
@@ -190,12 +191,16 @@ __global__ __launch_bounds__(256) void mx_dequant_kernel(const uint8_t *codes, c
   Raw8<T> r;
 #pragma unroll
   for (int i = 0; i < 8; ++i) r.v[i] = (T)v[i];
-  store8_tail(out + row * n + piece * 8, r, n - piece * 8);
+  store8_tail(out + row * n + col, r, n - col);
+}
+
+unsigned tiles(int64_t rows, int64_t groups) {
+  return (unsigned)((rows + TILE_ROWS - 1) / TILE_ROWS * groups);
 }
 
 template <typename T>
 hipError_t quantize(int nc_in, const QuantArgs &a, hipStream_t stream) {
-  const dim3 grid((unsigned)((a.chunks + 255) / 256));
+  const dim3 grid(tiles(a.rows, a.groups));
   switch (nc_in) {
     case 1: mx_quant_kernel<T, 1><<<grid, 256, 0, stream>>>(a); break;
     case 2: mx_quant_kernel<T, 2><<<grid, 256, 0, stream>>>(a); break;
@@ -216,7 +221,6 @@ hipError_t launch_mx4_quantize(int dtype, int nc_in, int nc, int64_t rows, int64
   a.rows = rows;
   a.n = n;
   a.groups = mx_groups(n);
-  a.chunks = rows * a.groups * 16;
   a.nc = nc;
   if (dtype == LM_F16) return quantize<_Float16>(nc_in, a, stream);
   if (dtype == LM_BF16) return quantize<__bf16>(nc_in, a, stream);
@@ -225,15 +229,15 @@ hipError_t launch_mx4_quantize(int dtype, int nc_in, int nc, int64_t rows, int64
 
 hipError_t launch_mx4_dequantize(int dtype, int nc, int64_t rows, int64_t n, const void *codes, const void *scales,
                                  void *out, hipStream_t stream) {
-  const int64_t per_row = (n + 7) / 8, chunks = rows * per_row, groups = mx_groups(n);
-  const dim3 grid((unsigned)((chunks + 255) / 256));
+  const int64_t groups = mx_groups(n);
+  const dim3 grid(tiles(rows, groups));
   const uint8_t *c = (const uint8_t *)codes, *s = (const uint8_t *)scales;
   if (dtype == LM_F16)
-    mx_dequant_kernel<_Float16><<<grid, 256, 0, stream>>>(c, s, (_Float16 *)out, nc, rows, n, groups, per_row, chunks);
+    mx_dequant_kernel<_Float16><<<grid, 256, 0, stream>>>(c, s, (_Float16 *)out, nc, rows, n, groups);
   else if (dtype == LM_BF16)
-    mx_dequant_kernel<__bf16><<<grid, 256, 0, stream>>>(c, s, (__bf16 *)out, nc, rows, n, groups, per_row, chunks);
+    mx_dequant_kernel<__bf16><<<grid, 256, 0, stream>>>(c, s, (__bf16 *)out, nc, rows, n, groups);
   else
-    mx_dequant_kernel<float><<<grid, 256, 0, stream>>>(c, s, (float *)out, nc, rows, n, groups, per_row, chunks);
+    mx_dequant_kernel<float><<<grid, 256, 0, stream>>>(c, s, (float *)out, nc, rows, n, groups);
   return hipGetLastError();
 }
 

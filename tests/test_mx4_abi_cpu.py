@@ -25,7 +25,7 @@ def test_quantize(L):
         assert L.mc_mx4_quantize(f, 1, 1, 4, 40, x, c, s, None) == E_DTYPE
     for nc_in, nc in ((0, 1), (5, 1), (1, 0), (1, 5)):
         assert L.mc_mx4_quantize(BF16, nc_in, nc, 4, 40, x, c, s, None) == E_NC
-    for rows, n in ((-1, 40), (4, -1), (1 << 41, 1), (1 << 34, 200)):
+    for rows, n in ((-1, 40), (4, -1), (1 << 41, 1), (1 << 34, 300), (1, 1 << 39), (1 << 36, 1)):
         assert L.mc_mx4_quantize(F16, 1, 1, rows, n, x, c, s, None) == E_SHAPE
     assert L.mc_mx4_quantize(F16, 1, 1, 0, 40, None, None, None, None) == OK
     assert L.mc_mx4_quantize(F16, 1, 1, 4, 0, None, None, None, None) == OK
