@@ -34,7 +34,8 @@ bool nc_ok(int nc) { return nc >= 1 && nc <= MAX_NC; }
 int64_t codes_bytes(int nc, int64_t rows, int64_t n) { return nc * rows * mcf::mx_groups(n) * 64; }
 int64_t scales_bytes(int nc, int64_t rows, int64_t n) { return nc * rows * mcf::mx_groups(n) * 4; }
 
-// rows x n of an MXFP4 tensor: a workgroup takes one group of 16 rows, numbered with 31 bits.
+// rows x n of an MXFP4 tensor: a workgroup takes 16 groups, of 4 or 16 rows; they are numbered with
+// 31 bits.
 int tensor_check(int64_t rows, int64_t n) {
   if (rows < 0 || n < 0 || rows > ((int64_t)1 << 40) || n > ((int64_t)1 << 40)) return MCF_E_SHAPE;
   const int64_t g = mcf::mx_groups(n);

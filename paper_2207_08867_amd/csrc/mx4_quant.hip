@@ -25,8 +25,8 @@ __device__ inline uint32_t block_max(uint32_t m) { return quad_max<0x4e>(quad_ma
 struct QuantArgs {
   const void *x;
   uint8_t *codes, *scales;
-  int64_t rows, n, groups;
-  int nc;
+  int64_t rows, n, groups, across;  // workgroups side by side along a row
+  int nc, shift;
 };
 
 __device__ inline uint32_t pack8(const float v[8], float scale) {
@@ -47,11 +47,13 @@ __device__ inline float round_odd(double d) {
   return __builtin_bit_cast(float, cut);
 }
 
-// A workgroup covers one group of TILE_ROWS rows: 256 bytes of binary16 side by side in each row, and
-// the scales of neighbouring rows, 64 bytes, in one line.  Measured (us, quantising and reading back):
-// 100000 x 100 binary16 7.3 and 10.3, against 37.9 and 35.4 with the 16 groups along one row; 8192 x
-// 8192 bfloat16 28 and 37 (6.1 and 4.6 TB/s), alike for every shape.
-constexpr int TILE_ROWS = 16;
+// A workgroup covers 16 groups of 16 lanes: 1 << tile_shift rows of 16 >> tile_shift groups each.  Short
+// rows take 16 rows of one group, so that no lane lies past a row's end and the scales of 16
+// neighbouring rows fall into one line; long rows 4 x 4, which reads longer runs.  Measured (us,
+// quantising and reading back), 100000 x 100 binary16: 7.3 and 10.3 as 16 rows, 22 and 18 as 4, 38
+// and 35 as one; 4099 x 4097 binary16 in two planes and components: 21.1 and 15.6, 18.7 and 15.4, 18.8
+// and 15.4; 8192 x 8192 bfloat16: 27 to 29 (6.2 TB/s) and 37 (4.6 TB/s) in all of them.
+int tile_shift(int64_t groups) { return groups >= 16 ? 2 : 4; }
 
 __device__ inline int64_t divide(int64_t a, int64_t b) {
   return (a | b) <= 0xffffffffll ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
@@ -122,11 +124,12 @@ __device__ inline void quantize64(const QuantArgs &a, const BlockAt &b, double v
 template <typename T, int NIN>
 __global__ __launch_bounds__(256) void mx_quant_kernel(QuantArgs a) {
   BlockAt b;
-  const int64_t tile = divide(blockIdx.x, a.groups);
+  const int64_t tile = divide(blockIdx.x, a.across);
+  const int g = threadIdx.x >> 4;
   b.in = (int)(threadIdx.x & 15);
-  b.row = tile * TILE_ROWS + (threadIdx.x >> 4);
-  b.group = blockIdx.x - tile * a.groups;
-  if (b.row >= a.rows) return;  // whole quads leave together
+  b.row = (tile << a.shift) + (g >> (4 - a.shift));
+  b.group = ((blockIdx.x - tile * a.across) << (4 - a.shift)) + (g & ((16 >> a.shift) - 1));
+  if (b.row >= a.rows || b.group >= a.groups) return;  // whole quads leave together
   const int64_t col = b.group * MX_GROUP + b.in * 8;
   const T *x = reinterpret_cast<const T *>(a.x) + b.row * a.n + col;
   float v[8];
@@ -172,10 +175,12 @@ __global__ __launch_bounds__(256) void mx_quant_kernel(QuantArgs a) {
 
 template <typename T>
 __global__ __launch_bounds__(256) void mx_dequant_kernel(const uint8_t *codes, const uint8_t *scales, T *out, int nc,
-                                                         int64_t rows, int64_t n, int64_t groups) {
-  const int64_t tile = divide(blockIdx.x, groups), group = blockIdx.x - tile * groups;
-  const int in = (int)(threadIdx.x & 15);
-  const int64_t row = tile * TILE_ROWS + (threadIdx.x >> 4);
+                                                         int64_t rows, int64_t n, int64_t groups, int64_t across,
+                                                         int shift) {
+  const int64_t tile = divide(blockIdx.x, across);
+  const int g = threadIdx.x >> 4, in = (int)(threadIdx.x & 15);
+  const int64_t row = (tile << shift) + (g >> (4 - shift));
+  const int64_t group = ((blockIdx.x - tile * across) << (4 - shift)) + (g & ((16 >> shift) - 1));
   const int64_t col = group * MX_GROUP + in * 8;
   if (row >= rows || col >= n) return;
   float v[8] = {};
@@ -194,8 +199,11 @@ __global__ __launch_bounds__(256) void mx_dequant_kernel(const uint8_t *codes, c
   store8_tail(out + row * n + col, r, n - col);
 }
 
+// Workgroups along a row, and in all.
+int64_t tiles_across(int64_t groups) { return (groups + (16 >> tile_shift(groups)) - 1) >> (4 - tile_shift(groups)); }
 unsigned tiles(int64_t rows, int64_t groups) {
-  return (unsigned)((rows + TILE_ROWS - 1) / TILE_ROWS * groups);
+  const int s = tile_shift(groups);
+  return (unsigned)(((rows + (1 << s) - 1) >> s) * tiles_across(groups));
 }
 
 template <typename T>
@@ -221,6 +229,8 @@ hipError_t launch_mx4_quantize(int dtype, int nc_in, int nc, int64_t rows, int64
   a.rows = rows;
   a.n = n;
   a.groups = mx_groups(n);
+  a.across = tiles_across(a.groups);
+  a.shift = tile_shift(a.groups);
   a.nc = nc;
   if (dtype == LM_F16) return quantize<_Float16>(nc_in, a, stream);
   if (dtype == LM_BF16) return quantize<__bf16>(nc_in, a, stream);
@@ -230,14 +240,16 @@ hipError_t launch_mx4_quantize(int dtype, int nc_in, int nc, int64_t rows, int64
 hipError_t launch_mx4_dequantize(int dtype, int nc, int64_t rows, int64_t n, const void *codes, const void *scales,
                                  void *out, hipStream_t stream) {
   const int64_t groups = mx_groups(n);
+  const int64_t across = tiles_across(groups);
+  const int shift = tile_shift(groups);
   const dim3 grid(tiles(rows, groups));
   const uint8_t *c = (const uint8_t *)codes, *s = (const uint8_t *)scales;
   if (dtype == LM_F16)
-    mx_dequant_kernel<_Float16><<<grid, 256, 0, stream>>>(c, s, (_Float16 *)out, nc, rows, n, groups);
+    mx_dequant_kernel<_Float16><<<grid, 256, 0, stream>>>(c, s, (_Float16 *)out, nc, rows, n, groups, across, shift);
   else if (dtype == LM_BF16)
-    mx_dequant_kernel<__bf16><<<grid, 256, 0, stream>>>(c, s, (__bf16 *)out, nc, rows, n, groups);
+    mx_dequant_kernel<__bf16><<<grid, 256, 0, stream>>>(c, s, (__bf16 *)out, nc, rows, n, groups, across, shift);
   else
-    mx_dequant_kernel<float><<<grid, 256, 0, stream>>>(c, s, (float *)out, nc, rows, n, groups);
+    mx_dequant_kernel<float><<<grid, 256, 0, stream>>>(c, s, (float *)out, nc, rows, n, groups, across, shift);
   return hipGetLastError();
 }
 
