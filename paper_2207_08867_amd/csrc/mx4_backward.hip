@@ -148,9 +148,8 @@ void set_pairs(GemmArgs &a, int na, int nb, int below) {
 }
 
 // C [M][N] from staged a [na][M][ld] and b [nb][N][ld], pairs i + j < below.
-template <typename T, bool HALF>
-hipError_t staged(const uint16_t *a, int na, const uint16_t *b, int nb, int64_t M, int64_t N, int64_t ld, int below,
-                  void *c, void *partial, hipStream_t stream) {
+GemmArgs staged(const uint16_t *a, int na, const uint16_t *b, int nb, int64_t M, int64_t N, int64_t ld, int below, void *c,
+                void *partial) {
   GemmArgs g = {};
   g.a = (const char *)a;
   g.b = (const char *)b;
@@ -163,7 +162,7 @@ hipError_t staged(const uint16_t *a, int na, const uint16_t *b, int nb, int64_t 
   g.N = N;
   g.steps = (int)(ld / 64);
   set_pairs(g, na, nb, below);
-  return gemm<HALF ? GEMM_F16 : GEMM_BF16, T>(g, stream);
+  return g;
 }
 
 // db from the tiles' sums: a workgroup takes 64 columns, its wavefronts a quarter of the tiles each.
@@ -191,6 +190,10 @@ struct Plan {
   int64_t dy, wt, dyt, xt;  // bytes of the staged operands
   int64_t partx, partw;     // of the products' partial sums
   int64_t sums;             // of the column sums
+  // dX and dW in one launch where two.tile is not 0; planx and planw their tiles and slices, those of the
+  // call for every gradient also where one alone is asked for, so that its bits are the same
+  GemmTwoPlan two;
+  GemmPlan planx, planw;
 };
 
 Plan plan(int dtype, int nc, int64_t T, int64_t I, int64_t O, bool dx, bool dw, bool db) {
@@ -201,10 +204,14 @@ Plan plan(int dtype, int nc, int64_t T, int64_t I, int64_t O, bool dx, bool dw, 
   s.tp = up(T, MX_GROUP);
   s.dy = dx ? up(s.p * T * s.op * 2, 256) : 0;
   s.wt = dx ? up(nc * I * s.op * 2, 256) : 0;
-  s.partx = dx ? up(gemm_partial_bytes(T, I, s.op / 64 * s.p * nc), 256) : 0;
+  const int64_t steps_x = s.op / 64 * s.p * nc, steps_w = s.tp / 64 * (s.pw == 3 ? 6 : 1);
+  s.two = gemm_two_plan(T, I, steps_x, O, I, steps_w);
+  s.planx = s.two.tile ? GemmPlan{s.two.tile, s.two.slices1} : gemm_plan(T, I, steps_x);
+  s.planw = s.two.tile ? GemmPlan{s.two.tile, s.two.slices2} : gemm_plan(O, I, steps_w);
+  s.partx = dx ? up(gemm_slices_bytes(T, I, s.planx.slices), 256) : 0;
   s.dyt = dw ? up(s.pw * O * s.tp * 2, 256) : 0;
   s.xt = dw ? up(s.pw * I * s.tp * 2, 256) : 0;
-  s.partw = dw ? up(gemm_partial_bytes(O, I, s.tp / 64 * (s.pw == 3 ? 6 : 1)), 256) : 0;
+  s.partw = dw ? up(gemm_slices_bytes(O, I, s.planw.slices), 256) : 0;
   s.sums = db ? up(s.tp / 128 * O * 4, 256) : 0;
   return s;
 }
@@ -254,17 +261,19 @@ hipError_t backward(int nc, int64_t rows, int64_t in, int64_t out, const T *x, c
     }
     mx_stage_all_kernel<T, HALF><<<(unsigned)(a.n_dy + a.n_x + n_w), 256, 0, stream>>>(a);
   }
-  // reductions of nothing give zeros
-  if (dX) {
-    const hipError_t e = staged<T, false>(dy, s.p, wt, nc, rows, in, s.op, s.p + nc, dX, partx, stream);
-    if (e != hipSuccess) return e;
+  // Reductions of nothing give zeros.  Of two values in three pieces the pairs past i + j = 2 are
+  // left out of dW: each is within 2^-26 of |dY||x|, less than one rounding of the sum.
+  GemmArgs gx = staged(dy, s.p, wt, nc, rows, in, s.op, s.p + nc, dX, partx);
+  GemmArgs gw = staged(dyt, s.pw, xt, s.pw, out, in, s.tp, 3, dW, partw);
+  constexpr GemmKind KW = HALF ? GEMM_F16 : GEMM_BF16;
+  hipError_t e = hipSuccess;
+  if (dX && dW && s.two.tile) {
+    e = gemm_two<GEMM_BF16, KW, T>(gx, gw, s.two, stream);
+  } else {
+    if (dX) e = gemm<GEMM_BF16, T>(gx, s.planx, stream);
+    if (dW && e == hipSuccess) e = gemm<KW, T>(gw, s.planw, stream);
   }
-  if (dW) {
-    // of two values in three pieces the pairs past i + j = 2 are left out: each is within 2^-26 of
-    // |dY||x|, less than one rounding of the sum
-    const hipError_t e = staged<T, HALF>(dyt, s.pw, xt, s.pw, out, in, s.tp, 3, dW, partw, stream);
-    if (e != hipSuccess) return e;
-  }
+  if (e != hipSuccess) return e;
   if (db && row_tiles != 1) mx_db_kernel<T><<<(unsigned)((out + 63) / 64), 256, 0, stream>>>(sums, db, row_tiles, out);
   return hipGetLastError();
 }

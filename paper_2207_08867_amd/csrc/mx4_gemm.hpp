@@ -140,25 +140,29 @@ __device__ inline i32x8 widen(u32x4 v) {
   return __builtin_shufflevector(w, w, 0, 1, 2, 3, -1, -1, -1, -1);
 }
 
+// LDS of a workgroup: S stages.
+template <GemmKind KIND, int BM, int BN>
+struct alignas(128) GemmStage {
+  char a[BM * 128];
+  char b[BN * (gemm_mixed(KIND) ? 32 : 128)];
+  uint32_t as[KIND == GEMM_FP4 ? 2 * BM : 1], bs[KIND == GEMM_FP4 ? 2 * BN : (gemm_mixed(KIND) ? BN : 1)];
+};
+
+// One workgroup: tile `tile` of slice `slice`.
 template <GemmKind KIND, typename T, int WM, int WN, int TM, int TN, int S>
-__global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
+__device__ __forceinline__ void gemm_body(const GemmArgs &a, char *lds, uint32_t tile, int slice) {
   constexpr int BM = WM * TM * 32, BN = WN * TN * 32, NW = WM * WN;
   constexpr bool MIX = gemm_mixed(KIND);
   constexpr int BB = MIX ? 32 : 128;  // bytes of a row of B in a step
   constexpr bool SCALED_A = KIND == GEMM_FP4, SCALED_B = KIND == GEMM_FP4 || MIX;
   constexpr int SG = KIND == GEMM_FP4 ? 2 : 1;     // words of scales of a row in a step
-  struct alignas(128) Stage {
-    char a[BM * 128];
-    char b[BN * BB];
-    uint32_t as[SCALED_A ? SG * BM : 1], bs[SCALED_B ? SG * BN : 1];
-  };
-  __shared__ Stage st[S];
+  using Stage = GemmStage<KIND, BM, BN>;
+  Stage *const st = reinterpret_cast<Stage *>(lds);
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   uint32_t tm, tn;
-  gemm_tile(blockIdx.x, (uint32_t)((a.M + BM - 1) / BM), (uint32_t)((a.N + BN - 1) / BN), &tm, &tn);
+  gemm_tile(tile, (uint32_t)((a.M + BM - 1) / BM), (uint32_t)((a.N + BN - 1) / BN), &tm, &tn);
   const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
-  const int slice = blockIdx.y;
   const int s_begin = (int)((int64_t)a.total * slice / a.slices), s_end = (int)((int64_t)a.total * (slice + 1) / a.slices);
 
   // what this lane loads in a step: rows past the end repeat the last one
@@ -424,6 +428,26 @@ __global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
                                  (int)la - wm, (int)lb - wn);
 }
 
+template <GemmKind KIND, typename T, int WM, int WN, int TM, int TN, int S>
+__global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_kernel(GemmArgs a) {
+  __shared__ __attribute__((aligned(128))) char lds[sizeof(GemmStage<KIND, WM * TM * 32, WN * TN * 32>) * S];
+  gemm_body<KIND, T, WM, WN, TM, TN, S>(a, lds, blockIdx.x, blockIdx.y);
+}
+
+// Two products in one launch, of 16-bit operands: workgroups [0, n) are the first's tiles, slice by
+// slice, the others the second's.  Their loads and products overlap where one grid alone leaves the
+// chip half empty.
+template <GemmKind K1, GemmKind K2, typename T, int WM, int WN, int TM, int TN, int S>
+__global__ __launch_bounds__(64 * WM * WN, 1) void mx_gemm_two_kernel(GemmArgs a, GemmArgs b, uint32_t n, uint32_t tiles_a,
+                                                                     uint32_t tiles_b) {
+  static_assert(!gemm_mixed(K1) && K1 != GEMM_FP4 && !gemm_mixed(K2) && K2 != GEMM_FP4, "one size of LDS");
+  __shared__ __attribute__((aligned(128))) char lds[sizeof(GemmStage<K1, WM * TM * 32, WN * TN * 32>) * S];
+  if (blockIdx.x < n)
+    gemm_body<K1, T, WM, WN, TM, TN, S>(a, lds, blockIdx.x % tiles_a, blockIdx.x / tiles_a);
+  else
+    gemm_body<K2, T, WM, WN, TM, TN, S>(b, lds, (blockIdx.x - n) % tiles_b, (blockIdx.x - n) / tiles_b);
+}
+
 // The slices' sums, in the slices' order; eight slices are asked for at a time.
 template <typename T>
 __global__ __launch_bounds__(256) void mx_gemm_sum_kernel(GemmArgs a) {
@@ -494,42 +518,106 @@ struct GemmPlan {
 // the sizes alone.  Measured (us): a step of a grid of 256 workgroups, and of one of 512, which two
 // of the smaller tiles' workgroups a CU share; and what a launch costs besides its steps.  The
 // kinds differ by up to a fifth, mostly alike.
-inline GemmPlan gemm_plan(int64_t M, int64_t N, int64_t total) {
-  struct Row {
-    int tile;
-    double step1, step2, fixed;
-  };
-  constexpr Row rows[3] = {{256, 1.7, 3.4, 9.0}, {128, 0.6, 1.0, 5.0}, {64, 0.36, 0.52, 3.0}};
+struct GemmRow {
+  int tile;
+  double step1, step2, fixed;
+};
+constexpr GemmRow GEMM_ROWS[3] = {{256, 1.7, 3.4, 9.0}, {128, 0.6, 1.0, 5.0}, {64, 0.36, 0.52, 3.0}};
+constexpr int GEMM_SLICES[8] = {1, 2, 3, 4, 6, 8, 12, 16};
+
+inline int64_t gemm_tiles(int64_t M, int64_t N, int64_t tile) {
+  return ((M + tile - 1) / tile) * ((N + tile - 1) / tile);
+}
+// A slice keeps four steps or more; the partial sums stay below 2^28 bytes.
+inline bool gemm_slices_fit(int64_t M, int64_t N, int64_t total, int slices) {
+  return slices == 1 || (total >= 4 * slices && (double)M * (double)N * slices <= 67108864.0);
+}
+// The slices' sum: a launch, and its reads and writes at 4 TB/s.
+inline double gemm_sum_time(int64_t M, int64_t N, int slices) {
+  return slices == 1 ? 0.0 : 3.0 + (double)M * (double)N * (4.0 * slices + 4.0) / 4e6;
+}
+
+inline GemmPlan gemm_plan(int64_t M, int64_t N, int64_t total, double *time = nullptr) {
   GemmPlan best = {64, 1};
   double least = 1e300;
-  for (const Row &r : rows) {
-    const int64_t tiles = ((M + r.tile - 1) / r.tile) * ((N + r.tile - 1) / r.tile);
-    for (int slices : {1, 2, 3, 4, 6, 8, 12, 16}) {
-      // a slice keeps four steps or more; the partial sums stay below 2^28 bytes
-      if (slices > 1 && (total < 4 * slices || (double)M * (double)N * slices > 67108864.0)) break;
-      const int64_t n = tiles * slices, full = n / 512, rest = n % 512;
+  for (const GemmRow &r : GEMM_ROWS)
+    for (int slices : GEMM_SLICES) {
+      if (!gemm_slices_fit(M, N, total, slices)) break;
+      const int64_t n = gemm_tiles(M, N, r.tile) * slices, full = n / 512, rest = n % 512;
       const double steps = (double)((total + slices - 1) / slices);
-      double t = r.fixed + steps * ((double)full * r.step2 + (rest > 256 ? r.step2 : (rest > 0 ? r.step1 : 0.0)));
-      // the slices' sum: a launch, and its reads and writes at 4 TB/s
-      if (slices > 1) t += 3.0 + (double)M * (double)N * (4.0 * slices + 4.0) / 4e6;
+      const double t = r.fixed + gemm_sum_time(M, N, slices) +
+                       steps * ((double)full * r.step2 + (rest > 256 ? r.step2 : (rest > 0 ? r.step1 : 0.0)));
       if (t < least) {
         least = t;
         best = {r.tile, slices};
       }
     }
-  }
+  if (time) *time = least;
   return best;
 }
 
+// The same for two products in one launch: their workgroups share the chip, 512 at a time at the
+// larger grids' rate, and the longer chain of steps is a lower bound.  tile = 0 where two launches
+// are faster by the model.
+struct GemmTwoPlan {
+  int tile, slices1, slices2;
+};
+inline GemmTwoPlan gemm_two_plan(int64_t M1, int64_t N1, int64_t total1, int64_t M2, int64_t N2, int64_t total2) {
+  double t1, t2;
+  GemmTwoPlan best = {0, gemm_plan(M1, N1, total1, &t1).slices, gemm_plan(M2, N2, total2, &t2).slices};
+  if (M1 == 0 || N1 == 0 || total1 == 0 || M2 == 0 || N2 == 0 || total2 == 0) return best;
+  double least = t1 + t2;
+  for (const GemmRow &r : GEMM_ROWS)
+    for (int s1 : GEMM_SLICES)
+      for (int s2 : GEMM_SLICES) {
+        if (!gemm_slices_fit(M1, N1, total1, s1) || !gemm_slices_fit(M2, N2, total2, s2)) continue;
+        const double n1 = (double)gemm_tiles(M1, N1, r.tile) * s1, n2 = (double)gemm_tiles(M2, N2, r.tile) * s2;
+        const double c1 = (double)((total1 + s1 - 1) / s1), c2 = (double)((total2 + s2 - 1) / s2);
+        const double chain = c1 > c2 ? c1 : c2, work = (n1 * c1 + n2 * c2) / 512.0 * r.step2;
+        const double alone = chain * (n1 + n2 > 256.0 ? r.step2 : r.step1);
+        const double t = r.fixed + (work > alone ? work : alone) + gemm_sum_time(M1, N1, s1) + gemm_sum_time(M2, N2, s2);
+        if (n1 + n2 < 2147483648.0 && t < least) {
+          least = t;
+          best = {r.tile, s1, s2};
+        }
+      }
+  return best;
+}
+
+inline int64_t gemm_slices_bytes(int64_t M, int64_t N, int slices) { return slices > 1 ? slices * M * N * 4 : 0; }
 inline int64_t gemm_partial_bytes(int64_t M, int64_t N, int64_t total) {
-  const GemmPlan p = gemm_plan(M, N, total);
-  return p.slices > 1 ? p.slices * M * N * 4 : 0;
+  return gemm_slices_bytes(M, N, gemm_plan(M, N, total).slices);
+}
+
+template <typename T>
+void gemm_sum(const GemmArgs &a, hipStream_t stream) {
+  if (a.slices > 1) mx_gemm_sum_kernel<T><<<(unsigned)((a.M * a.N + 255) / 256), 256, 0, stream>>>(a);
+}
+
+// Both products by one launch at the plan's tile; a and b are complete but for total and slices.
+template <GemmKind K1, GemmKind K2, typename T>
+hipError_t gemm_two(GemmArgs &a, GemmArgs &b, const GemmTwoPlan &p, hipStream_t stream) {
+  a.total = a.steps * a.pairs;
+  b.total = b.steps * b.pairs;
+  a.slices = p.slices1;
+  b.slices = p.slices2;
+  const uint32_t ta = (uint32_t)gemm_tiles(a.M, a.N, p.tile), tb = (uint32_t)gemm_tiles(b.M, b.N, p.tile);
+  const uint32_t n = ta * (uint32_t)a.slices;
+  const dim3 grid(n + tb * (uint32_t)b.slices);
+  if (p.tile == 256)
+    mx_gemm_two_kernel<K1, K2, T, 2, 4, 4, 2, 2><<<grid, 512, 0, stream>>>(a, b, n, ta, tb);
+  else if (p.tile == 128)
+    mx_gemm_two_kernel<K1, K2, T, 2, 2, 2, 2, 2><<<grid, 256, 0, stream>>>(a, b, n, ta, tb);
+  else
+    mx_gemm_two_kernel<K1, K2, T, 2, 2, 1, 1, 4><<<grid, 256, 0, stream>>>(a, b, n, ta, tb);
+  gemm_sum<T>(a, stream);
+  gemm_sum<T>(b, stream);
+  return hipGetLastError();
 }
 
 template <GemmKind KIND, typename T>
-hipError_t gemm(GemmArgs &a, hipStream_t stream) {
+hipError_t gemm(GemmArgs &a, const GemmPlan &p, hipStream_t stream) {
   a.total = a.steps * a.pairs;
-  const GemmPlan p = gemm_plan(a.M, a.N, a.total);
   a.slices = p.slices;
   const dim3 grid((unsigned)(((a.M + p.tile - 1) / p.tile) * ((a.N + p.tile - 1) / p.tile)), (unsigned)p.slices);
   if (p.tile == 256)
@@ -538,9 +626,13 @@ hipError_t gemm(GemmArgs &a, hipStream_t stream) {
     mx_gemm_kernel<KIND, T, 2, 2, 2, 2, 2><<<grid, 256, 0, stream>>>(a);
   else
     mx_gemm_kernel<KIND, T, 2, 2, 1, 1, 4><<<grid, 256, 0, stream>>>(a);
-  if (p.slices > 1)
-    mx_gemm_sum_kernel<T><<<(unsigned)((a.M * a.N + 255) / 256), 256, 0, stream>>>(a);
+  gemm_sum<T>(a, stream);
   return hipGetLastError();
+}
+
+template <GemmKind KIND, typename T>
+hipError_t gemm(GemmArgs &a, hipStream_t stream) {
+  return gemm<KIND, T>(a, gemm_plan(a.M, a.N, a.steps * a.pairs), stream);
 }
 
 }  // namespace mcf
