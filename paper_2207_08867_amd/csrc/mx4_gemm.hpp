@@ -567,20 +567,34 @@ inline GemmTwoPlan gemm_two_plan(int64_t M1, int64_t N1, int64_t total1, int64_t
   GemmTwoPlan best = {0, gemm_plan(M1, N1, total1, &t1).slices, gemm_plan(M2, N2, total2, &t2).slices};
   if (M1 == 0 || N1 == 0 || total1 == 0 || M2 == 0 || N2 == 0 || total2 == 0) return best;
   double least = t1 + t2;
-  for (const GemmRow &r : GEMM_ROWS)
-    for (int s1 : GEMM_SLICES)
-      for (int s2 : GEMM_SLICES) {
-        if (!gemm_slices_fit(M1, N1, total1, s1) || !gemm_slices_fit(M2, N2, total2, s2)) continue;
-        const double n1 = (double)gemm_tiles(M1, N1, r.tile) * s1, n2 = (double)gemm_tiles(M2, N2, r.tile) * s2;
-        const double c1 = (double)((total1 + s1 - 1) / s1), c2 = (double)((total2 + s2 - 1) / s2);
-        const double chain = c1 > c2 ? c1 : c2, work = (n1 * c1 + n2 * c2) / 512.0 * r.step2;
-        const double alone = chain * (n1 + n2 > 256.0 ? r.step2 : r.step1);
-        const double t = r.fixed + (work > alone ? work : alone) + gemm_sum_time(M1, N1, s1) + gemm_sum_time(M2, N2, s2);
-        if (n1 + n2 < 2147483648.0 && t < least) {
+  for (const GemmRow &r : GEMM_ROWS) {
+    // by slices of one product: its workgroups, its steps, the time of its slices' sum
+    struct Choice {
+      double n, steps, sum;
+    } c[2][8];
+    int count[2] = {0, 0};
+    const int64_t sizes[2][3] = {{M1, N1, total1}, {M2, N2, total2}};
+    for (int p = 0; p < 2; ++p) {
+      const int64_t M = sizes[p][0], N = sizes[p][1], total = sizes[p][2];
+      const double tiles = (double)gemm_tiles(M, N, r.tile);
+      for (int i = 0; i < 8 && gemm_slices_fit(M, N, total, GEMM_SLICES[i]); ++i) {
+        const int k = GEMM_SLICES[i];
+        c[p][count[p]++] = {tiles * k, (double)(((int)total + k - 1) / k), gemm_sum_time(M, N, k)};
+      }
+    }
+    for (int i = 0; i < count[0]; ++i)
+      for (int j = 0; j < count[1]; ++j) {
+        const Choice &a = c[0][i], &b = c[1][j];
+        const double n = a.n + b.n, chain = a.steps > b.steps ? a.steps : b.steps;
+        const double work = (a.n * a.steps + b.n * b.steps) * (r.step2 / 512.0);
+        const double alone = chain * (n > 256.0 ? r.step2 : r.step1);
+        const double t = r.fixed + (work > alone ? work : alone) + a.sum + b.sum;
+        if (n < 2147483648.0 && t < least) {
           least = t;
-          best = {r.tile, s1, s2};
+          best = {r.tile, GEMM_SLICES[i], GEMM_SLICES[j]};
         }
       }
+  }
   return best;
 }
 
