@@ -5,7 +5,12 @@
 // operands are first staged: rows of the reduction, padded with zeros to whole groups of 128, as
 // 16-bit pieces whose sums are the values exactly (bfloat16; binary16 for dW of binary16 tensors,
 // which is one piece).  W is staged as its components' numbers, exact in bfloat16.  Then both are
-// products A B^T of staged tensors, summed over pairs of pieces in binary32.
+// products A B^T of staged tensors, summed over pairs of pieces in binary32.  They go out in one launch
+// where the time model finds that faster.
+//
+// Measured (MI355X, 4096 x 1024 -> 1024, binary16, one component): 48 us in all; staging 12.4, both
+// products 34 (the matrix instructions of three bfloat16-sized products take 18 at the rate of a large
+// one), the sum of dW's slices 4.9, db 3.9.
 #include "mcf_internal.hpp"
 #include "mx4.hpp"
 #include "mx4_gemm.hpp"
