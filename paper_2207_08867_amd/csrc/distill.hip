@@ -31,6 +31,7 @@ struct DistillArgs {
   void *dz;
   f32x2 *partial;  // [rows][chunks]
   int64_t rows, plane;
+  int64_t first;  // the launch's first row, where a workgroup takes one
   int vocab, k, nc, chunks;
   float temperature, c_hi, c_lo;  // c_hi + c_lo = log2(e) / T
 };
@@ -294,7 +295,7 @@ template <typename T, bool ONE, int NT, int CH, bool GRAD, int OCC>
 __global__ __launch_bounds__(NT, OCC) void distill_row_kernel(DistillArgs a) {
   constexpr int FLY = ONE ? 4 : 2;  // pieces in flight where the row is read again
   __shared__ Shared<NT> sh;
-  const int64_t row = blockIdx.x;
+  const int64_t row = a.first + blockIdx.x;
   const T *z = reinterpret_cast<const T *>(a.z) + row * a.vocab;
   MaxSum st = {-FLT_MAX, 0.0f};
   Raw8<T> keep[CH > 0 ? CH : 1];
@@ -451,31 +452,25 @@ __global__ __launch_bounds__(256) void distill_finish_kernel(DistillArgs a) {
 // Few rows of a long vocabulary go to several workgroups a row; else one workgroup a row.
 bool several(int64_t rows, int64_t vocab) { return rows < 256 && vocab > 2 * CHUNK; }
 
+// One workgroup a row, `count` rows from a.first.  The row in registers where it fits 64 of them a
+// thread, read again where it does not (MC logits, rows below one piece, long rows).
 template <typename T, bool ONE, bool GRAD>
-hipError_t run(const DistillArgs &a, hipStream_t stream) {
-  if (several(a.rows, a.vocab)) {
-    const dim3 grid((unsigned)a.chunks, (unsigned)a.rows);
-    if (!a.stats_in) distill_partial_kernel<T, ONE><<<grid, 256, 0, stream>>>(a);
-    distill_finish_kernel<T, ONE, GRAD><<<GRAD ? grid : dim3(1, (unsigned)a.rows), 256, 16 * a.k, stream>>>(a);
-    return hipGetLastError();
-  }
-  // The row in registers where it fits 64 of them a thread, read again where it does not (MC
-  // logits, rows below one piece, long rows).
-  const dim3 grid((unsigned)a.rows);
+void run_rows(const DistillArgs &a, int64_t count, hipStream_t stream) {
+  const dim3 grid((unsigned)count);
 #define ROW(NT, CH, OCC) distill_row_kernel<T, ONE, NT, CH, GRAD, OCC><<<grid, NT, 16 * a.k, stream>>>(a)
   if constexpr (ONE) {
     constexpr bool SHORT = sizeof(T) == 2;
     if (a.vocab >= 8) {
-      if (a.vocab <= 512) return ROW(64, 1, 8), hipGetLastError();
-      if (a.vocab <= 1024) return ROW(64, 2, 8), hipGetLastError();
-      if (a.vocab <= 2048) return ROW(64, 4, 8), hipGetLastError();
-      if (a.vocab <= 4096) return ROW(256, 2, 8), hipGetLastError();
-      if (a.vocab <= 8192) return ROW(256, 4, SHORT ? 8 : 6), hipGetLastError();
-      if (a.vocab <= 16384) return ROW(512, 4, SHORT ? 8 : 6), hipGetLastError();
-      if (a.vocab <= 32768) return ROW(512, 8, SHORT ? 8 : 4), hipGetLastError();
-      if (a.vocab <= 65536) return ROW(1024, 8, 4), hipGetLastError();
+      if (a.vocab <= 512) return ROW(64, 1, 8);
+      if (a.vocab <= 1024) return ROW(64, 2, 8);
+      if (a.vocab <= 2048) return ROW(64, 4, 8);
+      if (a.vocab <= 4096) return ROW(256, 2, 8);
+      if (a.vocab <= 8192) return ROW(256, 4, SHORT ? 8 : 6);
+      if (a.vocab <= 16384) return ROW(512, 4, SHORT ? 8 : 6);
+      if (a.vocab <= 32768) return ROW(512, 8, SHORT ? 8 : 4);
+      if (a.vocab <= 65536) return ROW(1024, 8, 4);
       if constexpr (SHORT)
-        if (a.vocab <= 131072) return ROW(1024, 16, 4), hipGetLastError();
+        if (a.vocab <= 131072) return ROW(1024, 16, 4);
     }
   }
   if (a.vocab <= 2048)
@@ -485,6 +480,18 @@ hipError_t run(const DistillArgs &a, hipStream_t stream) {
   else
     ROW(1024, 0, 4);
 #undef ROW
+}
+
+template <typename T, bool ONE, bool GRAD>
+hipError_t run(DistillArgs a, hipStream_t stream) {
+  if (several(a.rows, a.vocab)) {
+    const dim3 grid((unsigned)a.chunks, (unsigned)a.rows);
+    if (!a.stats_in) distill_partial_kernel<T, ONE><<<grid, 256, 0, stream>>>(a);
+    distill_finish_kernel<T, ONE, GRAD><<<GRAD ? grid : dim3(1, (unsigned)a.rows), 256, 16 * a.k, stream>>>(a);
+    return hipGetLastError();
+  }
+  for (a.first = 0; a.first < a.rows; a.first += LAUNCH_MAX)
+    run_rows<T, ONE, GRAD>(a, a.rows - a.first < LAUNCH_MAX ? a.rows - a.first : LAUNCH_MAX, stream);
   return hipGetLastError();
 }
 
@@ -497,7 +504,7 @@ int64_t distill_workspace_bytes(int64_t rows, int64_t vocab) {
 hipError_t launch_distill(int dtype, int nc, int64_t rows, int64_t vocab, int64_t k, const void *z, const void *ids,
                           const void *t, double temperature, const void *stats_in, const void *g, void *ws, void *loss,
                           void *stats, void *dz, hipStream_t stream) {
-  DistillArgs a;
+  DistillArgs a = {};
   a.z = z;
   a.t = t;
   a.ids = (const int32_t *)ids;

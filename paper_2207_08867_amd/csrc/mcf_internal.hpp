@@ -122,6 +122,10 @@ int64_t linreg_workspace_bytes(int dtype, int nc, int64_t n, int64_t d);
 hipError_t launch_linreg_step(int dtype, int nc, int64_t n, int64_t d, const void *X, const void *y_neg, void *W,
                               double s2n, double s1n, double neg_lr, void *ws, void *loss, hipStream_t stream);
 
+// Workgroups of one launch of a grid that may need more: a launch holds less than 2^32 threads, these
+// have up to 1024 each.
+constexpr int64_t LAUNCH_MAX = (int64_t)1 << 21;
+
 // Formats of the calls on MXFP4 tensors and of the distillation loss.
 constexpr int LM_F16 = 0, LM_F32 = 1, LM_BF16 = 4;
 

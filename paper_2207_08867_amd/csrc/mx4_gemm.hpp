@@ -486,9 +486,9 @@ struct Pieces {
 // src [rows][cols] -> dst [P][rows][ld], zeros from cols to ld.
 template <typename T, bool HALF>
 __global__ __launch_bounds__(256) void mx_stage_kernel(const T *src, uint16_t *dst, int64_t rows, int64_t cols,
-                                                       int64_t ld) {
+                                                       int64_t ld, int64_t first) {
   using S = Pieces<T, HALF>;
-  const int64_t per_row = ld / 8, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t per_row = ld / 8, id = (first + blockIdx.x) * 256 + threadIdx.x;
   if (id >= rows * per_row) return;
   const int64_t row = id <= 0xffffffffll ? (int64_t)((uint32_t)id / (uint32_t)per_row) : id / per_row;
   const int64_t col = (id - row * per_row) * 8;

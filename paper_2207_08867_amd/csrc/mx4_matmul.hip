@@ -365,8 +365,10 @@ hipError_t mix_gemm(GemmArgs &g, int dtype, int nc, const void *x, int64_t in, c
   const int64_t ld = g.groups * MX_GROUP;
   g.a = (const char *)x;
   if (!in_place(dtype, in, x)) {
-    mx_stage_kernel<T, HALF><<<(unsigned)((g.M * (ld / 8) + 255) / 256), 256, 0, stream>>>((const T *)x, (uint16_t *)ws,
-                                                                                          g.M, in, ld);
+    const int64_t all = (g.M * (ld / 8) + 255) / 256;
+    for (int64_t first = 0; first < all; first += LAUNCH_MAX)
+      mx_stage_kernel<T, HALF><<<(unsigned)(all - first < LAUNCH_MAX ? all - first : LAUNCH_MAX), 256, 0, stream>>>(
+          (const T *)x, (uint16_t *)ws, g.M, in, ld, first);
     g.a = ws;
   }
   ws += stage_bytes(dtype, g.M, in);

@@ -8,6 +8,8 @@
 // component (or back), so HBM bounds them (8192 x 8192 bfloat16: 27 us, 6.2 TB/s, and back 37 us, 4.6
 // TB/s).  A lane takes 8 elements and four lanes a block; the block's maximum is two DPP steps
 // inside a quad.
+#include <type_traits>
+
 #include "mcf_internal.hpp"
 #include "mx4.hpp"
 
@@ -27,6 +29,7 @@ struct QuantArgs {
   const void *x;
   uint8_t *codes, *scales;
   int64_t rows, n, groups, across;  // workgroups side by side along a row
+  int64_t first;                    // the launch's first workgroup
   int nc, shift;
 };
 
@@ -125,11 +128,11 @@ __device__ inline void quantize64(const QuantArgs &a, const BlockAt &b, double v
 template <typename T, int NIN>
 __global__ __launch_bounds__(256) void mx_quant_kernel(QuantArgs a) {
   BlockAt b;
-  const int64_t tile = divide(blockIdx.x, a.across);
+  const int64_t id = a.first + blockIdx.x, tile = divide(id, a.across);
   const int g = threadIdx.x >> 4;
   b.in = (int)(threadIdx.x & 15);
   b.row = (tile << a.shift) + (g >> (4 - a.shift));
-  b.group = ((blockIdx.x - tile * a.across) << (4 - a.shift)) + (g & ((16 >> a.shift) - 1));
+  b.group = ((id - tile * a.across) << (4 - a.shift)) + (g & ((16 >> a.shift) - 1));
   if (b.row >= a.rows || b.group >= a.groups) return;  // whole quads leave together
   const int64_t col = b.group * MX_GROUP + b.in * 8;
   const T *x = reinterpret_cast<const T *>(a.x) + b.row * a.n + col;
@@ -177,11 +180,11 @@ __global__ __launch_bounds__(256) void mx_quant_kernel(QuantArgs a) {
 template <typename T>
 __global__ __launch_bounds__(256) void mx_dequant_kernel(const uint8_t *codes, const uint8_t *scales, T *out, int nc,
                                                          int64_t rows, int64_t n, int64_t groups, int64_t across,
-                                                         int shift) {
-  const int64_t tile = divide(blockIdx.x, across);
+                                                         int shift, int64_t first) {
+  const int64_t id = first + blockIdx.x, tile = divide(id, across);
   const int g = threadIdx.x >> 4, in = (int)(threadIdx.x & 15);
   const int64_t row = (tile << shift) + (g >> (4 - shift));
-  const int64_t group = ((blockIdx.x - tile * across) << (4 - shift)) + (g & ((16 >> shift) - 1));
+  const int64_t group = ((id - tile * across) << (4 - shift)) + (g & ((16 >> shift) - 1));
   const int64_t col = group * MX_GROUP + in * 8;
   if (row >= rows || col >= n) return;
   float v[8] = {};
@@ -202,28 +205,36 @@ __global__ __launch_bounds__(256) void mx_dequant_kernel(const uint8_t *codes, c
 
 // Workgroups along a row, and in all.
 int64_t tiles_across(int64_t groups) { return (groups + (16 >> tile_shift(groups)) - 1) >> (4 - tile_shift(groups)); }
-unsigned tiles(int64_t rows, int64_t groups) {
+int64_t tiles(int64_t rows, int64_t groups) {
   const int s = tile_shift(groups);
-  return (unsigned)(((rows + (1 << s) - 1) >> s) * tiles_across(groups));
+  return ((rows + (1 << s) - 1) >> s) * tiles_across(groups);
+}
+// launch(first, workgroups) over all of them.
+template <typename F>
+hipError_t in_launches(int64_t all, F launch) {
+  for (int64_t first = 0; first < all; first += LAUNCH_MAX)
+    launch(first, dim3((unsigned)(all - first < LAUNCH_MAX ? all - first : LAUNCH_MAX)));
+  return hipGetLastError();
 }
 
 template <typename T>
-hipError_t quantize(int nc_in, const QuantArgs &a, hipStream_t stream) {
-  const dim3 grid(tiles(a.rows, a.groups));
-  switch (nc_in) {
-    case 1: mx_quant_kernel<T, 1><<<grid, 256, 0, stream>>>(a); break;
-    case 2: mx_quant_kernel<T, 2><<<grid, 256, 0, stream>>>(a); break;
-    case 3: mx_quant_kernel<T, 3><<<grid, 256, 0, stream>>>(a); break;
-    default: mx_quant_kernel<T, 4><<<grid, 256, 0, stream>>>(a); break;
-  }
-  return hipGetLastError();
+hipError_t quantize(int nc_in, QuantArgs a, hipStream_t stream) {
+  return in_launches(tiles(a.rows, a.groups), [&](int64_t first, dim3 grid) {
+    a.first = first;
+    switch (nc_in) {
+      case 1: mx_quant_kernel<T, 1><<<grid, 256, 0, stream>>>(a); break;
+      case 2: mx_quant_kernel<T, 2><<<grid, 256, 0, stream>>>(a); break;
+      case 3: mx_quant_kernel<T, 3><<<grid, 256, 0, stream>>>(a); break;
+      default: mx_quant_kernel<T, 4><<<grid, 256, 0, stream>>>(a); break;
+    }
+  });
 }
 
 }  // namespace
 
 hipError_t launch_mx4_quantize(int dtype, int nc_in, int nc, int64_t rows, int64_t n, const void *x, void *codes,
                                void *scales, hipStream_t stream) {
-  QuantArgs a;
+  QuantArgs a = {};
   a.x = x;
   a.codes = (uint8_t *)codes;
   a.scales = (uint8_t *)scales;
@@ -243,15 +254,16 @@ hipError_t launch_mx4_dequantize(int dtype, int nc, int64_t rows, int64_t n, con
   const int64_t groups = mx_groups(n);
   const int64_t across = tiles_across(groups);
   const int shift = tile_shift(groups);
-  const dim3 grid(tiles(rows, groups));
   const uint8_t *c = (const uint8_t *)codes, *s = (const uint8_t *)scales;
-  if (dtype == LM_F16)
-    mx_dequant_kernel<_Float16><<<grid, 256, 0, stream>>>(c, s, (_Float16 *)out, nc, rows, n, groups, across, shift);
-  else if (dtype == LM_BF16)
-    mx_dequant_kernel<__bf16><<<grid, 256, 0, stream>>>(c, s, (__bf16 *)out, nc, rows, n, groups, across, shift);
-  else
-    mx_dequant_kernel<float><<<grid, 256, 0, stream>>>(c, s, (float *)out, nc, rows, n, groups, across, shift);
-  return hipGetLastError();
+  const auto go = [&](auto *o) {
+    using T = std::remove_pointer_t<decltype(o)>;
+    return in_launches(tiles(rows, groups), [&](int64_t first, dim3 grid) {
+      mx_dequant_kernel<T><<<grid, 256, 0, stream>>>(c, s, o, nc, rows, n, groups, across, shift, first);
+    });
+  };
+  if (dtype == LM_F16) return go((_Float16 *)out);
+  if (dtype == LM_BF16) return go((__bf16 *)out);
+  return go((float *)out);
 }
 
 }  // namespace mcf

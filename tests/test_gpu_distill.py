@@ -240,3 +240,24 @@ def test_many_logits(mcf):
         l, d = mcf.mc_distill_fwd_bwd(z[i:i + 1], ids[i:i + 1], t[i:i + 1])
         assert torch.allclose(l, loss[i:i + 1], rtol=1e-5, atol=1e-5)
         assert (d.float() - dz[i:i + 1].float()).abs().max() <= 2.0 ** -7 * d.float().abs().max()
+
+
+def test_more_rows_than_one_launch(mcf):
+    """Past 2^21 rows the workgroups go out in several launches: the same rows over and over."""
+    import torch
+
+    part, times = 70001, 31
+    z = torch.randn(part, 5, device="cuda").half()
+    ids = torch.randint(0, 5, (part, 2), device="cuda", dtype=torch.int32)
+    t = torch.randn(part, 2, device="cuda").half()
+    loss, stats = mcf.mc_distill_fwd(z, ids, t)
+    _, dz = mcf.mc_distill_fwd_bwd(z, ids, t)
+    many = [v.repeat(times, 1) for v in (z, ids, t)]
+    assert many[0].shape[0] > 2 ** 21
+    got_loss, got_stats = mcf.mc_distill_fwd(*many)
+    assert torch.equal(got_loss.view(times, part), loss.expand(times, part))
+    assert torch.equal(got_stats.view(times, part, 2), stats.expand(times, part, 2))
+    got_loss, got = mcf.mc_distill_fwd_bwd(*many)
+    assert torch.equal(got_loss.view(times, part), loss.expand(times, part))
+    assert torch.equal(got.view(times, part, 5), dz.expand(times, part, 5))
+    assert torch.equal(mcf.mc_distill_bwd(*many, got_stats), got)

@@ -462,3 +462,42 @@ def test_binary16_layer_keeps_nan_blocks(mcf):
     assert torch.isnan(y[:, 7]).all()
     keep = torch.arange(90, device="cuda") != 7
     assert torch.isfinite(y[:, keep]).all()
+
+
+def test_more_rows_than_one_launch(mcf):
+    """Past 2^21 workgroups they go out in several launches: the same rows over and over."""
+    import torch
+
+    part, times, n = 1100003, 31, 5
+    x = torch.randn(part, n, device="cuda").bfloat16()
+    codes, scales = mcf.mc_mx4_quantize(x)
+    back = mcf.mc_mx4_dequantize(codes, scales, n, dtype=torch.bfloat16)
+    many = x.repeat(times, 1)
+    assert many.shape[0] > 2 ** 25
+    got_codes, got_scales = mcf.mc_mx4_quantize(many)
+    for i in range(times):
+        rows = slice(i * part, (i + 1) * part)
+        assert torch.equal(got_codes[:, rows], codes) and torch.equal(got_scales[:, :, rows], scales)
+    got = mcf.mc_mx4_dequantize(got_codes, got_scales, n, dtype=torch.bfloat16)
+    assert torch.equal(got.view(times, part, n), back.expand(times, part, n))
+
+
+def test_linear_of_more_rows_than_one_staging_launch(mcf):
+    """A binary16 x of more than 2^32 padded elements, with sums that binary16 holds exactly."""
+    import torch
+
+    T, n, out = 2 ** 20, 4100, 3
+    some = torch.randint(-1, 2, (1024, n), device="cuda").half()
+    x = some.repeat(T // 1024, 1)
+    pick = [0, 1, 1016801, 1016802, T - 1]  # the second launch begins in row 2^32 / 4224
+    for i in pick:
+        x[i] = torch.randint(-1, 2, (n,), device="cuda").half()
+    w = torch.randint(-1, 2, (out, n), device="cuda").half()
+    y = mcf.mc_mx4_linear_fwd(x, mcf.mc_mx4_quantize(w))
+    exact = some.double().cpu() @ w.double().cpu().T
+    picked = x[pick].double().cpu() @ w.double().cpu().T
+    assert float(max(exact.abs().max(), picked.abs().max())) <= 2048
+    assert torch.equal(y[pick].cpu(), picked.half())
+    same = y.view(T // 1024, 1024, out) == exact.half().cuda()
+    same.view(T, out)[pick] = True
+    assert bool(same.all())
