@@ -386,9 +386,11 @@ int64_t mc_linreg_workspace(int dtype, int nc, int64_t n, int64_t d);
  *   scales: [nc][G][rows][4] bytes, block b of group q of row r at byte 4 (q rows + r) + b of
  *           its component; zeros for blocks wholly past n; 4-byte aligned.
  * Sums of the products are held in binary32; results are rounded once to the call's format.
- * Non-finite inputs propagate by IEEE rules through the products of the single components
- * and of the pieces an input is split into, so an infinite factor may give NaN where the
- * product of the whole numbers would be infinite.
+ * Non-finite inputs propagate by IEEE rules through the products of the single components:
+ * with one component an infinity in x or dY gives y and dX what the whole numbers give,
+ * whatever the number of rows.  It may give NaN in place of an infinity where the weight has
+ * several components (infinity times a component that is 0 or of the other sign), and in dW of
+ * binary32, whose two factors are both split.
  * Workspaces: device memory of at least the matching ..._workspace(...) bytes, 16-byte
  * aligned, owned by the caller, not overlapping the other arguments; may be NULL when that
  * size is 0; contents on entry do not matter; calls sharing one must not overlap in time.

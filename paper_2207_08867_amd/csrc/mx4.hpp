@@ -103,38 +103,52 @@ constexpr int mx_pieces() {
   return sizeof(T) == 4 ? 3 : (__is_same(T, __bf16) ? 1 : 2);
 }
 
-// v = p[0] + p[1] + ...: each piece what is left rounded to bfloat16.  T: the format v comes from.
-// A binary32 value that would round past bfloat16's largest number is cut off instead.  An infinity
-// or NaN makes the later pieces NaN.
+// v = p[0] + p[1] + ..., each piece the leading 8 bits of what is left, of v's sign, its bfloat16 bits in
+// the upper half of p[i].  T: the format v comes from.  The median of the remainder, 0 and v is the
+// remainder of a finite v; of an infinity the remainder is NaN, which a median ignores, and the
+// later pieces are 0 or the infinity again: its products are those of one 16-bit number.
 template <typename T, int P>
-__device__ inline void mx_split(float v, __bf16 p[P]) {
-  p[0] = (__bf16)v;
-  if constexpr (sizeof(T) == 4) {
-    const uint32_t u = __builtin_bit_cast(uint32_t, v), a = u & 0x7fffffffu;
-    if (a >= 0x7f7f8000u && a < 0x7f800000u) p[0] = __builtin_bit_cast(__bf16, (uint16_t)(u >> 16));
-  }
-  float r = v;
+__device__ inline void mx_cut(float v, uint32_t p[P]) {
+  // a NaN of the lower half's bits alone would turn into an infinity
+  float r = sizeof(T) == 4 ? __builtin_canonicalizef(v) : v;
 #pragma unroll
-  for (int i = 1; i < P; ++i) {
-    r -= (float)p[i - 1];
-    p[i] = (__bf16)r;
+  for (int i = 0; i < P; ++i) {
+    p[i] = __builtin_bit_cast(uint32_t, r);
+    if (i + 1 < P) r = __builtin_amdgcn_fmed3f(r - __builtin_bit_cast(float, p[i] & 0xffff0000u), 0.0f, r);
   }
 }
 
 // Eight values into P registers of eight pieces.
 template <typename T, int P>
-__device__ inline void mx_split8(const Raw8<T> &x, bf16x8 f[P]) {
+__device__ inline void mx_cut8(const Raw8<T> &x, bf16x8 f[P]) {
   if constexpr (P == 1) {
     f[0] = __builtin_bit_cast(bf16x8, x);
   } else {
+    u32x4 w[P];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      __bf16 q[P];
-      mx_split<T, P>((float)x.v[i], q);
+    for (int i = 0; i < 8; i += 2) {
+      uint32_t p[P], q[P];
+      mx_cut<T, P>((float)x.v[i], p);
+      mx_cut<T, P>((float)x.v[i + 1], q);
 #pragma unroll
-      for (int p = 0; p < P; ++p) f[p][i] = q[p];
+      for (int k = 0; k < P; ++k) w[k][i / 2] = __builtin_amdgcn_perm(q[k], p[k], 0x07060302);
     }
+#pragma unroll
+    for (int k = 0; k < P; ++k) f[k] = __builtin_bit_cast(bf16x8, w[k]);
   }
+}
+
+// The same with each piece what is left rounded to bfloat16, which makes the later ones smaller: at most
+// 2^-8 and 2^-17 of v's power of two.  For products that leave pairs of pieces out.  A value that would
+// round past bfloat16's largest number is cut off instead.  An infinity or NaN makes the later pieces
+// NaN.
+__device__ inline void mx_round3(float v, __bf16 p[3]) {
+  p[0] = (__bf16)v;
+  const uint32_t u = __builtin_bit_cast(uint32_t, v), a = u & 0x7fffffffu;
+  if (a >= 0x7f7f8000u && a < 0x7f800000u) p[0] = __builtin_bit_cast(__bf16, (uint16_t)(u >> 16));
+  const float r = v - (float)p[0];
+  p[1] = (__bf16)r;
+  p[2] = (__bf16)(r - (float)p[1]);
 }
 
 // What lanes of a wavefront wrote to LDS is there for its other lanes.

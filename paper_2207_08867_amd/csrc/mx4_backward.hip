@@ -39,8 +39,7 @@ constexpr int TILE_ROW = 66;  // halfwords: the rows of one column lie in differ
 template <typename T, bool HALF>
 __device__ inline void stage_tile(const T *src, uint16_t *plain, uint16_t *dst, float *sums, T *whole, int64_t rows,
                                   int64_t cols, int64_t pld, int64_t ld, int64_t row_tile, int64_t col_tile, char *lds) {
-  using S = Pieces<T, HALF>;
-  using R = Pieces<T, false>;
+  constexpr int P = mx_pieces<T>(), PW = HALF ? 1 : P;
   uint16_t(*tile)[128][TILE_ROW] = reinterpret_cast<uint16_t(*)[128][TILE_ROW]>(lds);
   const int64_t c0 = col_tile * 64, r0 = row_tile * 128;
   float part[8] = {};
@@ -52,18 +51,22 @@ __device__ inline void stage_tile(const T *src, uint16_t *plain, uint16_t *dst, 
     for (int k = 0; k < 8; ++k) v.v[k] = (T)0.0f;
     if (r0 + r < rows) v = load8_tail(src + (r0 + r) * cols + c0 + c, cols - c0 - c);
     if (plain && r0 + r < rows) {
-      bf16x8 f[R::P];
-      mx_split8<T, R::P>(v, f);
+      bf16x8 f[P];
+      mx_cut8<T, P>(v, f);
 #pragma unroll
-      for (int q = 0; q < R::P; ++q)
+      for (int q = 0; q < P; ++q)
         *reinterpret_cast<bf16x8 *>(plain + ((int64_t)q * rows + r0 + r) * pld + c0 + c) = f[q];
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      uint16_t p[S::P];
-      S::of(v.v[k], p);
+      if constexpr (PW == 3) {
+        __bf16 p[3];
+        mx_round3(v.v[k], p);
 #pragma unroll
-      for (int q = 0; q < S::P; ++q) tile[q][r][c + k] = p[q];
+        for (int q = 0; q < 3; ++q) tile[q][r][c + k] = __builtin_bit_cast(uint16_t, p[q]);
+      } else {
+        tile[0][r][c + k] = __builtin_bit_cast(uint16_t, v.v[k]);
+      }
       part[k] += (float)v.v[k];
     }
   }
@@ -74,7 +77,7 @@ __device__ inline void stage_tile(const T *src, uint16_t *plain, uint16_t *dst, 
       const int c = i * 16 + (threadIdx.x >> 4), r = (threadIdx.x & 15) * 8;
       if (c0 + c < cols) {
 #pragma unroll
-        for (int q = 0; q < S::P; ++q) {
+        for (int q = 0; q < PW; ++q) {
           uint16_t out[8];
 #pragma unroll
           for (int k = 0; k < 8; ++k) out[k] = tile[q][r + k][c];
@@ -126,7 +129,7 @@ __device__ inline void unpack_tile(const StageArgs &a, int64_t grp, int64_t row_
 
 template <typename T, bool HALF>
 __global__ __launch_bounds__(256) void mx_stage_all_kernel(StageArgs a) {
-  constexpr int P = Pieces<T, HALF>::P, BYTES = P * 128 * TILE_ROW * 2;
+  constexpr int BYTES = (HALF ? 1 : mx_pieces<T>()) * 128 * TILE_ROW * 2;
   __shared__ __attribute__((aligned(16))) char lds[BYTES > 128 * 144 ? BYTES : 128 * 144];
   int64_t id = blockIdx.x;
   if (id < a.n_dy) {

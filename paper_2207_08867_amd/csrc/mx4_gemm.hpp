@@ -327,7 +327,7 @@ __device__ __forceinline__ void gemm_body(const GemmArgs &a, char *lds, uint32_t
     for (int i = 0; i < TM; ++i) {
       bf16x8 piece[2];
       if constexpr (KIND == GEMM_MIXH && decltype(wide)::value)
-        mx_split8<_Float16, 2>(__builtin_bit_cast(Raw8<_Float16>, o.a[i]), piece);
+        mx_cut8<_Float16, 2>(__builtin_bit_cast(Raw8<_Float16>, o.a[i]), piece);
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
         f32x16 &c = acc[i][j];
@@ -467,42 +467,21 @@ __global__ __launch_bounds__(256) void mx_gemm_sum_kernel(GemmArgs a) {
   reinterpret_cast<T *>(a.c)[i] = (T)v;
 }
 
-// Staged pieces of one element of T: bfloat16 pieces, or the binary16 number itself.
-template <typename T, bool HALF>
-struct Pieces {
-  static constexpr int P = HALF ? 1 : mx_pieces<T>();
-  static __device__ inline void of(T v, uint16_t p[P]) {
-    if constexpr (HALF) {
-      p[0] = __builtin_bit_cast(uint16_t, (_Float16)v);
-    } else {
-      __bf16 q[P];
-      mx_split<T, P>((float)v, q);
-#pragma unroll
-      for (int i = 0; i < P; ++i) p[i] = __builtin_bit_cast(uint16_t, q[i]);
-    }
-  }
-};
-
-// src [rows][cols] -> dst [P][rows][ld], zeros from cols to ld.
-template <typename T, bool HALF>
+// src [rows][cols] -> dst [P][rows][ld], zeros from cols to ld: the pieces of binary32, 16-bit numbers as
+// they are.
+template <typename T>
 __global__ __launch_bounds__(256) void mx_stage_kernel(const T *src, uint16_t *dst, int64_t rows, int64_t cols,
                                                        int64_t ld, int64_t first) {
-  using S = Pieces<T, HALF>;
+  constexpr int P = sizeof(T) == 4 ? mx_pieces<T>() : 1;
   const int64_t per_row = ld / 8, id = (first + blockIdx.x) * 256 + threadIdx.x;
   if (id >= rows * per_row) return;
   const int64_t row = id <= 0xffffffffll ? (int64_t)((uint32_t)id / (uint32_t)per_row) : id / per_row;
   const int64_t col = (id - row * per_row) * 8;
   const Raw8<T> r = load8_tail(src + row * cols + col, cols - col);
-  uint16_t out[S::P][8];
+  bf16x8 f[P];
+  mx_cut8<T, P>(r, f);
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    uint16_t p[S::P];
-    S::of(r.v[i], p);
-#pragma unroll
-    for (int k = 0; k < S::P; ++k) out[k][i] = p[k];
-  }
-#pragma unroll
-  for (int k = 0; k < S::P; ++k) __builtin_memcpy(dst + ((int64_t)k * rows + row) * ld + col, out[k], 16);
+  for (int k = 0; k < P; ++k) *reinterpret_cast<bf16x8 *>(dst + ((int64_t)k * rows + row) * ld + col) = f[k];
 }
 
 inline void gemm_pair(GemmArgs &a, int i, int j) {

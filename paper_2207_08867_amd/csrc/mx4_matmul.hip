@@ -45,7 +45,7 @@ __device__ inline f32x4 thin_group(f32x4 acc, u32x4 code, float scale, const XRo
   for (int j = 0; j < 4; ++j) {
     const bf16x8 wf = mx_bf16(code[j], scale);
     bf16x8 xf[P];
-    mx_split8<T, P>(x.v[j], xf);
+    mx_cut8<T, P>(x.v[j], xf);
 #pragma unroll
     for (int p = 0; p < P; ++p) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wf, xf[p], acc, 0, 0, 0);
   }
@@ -206,7 +206,7 @@ __global__ __launch_bounds__(64 * NW) void mx_token_kernel(ThinArgs a) {
 #pragma unroll
         for (int t = 0; t < XT; ++t) {
           bf16x8 f[P];
-          mx_split8<T, P>(raw[t], f);
+          mx_cut8<T, P>(raw[t], f);
 #pragma unroll
           for (int p = 0; p < P; ++p) pieces[wave][t][p][g][r] = f[p];
         }
@@ -367,7 +367,7 @@ hipError_t mix_gemm(GemmArgs &g, int dtype, int nc, const void *x, int64_t in, c
   if (!in_place(dtype, in, x)) {
     const int64_t all = (g.M * (ld / 8) + 255) / 256;
     for (int64_t first = 0; first < all; first += LAUNCH_MAX)
-      mx_stage_kernel<T, HALF><<<(unsigned)(all - first < LAUNCH_MAX ? all - first : LAUNCH_MAX), 256, 0, stream>>>(
+      mx_stage_kernel<T><<<(unsigned)(all - first < LAUNCH_MAX ? all - first : LAUNCH_MAX), 256, 0, stream>>>(
           (const T *)x, (uint16_t *)ws, g.M, in, ld, first);
     g.a = ws;
   }
