@@ -226,8 +226,8 @@ template <typename T, int NT>
 __device__ inline void row_loss(const DistillArgs &a, int64_t row, const MaxSum &st, const Shared<NT> &sh) {
   const T *t = reinterpret_cast<const T *>(a.t) + row * a.k;
   ENTRIES;
-  const float log_s = logf(st.s), log_sum = logf((float)sh.sum);
-  const double inv = sh.sum == 0.0 ? 0.0 : 1.0 / sh.sum;
+  const double log_s = (double)logf(st.s), log_sum = (double)logf((float)sh.sum);
+  const double inv = sh.sum == 0.0 ? 0.0 : 1.0 / sh.sum, inv_t = 1.0 / (double)a.temperature;
   double sum = 0.0;
   for (int i = threadIdx.x; i < a.k; i += 64) {
     const double p = (double)ee[i] * inv;
@@ -237,9 +237,11 @@ __device__ inline void row_loss(const DistillArgs &a, int64_t row, const MaxSum 
       continue;
     }
     const float zi = ez[i];
-    const float log_p = ((float)t[i] - sh.top) / a.temperature - log_sum;
-    const float log_q = zi == -INFINITY ? -INFINITY : (zi - st.m) / a.temperature - log_s;
-    sum += p * ((double)log_p - (double)log_q);
+    // binary64: below a temperature of 1 the logarithm of q at a mask of the type's lowest value passes
+    // binary32's range, where the loss, T^2 times it, need not
+    const double log_p = ((double)(float)t[i] - (double)sh.top) * inv_t - log_sum;
+    const double log_q = zi == -INFINITY ? -INFINITY : ((double)zi - (double)st.m) * inv_t - log_s;
+    sum += p * (log_p - log_q);
   }
   sum = wave_sum(sum);
   if (threadIdx.x == 0) a.loss[row] = (float)((double)a.temperature * (double)a.temperature * sum);
