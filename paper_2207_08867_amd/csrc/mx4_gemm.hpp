@@ -52,13 +52,17 @@ struct GemmArgs {
 
 // 16 (4) bytes a lane from base + off straight into LDS at `to` + 16 (4) lane.  The loads are
 // asm so that the compiler does not wait for them in front of every LDS read; gemm_wait does.
-// m0 holds the LDS address, and a load that reads it follows its write by a wait state.
+// m0 holds the LDS address, and a load that reads it follows its write by a wait state.  The compiler
+// sets m0 where it needs it and allots it to nothing, which it says of a clobber.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ inline void lds_load16(uint32_t to, uint32_t off, const void *base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base) : "m0", "memory");
 }
 __device__ inline void lds_load4(uint32_t to, uint32_t off, const void *base) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base) : "memory");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(off), "s"(base) : "m0", "memory");
 }
+#pragma clang diagnostic pop
 __device__ inline const char *uniform(const void *p) {
   const uint64_t u = (uint64_t)p;
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
