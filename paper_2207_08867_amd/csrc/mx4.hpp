@@ -138,15 +138,15 @@ __device__ inline void mx_cut8(const Raw8<T> &x, bf16x8 f[P]) {
   }
 }
 
-// The same with each piece what is left rounded to bfloat16, which makes the later ones smaller: at most
-// 2^-8 and 2^-17 of v's power of two.  For products that leave pairs of pieces out.  A value that would
-// round past bfloat16's largest number is cut off instead.  An infinity or NaN makes the later pieces
-// NaN.
+// The same of binary32 with each piece what is left rounded to bfloat16, which makes the later ones
+// smaller: at most 2^-8 and 2^-17 of v's power of two.  For products that leave pairs of pieces out.  A
+// value that would round past bfloat16's largest number is cut off instead; an infinity's later pieces
+// are 0.
 __device__ inline void mx_round3(float v, __bf16 p[3]) {
   p[0] = (__bf16)v;
   const uint32_t u = __builtin_bit_cast(uint32_t, v), a = u & 0x7fffffffu;
   if (a >= 0x7f7f8000u && a < 0x7f800000u) p[0] = __builtin_bit_cast(__bf16, (uint16_t)(u >> 16));
-  const float r = v - (float)p[0];
+  const float r = a == 0x7f800000u ? 0.0f : v - (float)p[0];
   p[1] = (__bf16)r;
   p[2] = (__bf16)(r - (float)p[1]);
 }

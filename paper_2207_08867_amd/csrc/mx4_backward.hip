@@ -50,20 +50,28 @@ __device__ inline void stage_tile(const T *src, uint16_t *plain, uint16_t *dst, 
 #pragma unroll
     for (int k = 0; k < 8; ++k) v.v[k] = (T)0.0f;
     if (r0 + r < rows) v = load8_tail(src + (r0 + r) * cols + c0 + c, cols - c0 - c);
-    if (plain && r0 + r < rows) {
-      bf16x8 f[P];
+    bf16x8 f[P];
+    if constexpr (P == 3) {  // dW leaves pairs of pieces out; dX takes the same ones
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        __bf16 p[3];
+        mx_round3(v.v[k], p);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) f[q][k] = p[q];
+      }
+    } else {
       mx_cut8<T, P>(v, f);
+    }
+    if (plain && r0 + r < rows) {
 #pragma unroll
       for (int q = 0; q < P; ++q)
         *reinterpret_cast<bf16x8 *>(plain + ((int64_t)q * rows + r0 + r) * pld + c0 + c) = f[q];
     }
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      if constexpr (PW == 3) {
-        __bf16 p[3];
-        mx_round3(v.v[k], p);
+      if constexpr (P == 3) {
 #pragma unroll
-        for (int q = 0; q < 3; ++q) tile[q][r][c + k] = __builtin_bit_cast(uint16_t, p[q]);
+        for (int q = 0; q < 3; ++q) tile[q][r][c + k] = __builtin_bit_cast(uint16_t, (__bf16)f[q][k]);
       } else {
         tile[0][r][c + k] = __builtin_bit_cast(uint16_t, v.v[k]);
       }
