@@ -278,7 +278,8 @@ hipError_t backward(int nc, int64_t rows, int64_t in, int64_t out, const T *x, c
     mx_stage_all_kernel<T, HALF><<<(unsigned)(a.n_dy + a.n_x + n_w), 256, 0, stream>>>(a);
   }
   // Reductions of nothing give zeros.  Of two values in three pieces the pairs past i + j = 2 are
-  // left out of dW: each is within 2^-26 of |dY||x|, less than one rounding of the sum.
+  // left out of dW, a third of its products: (1, 2) and (2, 1) are at most 2^-25 of |dY||x| each, all
+  // three just above 2^-24, as much as one rounding of a product to binary32.
   GemmArgs gx = staged(dy, s.p, wt, nc, rows, in, s.op, s.p + nc, dX, partx);
   GemmArgs gw = staged(dyt, s.pw, xt, s.pw, out, in, s.tp, 3, dW, partw);
   constexpr GemmKind KW = HALF ? GEMM_F16 : GEMM_BF16;
