@@ -528,7 +528,9 @@ inline GemmPlan gemm_plan(int64_t M, int64_t N, int64_t total, double *time = nu
     for (int slices : GEMM_SLICES) {
       if (!gemm_slices_fit(M, N, total, slices)) break;
       const int64_t n = gemm_tiles(M, N, r.tile) * slices, full = n / 512, rest = n % 512;
-      const double steps = (double)((total + slices - 1) / slices);
+      // a tile of no steps takes one's time too: its workgroups and stores, and a large result in
+      // small tiles would pass the 2^32 threads of a launch
+      const double steps = total == 0 ? 1.0 : (double)((total + slices - 1) / slices);
       const double t = r.fixed + gemm_sum_time(M, N, slices) +
                        steps * ((double)full * r.step2 + (rest > 256 ? r.step2 : (rest > 0 ? r.step1 : 0.0)));
       if (t < least) {
