@@ -9,7 +9,9 @@
 // p > 0) has loss 0 and gradient 0.  One pass over the row keeps the running maximum m and
 // s = sum exp((z_j - m) / T); the gradient is a second pass, in the fused call over registers.
 // The row is read once and the gradient written once, so HBM bounds it: 4096 rows of 32768 bfloat16
-// logits take 111 us (4.8 TB/s) for both, 50 us (5.4 TB/s) for the loss alone.
+// logits take 111 us (4.8 TB/s) for both, 50 us (5.4 TB/s) for the loss alone.  Where both are asked for
+// and the row does not stay in registers it is read twice: 1024 rows of 131072 binary32 logits 312 us (3.4
+// TB/s), 4096 of 32768 in two binary16 planes 275 us (2.9 TB/s).
 //
 // The row's sums are binary32.  m starts at the lowest finite number, so that a masked logit (-inf)
 // is exp(-inf) = 0 with no test, also in front of the first finite one; a row of nothing but
@@ -451,11 +453,20 @@ __global__ __launch_bounds__(256) void distill_finish_kernel(DistillArgs a) {
   }
 }
 
-// Few rows of a long vocabulary go to several workgroups a row; else one workgroup a row.
+// Few rows of a long vocabulary go to several workgroups a row; else one workgroup a row.  Loss and
+// gradient by one and by several (us, launches in a graph): 131072 bfloat16 logits, 1 row 17.8 and 8.5, 64
+// 20.7 and 17.2, 128 23.1 and 28.2, 255 28.6 and 47.2; of binary32 30.1 and 8.5, 36.2 and 23.2, 40.5 and
+// 39.6, 65.7 and 67.4; 32768 bfloat16, 1 row 7.9 and 8.4, 255 10.8 and 16.9; 16384, 16 rows 6.6 and 8.7.
+// Several pay at 131072 logits up to about 100 rows; at the shorter rows that the rule gives them they
+// lose 0.5 to 6 us, a launch and a second read of the row.
 bool several(int64_t rows, int64_t vocab) { return rows < 256 && vocab > 2 * CHUNK; }
 
 // One workgroup a row, `count` rows from a.first.  The row in registers where it fits 64 of them a
-// thread, read again where it does not (MC logits, rows below one piece, long rows).
+// thread, read again where it does not (MC logits, rows below one piece, long rows).  Loss and gradient
+// of bfloat16 rows (us, launches in a graph; threads x pieces, the rule's first): 32768 rows of 1000, 64 x 2
+// 40, 256 x 1 74, read again 150; 8192 of 4096, 256 x 2 30, 64 x 8 26 (binary32: 46 and 70), 512 x 1 44, read
+// again 51; 8192 of 8192, 256 x 4 46, 512 x 2 55, read again 67; 4096 of 32768, 512 x 8 110, 1024 x 4 105, read
+// again 162; 2048 of 65536, 1024 x 8 107, read again 168.
 template <typename T, bool ONE, bool GRAD>
 void run_rows(const DistillArgs &a, int64_t count, hipStream_t stream) {
   const dim3 grid((unsigned)count);

@@ -10,7 +10,8 @@
 //
 // Measured (MI355X, 4096 x 1024 -> 1024, binary16, one component): 48 us in all; staging 12.4, both
 // products 34 (the matrix instructions of three bfloat16-sized products take 18 at the rate of a large
-// one), the sum of dW's slices 4.9, db 3.9.
+// one), the sum of dW's slices 4.9, db 3.9.  bfloat16 41, binary32 124 (nine products of pieces, three for
+// dX and six for dW).  4096 x 4096 -> 4096: 359, 254 and 998 us.
 #include "mcf_internal.hpp"
 #include "mx4.hpp"
 #include "mx4_gemm.hpp"

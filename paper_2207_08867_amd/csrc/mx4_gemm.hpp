@@ -18,12 +18,15 @@
 // c ^ (r / 2 mod 8) of its row: 16 neighbouring rows' chunks c lie in 16 different groups of four of
 // the 64 banks.
 //
-// What bounds it.  Large tiles: the matrix instructions, busy 56% (FP4) and 60% (MIX) of the cycles
-// at a clock that the power limit holds at 1.7 to 2.0 GHz; LDS is busy a quarter of the time (a
-// wavefront of 128 x 64 outputs reads 6 KiB of it for 8 instructions), and the barrier's and the
-// loads' waits are 29%.  8192^3 FP4 263 us, 4.2 PFLOP/s; 4096^3 MIX 102 us, 1.34 PFLOP/s, where a
-// library product of plain bfloat16 takes 98.  Grids of about 256 small tiles: a step takes 0.36 to
-// 0.6 us whatever it multiplies, its loads' and reads' latency.
+// What bounds it.  Large tiles: the schedule.  The matrix instructions are busy 56% (FP4) and 60% (MIX)
+// of the cycles; two wavefronts a SIMD, two buffers and one barrier a step that all eight wavefronts
+// meet leave 29% of the wavefronts' cycles waiting at it and for loads.  LDS is busy a quarter of the
+// time (a wavefront of 128 x 64 outputs reads 6 KiB of it for 8 instructions).  The power limit holds
+// the clock at 1.7 to 2.0 GHz; under it a loop of the scaled instruction alone reaches 6.55 PFLOP/s.
+// 8192^3 FP4 262 to 272 us, 4.1 PFLOP/s; 4096^3 MIX 102 us, 1.34 PFLOP/s, where a library product of
+// plain bfloat16 takes 98; 4096^3 MIXH 107 us, 5 of them the pass over the scales.  Grids of about 256
+// small tiles: a step takes 0.36 to 0.6 us whatever it multiplies, its loads' and reads' latency
+// (4096 x 4096 by 256 rows: MIX 22 us, FP4 12, where bytes and operations need 6 and 2).
 #pragma once
 
 #include "mcf_internal.hpp"
@@ -500,8 +503,9 @@ struct GemmPlan {
 
 // Tile and slices for an M x N product of `total` steps: the least time by this model, a function of
 // the sizes alone.  Measured (us): a step of a grid of 256 workgroups, and of one of 512, which two
-// of the smaller tiles' workgroups a CU share; and what a launch costs besides its steps.  The
-// kinds differ by up to a fifth, mostly alike.
+// of the smaller tiles' workgroups a CU share; and what a launch costs besides its steps.  One row of
+// times serves all kinds, which are a third apart: it gives 227 us for 8192^3 FP4, which takes 265, and
+// 118 for 4096^3 MIX, which takes 102.
 struct GemmRow {
   int tile;
   double step1, step2, fixed;

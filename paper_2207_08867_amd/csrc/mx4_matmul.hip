@@ -171,9 +171,13 @@ __global__ __launch_bounds__(64 * NW) void mx_thin_kernel(ThinArgs a) {
 // One to XT rows of a binary16 or binary32 x.  As above, but the pieces of x are made once: a lane
 // splits 8 elements of each row, of the four groups that its wavefront holds, and the wavefront
 // reads them back from LDS as operands.  Splitting in the operands' layout instead repeats it in all
-// 16 lanes of a block, most of them for rows that x does not have: 4096 x 4096, one row of
-// binary16: 12.4 us so, 5.1 us in this kernel (1.7 TB/s, a launch
-// and its loads' latency); 32768 x 4096 24.5 us (2.9 TB/s).
+// 16 lanes of a block, most of them for rows that x does not have.  What bounds it is the latency of
+// its loads: 184 to 240 VGPRs leave one workgroup of eight wavefronts a CU, with nothing in flight
+// while it joins and leaves.  Measured, this kernel and the one above (us, launches in a graph):
+// 4096 x 4096, one row of binary16 3.8 and 5.6, of binary32 4.3 and 8.0; 32768 x 4096 23.4 (3.0 TB/s)
+// and 28.4, 26.2 and 41.7.  Four rows: 5.3 and 5.7, 6.5 and 8.4; 33.7 and 29.9, 43.8 and 46.1;
+// 1024 x 1024 4.5 and 3.4, 5.2 and 4.1.  (Eight rows of binary16 by the same kernel: 6.8, 6.1 by the
+// one above.)
 template <typename T, int XT, int NW>
 __global__ __launch_bounds__(64 * NW) void mx_token_kernel(ThinArgs a) {
   constexpr int P = mx_pieces<T>(), U = 4;
@@ -244,7 +248,9 @@ __global__ __launch_bounds__(64 * NW) void mx_token_kernel(ThinArgs a) {
 template <typename T, bool PACKED, int MT>
 hipError_t thin_mt(const ThinArgs &a, hipStream_t stream) {
   const dim3 grid((unsigned)((a.N + 15) / 16), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
-  // about four groups a wavefront
+  // about four groups a wavefront.  One row of binary16 by 4096 weight rows with 2, 4 and 8 wavefronts
+  // (us): 512 columns 3.2, 3.4, 3.4; 2048 4.0, 3.2, 3.9; 4096 5.9, 4.1, 3.8; MXFP4 and bfloat16 rows differ
+  // less, by 0.1 to 1
   constexpr int U = MT == 1 ? (sizeof(T) == 4 && !PACKED ? 2 : 4) : 2;
   if (a.G <= 4)
     mx_thin_kernel<T, PACKED, MT, 2, U><<<grid, 128, 0, stream>>>(a);
@@ -289,9 +295,16 @@ hipError_t thin_any(int dtype, const ThinArgs &a, hipStream_t stream) {
 
 }  // namespace
 
-// Up to so many rows of x the weight is read straight into registers; above, tiles go through LDS
-// (4096 x 4096, us: 64 and 65 rows of MXFP4 8.9 and 11.4; 32 and 64 rows of bfloat16 by registers 11.0
-// and 22.2, 65 by tiles 16.4; 16 and 64 rows of binary16 13.7 and 35.5, 65 by tiles 25.4).
+// Up to so many rows of x the weight is read straight into registers; above, tiles go through LDS.
+// Registers and tiles (us, launches in a graph), K = 4096:
+//   MXFP4     4096 weight rows: 64 rows of x 7.6 and 9.6, 96 11.7 and 11.5; 14336: 16 10.4 and 11.8, 64 26.3
+//             and 11.9
+//   bfloat16  4096: 32 10.5 and 12.0, 48 16.0 and 13.3; 14336: 16 20.8 and 22.4, 32 36.0 and 22.8
+//   binary16  4096: 16 7.4 and 14.7, 48 16.8 and 17.2; 14336: 16 22.2 and 26.8, 24 32.6 and 27.1
+//   binary32  4096: 16 12.4 and 20.8, 24 20.4 and 21.8; 14336: 16 42.7 and 54.5, 24 61.7 and 48.7
+// and 1024 x 1024 is faster by registers past 96 rows in every format (4.1 to 7.9 and 5.6 to 11.5).  So
+// where they cross depends on the weight's size too, which the rule leaves out: the first two limits
+// are those of 4096 x 4096 weights, the other two hold for larger ones as well.
 constexpr int64_t THIN_PACKED = 64;
 int64_t thin_rows(int dtype) { return dtype == LM_BF16 ? 32 : 16; }
 

@@ -5,8 +5,8 @@
 // number the element stands for, is the next component's input.  The remainder is exact in
 // binary32: it is a multiple of v_i's last place and no larger than v_i, or within 2^(X-2) of
 // zero.  Both directions stream: 2 to 4 bytes read and 17/32 of a byte written per element and
-// component (or back), so HBM bounds them (8192 x 8192 bfloat16: 27 us, 6.2 TB/s, and back 37 us, 4.6
-// TB/s).  A lane takes 8 elements and four lanes a block; the block's maximum is two DPP steps
+// component (or back), so HBM bounds them (8192 x 8192 bfloat16: 28 us, 6.1 TB/s, and back 35 us, 4.9
+// TB/s; binary32 45 us, 6.7 TB/s, and back 86 us, 3.6 TB/s: its 32 bytes a lane go out in two halves).  A lane takes 8 elements and four lanes a block; the block's maximum is two DPP steps
 // inside a quad.
 #include <type_traits>
 
@@ -56,7 +56,7 @@ __device__ inline float round_odd(double d) {
 // neighbouring rows fall into one line; long rows 4 x 4, which reads longer runs.  Measured (us,
 // quantising and reading back), 100000 x 100 binary16: 7.3 and 10.3 as 16 rows, 22 and 18 as 4, 38
 // and 35 as one; 4099 x 4097 binary16 in two planes and components: 21.1 and 15.6, 18.7 and 15.4, 18.8
-// and 15.4; 8192 x 8192 bfloat16: 27 to 29 (6.2 TB/s) and 37 (4.6 TB/s) in all of them.
+// and 15.4; 8192 x 8192 bfloat16: 27 to 29 (6.2 TB/s) and 35 to 37 (4.6 TB/s and more) in all of them.
 int tile_shift(int64_t groups) { return groups >= 16 ? 2 : 4; }
 
 __device__ inline int64_t divide(int64_t a, int64_t b) {
