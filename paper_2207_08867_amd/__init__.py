@@ -47,6 +47,7 @@ def lib() -> ctypes.CDLL:
         if not os.path.exists(LIB_PATH):
             raise MCFError(f"{LIB_PATH} is missing: build it with `python -m paper_2207_08867_amd.build` "
                            "(or __graft_entry__.build())")
+        _torch()  # first: the library then shares torch's HIP runtime instead of loading another
         L = ctypes.CDLL(LIB_PATH)
         vp, i64, ci = ctypes.c_void_p, ctypes.c_int64, ctypes.c_int
         for name in ("mc_add", "mc_mul", "mc_div"):
