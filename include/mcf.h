@@ -13,7 +13,8 @@
  *   arrays: a binary16 exponential table (128 KiB, built on the first mc_exp call on
  *   a device) and the 8 MiB scratch of mc_matmul_splitk_noalloc.  Calls that need
  *   scratch memory (mc_matmul_splitk, mc_matmul_exact, mc_linreg_gd_step, the MXFP4
- *   products, the distillation loss) take a caller-owned workspace.
+ *   products, the distillation loss, the norm's gradients, the 8-bit products, the log
+ *   probabilities) take a caller-owned workspace.
  * Layout.  Dense, component-major ("planar"): component c of element i of an MC
  *   array of n elements is at element offset c*n + i.  A plain tensor is one plane.
  *   Matrices are row-major inside each plane.  The paper's interleaved layout
@@ -70,8 +71,8 @@
 extern "C" {
 #endif
 
-/* MCF_BF16 (bfloat16) is taken by the mc_mx4_* and mc_distill_* calls alone; those take
- * MCF_F16, MCF_BF16 and MCF_F32. */
+/* MCF_BF16 (bfloat16) is taken by the mc_mx4_*, mc_distill_*, mc_rmsnorm_*, mc_int8_* and
+ * mc_logprobs_* calls alone; those take MCF_F16, MCF_BF16 and MCF_F32. */
 typedef enum { MCF_F16 = 0, MCF_F32 = 1, MCF_F64 = 2, MCF_F16S = 3, MCF_BF16 = 4 } mcf_dtype;
 
 typedef enum {
@@ -475,6 +476,109 @@ int mc_distill_fwd_bwd(int dtype, int nc, int64_t rows, int64_t vocab, int64_t k
                        const void *t, double temperature, const void *g, void *workspace, int64_t workspace_bytes,
                        void *loss, void *dz, void *stream);
 int64_t mc_distill_workspace(int64_t rows, int64_t vocab);
+
+/* ---------------------------------------------------------------------------------
+ * 8-bit tensors, the RMS norm that makes them, and their products
+ *
+ * An 8-bit tensor of `rows` rows of n elements, P = n rounded up to a multiple of 128:
+ *   codes:  [rows][P] signed bytes from -127 to 127, zeros past n; 16-byte aligned.
+ *   scales: [rows] binary32.  Element i of a row stands for code_i times the row's scale.
+ * Quantisation of a row p: with m its largest magnitude, code_i = 127 p_i / m rounded to the
+ *   nearest integer, ties to even (the binary64 quotient fl(fl(127 p_i) / m)), scale = m / 127
+ *   rounded once; a row of zeros has the scale 0.  A row with an infinity or NaN, or whose scale
+ *   passes binary32's range, has the scale NaN and zero codes.
+ * n <= 2^30; rows times P below 2^50.  Workspaces as for the MXFP4 calls. */
+
+/* x: plain [rows][n] or (nc_in > 1) an MC value [nc_in][rows][n], of which the planes' sum in
+ * binary64, the last one first, is quantised. */
+int mc_int8_quantize(int dtype, int nc_in, int64_t rows, int64_t n, const void *x, void *codes, void *scales,
+                     void *stream);
+
+/* Reading back: out [rows][n] = code times scale in binary32, rounded to the format. */
+int mc_int8_dequantize(int dtype, int64_t rows, int64_t n, const void *codes, const void *scales, void *out,
+                       void *stream);
+
+/* C = A B^T (+ bias) of two 8-bit tensors.  A: M rows of K (tokens), B: N rows of K (a weight's
+ * output channels), bias: [N] of the call's format or NULL, C: [M][N] in the call's format.  The
+ * integers' products are summed exactly; C_ij = (sum a_i) b_j + bias_j in binary32 (sum, a_i and b_j
+ * the scales of the rows), rounded once to the format: a row's result does not depend on
+ * the other rows.  M <= 2^20, N <= 2^24, K <= 131072. */
+int mc_int8_matmul(int dtype, int64_t M, int64_t N, int64_t K, const void *a_codes, const void *a_scales,
+                   const void *b_codes, const void *b_scales, const void *bias, void *workspace,
+                   int64_t workspace_bytes, void *C, void *stream);
+int64_t mc_int8_matmul_workspace(int dtype, int64_t M, int64_t N, int64_t K);
+
+/* Linear layer of a plain input with an 8-bit weight: y = x W^T (+ b), each row of x quantised as
+ * above; the same numbers as mc_int8_quantize and mc_int8_matmul.
+ * x: [batch][in]; codes, scales: W, `out` rows of `in`; b: [out] or NULL; y: [batch][out].
+ * batch <= 2^20, in <= 131072, out <= 2^24. */
+int mc_int8_linear_fwd(int dtype, int64_t batch, int64_t in, int64_t out, const void *x, const void *codes,
+                       const void *scales, const void *b, void *workspace, int64_t workspace_bytes, void *y,
+                       void *stream);
+int64_t mc_int8_linear_fwd_workspace(int dtype, int64_t batch, int64_t in, int64_t out);
+
+/* Root-mean-square norm of the rows of a residual stream, a layer's output x added to it first.
+ *   s = the planes of h summed in binary64, the last one first, plus x;
+ *   h_out = s split by successive rounding into nc planes (each through binary32 into the format;
+ *           nothing is left of a value past its range); v = the planes' sum again;
+ *   r = 1 / sqrt(sum of v_i^2 / n + eps);
+ *   y_i = v_i w_i r, rounded to the format.
+ * Without x, v is the sum of h's planes and h_out must be NULL.
+ * h: [nc][rows][n] (a plain stream: nc = 1); x: [rows][n] or NULL; w: [n] or NULL for ones; h_out:
+ * [nc][rows][n], may be h itself (in place); y: [rows][n].  Everything between the loads and the
+ * roundings is binary64.  n >= 1, eps >= 0 and finite. */
+int mc_rmsnorm_fwd(int dtype, int nc, int64_t rows, int64_t n, const void *h, const void *x, const void *w, double eps,
+                   void *h_out, void *y, void *stream);
+
+/* The same with the output as an 8-bit tensor: the quantisation of p_i = v_i w_i, of which the
+ * codes are a fixed function, with the scale r max |p| / 127. */
+int mc_rmsnorm_int8(int dtype, int nc, int64_t rows, int64_t n, const void *h, const void *x, const void *w, double eps,
+                    void *h_out, void *codes, void *scales, void *stream);
+
+/* The gradients of mc_rmsnorm_fwd, given dy, that of the loss with respect to y, and g, the
+ * gradient that reaches the stream behind the addition from elsewhere (NULL for none):
+ *   dh = g + r (w dy - v r^2 sum(v w dy) / n)   [rows][n]  with respect to that stream, and so to
+ *                                                          h and to x alike (plain, Section 2.1)
+ *   dw = sum over the rows of dy v r            [n]
+ * h: the stream the norm was taken of (h_out where x was added).  dh and dw may each be NULL (not
+ * computed); the workspace is needed for dw.  Sums over rows are joined in a fixed order. */
+int mc_rmsnorm_bwd(int dtype, int nc, int64_t rows, int64_t n, const void *h, const void *w, const void *dy,
+                   const void *g, double eps, void *dh, void *dw, void *workspace, int64_t workspace_bytes,
+                   void *stream);
+int64_t mc_rmsnorm_bwd_workspace(int dtype, int64_t rows, int64_t n);
+
+/* ---------------------------------------------------------------------------------
+ * Log probabilities of tokens
+ *
+ * With q the softmax over a row of z_j / T, j < vocab:
+ *   logp_i = log q_{ids_i}, of `given` tokens a row; 0 for an id outside [0, vocab) (no token);
+ *   entropy = -sum_j q_j log q_j;
+ *   the `top` most likely tokens, in the order (z descending, j ascending), and their log q.  Past
+ *   the last logit above -inf the id is -1 and the log probability -inf.
+ * A logit of -inf has q_j = 0 and log q_j = -inf.  A row of nothing but -inf: log probabilities
+ * -inf, entropy 0, no alternatives, gradient 0.  A row with a NaN or +inf: NaN everywhere, ids -1.
+ * z: plain [rows][vocab], or (nc > 1) an MC value [nc][rows][vocab] whose planes are summed in
+ *   binary32, the last one first; its gradient is plain, that of the sum (Section 2.1).
+ * ids: int32 [rows][given], 0 <= given <= 1024, in any order, also equal ones.
+ * temperature: positive and finite.
+ * logp: binary32 [rows][given]; entropy: binary32 [rows] or NULL; top_ids: int32 and top_logp:
+ *   binary32 [rows][top], 0 <= top <= 128.
+ * stats: binary32 [rows][3] or NULL, for the gradient: the row's largest logit m, L = log sum_j
+ *   exp((z_j - m) / T), and entropy - L.
+ * Statistics and sums are binary32; the log probability of a token the row is sure of keeps its relative
+ * accuracy.  No output may overlap an input or another output.  rows < 2^31,
+ * 1 <= vocab <= 2^30.  Workspace as for the MXFP4 calls. */
+int mc_logprobs_fwd(int dtype, int nc, int64_t rows, int64_t vocab, int64_t given, int64_t top, const void *z,
+                    const void *ids, double temperature, void *workspace, int64_t workspace_bytes, void *logp,
+                    void *entropy, void *top_ids, void *top_logp, void *stats, void *stream);
+int64_t mc_logprobs_workspace(int64_t rows, int64_t vocab, int64_t top);
+
+/* The gradient dz [rows][vocab], in z's format, of sum_i g_i logp_i + g_entropy entropy over each row:
+ *   dz_j = (sum of the g_i with ids_i = j - q_j (sum of all used g_i + g_entropy (log q_j + entropy))) / T.
+ * g: binary32 [rows][given] or NULL for ones; g_entropy: binary32 [rows] or NULL for zeros. */
+int mc_logprobs_bwd(int dtype, int nc, int64_t rows, int64_t vocab, int64_t given, const void *z, const void *ids,
+                    double temperature, const void *stats, const void *g, const void *g_entropy, void *dz,
+                    void *stream);
 
 /* Human-readable name of a status code (static storage). */
 const char *mc_status_str(int status);

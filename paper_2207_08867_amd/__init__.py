@@ -28,6 +28,9 @@ __all__ = [
     "mc_mx4_quantize", "mc_mx4_dequantize", "mc_mx4_matmul", "mc_mx4_matmul_workspace", "mc_mx4_linear_fwd",
     "mc_mx4_linear_fwd_workspace", "mc_mx4_linear_bwd", "mc_mx4_linear_bwd_workspace", "mc_distill_fwd",
     "mc_distill_bwd", "mc_distill_fwd_bwd", "mc_distill_workspace",
+    "mc_rmsnorm_fwd", "mc_rmsnorm_int8", "mc_rmsnorm_bwd", "mc_rmsnorm_bwd_workspace", "mc_int8_quantize",
+    "mc_int8_dequantize", "mc_int8_matmul", "mc_int8_matmul_workspace", "mc_int8_linear_fwd",
+    "mc_int8_linear_fwd_workspace", "mc_logprobs_fwd", "mc_logprobs_bwd", "mc_logprobs_workspace",
 ]
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libmcf.so")
@@ -110,6 +113,19 @@ def lib() -> ctypes.CDLL:
             ("mc_distill_bwd", [ci, ci, i64, i64, i64, vp, vp, vp, cd, vp, vp, vp, vp], ci),
             ("mc_distill_fwd_bwd", [ci, ci, i64, i64, i64, vp, vp, vp, cd, vp, vp, i64, vp, vp, vp], ci),
             ("mc_distill_workspace", [i64, i64], i64),
+            ("mc_rmsnorm_fwd", [ci, ci, i64, i64, vp, vp, vp, cd, vp, vp, vp], ci),
+            ("mc_rmsnorm_int8", [ci, ci, i64, i64, vp, vp, vp, cd, vp, vp, vp, vp], ci),
+            ("mc_rmsnorm_bwd", [ci, ci, i64, i64, vp, vp, vp, vp, cd, vp, vp, vp, i64, vp], ci),
+            ("mc_rmsnorm_bwd_workspace", [ci, i64, i64], i64),
+            ("mc_int8_quantize", [ci, ci, i64, i64, vp, vp, vp, vp], ci),
+            ("mc_int8_dequantize", [ci, i64, i64, vp, vp, vp, vp], ci),
+            ("mc_int8_matmul", [ci, i64, i64, i64, vp, vp, vp, vp, vp, vp, i64, vp, vp], ci),
+            ("mc_int8_matmul_workspace", [ci, i64, i64, i64], i64),
+            ("mc_int8_linear_fwd", [ci, i64, i64, i64, vp, vp, vp, vp, vp, i64, vp, vp], ci),
+            ("mc_int8_linear_fwd_workspace", [ci, i64, i64, i64], i64),
+            ("mc_logprobs_fwd", [ci, ci, i64, i64, i64, i64, vp, vp, cd, vp, i64, vp, vp, vp, vp, vp, vp], ci),
+            ("mc_logprobs_bwd", [ci, ci, i64, i64, i64, vp, vp, cd, vp, vp, vp, vp, vp], ci),
+            ("mc_logprobs_workspace", [i64, i64, i64], i64),
         ):
             f = getattr(L, name)
             f.argtypes, f.restype = args, res
@@ -137,7 +153,7 @@ def _check(status: int, what: str):
 # and the current stream's handle is read without building a Stream object (a 7850-element
 # MC-SGD update, two calls: 21 -> 15 us).
 _DTYPE_CODES = {}
-_PLAIN_CODES = {}  # the formats of the mc_mx4_* and mc_distill_* calls
+_PLAIN_CODES = {}  # the formats of the calls on low-precision tensors and on rows of logits
 _torch_module = None
 _raw_stream = None
 _plain_tensor = None
@@ -892,3 +908,251 @@ def mc_distill_fwd_bwd(z, ids, t, g=None, *, temperature: float = 1.0, out=None,
                                  _dev(out, "out"), _stream(z))
     _check(st, "mc_distill_fwd_bwd")
     return loss, out
+
+
+# 8-bit tensors are pairs (codes, scales): for a tensor of shape (*S, n), P = n rounded up to a
+# multiple of 128, codes (*S, P) int8 and scales (*S) float32.  The layout is in include/mcf.h.
+
+
+def _int8(pair, n, name):
+    """(S, codes pointer, scales pointer) of an 8-bit tensor of row length n."""
+    codes, scales = pair
+    torch = _torch_module or _torch()
+    if codes.dtype is not torch.int8 or scales.dtype is not torch.float32:
+        raise TypeError(f"{name}: codes must be int8 and scales float32")
+    if codes.get_device() != scales.get_device():
+        raise ValueError(f"{name}: codes and scales must be on one device")
+    cs = codes.shape
+    if n < 0 or len(cs) < 1 or cs[-1] != (n + 127) // 128 * 128 or scales.shape != cs[:-1]:
+        raise ValueError(f"{name}: codes {tuple(cs)} and scales {tuple(scales.shape)} are not an 8-bit tensor of "
+                         f"rows of {n}")
+    return cs[:-1], _dev(codes, name), _dev(scales, name)
+
+
+def _int8_out(out, like, lead, n):
+    codes, scales = out or (None, None)
+    return (_out(codes, like, (*lead, (n + 127) // 128 * 128), _torch_module.int8),
+            _out(scales, like, lead, _torch_module.float32))
+
+
+def _planes(x, x_mc, name):
+    """(nc, S, n) of a plain tensor (*S, n) or, with x_mc, an MC value (nc, *S, n)."""
+    shape = x.shape
+    if len(shape) < (2 if x_mc else 1):
+        raise ValueError(f"{name} must be (*S, n), or (planes, *S, n) of an MC value")
+    return (shape[0], shape[1:-1], shape[-1]) if x_mc else (1, shape[:-1], shape[-1])
+
+
+def mc_int8_quantize(x, *, x_mc: bool = False, out=None):
+    """x (*S, n), or with x_mc an MC value (planes, *S, n) -> its 8-bit tensor (codes, scales): a row's
+    largest magnitude becomes 127, the other elements the nearest integers, ties to even."""
+    code = _plain_code(x.dtype)
+    nc, lead, n = _planes(x, x_mc, "x")
+    codes, scales = _int8_out(out, x, lead, n)
+    st = (_lib or lib()).mc_int8_quantize(code, nc, math.prod(lead), n, _dev(x, "x"), _dev(codes, "codes"),
+                                          _dev(scales, "scales"), _stream(x))
+    _check(st, "mc_int8_quantize")
+    return codes, scales
+
+
+def mc_int8_dequantize(codes, scales, n: int, *, dtype, out=None):
+    """The numbers (*S, n) an 8-bit tensor stands for, in `dtype`."""
+    lead, cp, sp = _int8((codes, scales), n, "codes and scales")
+    code = _plain_code(dtype)
+    out = _out(out, codes, (*lead, n), dtype)
+    st = (_lib or lib()).mc_int8_dequantize(code, math.prod(lead), n, cp, sp, _dev(out, "out"), _stream(codes))
+    _check(st, "mc_int8_dequantize")
+    return out
+
+
+def _bias(b, n, dtype, like):
+    if b is None:
+        return None
+    _device(b, like, "bias")
+    if b.dtype != dtype or tuple(b.shape) != (n,):
+        raise ValueError("dtype or bias shape mismatch")
+    return _dev(b, "bias")
+
+
+def mc_int8_matmul_workspace(dtype, M: int, N: int, K: int) -> int:
+    """Workspace bytes of mc_int8_matmul."""
+    return _bytes("mc_int8_matmul_workspace", _plain_code(dtype), M, N, K)
+
+
+def mc_int8_matmul(a, b, K: int, bias=None, *, dtype, out=None, workspace=None):
+    """a b^T (+ bias) of two 8-bit tensors (codes, scales) with M and N rows of K -> (M, N) of
+    `dtype`; bias (N,) of `dtype` or None.  `workspace`: an optional device byte tensor; one is
+    allocated here when needed and not given."""
+    code = _plain_code(dtype)
+    sa, ac, asc = _int8(a, K, "a")
+    sb, bc, bsc = _int8(b, K, "b")
+    _device(b[0], a[0], "b")
+    if len(sa) != 1 or len(sb) != 1:
+        raise ValueError("a and b must be 8-bit tensors of matrices")
+    M, N = sa[0], sb[0]
+    bp = _bias(bias, N, dtype, a[0])
+    out = _out(out, a[0], (M, N), dtype)
+    keep, wp, wn = _space(workspace, _bytes("mc_int8_matmul_workspace", code, M, N, K), a[0])
+    st = (_lib or lib()).mc_int8_matmul(code, M, N, K, ac, asc, bc, bsc, bp, wp, wn, _dev(out, "out"), _stream(a[0]))
+    _check(st, "mc_int8_matmul")
+    return out
+
+
+def mc_int8_linear_fwd_workspace(dtype, batch: int, in_: int, out: int) -> int:
+    """Workspace bytes of mc_int8_linear_fwd."""
+    return _bytes("mc_int8_linear_fwd_workspace", _plain_code(dtype), batch, in_, out)
+
+
+def mc_int8_linear_fwd(x, W, b=None, *, out=None, workspace=None):
+    """y = x W^T + b, each row of x quantised to 8 bits on the way.  x: (batch, in) plain, W: the 8-bit
+    tensor (codes, scales) of an (out, in) weight, b: (out,) of x's dtype or None -> (batch, out).
+    `workspace`: an optional device byte tensor; one is allocated here when needed and not given."""
+    if x.dim() != 2:
+        raise ValueError("x must be (batch, in)")
+    T, I = x.shape
+    code = _plain_code(x.dtype)
+    s, wc, wsc = _int8(W, I, "W")
+    _device(W[0], x, "W")
+    if len(s) != 1:
+        raise ValueError("W must be the 8-bit tensor of a matrix")
+    O = s[0]
+    bp = _bias(b, O, x.dtype, x)
+    out = _out(out, x, (T, O), x.dtype)
+    keep, wp, wn = _space(workspace, _bytes("mc_int8_linear_fwd_workspace", code, T, I, O), x)
+    st = (_lib or lib()).mc_int8_linear_fwd(code, T, I, O, _dev(x, "x"), wc, wsc, bp, wp, wn, _dev(out, "out"),
+                                            _stream(x))
+    _check(st, "mc_int8_linear_fwd")
+    return out
+
+
+def _norm_args(h, w, h_mc, **others):
+    """(code, nc, S, n, pointer of w) of a norm's tensors; the others must be (*S, n)."""
+    code = _plain_code(h.dtype)
+    nc, lead, n = _planes(h, h_mc, "h")
+    for name, t in others.items():
+        if t is not None:
+            _device(t, h, name)
+            if t.dtype != h.dtype or tuple(t.shape) != (*lead, n):
+                raise ValueError(f"{name} must be {(*lead, n)} of h's dtype, got {tuple(t.shape)} of {t.dtype}")
+    if w is None:
+        return code, nc, lead, n, None
+    _device(w, h, "w")
+    if w.dtype != h.dtype or tuple(w.shape) != (n,):
+        raise ValueError(f"w must be {(n,)} of h's dtype, got {tuple(w.shape)} of {w.dtype}")
+    return code, nc, lead, n, _dev(w, "w")
+
+
+def _norm_stream(h, x, h_out):
+    """(the stream behind the addition, its pointer for the call)."""
+    if x is None:
+        if h_out is not None:
+            raise ValueError("h_out is the stream behind the addition of x, which is not given")
+        return h, None
+    h_out = _out(h_out, h, h.shape, h.dtype)
+    return h_out, _dev(h_out, "h_out")
+
+
+def mc_rmsnorm_fwd(h, w=None, *, x=None, eps: float = 1e-6, h_mc: bool = False, h_out=None, out=None):
+    """Root-mean-square norm of a residual stream h, (*S, n) or with h_mc an MC value (planes, *S, n), with
+    x (*S, n), a layer's output, added to the stream first (see include/mcf.h); w: (n,) or None for ones.
+    Returns (y (*S, n), the stream behind the addition: h itself without x).  h_out may be h (in place)."""
+    code, nc, lead, n, wp = _norm_args(h, w, h_mc, x=x)
+    stream, sp = _norm_stream(h, x, h_out)
+    out = _out(out, h, (*lead, n), h.dtype)
+    st = (_lib or lib()).mc_rmsnorm_fwd(code, nc, math.prod(lead), n, _dev(h, "h"), None if x is None else _dev(x, "x"),
+                                        wp, float(eps), sp, _dev(out, "out"), _stream(h))
+    _check(st, "mc_rmsnorm_fwd")
+    return out, stream
+
+
+def mc_rmsnorm_int8(h, w=None, *, x=None, eps: float = 1e-6, h_mc: bool = False, h_out=None, out=None):
+    """mc_rmsnorm_fwd with the output as an 8-bit tensor: ((codes, scales), the stream behind the addition)."""
+    code, nc, lead, n, wp = _norm_args(h, w, h_mc, x=x)
+    stream, sp = _norm_stream(h, x, h_out)
+    codes, scales = _int8_out(out, h, lead, n)
+    st = (_lib or lib()).mc_rmsnorm_int8(code, nc, math.prod(lead), n, _dev(h, "h"), None if x is None else _dev(x, "x"),
+                                         wp, float(eps), sp, _dev(codes, "codes"), _dev(scales, "scales"), _stream(h))
+    _check(st, "mc_rmsnorm_int8")
+    return (codes, scales), stream
+
+
+def mc_rmsnorm_bwd_workspace(dtype, rows: int, n: int) -> int:
+    """Workspace bytes of mc_rmsnorm_bwd with dw."""
+    return _bytes("mc_rmsnorm_bwd_workspace", _plain_code(dtype), rows, n)
+
+
+def mc_rmsnorm_bwd(h, w, dy, *, dh=None, eps: float = 1e-6, h_mc: bool = False, dx: bool = True, dw: bool = True,
+                   workspace=None):
+    """The gradients of mc_rmsnorm_fwd: (that of the stream the norm was taken of, (*S, n), which is the
+    gradient of h and of x alike, that of w (n,)); None for those not requested.  h: that stream (what
+    mc_rmsnorm_fwd returned with x), dy: (*S, n), dh: the gradient that reaches the stream from elsewhere, (*S, n)
+    or None.  `workspace`: an optional device byte tensor; one is allocated here when not given."""
+    code, nc, lead, n, wp = _norm_args(h, w, h_mc, dy=dy, dh=dh)
+    rows = math.prod(lead)
+    outs = [_empty(h, (*lead, n)) if dx else None, _empty(h, (n,)) if dw else None]
+    keep, sp, sn = _space(workspace, _bytes("mc_rmsnorm_bwd_workspace", code, rows, n) if dw else 0, h)
+    st = (_lib or lib()).mc_rmsnorm_bwd(code, nc, rows, n, _dev(h, "h"), wp, _dev(dy, "dy"),
+                                        None if dh is None else _dev(dh, "dh"), float(eps),
+                                        *(None if o is None else o.data_ptr() for o in outs), sp, sn, _stream(h))
+    _check(st, "mc_rmsnorm_bwd")
+    return tuple(outs)
+
+
+def _logprobs_args(z, ids):
+    """(code, nc, rows, vocab, given) of the tensors of a call on log probabilities."""
+    shape = z.shape
+    if len(shape) not in (2, 3):
+        raise ValueError("z must be (rows, vocab), or (nc, rows, vocab) of an MC value")
+    nc, (rows, vocab) = (shape[0] if len(shape) == 3 else 1), shape[-2:]
+    if ids.dtype is not (_torch_module or _torch()).int32:
+        raise TypeError(f"ids must be int32, got {ids.dtype}")
+    if len(ids.shape) != 2 or ids.shape[0] != rows:
+        raise ValueError(f"ids must be (rows = {rows}, given), got {tuple(ids.shape)}")
+    _device(ids, z, "ids")
+    return _plain_code(z.dtype), nc, rows, vocab, ids.shape[1]
+
+
+def mc_logprobs_workspace(rows: int, vocab: int, top: int) -> int:
+    """Workspace bytes of mc_logprobs_fwd."""
+    return _bytes("mc_logprobs_workspace", rows, vocab, top)
+
+
+def mc_logprobs_fwd(z, ids, *, top: int = 0, temperature: float = 1.0, workspace=None):
+    """Log probabilities under softmax(z / temperature) of given tokens, with the entropy and the `top` most
+    likely tokens of every row (see include/mcf.h).  z: (rows, vocab) plain or (nc, rows, vocab) MC; ids:
+    (rows, given) int32, an id outside the vocabulary is no token.  Returns (logp (rows, given), entropy (rows,),
+    top_ids (rows, top) int32, top_logp (rows, top), stats (rows, 3)), float32 but for the ids; stats are for
+    mc_logprobs_bwd.  `workspace`: an optional device byte tensor; one is allocated here when needed and not given."""
+    torch = _torch()
+    code, nc, rows, vocab, given = _logprobs_args(z, ids)
+    keep, wp, wn = _space(workspace, _bytes("mc_logprobs_workspace", rows, vocab, top), z)
+    logp, entropy, top_ids, top_logp, stats = (
+        _out(None, z, shape, dtype) for shape, dtype in (((rows, given), torch.float32), ((rows,), torch.float32),
+                                                         ((rows, top), torch.int32), ((rows, top), torch.float32),
+                                                         ((rows, 3), torch.float32)))
+    st = (_lib or lib()).mc_logprobs_fwd(code, nc, rows, vocab, given, top, _dev(z, "z"), _dev(ids, "ids"),
+                                         float(temperature), wp, wn, logp.data_ptr(), entropy.data_ptr(),
+                                         top_ids.data_ptr(), top_logp.data_ptr(), stats.data_ptr(), _stream(z))
+    _check(st, "mc_logprobs_fwd")
+    return logp, entropy, top_ids, top_logp, stats
+
+
+def mc_logprobs_bwd(z, ids, stats, g=None, g_entropy=None, *, temperature: float = 1.0, out=None):
+    """The gradient (rows, vocab) of sum g logp + sum g_entropy entropy with respect to z (of the planes' sum
+    for an MC z) from mc_logprobs_fwd's stats.  g: (rows, given) float32 or None for ones; g_entropy: (rows,)
+    float32 or None for zeros."""
+    f32 = _torch().float32
+    code, nc, rows, vocab, given = _logprobs_args(z, ids)
+    for name, t, shape in (("stats", stats, (rows, 3)), ("g", g, (rows, given)), ("g_entropy", g_entropy, (rows,))):
+        if t is None and name != "stats":
+            continue
+        if t.dtype != f32 or tuple(t.shape) != shape:
+            raise ValueError(f"{name} must be {shape} float32")
+        _device(t, z, name)
+    out = _out(out, z, (rows, vocab), z.dtype)
+    st = (_lib or lib()).mc_logprobs_bwd(code, nc, rows, vocab, given, _dev(z, "z"), _dev(ids, "ids"),
+                                         float(temperature), _dev(stats, "stats"), None if g is None else _dev(g, "g"),
+                                         None if g_entropy is None else _dev(g_entropy, "g_entropy"),
+                                         _dev(out, "out"), _stream(z))
+    _check(st, "mc_logprobs_bwd")
+    return out

@@ -159,4 +159,37 @@ hipError_t launch_distill(int dtype, int nc, int64_t rows, int64_t vocab, int64_
                           const void *t, double temperature, const void *stats_in, const void *g, void *ws, void *loss,
                           void *stats, void *dz, hipStream_t stream);
 
+// RMS norm of a residual stream with a layer's output added, plain (y) or 8-bit (codes, scales) output,
+// and 8-bit quantisation (norm false); reading back; the norm's gradients (rmsnorm.hip).  dh and dw may
+// each be null; ws holds rmsnorm_bwd_workspace_bytes(rows, n) bytes with dw.
+hipError_t launch_rmsnorm(int dtype, int nc, int64_t rows, int64_t n, const void *h, const void *x, const void *w,
+                          double eps, void *h_out, void *y, void *codes, void *scales, bool norm, hipStream_t stream);
+hipError_t launch_int8_dequantize(int dtype, int64_t rows, int64_t n, const void *codes, const void *scales, void *out,
+                                  hipStream_t stream);
+int64_t rmsnorm_bwd_workspace_bytes(int64_t rows, int64_t n);
+hipError_t launch_rmsnorm_bwd(int dtype, int nc, int64_t rows, int64_t n, const void *h, const void *w, const void *dy,
+                              const void *g, double eps, void *dh, void *dw, void *ws, hipStream_t stream);
+
+// C [M][N] = A B^T of two 8-bit tensors (+ bias), and the linear layer of a plain x with an 8-bit weight
+// (int8_matmul.hip).  ws holds the bytes of the matching workspace function.
+int64_t int8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K);
+hipError_t launch_int8_matmul(int dtype, int64_t M, int64_t N, int64_t K, const void *a_codes, const void *a_scales,
+                              const void *b_codes, const void *b_scales, const void *bias, void *ws, void *C,
+                              hipStream_t stream);
+int64_t int8_linear_workspace_bytes(int64_t batch, int64_t in, int64_t out);
+hipError_t launch_int8_linear(int dtype, int64_t batch, int64_t in, int64_t out, const void *x, const void *codes,
+                              const void *scales, const void *bias, void *ws, void *y, hipStream_t stream);
+
+// Log probabilities of given tokens, entropy and top alternatives of rows of logits, and their gradient
+// (logprobs.hip).
+constexpr int LOGP_TOP = 128;     // the most alternatives
+constexpr int LOGP_GIVEN = 1024;  // the most given tokens of a row
+int64_t logprobs_workspace_bytes(int64_t rows, int64_t vocab, int64_t top);
+hipError_t launch_logprobs_fwd(int dtype, int nc, int64_t rows, int64_t vocab, int64_t given, int64_t top, const void *z,
+                               const void *ids, double temperature, void *ws, void *logp, void *entropy, void *top_ids,
+                               void *top_logp, void *stats, hipStream_t stream);
+hipError_t launch_logprobs_bwd(int dtype, int nc, int64_t rows, int64_t vocab, int64_t given, const void *z,
+                               const void *ids, double temperature, const void *stats, const void *g,
+                               const void *g_entropy, void *dz, hipStream_t stream);
+
 }  // namespace mcf

@@ -21,12 +21,19 @@ inline __host__ __device__ int64_t mx_groups(int64_t n) { return (n + MX_GROUP -
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef double f64x2 __attribute__((ext_vector_type(2)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+template <bool B>
+struct Flag {
+  static constexpr bool value = B;
+};
 
 // Eight elements of a plain tensor.  The address is aligned to the element only: rows of odd
 // length start anywhere, and gfx950 loads 16 bytes from any address.

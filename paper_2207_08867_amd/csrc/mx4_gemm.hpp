@@ -1,5 +1,5 @@
 // mx4_gemm.hpp -- the large products C = sum over pairs (i, j) of A_i B_j^T behind the MXFP4 calls,
-// one kernel for three kinds of operands, all rows of the reduction:
+// and the 8-bit ones, one kernel for four kinds of operands, all rows of the reduction:
 //   GEMM_FP4   both sides MXFP4 codes with their scales (32 x 32 x 64 scaled products);
 //   GEMM_BF16, GEMM_F16   both sides 16-bit numbers (32 x 32 x 16 products);
 //   GEMM_MIX   A bfloat16, B MXFP4 codes, turned into bfloat16 in registers;
@@ -7,12 +7,14 @@
 //              relative to its largest scale, the power of two goes to the result's column.  36
 //              binades below that scale are exact in binary16; a tile with a number further down
 //              (which the rows' pass over the scales finds) splits A into two bfloat16 pieces
-//              instead, in registers, at half the rate.
+//              instead, in registers, at half the rate;
+//   GEMM_I8    both sides 8-bit integers (32 x 32 x 32 products, sums in 32-bit integers), a scale for
+//              each row of A and of B, which the result takes.
 // The operands of one instruction are 16 bytes a lane in every kind, and it takes as long (32
 // cycles of a SIMD at the full rate), so the kinds share tiles, staging and schedule.
 //
 // A workgroup computes BM x BN outputs, WM x WN wavefronts TM x TN tiles of 32 x 32 each.  A step
-// is 128 bytes of every row of A (256 codes or 64 16-bit numbers) and as much of the reduction of
+// is 128 bytes of every row of A (256 codes, 128 8-bit or 64 16-bit numbers) and as much of the reduction of
 // B.  Steps go into a ring of S LDS buffers by direct loads (no registers in between), S - 1 steps
 // ahead of the products; one barrier a step.  Chunk c (16 bytes) of row r lies at position
 // c ^ (r / 2 mod 8) of its row: 16 neighbouring rows' chunks c lie in 16 different groups of four of
@@ -29,12 +31,14 @@
 // (4096 x 4096 by 256 rows: MIX 22 us, FP4 12, where bytes and operations need 6 and 2).
 #pragma once
 
+#include <type_traits>
+
 #include "mcf_internal.hpp"
 #include "mx4.hpp"
 
 namespace mcf {
 
-enum GemmKind { GEMM_FP4 = 0, GEMM_BF16 = 1, GEMM_F16 = 2, GEMM_MIX = 3, GEMM_MIXH = 4 };
+enum GemmKind { GEMM_FP4 = 0, GEMM_BF16 = 1, GEMM_F16 = 2, GEMM_MIX = 3, GEMM_MIXH = 4, GEMM_I8 = 5 };
 
 struct GemmArgs {
   const char *a, *b;              // pieces' planes of rows
@@ -44,9 +48,10 @@ struct GemmArgs {
   int64_t groups;
   const uint8_t *top, *wide;      // MIXH: the largest scale of each row of B, and for every 64 rows
                                   // whether a number lies too far below it
+  const float *sa, *sb;           // I8: the scales of A's and B's rows
   void *c;                        // [M][N]
   const void *bias;               // [N] or null
-  float *partial;                 // [slices][M][N], with more than one slice
+  float *partial;                 // [slices][M][N], with more than one slice; I8: 32-bit integers
   int64_t M, N;
   int steps, total, slices;       // steps of a pair, of all pairs; slices of the reduction
   int pairs;                      // at most 16
@@ -93,11 +98,6 @@ __device__ inline void gemm_tile(uint32_t id, uint32_t gm, uint32_t gn, uint32_t
   *tn = in / rows;
 }
 
-template <bool B>
-struct Flag {
-  static constexpr bool value = B;
-};
-
 // A wavefront's tiles to `to`, its first element in the M x N result; `rows` and `cols` are what is
 // left of the result there.  Lane (r, g) holds column r of a tile, rows 8 (e / 4) + 4 g + e mod 4.
 // A row's start is scalar arithmetic, the lane's part a 32-bit offset.  SHIFT: the columns' powers
@@ -124,6 +124,46 @@ __device__ inline void gemm_store(const f32x16 (&acc)[TM][TN], T *to, const T *b
       }
   };
   // apart, so that a whole tile's stores carry no tests (15 us of the 8192 x 8192 result)
+  if (rows >= 32 * TM && cols >= 32 * TN)
+    store(Flag<true>());
+  else
+    store(Flag<false>());
+}
+
+// The same of integer sums.  WHOLE: the sums themselves, of a slice; else (sum sa) sb + bias, in binary32.
+template <typename T, bool WHOLE, int TM, int TN>
+__device__ inline void gemm_store_i8(const i32x16 (&acc)[TM][TN], T *to, const T *bias, const float *sa, const float *sb,
+                                     int64_t ld, int rows, int cols) {
+  if (rows <= 0 || cols <= 0) return;  // the scales end there too
+  const int lane = threadIdx.x & 63, r = lane & 31, g = lane >> 5;
+  const uint32_t off = (uint32_t)(4 * g * ld + r);
+  float col[TN], add[TN];
+#pragma unroll
+  for (int j = 0; j < TN; ++j) {
+    const bool in = j * 32 + r < cols;
+    col[j] = !WHOLE && in ? sb[j * 32 + r] : 0.0f;
+    add[j] = !WHOLE && in && bias ? (float)bias[j * 32 + r] : 0.0f;
+  }
+  const auto store = [&](auto whole) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int m = i * 32 + (e >> 2) * 8 + (e & 3);
+        T *row = to + m * ld;
+        const float scale = WHOLE ? 0.0f : sa[m + 4 * g < rows ? m + 4 * g : 0];
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+          if (decltype(whole)::value || (m + 4 * g < rows && j * 32 + r < cols)) {
+            if constexpr (WHOLE) {
+              row[off + j * 32] = acc[i][j][e];
+            } else {
+              const float v = (float)acc[i][j][e] * scale * col[j];
+              row[off + j * 32] = (T)(bias ? v + add[j] : v);
+            }
+          }
+      }
+  };
   if (rows >= 32 * TM && cols >= 32 * TN)
     store(Flag<true>());
   else
@@ -254,13 +294,14 @@ __device__ __forceinline__ void gemm_body(const GemmArgs &a, char *lds, uint32_t
     }
   };
 
-  f32x16 acc[TM][TN];
+  using Acc = std::conditional_t<KIND == GEMM_I8, i32x16, f32x16>;
+  Acc acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < TN; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.0f;
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0;
 
   const int r = lane & 31, g = lane >> 5, wm = (wave / WN) * TM * 32, wn = (wave % WN) * TN * 32;
   // The operands of quarter q of a step, of which a lane holds chunk 4 g + q (16-bit kinds) or
@@ -337,8 +378,10 @@ __device__ __forceinline__ void gemm_body(const GemmArgs &a, char *lds, uint32_t
         mx_cut8<_Float16, 2>(__builtin_bit_cast(Raw8<_Float16>, o.a[i]), piece);
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        f32x16 &c = acc[i][j];
-        if constexpr (KIND == GEMM_FP4) {
+        Acc &c = acc[i][j];
+        if constexpr (KIND == GEMM_I8) {
+          c = __builtin_amdgcn_mfma_i32_32x32x32_i8(__builtin_bit_cast(i32x4, o.a[i]), __builtin_bit_cast(i32x4, fb[j]), c, 0, 0, 0);
+        } else if constexpr (KIND == GEMM_FP4) {
           const i32x8 x = widen(o.a[i]), y = widen(fb[j]);
           const int sa = (int)sc.a[q >> 1][i], sb = (int)sc.b[q >> 1][j];
           if ((q & 1) == 0)
@@ -426,7 +469,15 @@ __device__ __forceinline__ void gemm_body(const GemmArgs &a, char *lds, uint32_t
 #pragma unroll
     for (int j = 0; j < TN; ++j) shift_of[j] = 0;
   }
-  if (a.slices > 1)
+  if constexpr (KIND == GEMM_I8) {
+    if (a.slices > 1)
+      gemm_store_i8<int, true, TM, TN>(acc, reinterpret_cast<int *>(a.partial) + slice * a.M * a.N + at, nullptr, nullptr,
+                                       nullptr, a.N, (int)la - wm, (int)lb - wn);
+    else
+      gemm_store_i8<T, false, TM, TN>(acc, reinterpret_cast<T *>(a.c) + at,
+                                      a.bias ? reinterpret_cast<const T *>(a.bias) + n0 + wn : nullptr, a.sa + m0 + wm,
+                                      a.sb + n0 + wn, a.N, (int)la - wm, (int)lb - wn);
+  } else if (a.slices > 1)
     gemm_store<float, SHIFT, TM, TN>(acc, a.partial + slice * a.M * a.N + at, nullptr, shift_of, a.N, (int)la - wm,
                                      (int)lb - wn);
   else
@@ -472,6 +523,26 @@ __global__ __launch_bounds__(256) void mx_gemm_sum_kernel(GemmArgs a) {
   // n stays below 2^26 with more than one slice
   if (a.bias) v += (float)reinterpret_cast<const T *>(a.bias)[(uint32_t)i % (uint32_t)a.N];
   reinterpret_cast<T *>(a.c)[i] = (T)v;
+}
+
+// The same of integer sums.
+template <typename T>
+__global__ __launch_bounds__(256) void int8_gemm_sum_kernel(GemmArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = a.M * a.N;
+  if (i >= n) return;
+  const int *partial = reinterpret_cast<const int *>(a.partial);
+  int v = 0;
+  for (int s0 = 0; s0 < a.slices; s0 += 8) {
+    int p[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) p[u] = s0 + u < a.slices ? partial[(s0 + u) * n + i] : 0;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v += p[u];
+  }
+  const uint32_t row = (uint32_t)i / (uint32_t)a.N, col = (uint32_t)i - row * (uint32_t)a.N;
+  float f = (float)v * a.sa[row] * a.sb[col];
+  if (a.bias) f += (float)reinterpret_cast<const T *>(a.bias)[col];
+  reinterpret_cast<T *>(a.c)[i] = (T)f;
 }
 
 // src [rows][cols] -> dst [P][rows][ld], zeros from cols to ld: the pieces of binary32, 16-bit numbers as
@@ -630,7 +701,11 @@ hipError_t gemm(GemmArgs &a, const GemmPlan &p, hipStream_t stream) {
     mx_gemm_kernel<KIND, T, 2, 2, 2, 2, 2><<<grid, 256, 0, stream>>>(a);
   else
     mx_gemm_kernel<KIND, T, 2, 2, 1, 1, 4><<<grid, 256, 0, stream>>>(a);
-  gemm_sum<T>(a, stream);
+  if constexpr (KIND == GEMM_I8) {
+    if (a.slices > 1) int8_gemm_sum_kernel<T><<<(unsigned)((a.M * a.N + 255) / 256), 256, 0, stream>>>(a);
+  } else {
+    gemm_sum<T>(a, stream);
+  }
   return hipGetLastError();
 }
 
