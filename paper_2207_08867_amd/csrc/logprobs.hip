@@ -18,6 +18,7 @@
 
 #include "mcf_internal.hpp"
 #include "mx4.hpp"
+#include "wave.hpp"
 
 namespace mcf {
 namespace {
@@ -70,9 +71,6 @@ __device__ inline float key_value(uint64_t k) {
 }
 __device__ inline int32_t key_index(uint64_t k) { return (int32_t)~(uint32_t)k; }
 
-__device__ inline uint64_t max64(uint64_t x, uint64_t y) { return x > y ? x : y; }
-__device__ inline uint64_t shfl64(uint64_t v, int d) { return (uint64_t)__shfl_xor((unsigned long long)v, d); }
-
 constexpr int GROUPS = 256;  // of the threads, for the alternatives; above LOGP_TOP
 constexpr int KEEP = 1024;   // candidates
 
@@ -80,77 +78,88 @@ struct Select {
   uint64_t group[GROUPS];
   uint64_t kept[KEEP];
   uint64_t bound;
-  int rank[GROUPS];
   int n;
 };
 
-// The k largest of the workgroup's keys, which are all different (but for 0).  each(f) calls f on every key of
-// the thread, own is its largest.  The k-th largest of 256 groups' largest keys bounds the k-th largest
-// key from below; the keys at or above it, k and a few more as a rule, are ranked by counting.
+// The largest b of the form "some leading bits, then zeros" that at least k keys reach, 1 where fewer
+// are there.  count(b) tells how many reach b.  It ends as soon as the keys that reach b are few.
+template <typename Count>
+__device__ inline uint64_t bound_of(int k, int few, Count count) {
+  uint64_t b = 0;
+  for (int bit = 63; bit >= 0; --bit) {
+    const uint64_t next = b | (uint64_t)1 << bit;
+    const int n = count(next);
+    if (n < k) continue;
+    b = next;
+    if (n <= few) break;
+  }
+  return b ? b : 1;
+}
+
+// The k largest of the workgroup's keys, which are all different (but for 0).  own is the thread's largest
+// key; each(b, f) calls f on every key of the thread that reaches b.  A bound that at least k of 256 groups'
+// largest keys reach, found by bisection over its bits in one wavefront, bounds the k-th largest key
+// from below; the keys that reach it, k and a few more as a rule, are ranked by counting.
 // out(r, key) takes the r-th largest, 0 where there is none.
 template <int NT, typename Each, typename Out>
 __device__ inline void select_top(Select &sh, int k, uint64_t own, Each each, Out out) {
   constexpr int PER = NT / GROUPS;
   static_assert(PER >= 1 && NT % GROUPS == 0 && GROUPS > LOGP_TOP, "a group has whole threads");
   const int t = threadIdx.x;
-  uint64_t big = own;
+  const uint64_t big = lanes_max<PER>(own);
+  if (t % PER == 0) sh.group[t / PER] = big;
+  if (t == 0) sh.n = 0;
+  __syncthreads();
+  if (t < 64) {
+    uint64_t g[GROUPS / 64];
 #pragma unroll
-  for (int d = 1; d < PER; d <<= 1) big = max64(big, shfl64(big, d));
-  if (t % PER == 0) sh.group[t / PER] = big, sh.rank[t / PER] = 0;
-  if (t == 0) sh.bound = 1, sh.n = 0;
-  __syncthreads();
-  {
-    const uint64_t mine = sh.group[t % GROUPS];
-    const int from = t / GROUPS * (GROUPS / PER);
-    int above = 0;
-#pragma unroll 16
-    for (int j = 0; j < GROUPS / PER; ++j) above += sh.group[from + j] > mine;
-    atomicAdd(&sh.rank[t % GROUPS], above);
-  }
-  __syncthreads();
-  if (t < GROUPS && sh.rank[t] == k - 1 && sh.group[t] != 0) sh.bound = sh.group[t];
-  __syncthreads();
-  const uint64_t bound = sh.bound;
-  if (own >= bound)
-    each([&](uint64_t key) {
-      if (key >= bound) {
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < KEEP) sh.kept[at] = key;
-      }
+    for (int i = 0; i < GROUPS / 64; ++i) g[i] = sh.group[t + 64 * i];
+    const uint64_t b = bound_of(k, k + k / 8, [&](uint64_t b) {
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < GROUPS / 64; ++i) n += __popcll(__ballot(g[i] >= b));
+      return n;
     });
+    if (t == 0) sh.bound = b;
+  }
   __syncthreads();
-  const int n = sh.n;
-  if (n <= KEEP) {
-    for (int i = t; i < n; i += NT) {
-      const uint64_t mine = sh.kept[i];
-      int above = 0;
+  uint64_t bound = sh.bound;
+  const auto collect = [&](uint64_t key) {
+    const int at = atomicAdd(&sh.n, 1);
+    if (at < KEEP) sh.kept[at] = key;
+  };
+  if (own >= bound) each(bound, collect);
+  __syncthreads();
+  int n = sh.n;
+  if (n > KEEP) {
+    // rows whose order follows the threads': the same bisection over all keys
+    bound = bound_of(k, KEEP, [&](uint64_t b) {
+      int c = 0;
+      if (own >= b) each(b, [&](uint64_t) { ++c; });
+      c = (int)lanes_sum((uint32_t)c);
+      __syncthreads();
+      if ((t & 63) == 0) sh.group[t >> 6] = (uint64_t)c;
+      __syncthreads();
+      c = 0;
+#pragma unroll
+      for (int w = 0; w < NT / 64; ++w) c += (int)sh.group[w];
+      return c;
+    });
+    __syncthreads();
+    if (t == 0) sh.n = 0;
+    __syncthreads();
+    if (own >= bound) each(bound, collect);
+    __syncthreads();
+    n = sh.n;
+  }
+  for (int i = t; i < n; i += NT) {
+    const uint64_t mine = sh.kept[i];
+    int above = 0;
 #pragma unroll 8
-      for (int j = 0; j < n; ++j) above += sh.kept[j] > mine;
-      if (above < k) out(above, mine);
-    }
-    for (int r = n + t; r < k; r += NT) out(r, (uint64_t)0);
-    return;
+    for (int j = 0; j < n; ++j) above += sh.kept[j] > mine;
+    if (above < k) out(above, mine);
   }
-  // rows whose order follows the threads': one by one
-  uint64_t last = ~(uint64_t)0;
-  for (int r = 0; r < k; ++r) {
-    uint64_t best = 0;
-    if (own < last) best = own;
-    else
-      each([&](uint64_t key) {
-        if (key < last) best = max64(best, key);
-      });
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) best = max64(best, shfl64(best, d));
-    __syncthreads();
-    if ((t & 63) == 0) sh.group[t >> 6] = best;
-    __syncthreads();
-    best = sh.group[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) best = max64(best, sh.group[w]);
-    if (t == 0) out(r, best);
-    last = best;
-  }
+  for (int r = n + t; r < k; r += NT) out(r, (uint64_t)0);
 }
 
 template <typename T, bool ONE>
@@ -163,10 +172,10 @@ __device__ inline float logit(const LogpArgs &a, const T *z, int64_t j) {
 
 // Eight logits from column col of a row, as they are held: plain ones in their format.  Past the row
 // they are -inf.
-template <typename T, bool ONE>
+template <typename T, bool ONE, bool WHOLE = false>
 __device__ inline Raw8<std::conditional_t<ONE, T, float>> logits8(const LogpArgs &a, const T *z, int64_t col) {
   using H = std::conditional_t<ONE, T, float>;
-  const int64_t left = a.vocab - col;
+  const int64_t left = WHOLE ? 8 : a.vocab - col;
   Raw8<H> r;
   if constexpr (ONE) {
     r = load8_tail(z + col, left);
@@ -228,20 +237,24 @@ __device__ inline void put_top(const LogpArgs &a, int64_t row, const Row &r, int
   a.top_logp[row * a.top + i] = some ? log_prob(a, r, key_value(key)) : (r.bad ? NAN : -INFINITY);
 }
 
-__device__ inline float wave_max(float v) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v = fmaxf(v, __shfl_xor(v, d));
-  return v;
-}
-__device__ inline float wave_add(float v) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-  return v;
+// The held elements as another value, so that the compiler works out again what follows from them (16-bit
+// ones in 32 bits, keys of all elements) instead of holding it.
+template <typename T>
+__device__ inline Raw8<T> renewed(const Raw8<T> &r) {
+  u32x4 u[sizeof(T) / 2];
+  __builtin_memcpy(&u, &r, sizeof(u));
+  if constexpr (sizeof(T) == 2)
+    asm volatile("" : "+v"(u[0]));
+  else
+    asm volatile("" : "+v"(u[0]), "+v"(u[1]));
+  Raw8<T> o;
+  __builtin_memcpy(&o, &u, sizeof(u));
+  return o;
 }
 
 // A chunk of NT CH pieces of 8 logits of a row, in registers; SPLIT: of several, which the kernel below joins.
-template <typename T, bool ONE, int NT, int CH, bool TOP, bool SPLIT>
-__global__ __launch_bounds__(NT) void logp_kernel(LogpArgs a) {
+template <typename T, bool ONE, int NT, int CH, bool TOP, bool SPLIT, int OCC>
+__global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
   using H = std::conditional_t<ONE, T, float>;
   constexpr int W = NT / 64;
   __shared__ float mx[W];
@@ -252,21 +265,26 @@ __global__ __launch_bounds__(NT) void logp_kernel(LogpArgs a) {
   const T *z = reinterpret_cast<const T *>(a.z) + row * a.vocab;
   Raw8<H> v[CH];
   float own = -FLT_MAX;
+  if (lo + (int64_t)(NT * CH * 8) <= a.vocab) {
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    const int64_t col = lo + (int64_t)(c * NT + (int)threadIdx.x) * 8;
-    if (col < a.vocab) {
-      v[c] = logits8<T, ONE>(a, z, col);
-    } else {
+    for (int c = 0; c < CH; ++c) v[c] = logits8<T, ONE, true>(a, z, lo + (c * NT + threadIdx.x) * 8);
+  } else {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[c].v[i] = (H)-INFINITY;
+    for (int c = 0; c < CH; ++c) {
+      const int64_t col = lo + (int64_t)(c * NT + (int)threadIdx.x) * 8;
+      if (col < a.vocab) {
+        v[c] = logits8<T, ONE>(a, z, col);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[c].v[i] = (H)-INFINITY;
+      }
     }
   }
 #pragma unroll
   for (int c = 0; c < CH; ++c)
 #pragma unroll
     for (int i = 0; i < 8; ++i) own = fmaxf(own, (float)v[c].v[i]);
-  float m = wave_max(own);
+  float m = lanes_max(own);
   if ((threadIdx.x & 63) == 0) mx[threadIdx.x >> 6] = m;
   __syncthreads();
   m = mx[0];
@@ -274,28 +292,35 @@ __global__ __launch_bounds__(NT) void logp_kernel(LogpArgs a) {
   for (int w = 1; w < W; ++w) m = fmaxf(m, mx[w]);
   float s = 0.0f, d1 = 0.0f, equal = 0.0f;
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
+  for (int c = 0; c < CH; ++c) {
+    const Raw8<H> u = renewed(v[c]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float d = m - (float)v[c].v[i], e = expd(a, d);
+      const float d = m - (float)u.v[i], e = expd(a, d);
       s += e;
       d1 += e * fminf(d, FLT_MAX);
     }
+    // here, or the compiler keeps d and e of every element for a later sum
+    asm volatile("" : "+v"(s), "+v"(d1));
+  }
   if (own == m) {
     // a thread with a largest logit sums the others alone
     s = 0.0f;
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < CH; ++c) {
+      const Raw8<H> u = renewed(v[c]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const float x = (float)v[c].v[i];
+        const float x = (float)u.v[i];
         equal += x == m ? 1.0f : 0.0f;
         s += x == m ? 0.0f : expd(a, m - x);
       }
+      asm volatile("" : "+v"(s), "+v"(equal));
+    }
   }
-  s = wave_add(s);
-  d1 = wave_add(d1);
-  equal = wave_add(equal);
+  s = lanes_sum(s);
+  d1 = lanes_sum(d1);
+  equal = lanes_sum(equal);
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = Part{equal, s, d1};
   __syncthreads();
   equal = sums[0].m, s = sums[0].s, d1 = sums[0].a;
@@ -311,23 +336,32 @@ __global__ __launch_bounds__(NT) void logp_kernel(LogpArgs a) {
     a.parts[row * a.chunks + chunk] = part;
   }
   if constexpr (TOP) {
-    const auto each = [&](auto f) {
+    const uint32_t first = lo + threadIdx.x * 8;
+    const auto each = [&](uint64_t bound, auto f) {
+      const float least = bound == 1 ? -FLT_MAX : key_value(bound);
 #pragma unroll
-      for (int c = 0; c < CH; ++c)
+      for (int c = 0; c < CH; ++c) {
+        const Raw8<H> u = renewed(v[c]);
+        uint32_t from = first + c * NT * 8;
+        asm volatile("" : "+v"(from));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f(key_of((float)v[c].v[i], lo + (c * NT + threadIdx.x) * 8 + i));
+        for (int i = 0; i < 8; ++i)
+          if ((float)u.v[i] >= least) {
+            const uint64_t key = key_of((float)u.v[i], from + i);
+            if (key >= bound) f(key);
+          }
+      }
     };
-    // the thread's first logit equal to its largest
-    uint32_t at = 0;
+    // the thread's first logit equal to its largest; none where all are -inf
+    uint32_t at = ~0u;
 #pragma unroll
-    for (int c = CH - 1; c >= 0; --c)
+    for (int c = CH - 1; c >= 0; --c) {
+      const Raw8<H> u = renewed(v[c]);
 #pragma unroll
-      for (int i = 7; i >= 0; --i) at = (float)v[c].v[i] == own ? (c * NT * 8 + i) : at;
-    uint64_t mine = key_of(own, lo + threadIdx.x * 8 + at);
-    if (own == -FLT_MAX) {  // perhaps of no logit
-      mine = 0;
-      each([&](uint64_t key) { mine = max64(mine, key); });
+      for (int i = 7; i >= 0; --i) at = (float)u.v[i] == own ? c * NT * 8 + i : at;
+      asm volatile("" : "+v"(at));
     }
+    const uint64_t mine = at != ~0u ? key_of(own, first + at) : 0;
     select_top<NT>(sel, a.top, mine, each, [&](int i, uint64_t key) {
       if constexpr (SPLIT)
         a.keys[(row * a.chunks + chunk) * a.top + i] = key;
@@ -361,11 +395,14 @@ __global__ __launch_bounds__(256) void logp_join_kernel(LogpArgs a) {
   if constexpr (TOP) {
     const int64_t n = (int64_t)a.chunks * a.top;
     const uint64_t *keys = a.keys + row * n;
-    const auto each = [&](auto f) {
-      for (int64_t i = threadIdx.x; i < n; i += 256) f(keys[i]);
+    const auto each = [&](uint64_t bound, auto f) {
+      for (int64_t i = threadIdx.x; i < n; i += 256) {
+        const uint64_t key = keys[i];
+        if (key >= bound) f(key);
+      }
     };
     uint64_t mine = 0;
-    each([&](uint64_t key) { mine = max64(mine, key); });
+    each(0, [&](uint64_t key) { mine = key > mine ? key : mine; });
     select_top<256>(sel, a.top, mine, each, [&](int i, uint64_t key) { put_top(a, row, r, i, key); });
   }
 }
@@ -384,21 +421,22 @@ hipError_t run_fwd(LogpArgs a, hipStream_t stream) {
   for (a.first = 0; a.first < a.rows; a.first += most) {
     const int64_t rows = a.rows - a.first < most ? a.rows - a.first : most;
     const unsigned grid = (unsigned)(rows * a.chunks);
-#define ROW(NT, CH, SPLIT) logp_kernel<T, ONE, NT, CH, TOP, SPLIT><<<grid, NT, 0, stream>>>(a)
+    constexpr bool SHORT = ONE && sizeof(T) == 2;
+#define ROW(NT, CH, SPLIT, OCC) logp_kernel<T, ONE, NT, CH, TOP, SPLIT, OCC><<<grid, NT, 0, stream>>>(a)
     if (chunk == FEW)
-      ROW(256, 2, true);
+      ROW(256, 2, true, 8);
     else if (chunk == LONG)
-      ROW(512, 8, true);
+      ROW(512, 8, true, SHORT ? 8 : 4);
     else if (a.vocab <= 2048)
-      ROW(256, 1, false);
+      ROW(256, 1, false, 8);
     else if (a.vocab <= 4096)
-      ROW(256, 2, false);
+      ROW(256, 2, false, 8);
     else if (a.vocab <= 8192)
-      ROW(256, 4, false);
+      ROW(256, 4, false, SHORT ? 8 : 6);
     else if (a.vocab <= 16384)
-      ROW(512, 4, false);
+      ROW(512, 4, false, SHORT ? 8 : 6);
     else
-      ROW(512, 8, false);
+      ROW(512, 8, false, SHORT ? 8 : 4);
 #undef ROW
     if (chunk) logp_join_kernel<T, ONE, TOP><<<(unsigned)rows, 256, 0, stream>>>(a);
   }
