@@ -59,16 +59,17 @@ __device__ inline Part join(const LogpArgs &a, const Part &x, const Part &y) {
   return Part{hi.m, hi.s + n * f, hi.a + (lo.a + (f == 0.0f ? 0.0f : d) * n) * f};
 }
 
-// A logit's place in the order as one number: larger means earlier; 0 stands for none.
-__device__ inline uint64_t key_of(float v, uint32_t j) {
-  if (!(v > -INFINITY)) return 0;
+// Logits in the order of integers, and back.
+__device__ inline uint32_t ordered(float v) {
   const uint32_t u = __builtin_bit_cast(uint32_t, v + 0.0f);  // -0 is +0
-  return (uint64_t)(u ^ ((int32_t)u < 0 ? 0xffffffffu : 0x80000000u)) << 32 | (uint32_t)~j;
+  return u ^ ((int32_t)u < 0 ? 0xffffffffu : 0x80000000u);
 }
-__device__ inline float key_value(uint64_t k) {
-  const uint32_t u = (uint32_t)(k >> 32);
+__device__ inline float ordered_value(uint32_t u) {
   return __builtin_bit_cast(float, u ^ ((int32_t)u < 0 ? 0x80000000u : 0xffffffffu));
 }
+// A logit's place in the order of the alternatives as one number: larger means earlier; 0 stands for none.
+__device__ inline uint64_t key_of(float v, uint32_t j) { return (uint64_t)ordered(v) << 32 | (uint32_t)~j; }
+__device__ inline float key_value(uint64_t k) { return ordered_value((uint32_t)(k >> 32)); }
 __device__ inline int32_t key_index(uint64_t k) { return (int32_t)~(uint32_t)k; }
 
 constexpr int GROUPS = 256;  // of the threads, for the alternatives; above LOGP_TOP
@@ -78,88 +79,101 @@ struct Select {
   uint64_t group[GROUPS];
   uint64_t kept[KEEP];
   uint64_t bound;
-  int n;
+  int n, wave[16];
 };
 
-// The largest b of the form "some leading bits, then zeros" that at least k keys reach, 1 where fewer
-// are there.  count(b) tells how many reach b.  It ends as soon as the keys that reach b are few.
-template <typename Count>
-__device__ inline uint64_t bound_of(int k, int few, Count count) {
-  uint64_t b = 0;
-  for (int bit = 63; bit >= 0; --bit) {
-    const uint64_t next = b | (uint64_t)1 << bit;
-    const int n = count(next);
+// The largest b of the form "some leading bits, then zeros" that at least k numbers reach, 0 where fewer
+// are there.  count(b) tells how many reach b.  It ends as soon as the numbers that reach b are few.
+template <typename U, typename Count>
+__device__ inline U bound_of(int k, int few, Count count) {
+  U b = 0;
+#pragma unroll 1
+  for (U bit = (U)1 << (8 * sizeof(U) - 1); bit; bit >>= 1) {
+    const int n = count(b | bit);
     if (n < k) continue;
-    b = next;
+    b |= bit;
     if (n <= few) break;
   }
-  return b ? b : 1;
+  return b;
 }
 
-// The k largest of the workgroup's keys, which are all different (but for 0).  own is the thread's largest
-// key; each(b, f) calls f on every key of the thread that reaches b.  A bound that at least k of 256 groups'
-// largest keys reach, found by bisection over its bits in one wavefront, bounds the k-th largest key
-// from below; the keys that reach it, k and a few more as a rule, are ranked by counting.
-// out(r, key) takes the r-th largest, 0 where there is none.
-template <int NT, typename Each, typename Out>
-__device__ inline void select_top(Select &sh, int k, uint64_t own, Each each, Out out) {
-  constexpr int PER = NT / GROUPS;
-  static_assert(PER >= 1 && NT % GROUPS == 0 && GROUPS > LOGP_TOP, "a group has whole threads");
-  const int t = threadIdx.x;
-  const uint64_t big = lanes_max<PER>(own);
-  if (t % PER == 0) sh.group[t / PER] = big;
-  if (t == 0) sh.n = 0;
+// The same of the 256 groups' numbers in sh.group, by one wavefront, for all.
+template <typename U>
+__device__ inline U bound_of_groups(Select &sh, int k) {
   __syncthreads();
-  if (t < 64) {
-    uint64_t g[GROUPS / 64];
+  if (threadIdx.x < 64) {
+    U g[GROUPS / 64];
 #pragma unroll
-    for (int i = 0; i < GROUPS / 64; ++i) g[i] = sh.group[t + 64 * i];
-    const uint64_t b = bound_of(k, k + k / 8, [&](uint64_t b) {
+    for (int i = 0; i < GROUPS / 64; ++i) g[i] = (U)sh.group[threadIdx.x + 64 * i];
+    const U b = bound_of<U>(k, k + k / 8, [&](U b) {
       int n = 0;
 #pragma unroll
       for (int i = 0; i < GROUPS / 64; ++i) n += __popcll(__ballot(g[i] >= b));
       return n;
     });
-    if (t == 0) sh.bound = b;
+    if (threadIdx.x == 0) sh.bound = b, sh.n = 0;
   }
   __syncthreads();
-  uint64_t bound = sh.bound;
-  const auto collect = [&](uint64_t key) {
-    const int at = atomicAdd(&sh.n, 1);
-    if (at < KEEP) sh.kept[at] = key;
-  };
-  if (own >= bound) each(bound, collect);
-  __syncthreads();
-  int n = sh.n;
-  if (n > KEEP) {
-    // rows whose order follows the threads': the same bisection over all keys
-    bound = bound_of(k, KEEP, [&](uint64_t b) {
-      int c = 0;
-      if (own >= b) each(b, [&](uint64_t) { ++c; });
-      c = (int)lanes_sum((uint32_t)c);
-      __syncthreads();
-      if ((t & 63) == 0) sh.group[t >> 6] = (uint64_t)c;
-      __syncthreads();
-      c = 0;
-#pragma unroll
-      for (int w = 0; w < NT / 64; ++w) c += (int)sh.group[w];
-      return c;
-    });
-    __syncthreads();
-    if (t == 0) sh.n = 0;
-    __syncthreads();
-    if (own >= bound) each(bound, collect);
-    __syncthreads();
-    n = sh.n;
-  }
-  for (int i = t; i < n; i += NT) {
+  return (U)sh.bound;
+}
+
+// out(r, key) takes the r-th largest of the n <= KEEP kept keys, r < k, and 0 where there is none: ranks by
+// counting.
+template <int NT, typename Out>
+__device__ inline void rank_kept(const Select &sh, int k, int n, Out out) {
+  for (int i = threadIdx.x; i < n; i += NT) {
     const uint64_t mine = sh.kept[i];
     int above = 0;
 #pragma unroll 8
     for (int j = 0; j < n; ++j) above += sh.kept[j] > mine;
     if (above < k) out(above, mine);
   }
-  for (int r = n + t; r < k; r += NT) out(r, (uint64_t)0);
+  for (int r = n + (int)threadIdx.x; r < k; r += NT) out(r, (uint64_t)0);
+}
+
+// The sum of the workgroup's wavefronts' numbers.
+template <int NT>
+__device__ inline int waves_sum(Select &sh, int n) {
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sh.wave[threadIdx.x >> 6] = n;
+  __syncthreads();
+  n = 0;
+#pragma unroll
+  for (int w = 0; w < NT / 64; ++w) n += sh.wave[w];
+  return n;
+}
+
+// The k largest of a list of keys, which are all different (but for 0): by a bound that at least k of 256
+// groups' largest keys reach, which so bounds the k-th largest key from below.  More than KEEP keys at or
+// above it: the same bisection over all keys.
+template <int NT, typename Out>
+__device__ inline void select_keys(Select &sh, int k, const uint64_t *keys, int64_t n, Out out) {
+  static_assert(NT == GROUPS, "a group is a thread's keys");
+  uint64_t own = 0;
+  for (int64_t i = threadIdx.x; i < n; i += NT) own = keys[i] > own ? keys[i] : own;
+  sh.group[threadIdx.x] = own;
+  uint64_t bound = bound_of_groups<uint64_t>(sh, k);
+  int kept;
+  for (int pass = 0;; ++pass) {
+    if (bound == 0) bound = 1;
+    if (own >= bound)
+      for (int64_t i = threadIdx.x; i < n; i += NT)
+        if (keys[i] >= bound) {
+          const int at = atomicAdd(&sh.n, 1);
+          if (at < KEEP) sh.kept[at] = keys[i];
+        }
+    __syncthreads();
+    kept = sh.n;
+    if (kept <= KEEP || pass == 1) break;
+    bound = bound_of<uint64_t>(k, KEEP, [&](uint64_t b) {
+      uint32_t c = 0;
+      for (int64_t i = threadIdx.x; i < n; i += NT) c += keys[i] >= b;
+      return waves_sum<NT>(sh, (int)lanes_sum(c));
+    });
+    if (threadIdx.x == 0) sh.n = 0;
+    __syncthreads();
+  }
+  rank_kept<NT>(sh, k, kept, out);
 }
 
 template <typename T, bool ONE>
@@ -237,6 +251,12 @@ __device__ inline void put_top(const LogpArgs &a, int64_t row, const Row &r, int
   a.top_logp[row * a.top + i] = some ? log_prob(a, r, key_value(key)) : (r.bad ? NAN : -INFINITY);
 }
 
+// A wavefront's sums: all exp(-d / T) relative to its largest logit, or, of one with the row's largest, those of the
+// others and the number of largest ones.
+struct Wave {
+  float m, s, a, equal;
+};
+
 // The held elements as another value, so that the compiler works out again what follows from them (16-bit
 // ones in 32 bits, keys of all elements) instead of holding it.
 template <typename T>
@@ -252,13 +272,106 @@ __device__ inline Raw8<T> renewed(const Raw8<T> &r) {
   return o;
 }
 
+// The k largest of the workgroup's logits by (logit, index), those of -inf apart, where they are held: v, the
+// pieces' largest logits pm and the thread's, own (at least -FLT_MAX); first: the index of the thread's first.
+// A bound that at least k of 256 groups' largest logits reach bounds the k-th largest logit from
+// below; the logits that reach it, k and a few more as a rule, are ranked.
+template <int NT, int CH, typename H, typename Out>
+__device__ inline void select_logits(Select &sh, int k, const Raw8<H> (&v)[CH], const float (&pm)[CH], float own,
+                                     uint32_t first, Out out) {
+  constexpr int PER = NT / GROUPS;
+  static_assert(PER >= 1 && NT % GROUPS == 0 && GROUPS > LOGP_TOP, "a group has whole threads");
+  const float big = lanes_max<PER>(own);
+  if (threadIdx.x % PER == 0) sh.group[threadIdx.x / PER] = ordered(big);
+  const uint32_t b = bound_of_groups<uint32_t>(sh, k);
+  const uint32_t lowest = ordered(-FLT_MAX);
+  float bound = ordered_value(b < lowest ? lowest : b);
+  // each(test, f): f(mask of the lanes whose element passes, the element, its index), element by element, of
+  // the pieces in which a lane has one at or above `least`
+  const auto each = [&](float least, auto test, auto f) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+      if (__any(pm[c] >= least)) {
+        const Raw8<H> u = renewed(v[c]);
+        uint32_t from = first + c * NT * 8;
+        asm volatile("" : "+v"(from));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f(__ballot(test((float)u.v[i])), (float)u.v[i], from + i);
+      }
+  };
+  const auto count = [&](auto test, float least) {
+    int n = 0;
+    each(least, test, [&](uint64_t lanes, float, uint32_t) { n += __popcll(lanes); });
+    return n;
+  };
+  // keeps the elements that pass
+  const auto keep = [&](auto test, float least) {
+    const int n = count(test, least);
+    int at = 0;
+    if ((threadIdx.x & 63) == 0 && n > 0) at = atomicAdd(&sh.n, n);
+    at = __builtin_amdgcn_readfirstlane(at);
+    if (n > 0)
+      each(least, test, [&](uint64_t lanes, float x, uint32_t j) {
+        if (lanes == 0) return;
+        const int mine = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0));
+        if ((lanes >> (threadIdx.x & 63) & 1) && mine < KEEP) sh.kept[mine] = key_of(x, j);
+        at += __popcll(lanes);
+      });
+    __syncthreads();
+  };
+  keep([&](float x) { return x >= bound; }, bound);
+  int n = sh.n;
+  if (n > KEEP) {
+    // Many equal logits at the bound, or a row whose order follows the threads'.  The k-th largest logit by
+    // bisection over all of them; the larger ones, fewer than k, and the first of those equal to it.
+    const uint32_t e = bound_of<uint32_t>(k, k, [&](uint32_t b) {
+      const float least = ordered_value(b < lowest ? lowest : b);
+      return waves_sum<NT>(sh, count([&](float x) { return x >= least; }, least));
+    });
+    bound = ordered_value(e < lowest ? lowest : e);
+    __syncthreads();
+    if (threadIdx.x == 0) sh.n = 0;
+    __syncthreads();
+    keep([&](float x) { return x > bound; }, bound);
+    n = sh.n;
+    if (n < k) {
+      int need = k - n;
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const Raw8<H> u = renewed(v[c]);
+        int mine = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) mine += (float)u.v[i] == bound;
+        // the equal ones of the lanes before this one, and of the wavefronts before this one
+        int before = mine;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+          const int o = __shfl_up(before, d);
+          before += (int)(threadIdx.x & 63) >= d ? o : 0;
+        }
+        const int all = waves_sum<NT>(sh, __shfl(before, 63));
+        before -= mine;
+        for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) before += sh.wave[w];
+        uint32_t j = first + c * NT * 8;
+#pragma unroll
+        for (int i = 0; i < 8; ++i, ++j)
+          if ((float)u.v[i] == bound && before < need) sh.kept[k - need + before++] = key_of(bound, j);
+        need -= all;
+        if (need <= 0) break;
+      }
+      n = k - (need > 0 ? need : 0);
+      __syncthreads();
+    }
+  }
+  rank_kept<NT>(sh, k, n, out);
+}
+
 // A chunk of NT CH pieces of 8 logits of a row, in registers; SPLIT: of several, which the kernel below joins.
 template <typename T, bool ONE, int NT, int CH, bool TOP, bool SPLIT, int OCC>
 __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
   using H = std::conditional_t<ONE, T, float>;
   constexpr int W = NT / 64;
-  __shared__ float mx[W];
-  __shared__ Part sums[W];
+  __shared__ Wave sums[W];
   __shared__ std::conditional_t<TOP, Select, int> sel;
   const int64_t row = SPLIT ? a.first + blockIdx.x / a.chunks : a.first + blockIdx.x;
   const int chunk = SPLIT ? blockIdx.x % a.chunks : 0, lo = chunk * (NT * CH * 8);
@@ -280,31 +393,39 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
       }
     }
   }
+  float pm[CH];
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
+  for (int c = 0; c < CH; ++c) {
+    pm[c] = (float)v[c].v[0];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) own = fmaxf(own, (float)v[c].v[i]);
-  float m = lanes_max(own);
-  if ((threadIdx.x & 63) == 0) mx[threadIdx.x >> 6] = m;
-  __syncthreads();
-  m = mx[0];
-#pragma unroll
-  for (int w = 1; w < W; ++w) m = fmaxf(m, mx[w]);
-  float s = 0.0f, d1 = 0.0f, equal = 0.0f;
+    for (int i = 1; i < 8; ++i) pm[c] = fmaxf(pm[c], (float)v[c].v[i]);
+    own = fmaxf(own, pm[c]);
+  }
+  // Each wavefront's sums relative to its own largest logit, so that it works on its logits while the others'
+  // are on their way; those with the row's largest then sum the others alone.
+  const float mw = lanes_max(own);
+  float s = 0.0f, d1 = 0.0f;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const Raw8<H> u = renewed(v[c]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float d = m - (float)u.v[i], e = expd(a, d);
+      const float d = mw - (float)u.v[i], e = expd(a, d);
       s += e;
-      d1 += e * fminf(d, FLT_MAX);
+      d1 = fmaf(e, fminf(d, FLT_MAX), d1);
     }
     // here, or the compiler keeps d and e of every element for a later sum
     asm volatile("" : "+v"(s), "+v"(d1));
   }
-  if (own == m) {
-    // a thread with a largest logit sums the others alone
+  s = lanes_sum(s);
+  d1 = lanes_sum(d1);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = Wave{mw, s, d1, 0.0f};
+  __syncthreads();
+  float m = sums[0].m;
+#pragma unroll
+  for (int w = 1; w < W; ++w) m = fmaxf(m, sums[w].m);
+  if (mw == m) {
+    float equal = 0.0f;
     s = 0.0f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -317,17 +438,24 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
       }
       asm volatile("" : "+v"(s), "+v"(equal));
     }
+    s = lanes_sum(s);
+    equal = lanes_sum(equal);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6].s = s, sums[threadIdx.x >> 6].equal = equal;
   }
-  s = lanes_sum(s);
-  d1 = lanes_sum(d1);
-  equal = lanes_sum(equal);
-  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = Part{equal, s, d1};
   __syncthreads();
-  equal = sums[0].m, s = sums[0].s, d1 = sums[0].a;
+  Part part = {m, 0.0f, 0.0f};
+  float equal = 0.0f;
 #pragma unroll
-  for (int w = 1; w < W; ++w) equal += sums[w].m, s += sums[w].s, d1 += sums[w].a;
+  for (int w = 0; w < W; ++w) {
+    const Wave x = sums[w];
+    const float d = m - x.m, f = expd(a, d);  // 1 where the largest is the row's
+    equal += x.equal;
+    part.s += x.s * f;
+    part.a += (x.a + (f == 0.0f ? 0.0f : d) * x.s) * f;
+  }
   // no largest logit: nothing but -inf, or NaN, which s then is
-  const Part part = {m, m == INFINITY ? NAN : (s + (equal - 1.0f)), d1};
+  part.s += equal - 1.0f;
+  if (m == INFINITY) part.s = NAN;
   Row r;
   if constexpr (!SPLIT) {
     r = row_of(a, part);
@@ -336,33 +464,7 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
     a.parts[row * a.chunks + chunk] = part;
   }
   if constexpr (TOP) {
-    const uint32_t first = lo + threadIdx.x * 8;
-    const auto each = [&](uint64_t bound, auto f) {
-      const float least = bound == 1 ? -FLT_MAX : key_value(bound);
-#pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        const Raw8<H> u = renewed(v[c]);
-        uint32_t from = first + c * NT * 8;
-        asm volatile("" : "+v"(from));
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if ((float)u.v[i] >= least) {
-            const uint64_t key = key_of((float)u.v[i], from + i);
-            if (key >= bound) f(key);
-          }
-      }
-    };
-    // the thread's first logit equal to its largest; none where all are -inf
-    uint32_t at = ~0u;
-#pragma unroll
-    for (int c = CH - 1; c >= 0; --c) {
-      const Raw8<H> u = renewed(v[c]);
-#pragma unroll
-      for (int i = 7; i >= 0; --i) at = (float)u.v[i] == own ? c * NT * 8 + i : at;
-      asm volatile("" : "+v"(at));
-    }
-    const uint64_t mine = at != ~0u ? key_of(own, first + at) : 0;
-    select_top<NT>(sel, a.top, mine, each, [&](int i, uint64_t key) {
+    select_logits<NT, CH>(sel, a.top, v, pm, own, lo + threadIdx.x * 8, [&](int i, uint64_t key) {
       if constexpr (SPLIT)
         a.keys[(row * a.chunks + chunk) * a.top + i] = key;
       else
@@ -394,16 +496,7 @@ __global__ __launch_bounds__(256) void logp_join_kernel(LogpArgs a) {
   finish<T, ONE, 256>(a, row, r, reinterpret_cast<const T *>(a.z) + row * a.vocab);
   if constexpr (TOP) {
     const int64_t n = (int64_t)a.chunks * a.top;
-    const uint64_t *keys = a.keys + row * n;
-    const auto each = [&](uint64_t bound, auto f) {
-      for (int64_t i = threadIdx.x; i < n; i += 256) {
-        const uint64_t key = keys[i];
-        if (key >= bound) f(key);
-      }
-    };
-    uint64_t mine = 0;
-    each(0, [&](uint64_t key) { mine = key > mine ? key : mine; });
-    select_top<256>(sel, a.top, mine, each, [&](int i, uint64_t key) { put_top(a, row, r, i, key); });
+    select_keys<256>(sel, a.top, a.keys + row * n, n, [&](int i, uint64_t key) { put_top(a, row, r, i, key); });
   }
 }
 
@@ -448,8 +541,9 @@ hipError_t run_fwd(LogpArgs a, hipStream_t stream) {
 // The given tokens' ids and gradients, 8 bytes of LDS each.
 extern __shared__ float given_space[];
 
-// A workgroup takes 8 CH NT logits of a row.
-template <typename T, bool ONE, int NT, int CH>
+// A workgroup takes 8 CH NT logits of a row.  FEW: few given tokens, for which every piece of 8 logits looks;
+// else they are written over what the pass left there.
+template <typename T, bool ONE, int NT, int CH, bool FEW>
 __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
   int *const id = (int *)given_space;
   float *const g = given_space + a.given;
@@ -457,12 +551,6 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
   const int lo = (int)(blockIdx.x % a.chunks) * (NT * CH * 8);
   const T *z = reinterpret_cast<const T *>(a.z) + row * a.vocab;
   T *dz = reinterpret_cast<T *>(a.dz) + row * a.vocab;
-  Raw8<std::conditional_t<ONE, T, float>> v[CH];
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    const int64_t col = lo + (int64_t)(c * NT + (int)threadIdx.x) * 8;
-    if (col < a.vocab) v[c] = logits8<T, ONE>(a, z, col);
-  }
   for (int i = threadIdx.x; i < a.given; i += NT) {
     const int j = a.ids[row * a.given + i];
     const bool used = j >= 0 && j < a.vocab;
@@ -471,7 +559,22 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
   }
   const float m = a.stats[3 * row], L = a.stats[3 * row + 1], B = a.stats[3 * row + 2];
   const float gh = a.gh ? a.gh[row] : 0.0f;
-  __syncthreads();
+  Raw8<std::conditional_t<ONE, T, float>> v[CH];
+  const bool whole = lo + NT * CH * 8 <= a.vocab;
+  if (whole) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) v[c] = logits8<T, ONE, true>(a, z, lo + (c * NT + threadIdx.x) * 8);
+  } else {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int64_t col = lo + (int64_t)(c * NT + (int)threadIdx.x) * 8;
+      if (col < a.vocab) v[c] = logits8<T, ONE>(a, z, col);
+    }
+  }
+  if constexpr (NT > 64)
+    __syncthreads();
+  else
+    wave_sync();
   float all = 0.0f;
   for (int i = 0; i < a.given; ++i) all += g[i];
   const bool none = m == -INFINITY;
@@ -480,41 +583,59 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
     const float d = m - x, q = expd(a, d) * inv_s;
     return q == 0.0f ? 0.0f : -q * (all + gh * (B - d * a.inv_t));
   };
+  // what the given tokens add; equal ids add up
+  const auto given = [&](int j) {
+    float sum = 0.0f;
+    for (int k = 0; k < a.given; ++k) sum += id[k] == j ? g[k] : 0.0f;
+    return sum * a.inv_t;
+  };
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const int64_t col = lo + (int64_t)(c * NT + (int)threadIdx.x) * 8;
-    if (col >= a.vocab) break;
+    if (!whole && col >= a.vocab) break;
+    float d[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) d[i] = none ? 0.0f : grad((float)v[c].v[i]);
+    if constexpr (FEW) {
+      bool hit = false;
+      for (int k = 0; k < a.given; ++k) hit = hit || (uint32_t)(id[k] - (int)col) < 8;
+      if (hit && !none) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] += given((int)col + i);
+      }
+    }
     Raw8<T> o;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o.v[i] = none ? (T)0.0f : (T)grad((float)v[c].v[i]);
-    store8_tail(dz + col, o, a.vocab - col);
+    for (int i = 0; i < 8; ++i) o.v[i] = (T)d[i];
+    store8_tail(dz + col, o, whole ? 8 : a.vocab - col);
   }
-  if (none) return;
-  __syncthreads();  // the pass's stores come before the tokens'
-  const int hi = lo + NT * CH * 8;
-  for (int i = threadIdx.x; i < a.given; i += NT) {
-    const int j = id[i];
-    if (j < lo || j >= hi) continue;
-    // equal ids write the same sum
-    float sum = 0.0f;
-    for (int k = 0; k < a.given; ++k) sum += id[k] == j ? g[k] : 0.0f;
-    dz[j] = (T)(sum * a.inv_t + grad(logit<T, ONE>(a, z, j)));
+  if constexpr (!FEW) {
+    if (none) return;
+    __syncthreads();  // the pass's stores come before the tokens'
+    const int hi = lo + NT * CH * 8;
+    for (int i = threadIdx.x; i < a.given; i += NT) {
+      const int j = id[i];
+      if (j >= lo && j < hi) dz[j] = (T)(grad(logit<T, ONE>(a, z, j)) + given(j));
+    }
   }
 }
 
 template <typename T, bool ONE>
 hipError_t run_bwd(LogpArgs a, hipStream_t stream) {
-  const bool small = a.vocab <= 512;
+  const bool small = a.vocab <= 512 && a.given <= 8;
   const int per = small ? 512 : 8192;
   a.chunks = (a.vocab + per - 1) / per;
   const int64_t most = LAUNCH_MAX / a.chunks > 0 ? LAUNCH_MAX / a.chunks : 1;
   for (a.first = 0; a.first < a.rows; a.first += most) {
     const int64_t rows = a.rows - a.first < most ? a.rows - a.first : most;
     const unsigned grid = (unsigned)(rows * a.chunks);
-    if (small)
-      logp_bwd_kernel<T, ONE, 64, 1><<<grid, 64, 8 * a.given, stream>>>(a);
+    const int space = 8 * a.given;
+    if (a.given > 8)
+      logp_bwd_kernel<T, ONE, 256, 4, false><<<grid, 256, space, stream>>>(a);
+    else if (small)
+      logp_bwd_kernel<T, ONE, 64, 1, true><<<grid, 64, space, stream>>>(a);
     else
-      logp_bwd_kernel<T, ONE, 256, 4><<<grid, 256, 8 * a.given, stream>>>(a);
+      logp_bwd_kernel<T, ONE, 256, 4, true><<<grid, 256, space, stream>>>(a);
   }
   return hipGetLastError();
 }
