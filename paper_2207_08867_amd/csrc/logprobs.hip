@@ -229,14 +229,14 @@ __device__ inline float log_prob(const LogpArgs &a, const Row &r, float z) {
   return (float)(((double)z - (double)r.m) / (double)a.temperature - (double)r.L);
 }
 
-// A row's outputs but for the alternatives.
+// A row's outputs but for the alternatives, by NT threads of which this is the t-th; the given tokens from `from` on.
 template <typename T, bool ONE, int NT>
-__device__ inline void finish(const LogpArgs &a, int64_t row, const Row &r, const T *z) {
-  for (int i = threadIdx.x; i < a.given; i += NT) {
+__device__ inline void finish(const LogpArgs &a, int64_t row, const Row &r, const T *z, int from, int t) {
+  for (int i = from + t; i < a.given; i += NT) {
     const int id = a.ids[row * a.given + i];
     a.logp[row * a.given + i] = id >= 0 && id < a.vocab ? log_prob(a, r, logit<T, ONE>(a, z, id)) : 0.0f;
   }
-  if (threadIdx.x == 0) {
+  if (t == 0) {
     if (a.entropy) a.entropy[row] = r.L + r.B;
     if (a.stats_out) {
       a.stats_out[3 * row] = r.m;
@@ -250,12 +250,6 @@ __device__ inline void put_top(const LogpArgs &a, int64_t row, const Row &r, int
   a.top_ids[row * a.top + i] = some ? key_index(key) : -1;
   a.top_logp[row * a.top + i] = some ? log_prob(a, r, key_value(key)) : (r.bad ? NAN : -INFINITY);
 }
-
-// A wavefront's sums: all exp(-d / T) relative to its largest logit, or, of one with the row's largest, those of the
-// others and the number of largest ones.
-struct Wave {
-  float m, s, a, equal;
-};
 
 // The held elements as another value, so that the compiler works out again what follows from them (16-bit
 // ones in 32 bits, keys of all elements) instead of holding it.
@@ -286,8 +280,8 @@ __device__ inline void select_logits(Select &sh, int k, const Raw8<H> (&v)[CH], 
   const uint32_t b = bound_of_groups<uint32_t>(sh, k);
   const uint32_t lowest = ordered(-FLT_MAX);
   float bound = ordered_value(b < lowest ? lowest : b);
-  // each(test, f): f(mask of the lanes whose element passes, the element, its index), element by element, of
-  // the pieces in which a lane has one at or above `least`
+  // f(ballots of the lanes whose eight elements pass, the elements, the first one's index) for the pieces in which a
+  // lane has one at or above `least`
   const auto each = [&](float least, auto test, auto f) {
 #pragma unroll
     for (int c = 0; c < CH; ++c)
@@ -295,28 +289,35 @@ __device__ inline void select_logits(Select &sh, int k, const Raw8<H> (&v)[CH], 
         const Raw8<H> u = renewed(v[c]);
         uint32_t from = first + c * NT * 8;
         asm volatile("" : "+v"(from));
+        uint64_t lanes[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) f(__ballot(test((float)u.v[i])), (float)u.v[i], from + i);
+        for (int i = 0; i < 8; ++i) lanes[i] = __ballot(test((float)u.v[i]));
+        f(lanes, u, from);
       }
   };
-  const auto count = [&](auto test, float least) {
+  const auto sum8 = [](const uint64_t(&lanes)[8]) {
     int n = 0;
-    each(least, test, [&](uint64_t lanes, float, uint32_t) { n += __popcll(lanes); });
+#pragma unroll
+    for (int i = 0; i < 8; ++i) n += __popcll(lanes[i]);
     return n;
   };
   // keeps the elements that pass
   const auto keep = [&](auto test, float least) {
-    const int n = count(test, least);
-    int at = 0;
-    if ((threadIdx.x & 63) == 0 && n > 0) at = atomicAdd(&sh.n, n);
-    at = __builtin_amdgcn_readfirstlane(at);
-    if (n > 0)
-      each(least, test, [&](uint64_t lanes, float x, uint32_t j) {
-        if (lanes == 0) return;
-        const int mine = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0));
-        if ((lanes >> (threadIdx.x & 63) & 1) && mine < KEEP) sh.kept[mine] = key_of(x, j);
-        at += __popcll(lanes);
-      });
+    each(least, test, [&](const uint64_t(&lanes)[8], const Raw8<H> &u, uint32_t from) {
+      const int n = sum8(lanes);
+      if (n == 0) return;
+      int at = 0;
+      if ((threadIdx.x & 63) == 0) at = atomicAdd(&sh.n, n);
+      at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (lanes[i]) {
+          const int mine =
+              at + __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes[i], 0));
+          if ((lanes[i] >> (threadIdx.x & 63) & 1) && mine < KEEP) sh.kept[mine] = key_of((float)u.v[i], from + i);
+          at += __popcll(lanes[i]);
+        }
+    });
     __syncthreads();
   };
   keep([&](float x) { return x >= bound; }, bound);
@@ -326,7 +327,10 @@ __device__ inline void select_logits(Select &sh, int k, const Raw8<H> (&v)[CH], 
     // bisection over all of them; the larger ones, fewer than k, and the first of those equal to it.
     const uint32_t e = bound_of<uint32_t>(k, k, [&](uint32_t b) {
       const float least = ordered_value(b < lowest ? lowest : b);
-      return waves_sum<NT>(sh, count([&](float x) { return x >= least; }, least));
+      int c = 0;
+      each(least, [&](float x) { return x >= least; },
+           [&](const uint64_t(&lanes)[8], const Raw8<H> &, uint32_t) { c += sum8(lanes); });
+      return waves_sum<NT>(sh, c);
     });
     bound = ordered_value(e < lowest ? lowest : e);
     __syncthreads();
@@ -371,13 +375,17 @@ template <typename T, bool ONE, int NT, int CH, bool TOP, bool SPLIT, int OCC>
 __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
   using H = std::conditional_t<ONE, T, float>;
   constexpr int W = NT / 64;
-  __shared__ Wave sums[W];
+  __shared__ Part sums[W];
+  __shared__ std::conditional_t<TOP, Row, int> result;
   __shared__ std::conditional_t<TOP, Select, int> sel;
   const int64_t row = SPLIT ? a.first + blockIdx.x / a.chunks : a.first + blockIdx.x;
   const int chunk = SPLIT ? blockIdx.x % a.chunks : 0, lo = chunk * (NT * CH * 8);
   const T *z = reinterpret_cast<const T *>(a.z) + row * a.vocab;
+  // the first given tokens, each wavefront's lane one: asked for ahead of the row
+  const int lane = threadIdx.x & 63;
+  int id = -1;
+  if (!SPLIT && lane < a.given) id = a.ids[row * a.given + lane];
   Raw8<H> v[CH];
-  float own = -FLT_MAX;
   if (lo + (int64_t)(NT * CH * 8) <= a.vocab) {
 #pragma unroll
     for (int c = 0; c < CH; ++c) v[c] = logits8<T, ONE, true>(a, z, lo + (c * NT + threadIdx.x) * 8);
@@ -393,16 +401,23 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
       }
     }
   }
-  float pm[CH];
+  float given = 0.0f;
+  if (id >= 0 && id < a.vocab) given = logit<T, ONE>(a, z, id);
+  float own = -FLT_MAX, pm[CH];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    pm[c] = (float)v[c].v[0];
+    if constexpr (TOP) {
+      pm[c] = (float)v[c].v[0];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) pm[c] = fmaxf(pm[c], (float)v[c].v[i]);
-    own = fmaxf(own, pm[c]);
+      for (int i = 1; i < 8; ++i) pm[c] = fmaxf(pm[c], (float)v[c].v[i]);
+      own = fmaxf(own, pm[c]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) own = fmaxf(own, (float)v[c].v[i]);
+    }
   }
   // Each wavefront's sums relative to its own largest logit, so that it works on its logits while the others'
-  // are on their way; those with the row's largest then sum the others alone.
+  // are on their way.
   const float mw = lanes_max(own);
   float s = 0.0f, d1 = 0.0f;
 #pragma unroll
@@ -417,14 +432,17 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
     // here, or the compiler keeps d and e of every element for a later sum
     asm volatile("" : "+v"(s), "+v"(d1));
   }
-  s = lanes_sum(s);
-  d1 = lanes_sum(d1);
-  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = Wave{mw, s, d1, 0.0f};
+  const float sw = lanes_sum(s), aw = lanes_sum(d1);
+  if (lane == 0) sums[threadIdx.x >> 6] = Part{mw, sw, aw};
   __syncthreads();
   float m = sums[0].m;
+  int first = 0;
 #pragma unroll
-  for (int w = 1; w < W; ++w) m = fmaxf(m, sums[w].m);
-  if (mw == m) {
+  for (int w = 1; w < W; ++w)
+    if (sums[w].m > m) m = sums[w].m, first = w;
+  // The first wavefront with the row's largest logit finishes.  It sums its others alone; one more largest logit
+  // elsewhere makes the sum 1 or more, which then needs no such care.
+  if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) == __builtin_amdgcn_readfirstlane(first)) {
     float equal = 0.0f;
     s = 0.0f;
 #pragma unroll
@@ -440,35 +458,34 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
     }
     s = lanes_sum(s);
     equal = lanes_sum(equal);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6].s = s, sums[threadIdx.x >> 6].equal = equal;
-  }
-  __syncthreads();
-  Part part = {m, 0.0f, 0.0f};
-  float equal = 0.0f;
+    Part part = {m, s, aw};
+    // no largest logit: nothing but -inf, or NaN, which s then is
+    float more = equal - 1.0f;
 #pragma unroll
-  for (int w = 0; w < W; ++w) {
-    const Wave x = sums[w];
-    const float d = m - x.m, f = expd(a, d);  // 1 where the largest is the row's
-    equal += x.equal;
-    part.s += x.s * f;
-    part.a += (x.a + (f == 0.0f ? 0.0f : d) * x.s) * f;
-  }
-  // no largest logit: nothing but -inf, or NaN, which s then is
-  part.s += equal - 1.0f;
-  if (m == INFINITY) part.s = NAN;
-  Row r;
-  if constexpr (!SPLIT) {
-    r = row_of(a, part);
-    finish<T, ONE, NT>(a, row, r, z);
-  } else if (threadIdx.x == 0) {
-    a.parts[row * a.chunks + chunk] = part;
+    for (int w = 0; w < W; ++w) {
+      const Part x = sums[w];
+      const float d = m - x.m, f = w == first ? 0.0f : expd(a, d);
+      part.s += w == first ? 0.0f : x.s * f;
+      part.a += w == first ? 0.0f : (x.a + (f == 0.0f ? 0.0f : d) * x.s) * f;
+    }
+    part.s += more;
+    if (m == INFINITY) part.s = NAN;
+    if constexpr (SPLIT) {
+      if (lane == 0) a.parts[row * a.chunks + chunk] = part;
+    } else {
+      const Row r = row_of(a, part);
+      if constexpr (TOP)
+        if (lane == 0) result = r;
+      if (lane < a.given) a.logp[row * a.given + lane] = id >= 0 && id < a.vocab ? log_prob(a, r, given) : 0.0f;
+      finish<T, ONE, 64>(a, row, r, z, 64, lane);
+    }
   }
   if constexpr (TOP) {
     select_logits<NT, CH>(sel, a.top, v, pm, own, lo + threadIdx.x * 8, [&](int i, uint64_t key) {
       if constexpr (SPLIT)
         a.keys[(row * a.chunks + chunk) * a.top + i] = key;
       else
-        put_top(a, row, r, i, key);
+        put_top(a, row, result, i, key);
     });
   }
 }
@@ -493,7 +510,7 @@ __global__ __launch_bounds__(256) void logp_join_kernel(LogpArgs a) {
 #pragma unroll
   for (int w = 1; w < 4; ++w) p = join(a, p, sums[w]);
   const Row r = row_of(a, p);
-  finish<T, ONE, 256>(a, row, r, reinterpret_cast<const T *>(a.z) + row * a.vocab);
+  finish<T, ONE, 256>(a, row, r, reinterpret_cast<const T *>(a.z) + row * a.vocab, 0, threadIdx.x);
   if constexpr (TOP) {
     const int64_t n = (int64_t)a.chunks * a.top;
     select_keys<256>(sel, a.top, a.keys + row * n, n, [&](int i, uint64_t key) { put_top(a, row, r, i, key); });
