@@ -75,11 +75,16 @@ __device__ inline int32_t key_index(uint64_t k) { return (int32_t)~(uint32_t)k; 
 constexpr int GROUPS = 256;  // of the threads, for the alternatives; above LOGP_TOP
 constexpr int KEEP = 1024;   // candidates
 
+constexpr int RANKS = 512;   // candidates whose ranks all wavefronts count together
+
 struct Select {
-  uint64_t group[GROUPS];
+  union {
+    uint64_t group[GROUPS];
+    int rank[RANKS];  // once the groups are done with
+  };
   uint64_t kept[KEEP];
   uint64_t bound;
-  int n, wave[16];
+  int n, slots, wave[16];
 };
 
 // The largest b of the form "some leading bits, then zeros" that at least k numbers reach, 0 where fewer
@@ -98,7 +103,7 @@ __device__ inline U bound_of(int k, int few, Count count) {
 }
 
 // The same of the 256 groups' numbers in sh.group, by one wavefront, for all.
-template <typename U>
+template <int NT, typename U>
 __device__ inline U bound_of_groups(Select &sh, int k) {
   __syncthreads();
   if (threadIdx.x < 64) {
@@ -111,22 +116,39 @@ __device__ inline U bound_of_groups(Select &sh, int k) {
       for (int i = 0; i < GROUPS / 64; ++i) n += __popcll(__ballot(g[i] >= b));
       return n;
     });
-    if (threadIdx.x == 0) sh.bound = b, sh.n = 0;
+    if (threadIdx.x == 0) sh.bound = b, sh.n = 0, sh.slots = 0;
   }
   __syncthreads();
+  for (int i = threadIdx.x; i < RANKS; i += NT) sh.rank[i] = 0;
   return (U)sh.bound;
 }
 
 // out(r, key) takes the r-th largest of the n <= KEEP kept keys, r < k, and 0 where there is none: ranks by
-// counting.
+// counting, each wavefront a part of the comparisons.
 template <int NT, typename Out>
-__device__ inline void rank_kept(const Select &sh, int k, int n, Out out) {
-  for (int i = threadIdx.x; i < n; i += NT) {
-    const uint64_t mine = sh.kept[i];
-    int above = 0;
+__device__ inline void rank_kept(Select &sh, int k, int n, Out out) {
+  constexpr int W = NT / 64;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (n <= RANKS) {
+    const int from = n * wave / W, to = n * (wave + 1) / W;
+    for (int i = lane; i < n; i += 64) {
+      const uint64_t mine = sh.kept[i];
+      int above = 0;
+#pragma unroll 4
+      for (int j = from; j < to; ++j) above += sh.kept[j] > mine;
+      atomicAdd(&sh.rank[i], above);
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += NT)
+      if (sh.rank[i] < k) out(sh.rank[i], sh.kept[i]);
+  } else {
+    for (int i = threadIdx.x; i < n; i += NT) {
+      const uint64_t mine = sh.kept[i];
+      int above = 0;
 #pragma unroll 8
-    for (int j = 0; j < n; ++j) above += sh.kept[j] > mine;
-    if (above < k) out(above, mine);
+      for (int j = 0; j < n; ++j) above += sh.kept[j] > mine;
+      if (above < k) out(above, mine);
+    }
   }
   for (int r = n + (int)threadIdx.x; r < k; r += NT) out(r, (uint64_t)0);
 }
@@ -152,7 +174,7 @@ __device__ inline void select_keys(Select &sh, int k, const uint64_t *keys, int6
   uint64_t own = 0;
   for (int64_t i = threadIdx.x; i < n; i += NT) own = keys[i] > own ? keys[i] : own;
   sh.group[threadIdx.x] = own;
-  uint64_t bound = bound_of_groups<uint64_t>(sh, k);
+  uint64_t bound = bound_of_groups<NT, uint64_t>(sh, k);
   int kept;
   for (int pass = 0;; ++pass) {
     if (bound == 0) bound = 1;
@@ -224,8 +246,10 @@ __device__ inline Row row_of(const LogpArgs &a, const Part &p) {
 }
 __device__ inline float log_prob(const LogpArgs &a, const Row &r, float z) {
   if (r.none) return -INFINITY;
-  // binary64: the difference of a largest and a lowest number passes binary32's range, where its quotient
-  // by the temperature need not
+  const float d = z - r.m;
+  if (d != -INFINITY) return d / a.temperature - r.L;
+  // the difference of a largest and a lowest number passes binary32's range, where its quotient by the
+  // temperature need not
   return (float)(((double)z - (double)r.m) / (double)a.temperature - (double)r.L);
 }
 
@@ -266,77 +290,94 @@ __device__ inline Raw8<T> renewed(const Raw8<T> &r) {
   return o;
 }
 
-// The k largest of the workgroup's logits by (logit, index), those of -inf apart, where they are held: v, the
-// pieces' largest logits pm and the thread's, own (at least -FLT_MAX); first: the index of the thread's first.
-// A bound that at least k of 256 groups' largest logits reach bounds the k-th largest logit from
-// below; the logits that reach it, k and a few more as a rule, are ranked.
+// Threads whose logits go through LDS, 16 bytes a plain 16-bit piece.
+constexpr int POOL = 152;
+template <int CH, typename H>
+struct Pool {
+  Raw8<H> piece[POOL][CH];
+  uint16_t owner[POOL];
+};
+
+// The k largest of the workgroup's logits by (logit, index), those of -inf apart, where they are held: v, and the
+// thread's largest, own (at least -FLT_MAX); first: the index of thread 0's first.  A bound that at least k of 256
+// groups' largest logits reach bounds the k-th largest logit from below.  The threads with a logit that reaches it, k
+// and a few more as a rule, hand theirs to the workgroup, which looks through them and ranks those that reach it.
 template <int NT, int CH, typename H, typename Out>
-__device__ inline void select_logits(Select &sh, int k, const Raw8<H> (&v)[CH], const float (&pm)[CH], float own,
+__device__ inline void select_logits(Select &sh, Pool<CH, H> &pool, int k, const Raw8<H> (&v)[CH], float own,
                                      uint32_t first, Out out) {
   constexpr int PER = NT / GROUPS;
   static_assert(PER >= 1 && NT % GROUPS == 0 && GROUPS > LOGP_TOP, "a group has whole threads");
   const float big = lanes_max<PER>(own);
   if (threadIdx.x % PER == 0) sh.group[threadIdx.x / PER] = ordered(big);
-  const uint32_t b = bound_of_groups<uint32_t>(sh, k);
+  const uint32_t b = bound_of_groups<NT, uint32_t>(sh, k);
   const uint32_t lowest = ordered(-FLT_MAX);
   float bound = ordered_value(b < lowest ? lowest : b);
-  // f(ballots of the lanes whose eight elements pass, the elements, the first one's index) for the pieces in which a
-  // lane has one at or above `least`
-  const auto each = [&](float least, auto test, auto f) {
+  if (own >= bound) {
+    const int at = atomicAdd(&sh.slots, 1);
+    if (at < POOL) {
+      pool.owner[at] = (uint16_t)threadIdx.x;
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
-      if (__any(pm[c] >= least)) {
-        const Raw8<H> u = renewed(v[c]);
-        uint32_t from = first + c * NT * 8;
-        asm volatile("" : "+v"(from));
-        uint64_t lanes[8];
+      for (int c = 0; c < CH; ++c) pool.piece[at][c] = v[c];
+    }
+  }
+  __syncthreads();
+  const int slots = sh.slots;
+  if (slots <= POOL) {
+    for (int i = threadIdx.x; i < slots * CH; i += NT) {
+      const Raw8<H> u = pool.piece[0][i];
+      uint32_t mask = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) lanes[i] = __ballot(test((float)u.v[i]));
-        f(lanes, u, from);
-      }
-  };
-  const auto sum8 = [](const uint64_t(&lanes)[8]) {
-    int n = 0;
+      for (int e = 0; e < 8; ++e) mask |= (float)u.v[e] >= bound ? 1u << e : 0u;
+      if (mask == 0) continue;
+      const uint32_t j = first + (i % CH * NT + pool.owner[i / CH]) * 8;
+      int at = atomicAdd(&sh.n, __popc(mask));
 #pragma unroll
-    for (int i = 0; i < 8; ++i) n += __popcll(lanes[i]);
-    return n;
-  };
-  // keeps the elements that pass
-  const auto keep = [&](auto test, float least) {
-    each(least, test, [&](const uint64_t(&lanes)[8], const Raw8<H> &u, uint32_t from) {
-      const int n = sum8(lanes);
-      if (n == 0) return;
-      int at = 0;
-      if ((threadIdx.x & 63) == 0) at = atomicAdd(&sh.n, n);
-      at = __builtin_amdgcn_readfirstlane(at);
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (lanes[i]) {
-          const int mine =
-              at + __builtin_amdgcn_mbcnt_hi((uint32_t)(lanes[i] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes[i], 0));
-          if ((lanes[i] >> (threadIdx.x & 63) & 1) && mine < KEEP) sh.kept[mine] = key_of((float)u.v[i], from + i);
-          at += __popcll(lanes[i]);
+      for (int e = 0; e < 8; ++e)
+        if (mask >> e & 1) {
+          if (at < KEEP) sh.kept[at] = key_of((float)u.v[e], j + e);
+          ++at;
         }
-    });
+    }
     __syncthreads();
-  };
-  keep([&](float x) { return x >= bound; }, bound);
+  }
   int n = sh.n;
-  if (n > KEEP) {
+  if (slots > POOL || n > KEEP) {
     // Many equal logits at the bound, or a row whose order follows the threads'.  The k-th largest logit by
     // bisection over all of them; the larger ones, fewer than k, and the first of those equal to it.
+    const uint32_t mine0 = first + threadIdx.x * 8;
+    const auto count = [&](auto test) {
+      int n = 0;
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const Raw8<H> u = renewed(v[c]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) n += __popcll(__ballot(test((float)u.v[i])));
+      }
+      return n;
+    };
     const uint32_t e = bound_of<uint32_t>(k, k, [&](uint32_t b) {
       const float least = ordered_value(b < lowest ? lowest : b);
-      int c = 0;
-      each(least, [&](float x) { return x >= least; },
-           [&](const uint64_t(&lanes)[8], const Raw8<H> &, uint32_t) { c += sum8(lanes); });
-      return waves_sum<NT>(sh, c);
+      return waves_sum<NT>(sh, count([&](float x) { return x >= least; }));
     });
     bound = ordered_value(e < lowest ? lowest : e);
     __syncthreads();
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
-    keep([&](float x) { return x > bound; }, bound);
+    if (own > bound) {
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const Raw8<H> u = renewed(v[c]);
+        uint32_t j = mine0 + c * NT * 8;
+        asm volatile("" : "+v"(j));
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          if ((float)u.v[i] > bound) {
+            const int at = atomicAdd(&sh.n, 1);
+            if (at < KEEP) sh.kept[at] = key_of((float)u.v[i], j + i);
+          }
+      }
+    }
+    __syncthreads();
     n = sh.n;
     if (n < k) {
       int need = k - n;
@@ -356,7 +397,8 @@ __device__ inline void select_logits(Select &sh, int k, const Raw8<H> (&v)[CH], 
         const int all = waves_sum<NT>(sh, __shfl(before, 63));
         before -= mine;
         for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) before += sh.wave[w];
-        uint32_t j = first + c * NT * 8;
+        uint32_t j = mine0 + c * NT * 8;
+        asm volatile("" : "+v"(j));
 #pragma unroll
         for (int i = 0; i < 8; ++i, ++j)
           if ((float)u.v[i] == bound && before < need) sh.kept[k - need + before++] = key_of(bound, j);
@@ -377,6 +419,7 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
   constexpr int W = NT / 64;
   __shared__ Part sums[W];
   __shared__ std::conditional_t<TOP, Row, int> result;
+  __shared__ std::conditional_t<TOP, Pool<CH, H>, int> pool;
   __shared__ std::conditional_t<TOP, Select, int> sel;
   const int64_t row = SPLIT ? a.first + blockIdx.x / a.chunks : a.first + blockIdx.x;
   const int chunk = SPLIT ? blockIdx.x % a.chunks : 0, lo = chunk * (NT * CH * 8);
@@ -403,19 +446,11 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
   }
   float given = 0.0f;
   if (id >= 0 && id < a.vocab) given = logit<T, ONE>(a, z, id);
-  float own = -FLT_MAX, pm[CH];
+  float own = -FLT_MAX;
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    if constexpr (TOP) {
-      pm[c] = (float)v[c].v[0];
+  for (int c = 0; c < CH; ++c)
 #pragma unroll
-      for (int i = 1; i < 8; ++i) pm[c] = fmaxf(pm[c], (float)v[c].v[i]);
-      own = fmaxf(own, pm[c]);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) own = fmaxf(own, (float)v[c].v[i]);
-    }
-  }
+    for (int i = 0; i < 8; ++i) own = fmaxf(own, (float)v[c].v[i]);
   // Each wavefront's sums relative to its own largest logit, so that it works on its logits while the others'
   // are on their way.
   const float mw = lanes_max(own);
@@ -481,7 +516,7 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
     }
   }
   if constexpr (TOP) {
-    select_logits<NT, CH>(sel, a.top, v, pm, own, lo + threadIdx.x * 8, [&](int i, uint64_t key) {
+    select_logits<NT, CH>(sel, pool, a.top, v, own, lo, [&](int i, uint64_t key) {
       if constexpr (SPLIT)
         a.keys[(row * a.chunks + chunk) * a.top + i] = key;
       else
@@ -542,7 +577,7 @@ hipError_t run_fwd(LogpArgs a, hipStream_t stream) {
     else if (a.vocab <= 4096)
       ROW(256, 2, false, 8);
     else if (a.vocab <= 8192)
-      ROW(256, 4, false, SHORT ? 8 : 6);
+      ROW(256, 4, false, SHORT ? 8 : (TOP ? 5 : 6));
     else if (a.vocab <= 16384)
       ROW(512, 4, false, SHORT ? 8 : 6);
     else
