@@ -275,21 +275,6 @@ __device__ inline void put_top(const LogpArgs &a, int64_t row, const Row &r, int
   a.top_logp[row * a.top + i] = some ? log_prob(a, r, key_value(key)) : (r.bad ? NAN : -INFINITY);
 }
 
-// The held elements as another value, so that the compiler works out again what follows from them (16-bit
-// ones in 32 bits, keys of all elements) instead of holding it.
-template <typename T>
-__device__ inline Raw8<T> renewed(const Raw8<T> &r) {
-  u32x4 u[sizeof(T) / 2];
-  __builtin_memcpy(&u, &r, sizeof(u));
-  if constexpr (sizeof(T) == 2)
-    asm volatile("" : "+v"(u[0]));
-  else
-    asm volatile("" : "+v"(u[0]), "+v"(u[1]));
-  Raw8<T> o;
-  __builtin_memcpy(&o, &u, sizeof(u));
-  return o;
-}
-
 // Threads whose logits go through LDS, 16 bytes a plain 16-bit piece.
 constexpr int POOL = 152;
 template <int CH, typename H>

@@ -59,6 +59,23 @@ __device__ inline Raw8<T> load8_tail(const T *p, int64_t left) {
   return r;
 }
 
+// Eight elements from column col < n of a row of n >= 8, those past n as `fill`.  The load itself has no other form
+// for the row's end, where it starts early and its elements move down: a second form between a wavefront's
+// loads makes it wait for each of them (a 4096 x 4096 bfloat16 norm 41 us, 27 so).  EVEN: n is a multiple of 8.
+template <bool EVEN, typename T>
+__device__ inline Raw8<T> load8_row(const T *row, int64_t col, int64_t n, T fill) {
+  if constexpr (EVEN) return load8(row + col);
+  const int over = n - col < 8 ? (int)(col + 8 - n) : 0;
+  Raw8<T> r = load8(row + col - over);
+  if (over) {
+#pragma unroll
+    for (int b = 4; b; b >>= 1)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r.v[i] = over & b ? (i + b < 8 ? r.v[i + b] : fill) : r.v[i];
+  }
+  return r;
+}
+
 template <typename T>
 __device__ inline void store8_tail(T *p, const Raw8<T> &r, int64_t left) {
   if (left >= 8) {
@@ -68,6 +85,21 @@ __device__ inline void store8_tail(T *p, const Raw8<T> &r, int64_t left) {
     for (int i = 0; i < 8; ++i)
       if (i < left) p[i] = r.v[i];
   }
+}
+
+// Held elements as another value, so that the compiler works out again what follows from them (wider forms of 16-bit
+// ones, say) instead of holding it.
+template <typename T>
+__device__ inline Raw8<T> renewed(const Raw8<T> &r) {
+  u32x4 u[sizeof(T) / 2];
+  __builtin_memcpy(&u, &r, sizeof(u));
+  if constexpr (sizeof(T) == 2)
+    asm volatile("" : "+v"(u[0]));
+  else
+    asm volatile("" : "+v"(u[0]), "+v"(u[1]));
+  Raw8<T> o;
+  __builtin_memcpy(&o, &u, sizeof(u));
+  return o;
 }
 
 // Eight E2M1 codes (one word) of a block as bfloat16 values.  scale: the binary32 number whose

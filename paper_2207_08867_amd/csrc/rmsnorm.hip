@@ -13,11 +13,15 @@
 // Gradients, given dy and the gradient g that reaches the new stream from later layers:
 //   dh = g + r (w dy - v r^2 sum(v w dy) / n),   dw = sum over rows of dy v r.
 // r is computed again: v is read in any case.
+#include <float.h>
 #include <math.h>
+
+#include <type_traits>
 
 #include "int8.hpp"
 #include "mcf_internal.hpp"
 #include "mx4.hpp"
+#include "wave.hpp"
 
 namespace mcf {
 namespace {
@@ -29,21 +33,31 @@ struct NormArgs {
   float *scales;          // [rows]
   int64_t rows, n, plane, pitch;
   int64_t first;          // the launch's first row
-  double eps;
+  double eps, inv_n;
   int nc;
 };
 
-// Sum and maximum over the NT threads of a row, in a fixed order; every thread gets both.
-struct SumMax {
-  double sum, max;
-};
-template <int NT>
-__device__ inline SumMax row_join(SumMax v, SumMax *lds) {
+// 1 / sqrt(x): the hardware's estimate and two Newton steps, each of which squares its error of 2^-26 or
+// less; IEEE's results at zero and infinity.
+__device__ inline double inverse_root(double x) {
+  double y = __builtin_amdgcn_rsq(x);
+  if (!(x > 0.0 && x < INFINITY)) return y;
+  const double half = 0.5 * x;
 #pragma unroll
-  for (int d = 1; d < (NT < 64 ? NT : 64); d <<= 1) {
-    v.sum += __shfl_xor(v.sum, d);
-    v.max = fmax(v.max, __shfl_xor(v.max, d));
-  }
+  for (int i = 0; i < 2; ++i) y = fma(y, fma(-half * y, y, 0.5), y);
+  return y;
+}
+
+// Sum and maximum over the NT threads of a row, in a fixed order; every thread gets both.
+template <typename M>
+struct SumMax {
+  double sum;
+  M max;
+};
+template <int NT, typename M>
+__device__ inline SumMax<M> row_join(SumMax<M> v, SumMax<M> *lds) {
+  v.sum = lanes_sum<(NT < 64 ? NT : 64)>(v.sum);
+  v.max = lanes_max<(NT < 64 ? NT : 64)>(v.max);
   if constexpr (NT > 64) {
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -51,43 +65,52 @@ __device__ inline SumMax row_join(SumMax v, SumMax *lds) {
 #pragma unroll
     for (int w = 1; w < NT / 64; ++w) {
       v.sum += lds[w].sum;
-      v.max = fmax(v.max, lds[w].max);
+      v.max = v.max > lds[w].max ? v.max : lds[w].max;
     }
   }
   return v;
 }
 
-// Eight elements from column col as binary64; zeros past the row.
-template <typename T>
-__device__ inline void wide8(const T *p, int64_t left, double v[8]) {
-  const Raw8<T> r = load8_tail(p, left);
+// How a row's pieces of 8 elements end: n is a multiple of 8, at least 8, or less.
+enum End { END_EVEN = 0, END_ODD = 1, END_SHORT = 2 };
+inline End end_of(int64_t n) { return n % 8 == 0 ? END_EVEN : (n >= 8 ? END_ODD : END_SHORT); }
+
+// Eight elements from column col of a row of n as binary64; zeros past its end.
+template <End E, typename T>
+__device__ inline void wide8(const T *row, int64_t col, int64_t n, double v[8]) {
+  Raw8<T> r;
+  if constexpr (E == END_SHORT)
+    r = load8_tail(row + col, n - col);
+  else
+    r = load8_row<E == END_EVEN>(row, col, n, (T)0.0f);
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = (double)(float)r.v[i];
 }
 
 // The planes' sum, the last one first.
-template <typename T>
-__device__ inline void planes8(const T *p, int64_t plane, int nc, int64_t left, double v[8]) {
-  wide8(p + (nc - 1) * plane, left, v);
+template <End E, typename T>
+__device__ inline void planes8(const T *row, int64_t plane, int nc, int64_t col, int64_t n, double v[8]) {
+  wide8<E>(row + (nc - 1) * plane, col, n, v);
   for (int c = nc - 2; c >= 0; --c) {
     double u[8];
-    wide8(p + c * plane, left, u);
+    wide8<E>(row + c * plane, col, n, u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] += u[i];
   }
 }
 
 // v, eight values of the stream from column col of a row; with x the new stream is written.
-template <typename T, bool ONE>
-__device__ inline void stream8(const NormArgs &a, int64_t at, int64_t left, double v[8]) {
+template <typename T, bool ONE, End E>
+__device__ inline void stream8(const NormArgs &a, int64_t at, int64_t col, double v[8]) {
   const int nc = ONE ? 1 : a.nc;
-  planes8(reinterpret_cast<const T *>(a.h) + at, a.plane, nc, left, v);
+  planes8<E>(reinterpret_cast<const T *>(a.h) + at, a.plane, nc, col, a.n, v);
   if (!a.x) return;
   double u[8];
-  wide8(reinterpret_cast<const T *>(a.x) + at, left, u);
+  wide8<E>(reinterpret_cast<const T *>(a.x) + at, col, a.n, u);
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] += u[i];
-  T *out = reinterpret_cast<T *>(a.h_out) + at;
+  T *out = reinterpret_cast<T *>(a.h_out) + at + col;
+  const int64_t left = E == END_EVEN ? 8 : a.n - col;
   double total[8];
   Raw8<T> part[ONE ? 1 : 4];
 #pragma unroll
@@ -113,11 +136,11 @@ __device__ inline void stream8(const NormArgs &a, int64_t at, int64_t left, doub
 }
 
 // p = v w.
-template <typename T>
-__device__ inline void weigh8(const NormArgs &a, int64_t col, int64_t left, double v[8]) {
+template <End E, typename T>
+__device__ inline void weigh8(const NormArgs &a, int64_t col, double v[8]) {
   if (!a.w) return;
   double u[8];
-  wide8(reinterpret_cast<const T *>(a.w) + col, left, u);
+  wide8<E>(reinterpret_cast<const T *>(a.w), col, a.n, u);
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] *= u[i];
 }
@@ -149,23 +172,23 @@ __device__ inline uint64_t codes8(const double p[8], const Scale &s) {
 // NT threads a row, CH pieces of 8 elements a thread, which stay in registers between the sums and the
 // output; CH = 0: any length, read again.  The row's threads are one wavefront's lanes or a whole
 // workgroup.  NORM false: quantisation alone.
-template <typename T, bool ONE, int NT, int CH, bool NORM, bool INT8>
-__global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_kernel(NormArgs a) {
-  constexpr int BLOCK = NT < 256 ? 256 : NT, HOLD = CH > 0 ? CH : 1;
-  __shared__ SumMax lds[BLOCK / 64];
+template <typename T, bool ONE, int NT, int CH, bool NORM, bool INT8, End E>
+__global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
+  constexpr int BLOCK = NT <= 64 ? 256 : NT, HOLD = CH > 0 ? CH : 1;
+  __shared__ SumMax<double> lds[BLOCK / 64];
   const int64_t row = a.first + (int64_t)blockIdx.x * (BLOCK / NT) + threadIdx.x / NT;
   if (NT <= 64 && row >= a.rows) return;
   const int t = threadIdx.x % NT;
   const int64_t at = row * a.n, width = INT8 ? a.pitch : a.n;
   double v[HOLD][8];
-  SumMax s = {0.0, 0.0};
+  SumMax<double> s = {0.0, 0.0};
   bool nan = false;
   // a piece's part in the sums; INT8: it becomes p
   const auto count = [&](double *p, int64_t col) {
     if (NORM)
 #pragma unroll
       for (int i = 0; i < 8; ++i) s.sum += p[i] * p[i];
-    if (NORM) weigh8<T>(a, col, a.n - col, p);
+    if (NORM) weigh8<E, T>(a, col, p);
     if (INT8)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
@@ -180,19 +203,19 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_kernel(NormArgs a) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[c][i] = 0.0;
       if (col < a.n) {
-        stream8<T, ONE>(a, at + col, a.n - col, v[c]);
+        stream8<T, ONE, E>(a, at, col, v[c]);
         count(v[c], col);
       }
     }
   } else {
     for (int64_t col = t * 8; col < a.n; col += NT * 8) {
-      stream8<T, ONE>(a, at + col, a.n - col, v[0]);
+      stream8<T, ONE, E>(a, at, col, v[0]);
       count(v[0], col);
     }
   }
   if (INT8 && nan) s.max = INFINITY;
   s = row_join<NT>(s, lds);
-  const double r = NORM ? 1.0 / sqrt(s.sum / (double)a.n + a.eps) : 1.0;
+  const double r = NORM ? inverse_root(s.sum * a.inv_n + a.eps) : 1.0;
   Scale sc;
   if constexpr (INT8) {
     sc = row_scale(s.max, r);
@@ -205,7 +228,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_kernel(NormArgs a) {
       Raw8<T> o;
 #pragma unroll
       for (int i = 0; i < 8; ++i) o.v[i] = (T)(float)(p[i] * r);
-      store8_tail(reinterpret_cast<T *>(a.y) + at + col, o, a.n - col);
+      store8_tail(reinterpret_cast<T *>(a.y) + at + col, o, E == END_EVEN ? 8 : a.n - col);
     }
   };
   if constexpr (CH > 0) {
@@ -218,9 +241,165 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_kernel(NormArgs a) {
     // the thread's own columns again: of the new stream, which it wrote, where there is one
     const T *h = reinterpret_cast<const T *>(a.x ? a.h_out : a.h) + at;
     for (int64_t col = t * 8; col < width; col += NT * 8) {
-      planes8(h + col, a.plane, ONE ? 1 : a.nc, a.n - col, v[0]);
-      if (NORM && col < a.n) weigh8<T>(a, col, a.n - col, v[0]);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[0][i] = 0.0;
+      if (col < a.n) {
+        planes8<E>(h, a.plane, ONE ? 1 : a.nc, col, a.n, v[0]);
+        if (NORM) weigh8<E, T>(a, col, v[0]);
+      }
       out(v[0], col);
+    }
+  }
+}
+
+// The same of plain 16-bit rows, with binary32 between the loads and the roundings where that is exact or enough: v
+// and, in its range, p = v w are exact there, and their squares are summed in binary64.  A code is the nearest
+// integer of p fl(127 / m), within 2^-16 of the quotient; next to a tie (a few of a thousand bfloat16 numbers have
+// the largest one's significand and are ties) the exact difference decides.  Rows whose m lies near the ends of
+// binary32's range, and outputs whose r or p do, take the binary64 forms.
+template <typename T, int NT, int CH, bool NORM, bool INT8, bool EVEN, int OCC>
+__global__ __launch_bounds__(NT <= 64 ? 256 : NT, OCC) void norm16_kernel(NormArgs a) {
+  constexpr int BLOCK = NT <= 64 ? 256 : NT;
+  __shared__ SumMax<uint32_t> lds[BLOCK / 64];
+  __shared__ SumMax<double> lds_wide[BLOCK / 64];
+  const int64_t row = a.first + (int64_t)blockIdx.x * (BLOCK / NT) + threadIdx.x / NT;
+  if (NT <= 64 && row >= a.rows) return;
+  const int t = threadIdx.x % NT;
+  const int64_t at = row * a.n;
+  const int n = (int)a.n, width = INT8 ? (int)a.pitch : n;
+  const T *h = reinterpret_cast<const T *>(a.h) + at, *x = reinterpret_cast<const T *>(a.x) + at;
+  const T *w = reinterpret_cast<const T *>(a.w);
+  const auto column = [&](int c) { return (c * NT + t) * 8; };
+  Raw8<T> hr[CH], xr[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int col = column(c), left = n - col;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) hr[c].v[i] = (T)0.0f;
+    if (left <= 0) continue;
+    hr[c] = load8_row<EVEN>(h, col, n, (T)0.0f);
+    if (a.x) xr[c] = load8_row<EVEN>(x, col, n, (T)0.0f);
+  }
+  // p of a piece; the weight is read again, from the first-level cache as a rule
+  const auto weighed = [&](int c, float p[8]) {
+    Raw8<T> u;
+    const bool weight = NORM && w && column(c) < n;
+    if (weight) u = load8_row<EVEN>(w, column(c), n, (T)0.0f);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = weight ? (float)hr[c].v[i] * (float)u.v[i] : (float)hr[c].v[i];
+  };
+  SumMax<uint32_t> s = {0.0, 0};
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    const int col = column(c), left = n - col;
+    if (left <= 0) continue;
+    if (a.x) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) hr[c].v[i] = (T)((float)hr[c].v[i] + (float)xr[c].v[i]);
+      store8_tail(reinterpret_cast<T *>(a.h_out) + at + col, hr[c], EVEN ? 8 : left);
+    }
+    if (NORM)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s.sum = fma((double)(float)hr[c].v[i], (double)(float)hr[c].v[i], s.sum);
+    if constexpr (INT8) {
+      float p[8];
+      weighed(c, p);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        // as integers, of which NaN's are the largest
+        const uint32_t u = __builtin_bit_cast(uint32_t, p[i]) & 0x7fffffffu;
+        s.max = u > s.max ? u : s.max;
+      }
+    }
+  }
+  s = row_join<NT>(s, lds);
+  const double r = NORM ? inverse_root(s.sum * a.inv_n + a.eps) : 1.0;
+  // p of an element in binary64, read again, one by one: rare, and so without registers of its own
+  const T *again = a.x ? reinterpret_cast<const T *>(a.h_out) + at : h;
+  const auto wide = [&](int col) {
+    const double v = (double)(float)again[col];
+    return NORM && w ? v * (double)(float)w[col] : v;
+  };
+  if constexpr (INT8) {
+    // 2^-60 to 2^100
+    const bool fast = s.max >= 0x21800000u && s.max <= 0x71800000u;
+    double m = (double)__builtin_bit_cast(float, s.max);
+    if (!fast) {
+      SumMax<double> d = {0.0, 0.0};
+#pragma unroll 1
+      for (int c = 0; c < CH; ++c)
+#pragma unroll 1
+        for (int col = column(c); col < column(c) + 8 && col < n; ++col) {
+          const double v = wide(col);
+          d.max = fmax(d.max, v == v ? fabs(v) : INFINITY);
+        }
+      m = row_join<NT>(d, lds_wide).max;
+    }
+    const Scale sc = row_scale(m, r);
+    if (t == 0) a.scales[row] = sc.scale;
+    const float inv = (float)(127.0 * sc.inv);
+    constexpr float MAGIC = 12582912.0f;  // 1.5 2^23: its unit in the last place is 1
+    constexpr float NEAR = 0.5f - 0x1p-15f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = column(c);
+      if (col >= width) break;
+      uint32_t k[8];
+      float off = 0.0f, p[8];
+      weighed(c, p);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float q = fmaf(p[i], inv, MAGIC);
+        k[i] = __builtin_bit_cast(uint32_t, q);
+        off = fmaxf(off, fabsf(fmaf(p[i], inv, MAGIC - q)));
+      }
+      uint64_t codes;
+      if (fast && sc.inv != 0.0) {
+        if (off >= NEAR) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float q = fabsf(p[i]) * inv, whole = floorf(q);
+            if (fabsf(q - whole - 0.5f) > 0.5f - NEAR) continue;
+            // 254 |p| and (2 whole + 1) m are exact in binary64: p and m have 22 bits
+            const double over = fma(254.0, fabs((double)p[i]), -(double)(2.0f * whole + 1.0f) * m);
+            const int up = over > 0.0 || (over == 0.0 && ((int)whole & 1)), size = (int)whole + up;
+            k[i] = (uint32_t)(p[i] < 0.0f ? -size : size);
+          }
+        }
+        const uint32_t a01 = __builtin_amdgcn_perm(k[1], k[0], 0x0c0c0400), a23 = __builtin_amdgcn_perm(k[3], k[2], 0x04000c0c);
+        const uint32_t a45 = __builtin_amdgcn_perm(k[5], k[4], 0x0c0c0400), a67 = __builtin_amdgcn_perm(k[7], k[6], 0x04000c0c);
+        codes = (uint64_t)(a45 | a67) << 32 | (a01 | a23);
+      } else {
+        codes = 0;
+#pragma unroll 1
+        for (int i = 0; i < 8 && col + i < n && sc.inv != 0.0; ++i)
+          codes |= (uint64_t)(int8_code(wide(col + i), sc.m, sc.inv) & 255) << (8 * i);
+      }
+      a.codes[(row * a.pitch + col) >> 3] = codes;
+    }
+  } else {
+    const float r32 = (float)r;
+    const bool fast = r >= 0x1p-100 && r <= 0x1p10;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = column(c);
+      if (col >= n) break;
+      Raw8<T> o;
+      T *to = reinterpret_cast<T *>(a.y) + at + col;
+      float big = 0.0f, p[8];
+      weighed(c, p);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float y = p[i] * r32;
+        big = y <= FLT_MAX && y >= -FLT_MAX ? big : INFINITY;
+        o.v[i] = (T)y;
+      }
+      if (fast && big == 0.0f) {
+        store8_tail(to, o, EVEN ? 8 : n - col);
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < 8 && col + i < n; ++i) to[i] = (T)(float)(wide(col + i) * r);
+      }
     }
   }
 }
@@ -228,7 +407,7 @@ __global__ __launch_bounds__(NT < 256 ? 256 : NT) void norm_kernel(NormArgs a) {
 template <typename T, bool ONE, bool NORM, bool INT8>
 hipError_t run_norm(NormArgs a, hipStream_t stream) {
   const auto go = [&](auto kernel, int nt) {
-    const int per = nt < 256 ? 256 / nt : 1, block = nt < 256 ? 256 : nt;
+    const int per = nt <= 64 ? 256 / nt : 1, block = nt <= 64 ? 256 : nt;
     for (a.first = 0; a.first < a.rows; a.first += LAUNCH_MAX * per) {
       const int64_t left = a.rows - a.first, groups = (left + per - 1) / per;
       kernel<<<(unsigned)(groups < LAUNCH_MAX ? groups : LAUNCH_MAX), block, 0, stream>>>(a);
@@ -236,37 +415,63 @@ hipError_t run_norm(NormArgs a, hipStream_t stream) {
     return hipGetLastError();
   };
   const int64_t width = INT8 ? a.pitch : a.n;
-  if (width <= 128) return go(norm_kernel<T, ONE, 16, 1, NORM, INT8>, 16);
-  if (width <= 512) return go(norm_kernel<T, ONE, 64, 1, NORM, INT8>, 64);
-  if (width <= 2048) return go(norm_kernel<T, ONE, 256, 1, NORM, INT8>, 256);
-  if (width <= 4096) return go(norm_kernel<T, ONE, 512, 1, NORM, INT8>, 512);
-  if (width <= 8192) return go(norm_kernel<T, ONE, 1024, 1, NORM, INT8>, 1024);
-  if (width <= 16384) return go(norm_kernel<T, ONE, 1024, 2, NORM, INT8>, 1024);
-  return go(norm_kernel<T, ONE, 1024, 0, NORM, INT8>, 1024);
+  const auto pick = [&](auto end) {
+    constexpr End E = decltype(end)::value;
+    if constexpr (ONE && sizeof(T) == 2 && E != END_SHORT) {
+#define ROW(NT, CH) return go(norm16_kernel<T, NT, CH, NORM, INT8, E == END_EVEN, 8>, NT)
+      if (width <= 128) ROW(16, 1);
+      if (width <= 512) ROW(64, 1);
+      if (width <= 1024) ROW(64, 2);
+      if (width <= 2048) ROW(128, 2);
+      if (width <= 4096) ROW(256, 2);
+      if (width <= 8192) ROW(512, 2);
+      if (width <= 16384) ROW(1024, 2);
+#undef ROW
+    }
+#define ROW(NT, CH) return go(norm_kernel<T, ONE, NT, CH, NORM, INT8, E>, NT)
+    if (E == END_SHORT || width <= 128) ROW(16, 1);
+    if constexpr (E != END_SHORT) {
+      if (width <= 512) ROW(64, 1);
+      if (width <= 2048) ROW(256, 1);
+      if (width <= 4096) ROW(512, 1);
+      if (width <= 8192) ROW(1024, 1);
+      if (width <= 16384) ROW(1024, 2);
+      ROW(1024, 0);
+    }
+#undef ROW
+  };
+  switch (end_of(a.n)) {
+    case END_EVEN: return pick(std::integral_constant<End, END_EVEN>());
+    case END_ODD: return pick(std::integral_constant<End, END_ODD>());
+    default: return pick(std::integral_constant<End, END_SHORT>());
+  }
 }
 
-// code scale, eight elements a thread.
+// code scale, 16 elements a thread.
 template <typename T>
-__global__ __launch_bounds__(256) void int8_read_kernel(const uint64_t *codes, const float *scales, T *out, int64_t rows,
+__global__ __launch_bounds__(256) void int8_read_kernel(const u32x4 *codes, const float *scales, T *out, int64_t rows,
                                                         int64_t n, int64_t across, int64_t first) {
   const int64_t id = (first + blockIdx.x) * 256 + threadIdx.x;
   if (id >= rows * across) return;
   const int64_t row = id <= 0xffffffffll ? (int64_t)((uint32_t)id / (uint32_t)across) : id / across;
-  const int64_t col = (id - row * across) * 8;
-  const uint64_t w = codes[row * (int8_pitch(n) >> 3) + (col >> 3)];
+  const int64_t col = (id - row * across) * 16;
+  const u32x4 w = codes[row * (int8_pitch(n) >> 4) + (col >> 4)];
   const float s = scales[row];
-  Raw8<T> o;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) o.v[i] = (T)((float)(int8_t)(w >> (8 * i)) * s);
-  store8_tail(out + row * n + col, o, n - col);
+  for (int half = 0; half < 2; ++half) {
+    Raw8<T> o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o.v[i] = (T)((float)(int8_t)(w[2 * half + i / 4] >> (8 * (i % 4))) * s);
+    if (half == 0 || col + 8 < n) store8_tail(out + row * n + col + 8 * half, o, n - col - 8 * half);
+  }
 }
 
 template <typename T>
 hipError_t read_back(int64_t rows, int64_t n, const void *codes, const void *scales, void *out, hipStream_t stream) {
-  const int64_t across = (n + 7) / 8, groups = (rows * across + 255) / 256;
+  const int64_t across = (n + 15) / 16, groups = (rows * across + 255) / 256;
   for (int64_t first = 0; first < groups; first += LAUNCH_MAX)
     int8_read_kernel<T><<<(unsigned)(groups - first < LAUNCH_MAX ? groups - first : LAUNCH_MAX), 256, 0, stream>>>(
-        (const uint64_t *)codes, (const float *)scales, (T *)out, rows, n, across, first);
+        (const u32x4 *)codes, (const float *)scales, (T *)out, rows, n, across, first);
   return hipGetLastError();
 }
 
@@ -276,20 +481,18 @@ struct NormBwdArgs {
   const void *h, *w, *dy, *g;  // [nc][rows][n]; [n] or null; [rows][n]; [rows][n] or null
   void *dh, *dw;               // [rows][n] or null; [n] or null
   float *partial;              // [groups][n], with dw
+  double *r;                   // [rows], of long rows
   int64_t rows, n, plane;
-  double eps;
+  double eps, inv_n;
   int nc, groups;
 };
 
+// Two sums over the NT threads of a row.  lds: room for a row, another one for the next.
 template <int NT>
 __device__ inline f64x2 row_sum2(f64x2 v, f64x2 *lds) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    v[0] += __shfl_xor(v[0], d);
-    v[1] += __shfl_xor(v[1], d);
-  }
+  v[0] = lanes_sum<(NT < 64 ? NT : 64)>(v[0]);
+  v[1] = lanes_sum<(NT < 64 ? NT : 64)>(v[1]);
   if constexpr (NT > 64) {
-    __syncthreads();  // the row before has been read
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
     v = lds[0];
@@ -299,76 +502,153 @@ __device__ inline f64x2 row_sum2(f64x2 v, f64x2 *lds) {
   return v;
 }
 
-// A workgroup takes rows blockIdx.x, blockIdx.x + groups, ...; a thread the same columns of each, of which
-// it keeps dw's sums.
-template <typename T, bool ONE, int NT, int CH>
-__global__ __launch_bounds__(NT) void norm_bwd_kernel(NormBwdArgs a) {
-  __shared__ f64x2 lds[NT / 64];
-  const int nc = ONE ? 1 : a.nc;
+// What a thread asks for of a row, ahead of the row before.
+template <typename T, bool ONE, int CH>
+struct BwdRow {
+  Raw8<T> h[ONE ? CH : 1], dy[CH], g[CH];
+};
+
+// A workgroup takes every groups-th SLOTS rows; a thread the same columns of each, of which it keeps dw's sums.  While a
+// row is worked on the next one is on its way.  E, NT, CH as above.
+template <typename T, bool ONE, int NT, int CH, End E>
+__global__ __launch_bounds__(NT <= 64 ? 256 : NT, 4) void norm_bwd_kernel(NormBwdArgs a) {
+  constexpr int BLOCK = NT <= 64 ? 256 : NT, SLOTS = BLOCK / NT;
+  constexpr bool AHEAD = ONE && E != END_SHORT && CH * sizeof(T) <= 4;
+  __shared__ f64x2 lds[2][BLOCK / 64];
+  __shared__ double joined[SLOTS > 1 ? BLOCK : 1][8];
+  const int t = threadIdx.x % NT, n = (int)a.n;
+  const auto column = [&](int c) { return (c * NT + t) * 8; };
+  const auto load = [&](int64_t row, BwdRow<T, ONE, CH> &b) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      const int col = column(c);
+      if (col >= n) break;
+      const int64_t at = row * a.n;
+      const auto one = [&](const void *p) {
+        if constexpr (E == END_SHORT)
+          return load8_tail(reinterpret_cast<const T *>(p) + at + col, (int64_t)(n - col));
+        else
+          return load8_row<E == END_EVEN>(reinterpret_cast<const T *>(p) + at, col, n, (T)0.0f);
+      };
+      if constexpr (ONE) b.h[c] = one(a.h);
+      b.dy[c] = one(a.dy);
+      if (a.g && a.dh) b.g[c] = one(a.g);
+    }
+  };
   double dw[CH][8];
 #pragma unroll
   for (int c = 0; c < CH; ++c)
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw[c][i] = 0.0;
-  for (int64_t row = blockIdx.x; row < a.rows; row += a.groups) {
-    const int64_t at = row * a.n;
-    double v[CH][8], d[CH][8], w[CH][8];
+  const int64_t step = (int64_t)a.groups * SLOTS;
+  int64_t row = (int64_t)blockIdx.x * SLOTS + threadIdx.x / NT;
+  BwdRow<T, ONE, CH> next;
+  if (AHEAD && row < a.rows) load(row, next);
+  for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
+    BwdRow<T, ONE, CH> b;
+    if constexpr (AHEAD) {
+      b = next;
+      if (row + step < a.rows) load(row + step, next);
+    } else {
+      load(row, b);
+    }
+    // v, dy, and w dy, which is exact in binary64, of a piece
+    double sum[ONE ? 1 : CH][8];
+    const auto wide = [&](int c, double v[8], double d[8], double q[8]) {
+      const int col = column(c);
+      const Raw8<T> dr = renewed(b.dy[c]);
+      if constexpr (ONE) {
+        const Raw8<T> hr = renewed(b.h[c]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = (double)(float)hr.v[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = sum[c][i];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) q[i] = 1.0;
+      if (a.w) wide8<E>(reinterpret_cast<const T *>(a.w), col, a.n, q);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        d[i] = (double)(float)dr.v[i];
+        q[i] *= d[i];
+      }
+    };
     f64x2 s = {0.0, 0.0};
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int64_t col = (c * NT + (int)threadIdx.x) * 8, left = a.n - col;
-      if (left <= 0) break;
-      planes8(reinterpret_cast<const T *>(a.h) + at + col, a.plane, nc, left, v[c]);
-      wide8(reinterpret_cast<const T *>(a.dy) + at + col, left, d[c]);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) w[c][i] = 1.0;
-      if (a.w) wide8(reinterpret_cast<const T *>(a.w) + col, left, w[c]);
+      const int col = column(c);
+      if (col >= n) break;
+      double v[8], d[8], q[8];
+      if constexpr (!ONE) planes8<E>(reinterpret_cast<const T *>(a.h) + row * a.n, a.plane, a.nc, col, a.n, sum[c]);
+      wide(c, v, d, q);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        s[0] += v[c][i] * v[c][i];
-        s[1] += v[c][i] * (w[c][i] * d[c][i]);
+        s[0] = fma(v[i], v[i], s[0]);
+        s[1] = fma(v[i], q[i], s[1]);
       }
     }
-    s = row_sum2<NT>(s, lds);
-    const double r = 1.0 / sqrt(s[0] / (double)a.n + a.eps), k = s[1] / (double)a.n * r * r;
+    s = row_sum2<NT>(s, lds[turn]);
+    const double r = inverse_root(s[0] * a.inv_n + a.eps), k = s[1] * a.inv_n * r * r;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-      const int64_t col = (c * NT + (int)threadIdx.x) * 8, left = a.n - col;
-      if (left <= 0) break;
+      const int col = column(c);
+      if (col >= n) break;
+      double v[8], d[8], q[8];
+      wide(c, v, d, q);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) dw[c][i] += d[c][i] * (v[c][i] * r);
+      for (int i = 0; i < 8; ++i) dw[c][i] = fma(d[i], v[i] * r, dw[c][i]);
       if (!a.dh) continue;
-      double g[8] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
-      if (a.g) wide8(reinterpret_cast<const T *>(a.g) + at + col, left, g);
       Raw8<T> o;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o.v[i] = (T)(float)(g[i] + r * (w[c][i] * d[c][i] - v[c][i] * k));
-      store8_tail(reinterpret_cast<T *>(a.dh) + at + col, o, left);
+      for (int i = 0; i < 8; ++i) {
+        const double e = fma(-v[i], k, q[i]) * r;
+        o.v[i] = (T)(float)(a.g ? e + (double)(float)b.g[c].v[i] : e);
+      }
+      store8_tail(reinterpret_cast<T *>(a.dh) + row * a.n + col, o, E == END_EVEN ? 8 : n - col);
     }
   }
   if (!a.dw) return;
   float *p = a.partial + (int64_t)blockIdx.x * a.n;
+  if constexpr (SLOTS > 1) {
+    // the rows side by side, in order
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
+    for (int c = 0; c < CH; ++c) {
+      __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int64_t col = (c * NT + (int)threadIdx.x) * 8 + i;
-      if (col < a.n) p[col] = (float)dw[c][i];
+      for (int i = 0; i < 8; ++i) joined[threadIdx.x][i] = dw[c][i];
+      __syncthreads();
+      for (int e = threadIdx.x; e < NT * 8; e += BLOCK) {
+        const int col = c * NT * 8 + e;
+        if (col >= n) break;
+        double sum = 0.0;
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k) sum += joined[k * NT + e / 8][e % 8];
+        p[col] = (float)sum;
+      }
     }
+  } else {
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (column(c) + i < n) p[column(c) + i] = (float)dw[c][i];
+  }
 }
 
-// Rows of any length, read twice; dw by the kernel below.  r and k of each row go to partial.
+// Rows of any length, read twice; dw by the kernel below, which takes r from here.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(NormBwdArgs a) {
-  __shared__ f64x2 lds[16];
-  for (int64_t row = blockIdx.x; row < a.rows; row += a.groups) {
+  __shared__ f64x2 lds[2][16];
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += a.groups, turn ^= 1) {
     const int64_t at = row * a.n;
     f64x2 s = {0.0, 0.0};
     const auto piece = [&](int64_t col, double v[8], double d[8], double p[8]) {
-      planes8(reinterpret_cast<const T *>(a.h) + at + col, a.plane, a.nc, a.n - col, v);
-      wide8(reinterpret_cast<const T *>(a.dy) + at + col, a.n - col, d);
+      planes8<END_ODD>(reinterpret_cast<const T *>(a.h) + at, a.plane, a.nc, col, a.n, v);
+      wide8<END_ODD>(reinterpret_cast<const T *>(a.dy) + at, col, a.n, d);
       double w[8] = {1.0, 1.0, 1.0, 1.0, 1.0, 1.0, 1.0, 1.0};
-      if (a.w) wide8(reinterpret_cast<const T *>(a.w) + col, a.n - col, w);
+      if (a.w) wide8<END_ODD>(reinterpret_cast<const T *>(a.w), col, a.n, w);
 #pragma unroll
       for (int i = 0; i < 8; ++i) p[i] = w[i] * d[i];
     };
@@ -381,14 +661,14 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(NormBwdArgs a) {
         s[1] += v[i] * p[i];
       }
     }
-    s = row_sum2<1024>(s, lds);
-    const double r = 1.0 / sqrt(s[0] / (double)a.n + a.eps), k = s[1] / (double)a.n * r * r;
-    if (a.dw && threadIdx.x == 0) reinterpret_cast<double *>(a.partial)[row] = r;
+    s = row_sum2<1024>(s, lds[turn]);
+    const double r = inverse_root(s[0] * a.inv_n + a.eps), k = s[1] * a.inv_n * r * r;
+    if (a.dw && threadIdx.x == 0) a.r[row] = r;
     if (!a.dh) continue;
     for (int64_t col = threadIdx.x * 8; col < a.n; col += 8192) {
       piece(col, v, d, p);
       double g[8] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
-      if (a.g) wide8(reinterpret_cast<const T *>(a.g) + at + col, a.n - col, g);
+      if (a.g) wide8<END_ODD>(reinterpret_cast<const T *>(a.g) + at, col, a.n, g);
       Raw8<T> o;
 #pragma unroll
       for (int i = 0; i < 8; ++i) o.v[i] = (T)(float)(g[i] + r * (p[i] - v[i] * k));
@@ -397,25 +677,25 @@ __global__ __launch_bounds__(1024) void norm_bwd_long_kernel(NormBwdArgs a) {
   }
 }
 
-// dw of long rows: a thread 8 columns of every row, in order.
+// dw of long rows: a thread 8 columns of every groups-th row, in order.
 template <typename T>
-__global__ __launch_bounds__(64) void norm_bwd_long_dw_kernel(NormBwdArgs a) {
-  const int64_t col = ((int64_t)blockIdx.x * 64 + threadIdx.x) * 8;
+__global__ __launch_bounds__(256) void norm_bwd_long_dw_kernel(NormBwdArgs a) {
+  const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (col >= a.n) return;
   double sum[8] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
 #pragma unroll 2
-  for (int64_t row = 0; row < a.rows; ++row) {
+  for (int64_t row = blockIdx.y; row < a.rows; row += a.groups) {
     double v[8], d[8];
-    planes8(reinterpret_cast<const T *>(a.h) + row * a.n + col, a.plane, a.nc, a.n - col, v);
-    wide8(reinterpret_cast<const T *>(a.dy) + row * a.n + col, a.n - col, d);
-    const double r = reinterpret_cast<const double *>(a.partial)[row];
+    planes8<END_ODD>(reinterpret_cast<const T *>(a.h) + row * a.n, a.plane, a.nc, col, a.n, v);
+    wide8<END_ODD>(reinterpret_cast<const T *>(a.dy) + row * a.n, col, a.n, d);
+    const double r = a.r[row];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum[i] += d[i] * (v[i] * r);
+    for (int i = 0; i < 8; ++i) sum[i] = fma(d[i], v[i] * r, sum[i]);
   }
-  Raw8<T> o;
+  float *p = a.partial + (int64_t)blockIdx.y * a.n;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) o.v[i] = (T)(float)sum[i];
-  store8_tail(reinterpret_cast<T *>(a.dw) + col, o, a.n - col);
+  for (int i = 0; i < 8; ++i)
+    if (col + i < a.n) p[col + i] = (float)sum[i];
 }
 
 // The workgroups' sums: 64 columns by 16 parts of the workgroups, each in order, then the parts.
@@ -439,34 +719,46 @@ __global__ __launch_bounds__(1024) void norm_bwd_sum_kernel(NormBwdArgs a) {
 
 constexpr int64_t BWD_LONG = 16384;  // the longest row that stays in registers
 
-int bwd_groups(int64_t rows) { return (int)(rows < 512 ? rows : 512); }
+// Workgroups: two a CU of long rows, whose next rows are on their way, four of short ones; of rows that do not stay,
+// parts of the rows for dw.
+int bwd_groups(int64_t rows, int64_t n) {
+  if (n > BWD_LONG) return (int)(rows < 64 ? rows : 64);
+  const int64_t slots = n <= 128 ? 16 : (n <= 512 ? 4 : 1), most = n <= 2048 ? 1024 : 512, wanted = (rows + slots - 1) / slots;
+  return (int)(wanted < most ? wanted : most);
+}
 
 template <typename T>
-hipError_t run_bwd(const NormBwdArgs &a, hipStream_t stream) {
+hipError_t run_bwd(NormBwdArgs a, hipStream_t stream) {
   const unsigned grid = (unsigned)a.groups;
   if (a.n > BWD_LONG) {
-    if (grid) norm_bwd_long_kernel<T><<<grid, 1024, 0, stream>>>(a);
-    if (a.dw) norm_bwd_long_dw_kernel<T><<<(unsigned)((a.n + 511) / 512), 64, 0, stream>>>(a);
-    return hipGetLastError();
+    if (grid) {
+      NormBwdArgs b = a;
+      b.groups = (int)(a.rows < 1024 ? a.rows : 1024);
+      norm_bwd_long_kernel<T><<<(unsigned)b.groups, 1024, 0, stream>>>(b);
+      if (a.dw) norm_bwd_long_dw_kernel<T><<<dim3((unsigned)((a.n + 2047) / 2048), grid), 256, 0, stream>>>(a);
+    }
+  } else if (grid) {
+    const auto go = [&](auto one, auto end) {
+      constexpr bool ONE = decltype(one)::value;
+      constexpr End E = decltype(end)::value;
+#define ROW(NT, CH) return norm_bwd_kernel<T, ONE, NT, CH, E><<<grid, NT <= 64 ? 256 : NT, 0, stream>>>(a)
+      if (E == END_SHORT || a.n <= 128) ROW(16, 1);
+      if constexpr (E != END_SHORT) {
+        if (a.n <= 512) ROW(64, 1);
+        if (a.n <= 2048) ROW(256, 1);
+        if (a.n <= 4096) ROW(512, 1);
+        if (a.n <= 8192) ROW(512, 2);
+        ROW(1024, 2);
+      }
+#undef ROW
+    };
+    const auto pick = [&](auto end) { a.nc == 1 ? go(Flag<true>(), end) : go(Flag<false>(), end); };
+    switch (end_of(a.n)) {
+      case END_EVEN: pick(std::integral_constant<End, END_EVEN>()); break;
+      case END_ODD: pick(std::integral_constant<End, END_ODD>()); break;
+      default: pick(std::integral_constant<End, END_SHORT>());
+    }
   }
-  const auto go = [&](auto one) {
-    constexpr bool ONE = decltype(one)::value;
-    if (grid == 0) return;  // dw is zero
-    if (a.n <= 512)
-      norm_bwd_kernel<T, ONE, 64, 1><<<grid, 64, 0, stream>>>(a);
-    else if (a.n <= 2048)
-      norm_bwd_kernel<T, ONE, 256, 1><<<grid, 256, 0, stream>>>(a);
-    else if (a.n <= 4096)
-      norm_bwd_kernel<T, ONE, 512, 1><<<grid, 512, 0, stream>>>(a);
-    else if (a.n <= 8192)
-      norm_bwd_kernel<T, ONE, 1024, 1><<<grid, 1024, 0, stream>>>(a);
-    else
-      norm_bwd_kernel<T, ONE, 1024, 2><<<grid, 1024, 0, stream>>>(a);
-  };
-  if (a.nc == 1)
-    go(Flag<true>());
-  else
-    go(Flag<false>());
   if (a.dw) norm_bwd_sum_kernel<T><<<(unsigned)((a.n + 63) / 64), 1024, 0, stream>>>(a);
   return hipGetLastError();
 }
@@ -488,6 +780,7 @@ hipError_t launch_rmsnorm(int dtype, int nc, int64_t rows, int64_t n, const void
   a.plane = rows * n;
   a.pitch = int8_pitch(n);
   a.eps = eps;
+  a.inv_n = n > 0 ? 1.0 / (double)n : 0.0;
   a.nc = nc;
   const auto go = [&](auto zero) {
     using T = decltype(zero);
@@ -511,7 +804,7 @@ hipError_t launch_int8_dequantize(int dtype, int64_t rows, int64_t n, const void
 }
 
 int64_t rmsnorm_bwd_workspace_bytes(int64_t rows, int64_t n) {
-  return n > BWD_LONG ? rows * 8 : bwd_groups(rows) * n * 4;
+  return bwd_groups(rows, n) * n * 4 + (n > BWD_LONG ? rows * 8 + 8 : 0);
 }
 
 hipError_t launch_rmsnorm_bwd(int dtype, int nc, int64_t rows, int64_t n, const void *h, const void *w, const void *dy,
@@ -528,8 +821,10 @@ hipError_t launch_rmsnorm_bwd(int dtype, int nc, int64_t rows, int64_t n, const 
   a.n = n;
   a.plane = rows * n;
   a.eps = eps;
+  a.inv_n = n > 0 ? 1.0 / (double)n : 0.0;
   a.nc = nc;
-  a.groups = bwd_groups(rows);
+  a.groups = bwd_groups(rows, n);
+  a.r = (double *)((char *)ws + (a.groups * n * 4 + 7) / 8 * 8);
   if (dtype == LM_F16) return run_bwd<_Float16>(a, stream);
   if (dtype == LM_BF16) return run_bwd<__bf16>(a, stream);
   return run_bwd<float>(a, stream);

@@ -88,6 +88,10 @@ __device__ inline double lanes_max(double v) {
   return lanes_join<N>(v, [](double a, double b) { return fmax(a, b); });
 }
 template <int N = 64>
+__device__ inline uint32_t lanes_max(uint32_t v) {
+  return lanes_join<N>(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+template <int N = 64>
 __device__ inline uint64_t lanes_max(uint64_t v) {
   return lanes_join<N>(v, [](uint64_t a, uint64_t b) { return a > b ? a : b; });
 }
