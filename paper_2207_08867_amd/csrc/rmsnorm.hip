@@ -61,12 +61,9 @@ __device__ inline SumMax<M> row_join(SumMax<M> v, SumMax<M> *lds) {
   if constexpr (NT > 64) {
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = lds[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) {
-      v.sum += lds[w].sum;
-      v.max = v.max > lds[w].max ? v.max : lds[w].max;
-    }
+    v = lds[threadIdx.x % (NT / 64)];
+    v.sum = lanes_sum<NT / 64>(v.sum);
+    v.max = lanes_max<NT / 64>(v.max);
   }
   return v;
 }
@@ -447,31 +444,38 @@ hipError_t run_norm(NormArgs a, hipStream_t stream) {
   }
 }
 
-// code scale, 16 elements a thread.
+// code scale, a thread two pieces of 8 elements, 256 pieces apart.
 template <typename T>
-__global__ __launch_bounds__(256) void int8_read_kernel(const u32x4 *codes, const float *scales, T *out, int64_t rows,
+__global__ __launch_bounds__(256) void int8_read_kernel(const uint64_t *codes, const float *scales, T *out, int64_t rows,
                                                         int64_t n, int64_t across, int64_t first) {
-  const int64_t id = (first + blockIdx.x) * 256 + threadIdx.x;
-  if (id >= rows * across) return;
-  const int64_t row = id <= 0xffffffffll ? (int64_t)((uint32_t)id / (uint32_t)across) : id / across;
-  const int64_t col = (id - row * across) * 16;
-  const u32x4 w = codes[row * (int8_pitch(n) >> 4) + (col >> 4)];
-  const float s = scales[row];
+  const int64_t total = rows * across, pitch = int8_pitch(n) >> 3;
+  int64_t row[2], col[2];
+  uint64_t w[2];
+  float s[2];
 #pragma unroll
-  for (int half = 0; half < 2; ++half) {
+  for (int k = 0; k < 2; ++k) {
+    int64_t id = (first + blockIdx.x) * 512 + k * 256 + threadIdx.x;
+    if (id >= total) id = total - 1;  // again
+    row[k] = id <= 0xffffffffll ? (int64_t)((uint32_t)id / (uint32_t)across) : id / across;
+    col[k] = id - row[k] * across;
+    w[k] = codes[row[k] * pitch + col[k]];
+    s[k] = scales[row[k]];
+  }
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
     Raw8<T> o;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o.v[i] = (T)((float)(int8_t)(w[2 * half + i / 4] >> (8 * (i % 4))) * s);
-    if (half == 0 || col + 8 < n) store8_tail(out + row * n + col + 8 * half, o, n - col - 8 * half);
+    for (int i = 0; i < 8; ++i) o.v[i] = (T)((float)(int8_t)(w[k] >> (8 * i)) * s[k]);
+    store8_tail(out + row[k] * n + col[k] * 8, o, n - col[k] * 8);
   }
 }
 
 template <typename T>
 hipError_t read_back(int64_t rows, int64_t n, const void *codes, const void *scales, void *out, hipStream_t stream) {
-  const int64_t across = (n + 15) / 16, groups = (rows * across + 255) / 256;
+  const int64_t across = (n + 7) / 8, groups = (rows * across + 511) / 512;
   for (int64_t first = 0; first < groups; first += LAUNCH_MAX)
     int8_read_kernel<T><<<(unsigned)(groups - first < LAUNCH_MAX ? groups - first : LAUNCH_MAX), 256, 0, stream>>>(
-        (const u32x4 *)codes, (const float *)scales, (T *)out, rows, n, across, first);
+        (const uint64_t *)codes, (const float *)scales, (T *)out, rows, n, across, first);
   return hipGetLastError();
 }
 
@@ -495,9 +499,9 @@ __device__ inline f64x2 row_sum2(f64x2 v, f64x2 *lds) {
   if constexpr (NT > 64) {
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
-    v = lds[0];
-#pragma unroll
-    for (int w = 1; w < NT / 64; ++w) v += lds[w];
+    v = lds[threadIdx.x % (NT / 64)];
+    v[0] = lanes_sum<NT / 64>(v[0]);
+    v[1] = lanes_sum<NT / 64>(v[1]);
   }
   return v;
 }
@@ -513,7 +517,7 @@ struct BwdRow {
 template <typename T, bool ONE, int NT, int CH, End E>
 __global__ __launch_bounds__(NT <= 64 ? 256 : NT, 4) void norm_bwd_kernel(NormBwdArgs a) {
   constexpr int BLOCK = NT <= 64 ? 256 : NT, SLOTS = BLOCK / NT;
-  constexpr bool AHEAD = ONE && E != END_SHORT && CH * sizeof(T) <= 4;
+  constexpr bool AHEAD = ONE && E != END_SHORT && CH == 1;
   __shared__ f64x2 lds[2][BLOCK / 64];
   __shared__ double joined[SLOTS > 1 ? BLOCK : 1][8];
   const int t = threadIdx.x % NT, n = (int)a.n;
@@ -536,42 +540,44 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT, 4) void norm_bwd_kernel(NormBw
     }
   };
   double dw[CH][8];
+  Raw8<T> weight[CH];
+  BwdRow<T, ONE, CH> next;
 #pragma unroll
-  for (int c = 0; c < CH; ++c)
+  for (int c = 0; c < CH; ++c) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) dw[c][i] = 0.0;
+    for (int i = 0; i < 8; ++i) dw[c][i] = 0.0, weight[c].v[i] = (T)1.0f, next.g[c].v[i] = (T)0.0f;
+    if (a.w && column(c) < n) {
+      if constexpr (E == END_SHORT)
+        weight[c] = load8_tail(reinterpret_cast<const T *>(a.w) + column(c), (int64_t)(n - column(c)));
+      else
+        weight[c] = load8_row<E == END_EVEN>(reinterpret_cast<const T *>(a.w), column(c), n, (T)0.0f);
+    }
+  }
   const int64_t step = (int64_t)a.groups * SLOTS;
   int64_t row = (int64_t)blockIdx.x * SLOTS + threadIdx.x / NT;
-  BwdRow<T, ONE, CH> next;
   if (AHEAD && row < a.rows) load(row, next);
   for (int turn = 0; row < a.rows; row += step, turn ^= 1) {
-    BwdRow<T, ONE, CH> b;
+    BwdRow<T, ONE, CH> b = next;
     if constexpr (AHEAD) {
-      b = next;
       if (row + step < a.rows) load(row + step, next);
     } else {
       load(row, b);
     }
-    // v, dy, and w dy, which is exact in binary64, of a piece
+    // f(i, v, dy, w dy) of a piece's elements, in binary64, where all products here are exact but for those with r; the
+    // fences keep the wide forms of few elements at a time in registers
     double sum[ONE ? 1 : CH][8];
-    const auto wide = [&](int c, double v[8], double d[8], double q[8]) {
-      const int col = column(c);
-      const Raw8<T> dr = renewed(b.dy[c]);
-      if constexpr (ONE) {
-        const Raw8<T> hr = renewed(b.h[c]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = (double)(float)hr.v[i];
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = sum[c][i];
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) q[i] = 1.0;
-      if (a.w) wide8<E>(reinterpret_cast<const T *>(a.w), col, a.n, q);
+    const auto each = [&](int c, auto f) {
+      Raw8<T> hr = {};
+      const Raw8<T> dr = renewed(b.dy[c]), wr = renewed(weight[c]);
+      if constexpr (ONE) hr = renewed(b.h[c]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        d[i] = (double)(float)dr.v[i];
-        q[i] *= d[i];
+        if (i % 2 == 0) __builtin_amdgcn_sched_barrier(0);
+        const double d = (double)(float)dr.v[i], w = (double)(float)wr.v[i];
+        if constexpr (ONE)
+          f(i, (double)(float)hr.v[i], d, w * d);
+        else
+          f(i, sum[c][i], d, w * d);
       }
     };
     f64x2 s = {0.0, 0.0};
@@ -579,14 +585,11 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT, 4) void norm_bwd_kernel(NormBw
     for (int c = 0; c < CH; ++c) {
       const int col = column(c);
       if (col >= n) break;
-      double v[8], d[8], q[8];
       if constexpr (!ONE) planes8<E>(reinterpret_cast<const T *>(a.h) + row * a.n, a.plane, a.nc, col, a.n, sum[c]);
-      wide(c, v, d, q);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        s[0] = fma(v[i], v[i], s[0]);
-        s[1] = fma(v[i], q[i], s[1]);
-      }
+      each(c, [&](int, double v, double, double q) {
+        s[0] = fma(v, v, s[0]);
+        s[1] = fma(v, q, s[1]);
+      });
     }
     s = row_sum2<NT>(s, lds[turn]);
     const double r = inverse_root(s[0] * a.inv_n + a.eps), k = s[1] * a.inv_n * r * r;
@@ -594,17 +597,13 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT, 4) void norm_bwd_kernel(NormBw
     for (int c = 0; c < CH; ++c) {
       const int col = column(c);
       if (col >= n) break;
-      double v[8], d[8], q[8];
-      wide(c, v, d, q);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) dw[c][i] = fma(d[i], v[i] * r, dw[c][i]);
+      Raw8<T> o = {};
+      each(c, [&](int i, double v, double d, double q) {
+        dw[c][i] = fma(d, v * r, dw[c][i]);
+        const double e = fma(-v, k, q) * r;
+        o.v[i] = (T)(float)(e + (double)(float)b.g[c].v[i]);
+      });
       if (!a.dh) continue;
-      Raw8<T> o;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const double e = fma(-v[i], k, q[i]) * r;
-        o.v[i] = (T)(float)(a.g ? e + (double)(float)b.g[c].v[i] : e);
-      }
       store8_tail(reinterpret_cast<T *>(a.dh) + row * a.n + col, o, E == END_EVEN ? 8 : n - col);
     }
   }
@@ -747,7 +746,7 @@ hipError_t run_bwd(NormBwdArgs a, hipStream_t stream) {
         if (a.n <= 512) ROW(64, 1);
         if (a.n <= 2048) ROW(256, 1);
         if (a.n <= 4096) ROW(512, 1);
-        if (a.n <= 8192) ROW(512, 2);
+        if (a.n <= 8192) ROW(1024, 1);
         ROW(1024, 2);
       }
 #undef ROW
