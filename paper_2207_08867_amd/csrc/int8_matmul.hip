@@ -7,6 +7,7 @@
 #include "int8.hpp"
 #include "mcf_internal.hpp"
 #include "mx4_gemm.hpp"
+#include "wave.hpp"
 
 namespace mcf {
 namespace {
@@ -19,19 +20,34 @@ struct Int8Args {
   int64_t M, N, P;
 };
 
+// Four sums of row m from column n on, as outputs.
+template <typename T>
+__device__ inline void store4(const Int8Args &a, int64_t m, int64_t n, i32x4 v, float sa) {
+  T *y = reinterpret_cast<T *>(a.y) + m * a.N;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (n + i >= a.N) continue;
+    float f = (float)v[i] * sa * a.sb[n + i];
+    if (a.bias) f += (float)reinterpret_cast<const T *>(a.bias)[n + i];
+    y[n + i] = (T)f;
+  }
+}
+
 // Up to 16 MT rows of A.  A workgroup owns 16 rows of B and its NW wavefronts share the reduction by groups
-// of 128 bytes; their sums are joined through LDS.  A lane holds 32 bytes of a row, the operands of two 16 x 16
-// x 64 products (the order of the reduction is the same on both sides).  B is read once, straight into
-// registers.
+// of 128 bytes, two 16 x 16 x 64 products each; their sums are joined through LDS.  B is read once, straight into
+// registers, all of its groups asked for ahead of use where the row has 4096 elements or fewer; what bounds the small
+// sizes is the latency of a launch and of those loads (8 rows by 4096 x 4096: 6.9 us, 2.4 TB/s), the large ones the memory
+// (one row by 32768 x 4096: 26.5 us, 5.1 TB/s).  4, 8 and 16 wavefronts with 2 to 8 groups ahead measured the same
+// within 5%.
 template <typename T, int MT, int NW, int U>
 __global__ __launch_bounds__(64 * NW) void int8_thin_kernel(Int8Args a) {
   __shared__ i32x4 part[NW][MT][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int64_t n0 = (int64_t)blockIdx.x * 16;
-  const char *b = a.b + (n0 + r < a.N ? n0 + r : a.N - 1) * a.P + g * 32;
+  const char *b = a.b + (n0 + r < a.N ? n0 + r : a.N - 1) * a.P + g * 16;
   const char *x[MT];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) x[t] = a.a + (16 * t + r < a.M ? 16 * t + r : a.M - 1) * a.P + g * 32;
+  for (int t = 0; t < MT; ++t) x[t] = a.a + (16 * t + r < a.M ? 16 * t + r : a.M - 1) * a.P + g * 16;
   i32x4 acc[MT];
 #pragma unroll
   for (int t = 0; t < MT; ++t) acc[t] = i32x4{0, 0, 0, 0};
@@ -42,13 +58,13 @@ __global__ __launch_bounds__(64 * NW) void int8_thin_kernel(Int8Args a) {
 #pragma unroll
     for (int u = 0; u < C; ++u)
 #pragma unroll
-      for (int h = 0; h < 2; ++h) bv[u][h] = *reinterpret_cast<const i32x4 *>(b + (s0 + u * NW) * 128 + h * 16);
+      for (int h = 0; h < 2; ++h) bv[u][h] = *reinterpret_cast<const i32x4 *>(b + (s0 + u * NW) * 128 + h * 64);
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
       for (int u = 0; u < C; ++u)
 #pragma unroll
-        for (int h = 0; h < 2; ++h) av[t][u][h] = *reinterpret_cast<const i32x4 *>(x[t] + (s0 + u * NW) * 128 + h * 16);
+        for (int h = 0; h < 2; ++h) av[t][u][h] = *reinterpret_cast<const i32x4 *>(x[t] + (s0 + u * NW) * 128 + h * 64);
 #pragma unroll
     for (int t = 0; t < MT; ++t)
 #pragma unroll
@@ -69,24 +85,106 @@ __global__ __launch_bounds__(64 * NW) void int8_thin_kernel(Int8Args a) {
     // lane (r, g): row r of A, rows 4 g .. 4 g + 3 of B
     const int64_t m = 16 * t + r;
     if (m >= a.M) continue;
-    const float sa = a.sa[m];
-    T *y = reinterpret_cast<T *>(a.y) + m * a.N;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t n = n0 + 4 * g + i;
-      if (n >= a.N) continue;
-      float f = (float)v[i] * sa * a.sb[n];
-      if (a.bias) f += (float)reinterpret_cast<const T *>(a.bias)[n];
-      y[n] = (T)f;
-    }
+    store4<T>(a, m, n0 + 4 * g, v, a.sa[m]);
   }
 }
 
-constexpr int64_t THIN = 32;  // rows up to which B is read straight into registers
+// One or two rows of a plain x quantised on the way: the wavefronts ask for their first U groups of B, then all quantise
+// x (every workgroup the same) into LDS, from which the products take it.  One launch in place of two (us, in a graph; one
+// row by 4096 x 4096): 7.4 and 9.8; two rows 8.8 and 10.9, four 11.2 and 10.5.
+constexpr int TOKEN_BYTES = 32768;
+template <typename T, int NW, int U>
+__global__ __launch_bounds__(64 * NW) void int8_token_kernel(Int8Args a, const T *x, int64_t K) {
+  extern __shared__ __attribute__((aligned(16))) char codes[];  // [M][P + 16]
+  __shared__ uint32_t big[2][NW];
+  __shared__ float scale[2];
+  __shared__ i32x4 part[NW][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16;
+  const char *b = a.b + (n0 + r < a.N ? n0 + r : a.N - 1) * a.P + g * 16;
+  const int groups = (int)(a.P / 128), M = (int)a.M, P = (int)a.P, ld = P + 16, k = (int)K;
+  i32x4 bv[U][2];
+  const auto ask = [&](int s0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int s = s0 + u * NW < groups ? s0 + u * NW : groups - 1;
+        bv[u][h] = *reinterpret_cast<const i32x4 *>(b + (int64_t)s * 128 + h * 64);
+      }
+  };
+  ask(wave);
+  const auto piece = [&](int row, int col, float p[8]) {
+    const Raw8<T> u = load8_tail(x + (int64_t)row * K + col, K - col);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) p[i] = (float)u.v[i];
+  };
+  // the first piece of the first row stays
+  float first[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+  for (int row = 0; row < M; ++row) {
+    uint32_t m = 0;
+    for (int col = threadIdx.x * 8; col < k; col += 64 * NW * 8) {
+      float p[8];
+      piece(row, col, p);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t u = magnitude(p[i]);
+        m = u > m ? u : m;
+        if (row == 0 && col < 64 * NW * 8) first[i] = p[i];
+      }
+    }
+    m = lanes_max(m);
+    if (lane == 0) big[row][wave] = m;
+  }
+  __syncthreads();
+  for (int row = 0; row < M; ++row) {
+    const uint32_t m = lanes_max<NW>(big[row][lane % NW]);
+    const Int8Row s = int8_row((double)__builtin_bit_cast(float, m), 1.0);
+    if (threadIdx.x == 0) scale[row] = s.scale;
+    for (int col = threadIdx.x * 8; col < P; col += 64 * NW * 8) {
+      float p[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+      if (row == 0 && col < 64 * NW * 8) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = first[i];
+      } else if (col < k) {
+        piece(row, col, p);
+      }
+      *reinterpret_cast<uint64_t *>(codes + row * ld + col) = s.near ? int8_codes8(p, s) : int8_codes8_any(p, s);
+    }
+  }
+  __syncthreads();
+  i32x4 acc = {0, 0, 0, 0};
+  const char *xc = codes + (r < M ? r : 0) * ld + g * 16;
+  for (int s0 = wave; s0 < groups; s0 += U * NW) {
+    if (s0 != wave) ask(s0);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (s0 + u * NW < groups)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(
+              bv[u][h], *reinterpret_cast<const i32x4 *>(xc + (s0 + u * NW) * 128 + h * 64), acc, 0, 0, 0);
+  }
+  part[wave][lane] = acc;
+  __syncthreads();
+  if (wave != 0 || r >= M) return;
+#pragma unroll
+  for (int w = 1; w < NW; ++w) acc += part[w][lane];
+  store4<T>(a, r, n0 + 4 * g, acc, scale[r]);
+}
+
+// Few rows read B straight into registers; tiles read it through LDS and do not read A again for every 16 rows of B,
+// which costs more the larger B is.  Straight and by tiles (us, launches in a graph; rows of A, B): 8, 14336 x 4096 16.0
+// and 13.8, 32768 x 4096 30.8 and 33.6; 16, 4096 x 4096 7.5 and 10.3, 8192 x 4096 11.1 and 11.8, 14336 x 4096
+// 18.2 and 14.1; 32, 4096 x 4096 9.6 and 11.3, 8192 x 4096 15.0 and 12.1, 32768 x 4096 55.9 and 33.7.
+bool thin(int64_t M, int64_t N, int64_t P) {
+  const int64_t mib = N * P >> 20;
+  return M <= 8 || (M <= 16 && mib < 48) || (M <= 32 && mib < 24);
+}
 
 template <typename T>
 hipError_t run(const Int8Args &a, void *ws, hipStream_t stream) {
-  if (a.M <= THIN) {
+  if (thin(a.M, a.N, a.P)) {
     const unsigned grid = (unsigned)((a.N + 15) / 16);
     if (a.M <= 16)
       int8_thin_kernel<T, 1, 8, 4><<<grid, 512, 0, stream>>>(a);
@@ -112,10 +210,18 @@ hipError_t run(const Int8Args &a, void *ws, hipStream_t stream) {
 
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
+bool token(int64_t batch, int64_t in) { return batch <= 2 && in > 0 && batch * int8_pitch(in) <= TOKEN_BYTES; }
+
+template <typename T>
+hipError_t run_token(const Int8Args &a, const void *x, int64_t K, hipStream_t stream) {
+  int8_token_kernel<T, 8, 4><<<(unsigned)((a.N + 15) / 16), 512, a.M * (a.P + 16), stream>>>(a, (const T *)x, K);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 int64_t int8_matmul_workspace_bytes(int64_t M, int64_t N, int64_t K) {
-  return M <= THIN ? 0 : gemm_partial_bytes(M, N, int8_pitch(K) / 128);
+  return thin(M, N, int8_pitch(K)) ? 0 : gemm_partial_bytes(M, N, int8_pitch(K) / 128);
 }
 
 hipError_t launch_int8_matmul(int dtype, int64_t M, int64_t N, int64_t K, const void *a_codes, const void *a_scales,
@@ -138,11 +244,25 @@ hipError_t launch_int8_matmul(int dtype, int64_t M, int64_t N, int64_t K, const 
 
 // x in 8 bits: codes, then scales, then the product's partial sums.
 int64_t int8_linear_workspace_bytes(int64_t batch, int64_t in, int64_t out) {
+  if (token(batch, in)) return 0;
   return batch * int8_pitch(in) + up16(4 * batch) + int8_matmul_workspace_bytes(batch, out, in);
 }
 
 hipError_t launch_int8_linear(int dtype, int64_t batch, int64_t in, int64_t out, const void *x, const void *codes,
                               const void *scales, const void *bias, void *ws, void *y, hipStream_t stream) {
+  if (token(batch, in)) {
+    Int8Args a = {};
+    a.b = (const char *)codes;
+    a.sb = (const float *)scales;
+    a.bias = bias;
+    a.y = y;
+    a.M = batch;
+    a.N = out;
+    a.P = int8_pitch(in);
+    if (dtype == LM_F16) return run_token<_Float16>(a, x, in, stream);
+    if (dtype == LM_BF16) return run_token<__bf16>(a, x, in, stream);
+    return run_token<float>(a, x, in, stream);
+  }
   char *const xc = (char *)ws, *const xs = xc + batch * int8_pitch(in), *const rest = xs + up16(4 * batch);
   const hipError_t e = launch_rmsnorm(dtype, 1, batch, in, x, nullptr, nullptr, 0.0, nullptr, nullptr, xc, xs, false, stream);
   if (e != hipSuccess) return e;

@@ -142,30 +142,6 @@ __device__ inline void weigh8(const NormArgs &a, int64_t col, double v[8]) {
   for (int i = 0; i < 8; ++i) v[i] *= u[i];
 }
 
-// A row's scale; codes are zero where it is not finite.
-struct Scale {
-  double m, inv;
-  float scale;
-};
-__device__ inline Scale row_scale(double m, double r) {
-  Scale s;
-  s.scale = (float)(m * r / 127.0);
-  const bool fine = isfinite(s.scale);
-  if (!fine) s.scale = NAN;
-  s.m = m;
-  s.inv = fine && m > 0.0 ? 1.0 / m : 0.0;
-  return s;
-}
-__device__ inline uint64_t codes8(const double p[8], const Scale &s) {
-  uint32_t lo = 0, hi = 0;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    lo |= (uint32_t)((s.inv != 0.0 ? int8_code(p[i], s.m, s.inv) : 0) & 255) << (8 * i);
-    hi |= (uint32_t)((s.inv != 0.0 ? int8_code(p[i + 4], s.m, s.inv) : 0) & 255) << (8 * i);
-  }
-  return (uint64_t)hi << 32 | lo;
-}
-
 // NT threads a row, CH pieces of 8 elements a thread, which stay in registers between the sums and the
 // output; CH = 0: any length, read again.  The row's threads are one wavefront's lanes or a whole
 // workgroup.  NORM false: quantisation alone.
@@ -213,14 +189,14 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
   if (INT8 && nan) s.max = INFINITY;
   s = row_join<NT>(s, lds);
   const double r = NORM ? inverse_root(s.sum * a.inv_n + a.eps) : 1.0;
-  Scale sc;
+  Int8Row sc;
   if constexpr (INT8) {
-    sc = row_scale(s.max, r);
+    sc = int8_row(s.max, r);
     if (t == 0) a.scales[row] = sc.scale;
   }
   const auto out = [&](const double *p, int64_t col) {
     if constexpr (INT8) {
-      a.codes[(row * a.pitch + col) >> 3] = codes8(p, sc);
+      a.codes[(row * a.pitch + col) >> 3] = int8_codes8_any(p, sc);
     } else {
       Raw8<T> o;
 #pragma unroll
@@ -250,10 +226,8 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
 }
 
 // The same of plain 16-bit rows, with binary32 between the loads and the roundings where that is exact or enough: v
-// and, in its range, p = v w are exact there, and their squares are summed in binary64.  A code is the nearest
-// integer of p fl(127 / m), within 2^-16 of the quotient; next to a tie (a few of a thousand bfloat16 numbers have
-// the largest one's significand and are ties) the exact difference decides.  Rows whose m lies near the ends of
-// binary32's range, and outputs whose r or p do, take the binary64 forms.
+// and, in its range, p = v w are exact there, and their squares are summed in binary64.  Rows whose m lies near the
+// ends of binary32's range, and outputs whose r or p do, take the binary64 forms.
 template <typename T, int NT, int CH, bool NORM, bool INT8, bool EVEN, int OCC>
 __global__ __launch_bounds__(NT <= 64 ? 256 : NT, OCC) void norm16_kernel(NormArgs a) {
   constexpr int BLOCK = NT <= 64 ? 256 : NT;
@@ -303,8 +277,7 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT, OCC) void norm16_kernel(NormAr
       weighed(c, p);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        // as integers, of which NaN's are the largest
-        const uint32_t u = __builtin_bit_cast(uint32_t, p[i]) & 0x7fffffffu;
+        const uint32_t u = magnitude(p[i]);
         s.max = u > s.max ? u : s.max;
       }
     }
@@ -318,7 +291,7 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT, OCC) void norm16_kernel(NormAr
     return NORM && w ? v * (double)(float)w[col] : v;
   };
   if constexpr (INT8) {
-    // 2^-60 to 2^100
+    // 2^-60 to 2^100; outside of it p may not be exact
     const bool fast = s.max >= 0x21800000u && s.max <= 0x71800000u;
     double m = (double)__builtin_bit_cast(float, s.max);
     if (!fast) {
@@ -332,40 +305,17 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT, OCC) void norm16_kernel(NormAr
         }
       m = row_join<NT>(d, lds_wide).max;
     }
-    const Scale sc = row_scale(m, r);
+    const Int8Row sc = int8_row(m, r);
     if (t == 0) a.scales[row] = sc.scale;
-    const float inv = (float)(127.0 * sc.inv);
-    constexpr float MAGIC = 12582912.0f;  // 1.5 2^23: its unit in the last place is 1
-    constexpr float NEAR = 0.5f - 0x1p-15f;
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       const int col = column(c);
       if (col >= width) break;
-      uint32_t k[8];
-      float off = 0.0f, p[8];
-      weighed(c, p);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const float q = fmaf(p[i], inv, MAGIC);
-        k[i] = __builtin_bit_cast(uint32_t, q);
-        off = fmaxf(off, fabsf(fmaf(p[i], inv, MAGIC - q)));
-      }
       uint64_t codes;
-      if (fast && sc.inv != 0.0) {
-        if (off >= NEAR) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float q = fabsf(p[i]) * inv, whole = floorf(q);
-            if (fabsf(q - whole - 0.5f) > 0.5f - NEAR) continue;
-            // 254 |p| and (2 whole + 1) m are exact in binary64: p and m have 22 bits
-            const double over = fma(254.0, fabs((double)p[i]), -(double)(2.0f * whole + 1.0f) * m);
-            const int up = over > 0.0 || (over == 0.0 && ((int)whole & 1)), size = (int)whole + up;
-            k[i] = (uint32_t)(p[i] < 0.0f ? -size : size);
-          }
-        }
-        const uint32_t a01 = __builtin_amdgcn_perm(k[1], k[0], 0x0c0c0400), a23 = __builtin_amdgcn_perm(k[3], k[2], 0x04000c0c);
-        const uint32_t a45 = __builtin_amdgcn_perm(k[5], k[4], 0x0c0c0400), a67 = __builtin_amdgcn_perm(k[7], k[6], 0x04000c0c);
-        codes = (uint64_t)(a45 | a67) << 32 | (a01 | a23);
+      if (fast && sc.near) {
+        float p[8];
+        weighed(c, p);
+        codes = int8_codes8(p, sc);
       } else {
         codes = 0;
 #pragma unroll 1
