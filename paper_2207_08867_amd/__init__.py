@@ -922,16 +922,15 @@ def _int8(pair, n, name):
         raise TypeError(f"{name}: codes must be int8 and scales float32")
     if codes.get_device() != scales.get_device():
         raise ValueError(f"{name}: codes and scales must be on one device")
-    cs = codes.shape
-    if n < 0 or len(cs) < 1 or cs[-1] != (n + 127) // 128 * 128 or scales.shape != cs[:-1]:
-        raise ValueError(f"{name}: codes {tuple(cs)} and scales {tuple(scales.shape)} are not an 8-bit tensor of "
-                         f"rows of {n}")
-    return cs[:-1], _dev(codes, name), _dev(scales, name)
+    cs, lead = codes.shape, scales.shape
+    if n < 0 or cs != lead + ((n + 127) // 128 * 128,):
+        raise ValueError(f"{name}: codes {tuple(cs)} and scales {tuple(lead)} are not an 8-bit tensor of rows of {n}")
+    return lead, _dev(codes, name), _dev(scales, name)
 
 
 def _int8_out(out, like, lead, n):
     codes, scales = out or (None, None)
-    return (_out(codes, like, (*lead, (n + 127) // 128 * 128), _torch_module.int8),
+    return (_out(codes, like, lead + ((n + 127) // 128 * 128,), _torch_module.int8),
             _out(scales, like, lead, _torch_module.float32))
 
 
@@ -959,7 +958,7 @@ def mc_int8_dequantize(codes, scales, n: int, *, dtype, out=None):
     """The numbers (*S, n) an 8-bit tensor stands for, in `dtype`."""
     lead, cp, sp = _int8((codes, scales), n, "codes and scales")
     code = _plain_code(dtype)
-    out = _out(out, codes, (*lead, n), dtype)
+    out = _out(out, codes, lead + (n,), dtype)
     st = (_lib or lib()).mc_int8_dequantize(code, math.prod(lead), n, cp, sp, _dev(out, "out"), _stream(codes))
     _check(st, "mc_int8_dequantize")
     return out
@@ -1025,21 +1024,14 @@ def mc_int8_linear_fwd(x, W, b=None, *, out=None, workspace=None):
     return out
 
 
-def _norm_args(h, w, h_mc, **others):
-    """(code, nc, S, n, pointer of w) of a norm's tensors; the others must be (*S, n)."""
-    code = _plain_code(h.dtype)
-    nc, lead, n = _planes(h, h_mc, "h")
-    for name, t in others.items():
-        if t is not None:
-            _device(t, h, name)
-            if t.dtype != h.dtype or tuple(t.shape) != (*lead, n):
-                raise ValueError(f"{name} must be {(*lead, n)} of h's dtype, got {tuple(t.shape)} of {t.dtype}")
-    if w is None:
-        return code, nc, lead, n, None
-    _device(w, h, "w")
-    if w.dtype != h.dtype or tuple(w.shape) != (n,):
-        raise ValueError(f"w must be {(n,)} of h's dtype, got {tuple(w.shape)} of {w.dtype}")
-    return code, nc, lead, n, _dev(w, "w")
+def _like(t, h, shape, name):
+    """Pointer of t, a tensor of h's dtype and device and of this shape; None for none."""
+    if t is None:
+        return None
+    if t.dtype is not h.dtype or t.shape != shape or t.get_device() != h.get_device():
+        raise ValueError(f"{name} must be {tuple(shape)} of h's dtype and device, got {tuple(t.shape)} of {t.dtype} on "
+                         f"{t.device}")
+    return _dev(t, name)
 
 
 def _norm_stream(h, x, h_out):
@@ -1056,22 +1048,27 @@ def mc_rmsnorm_fwd(h, w=None, *, x=None, eps: float = 1e-6, h_mc: bool = False, 
     """Root-mean-square norm of a residual stream h, (*S, n) or with h_mc an MC value (planes, *S, n), with
     x (*S, n), a layer's output, added to the stream first (see include/mcf.h); w: (n,) or None for ones.
     Returns (y (*S, n), the stream behind the addition: h itself without x).  h_out may be h (in place)."""
-    code, nc, lead, n, wp = _norm_args(h, w, h_mc, x=x)
+    code = _plain_code(h.dtype)
+    nc, lead, n = _planes(h, h_mc, "h")
+    row = lead + (n,)
+    wp, xp = _like(w, h, (n,), "w"), _like(x, h, row, "x")
     stream, sp = _norm_stream(h, x, h_out)
-    out = _out(out, h, (*lead, n), h.dtype)
-    st = (_lib or lib()).mc_rmsnorm_fwd(code, nc, math.prod(lead), n, _dev(h, "h"), None if x is None else _dev(x, "x"),
-                                        wp, float(eps), sp, _dev(out, "out"), _stream(h))
+    out = _out(out, h, row, h.dtype)
+    st = (_lib or lib()).mc_rmsnorm_fwd(code, nc, math.prod(lead), n, _dev(h, "h"), xp, wp, float(eps), sp,
+                                        _dev(out, "out"), _stream(h))
     _check(st, "mc_rmsnorm_fwd")
     return out, stream
 
 
 def mc_rmsnorm_int8(h, w=None, *, x=None, eps: float = 1e-6, h_mc: bool = False, h_out=None, out=None):
     """mc_rmsnorm_fwd with the output as an 8-bit tensor: ((codes, scales), the stream behind the addition)."""
-    code, nc, lead, n, wp = _norm_args(h, w, h_mc, x=x)
+    code = _plain_code(h.dtype)
+    nc, lead, n = _planes(h, h_mc, "h")
+    wp, xp = _like(w, h, (n,), "w"), _like(x, h, lead + (n,), "x")
     stream, sp = _norm_stream(h, x, h_out)
     codes, scales = _int8_out(out, h, lead, n)
-    st = (_lib or lib()).mc_rmsnorm_int8(code, nc, math.prod(lead), n, _dev(h, "h"), None if x is None else _dev(x, "x"),
-                                         wp, float(eps), sp, _dev(codes, "codes"), _dev(scales, "scales"), _stream(h))
+    st = (_lib or lib()).mc_rmsnorm_int8(code, nc, math.prod(lead), n, _dev(h, "h"), xp, wp, float(eps), sp,
+                                         _dev(codes, "codes"), _dev(scales, "scales"), _stream(h))
     _check(st, "mc_rmsnorm_int8")
     return (codes, scales), stream
 
@@ -1087,15 +1084,16 @@ def mc_rmsnorm_bwd(h, w, dy, *, dh=None, eps: float = 1e-6, h_mc: bool = False, 
     gradient of h and of x alike, that of w (n,)); None for those not requested.  h: that stream (what
     mc_rmsnorm_fwd returned with x), dy: (*S, n), dh: the gradient that reaches the stream from elsewhere, (*S, n)
     or None.  `workspace`: an optional device byte tensor; one is allocated here when not given."""
-    code, nc, lead, n, wp = _norm_args(h, w, h_mc, dy=dy, dh=dh)
-    rows = math.prod(lead)
-    outs = [_empty(h, (*lead, n)) if dx else None, _empty(h, (n,)) if dw else None]
+    code = _plain_code(h.dtype)
+    nc, lead, n = _planes(h, h_mc, "h")
+    rows, row = math.prod(lead), lead + (n,)
+    wp, yp, gp = _like(w, h, (n,), "w"), _like(dy, h, row, "dy"), _like(dh, h, row, "dh")
+    gx, gw = _empty(h, row) if dx else None, _empty(h, (n,)) if dw else None
     keep, sp, sn = _space(workspace, _bytes("mc_rmsnorm_bwd_workspace", code, rows, n) if dw else 0, h)
-    st = (_lib or lib()).mc_rmsnorm_bwd(code, nc, rows, n, _dev(h, "h"), wp, _dev(dy, "dy"),
-                                        None if dh is None else _dev(dh, "dh"), float(eps),
-                                        *(None if o is None else o.data_ptr() for o in outs), sp, sn, _stream(h))
+    st = (_lib or lib()).mc_rmsnorm_bwd(code, nc, rows, n, _dev(h, "h"), wp, yp, gp, float(eps),
+                                        gx.data_ptr() if dx else None, gw.data_ptr() if dw else None, sp, sn, _stream(h))
     _check(st, "mc_rmsnorm_bwd")
-    return tuple(outs)
+    return gx, gw
 
 
 def _logprobs_args(z, ids):
@@ -1126,10 +1124,9 @@ def mc_logprobs_fwd(z, ids, *, top: int = 0, temperature: float = 1.0, workspace
     torch = _torch()
     code, nc, rows, vocab, given = _logprobs_args(z, ids)
     keep, wp, wn = _space(workspace, _bytes("mc_logprobs_workspace", rows, vocab, top), z)
-    logp, entropy, top_ids, top_logp, stats = (
-        _out(None, z, shape, dtype) for shape, dtype in (((rows, given), torch.float32), ((rows,), torch.float32),
-                                                         ((rows, top), torch.int32), ((rows, top), torch.float32),
-                                                         ((rows, 3), torch.float32)))
+    f32 = torch.float32
+    logp, entropy, stats = _out(None, z, (rows, given), f32), _out(None, z, (rows,), f32), _out(None, z, (rows, 3), f32)
+    top_ids, top_logp = _out(None, z, (rows, top), torch.int32), _out(None, z, (rows, top), f32)
     st = (_lib or lib()).mc_logprobs_fwd(code, nc, rows, vocab, given, top, _dev(z, "z"), _dev(ids, "ids"),
                                          float(temperature), wp, wn, logp.data_ptr(), entropy.data_ptr(),
                                          top_ids.data_ptr(), top_logp.data_ptr(), stats.data_ptr(), _stream(z))
