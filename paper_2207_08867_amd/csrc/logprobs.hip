@@ -165,31 +165,42 @@ __device__ inline int waves_sum(Select &sh, int n) {
   return n;
 }
 
+// The first keys of a thread, held in registers.
+struct Held {
+  static constexpr int N = 4;
+  uint64_t key[N];
+};
+
 // The k largest of a list of keys, which are all different (but for 0): by a bound that at least k of 256
 // groups' largest keys reach, which so bounds the k-th largest key from below.  More than KEEP keys at or
 // above it: the same bisection over all keys.
 template <int NT, typename Out>
-__device__ inline void select_keys(Select &sh, int k, const uint64_t *keys, int64_t n, Out out) {
+__device__ inline void select_keys(Select &sh, int k, const uint64_t *keys, int64_t n, const Held &held, Out out) {
   static_assert(NT == GROUPS, "a group is a thread's keys");
+  const auto each = [&](auto f) {
+#pragma unroll
+    for (int i = 0; i < Held::N; ++i) f(held.key[i]);  // 0 past the list
+    for (int64_t i = threadIdx.x + Held::N * NT; i < n; i += NT) f(keys[i]);
+  };
   uint64_t own = 0;
-  for (int64_t i = threadIdx.x; i < n; i += NT) own = keys[i] > own ? keys[i] : own;
+  each([&](uint64_t key) { own = key > own ? key : own; });
   sh.group[threadIdx.x] = own;
   uint64_t bound = bound_of_groups<NT, uint64_t>(sh, k);
   int kept;
   for (int pass = 0;; ++pass) {
     if (bound == 0) bound = 1;
     if (own >= bound)
-      for (int64_t i = threadIdx.x; i < n; i += NT)
-        if (keys[i] >= bound) {
-          const int at = atomicAdd(&sh.n, 1);
-          if (at < KEEP) sh.kept[at] = keys[i];
-        }
+      each([&](uint64_t key) {
+        if (key < bound) return;
+        const int at = atomicAdd(&sh.n, 1);
+        if (at < KEEP) sh.kept[at] = key;
+      });
     __syncthreads();
     kept = sh.n;
     if (kept <= KEEP || pass == 1) break;
     bound = bound_of<uint64_t>(k, KEEP, [&](uint64_t b) {
       uint32_t c = 0;
-      for (int64_t i = threadIdx.x; i < n; i += NT) c += keys[i] >= b;
+      each([&](uint64_t key) { c += key >= b; });
       return waves_sum<NT>(sh, (int)lanes_sum(c));
     });
     if (threadIdx.x == 0) sh.n = 0;
@@ -206,28 +217,32 @@ __device__ inline float logit(const LogpArgs &a, const T *z, int64_t j) {
   return v;
 }
 
-// Eight logits from column col of a row, as they are held: plain ones in their format.  Past the row
-// they are -inf.
+// Eight logits from column col < vocab of a row, as they are held: plain ones in their format.  Past the row they
+// are -inf.  WHOLE: none is.
 template <typename T, bool ONE, bool WHOLE = false>
 __device__ inline Raw8<std::conditional_t<ONE, T, float>> logits8(const LogpArgs &a, const T *z, int64_t col) {
-  using H = std::conditional_t<ONE, T, float>;
-  const int64_t left = WHOLE ? 8 : a.vocab - col;
-  Raw8<H> r;
+  const auto plane = [&](const T *p) {
+    if constexpr (WHOLE) {
+      return load8(p + col);
+    } else {
+      if (a.vocab >= 8) return load8_row<false>(p, col, a.vocab, (T)-INFINITY);
+      Raw8<T> r;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r.v[i] = i < a.vocab ? p[i] : (T)-INFINITY;
+      return r;
+    }
+  };
   if constexpr (ONE) {
-    r = load8_tail(z + col, left);
+    return plane(z);
   } else {
+    Raw8<float> r;
     for (int p = a.nc - 1; p >= 0; --p) {
-      const Raw8<T> u = load8_tail(z + p * a.plane + col, left);
+      const Raw8<T> u = plane(z + p * a.plane);
 #pragma unroll
       for (int i = 0; i < 8; ++i) r.v[i] = p == a.nc - 1 ? (float)u.v[i] : r.v[i] + (float)u.v[i];
     }
+    return r;
   }
-  if (left < 8) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i >= left) r.v[i] = (H)-INFINITY;
-  }
-  return r;
 }
 
 // The numbers of a row from its part; every thread has them.
@@ -516,8 +531,21 @@ __global__ __launch_bounds__(256) void logp_join_kernel(LogpArgs a) {
   __shared__ Part sums[4];
   __shared__ std::conditional_t<TOP, Select, int> sel;
   const int64_t row = a.first + blockIdx.x;
+  // what has to wait for nothing is asked for first
+  const T *z = reinterpret_cast<const T *>(a.z) + row * a.vocab;
+  const int64_t n = (int64_t)a.chunks * a.top;
+  const uint64_t *keys = a.keys + row * n;
+  Held held = {};
+  if constexpr (TOP)
+#pragma unroll
+    for (int i = 0; i < Held::N; ++i)
+      if (threadIdx.x + i * 256 < n) held.key[i] = keys[threadIdx.x + i * 256];
+  int id = -1;
+  if ((int)threadIdx.x < a.given) id = a.ids[row * a.given + threadIdx.x];
   Part p = {-FLT_MAX, -1.0f, 0.0f};
   for (int c = threadIdx.x; c < a.chunks; c += 256) p = join(a, p, a.parts[row * a.chunks + c]);
+  float given = 0.0f;
+  if (id >= 0 && id < a.vocab) given = logit<T, ONE>(a, z, id);
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
     const Part o = {__shfl_xor(p.m, d), __shfl_xor(p.s, d), __shfl_xor(p.a, d)};
@@ -530,11 +558,10 @@ __global__ __launch_bounds__(256) void logp_join_kernel(LogpArgs a) {
 #pragma unroll
   for (int w = 1; w < 4; ++w) p = join(a, p, sums[w]);
   const Row r = row_of(a, p);
-  finish<T, ONE, 256>(a, row, r, reinterpret_cast<const T *>(a.z) + row * a.vocab, 0, threadIdx.x);
-  if constexpr (TOP) {
-    const int64_t n = (int64_t)a.chunks * a.top;
-    select_keys<256>(sel, a.top, a.keys + row * n, n, [&](int i, uint64_t key) { put_top(a, row, r, i, key); });
-  }
+  if ((int)threadIdx.x < a.given)
+    a.logp[row * a.given + threadIdx.x] = id >= 0 && id < a.vocab ? log_prob(a, r, given) : 0.0f;
+  finish<T, ONE, 256>(a, row, r, z, 256, threadIdx.x);
+  if constexpr (TOP) select_keys<256>(sel, a.top, keys, n, held, [&](int i, uint64_t key) { put_top(a, row, r, i, key); });
 }
 
 // Chunks of a row: one while it fits, 32768 logits; rows of few, 4096 each.
