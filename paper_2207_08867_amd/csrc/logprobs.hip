@@ -217,32 +217,36 @@ __device__ inline float logit(const LogpArgs &a, const T *z, int64_t j) {
   return v;
 }
 
-// Eight logits from column col < vocab of a row, as they are held: plain ones in their format.  Past the row they
-// are -inf.  WHOLE: none is.
-template <typename T, bool ONE, bool WHOLE = false>
-__device__ inline Raw8<std::conditional_t<ONE, T, float>> logits8(const LogpArgs &a, const T *z, int64_t col) {
-  const auto plane = [&](const T *p) {
-    if constexpr (WHOLE) {
-      return load8(p + col);
-    } else {
-      if (a.vocab >= 8) return load8_row<false>(p, col, a.vocab, (T)-INFINITY);
-      Raw8<T> r;
+// CH pieces of 8 logits of a row, piece c from column lo + 8 (c NT + t) of thread t, as they are held: plain ones in their
+// format.  Past the row they are -inf.
+template <typename T, bool ONE, int NT, int CH>
+__device__ inline void logits(const LogpArgs &a, const T *z, int lo, Raw8<std::conditional_t<ONE, T, float>> (&v)[CH]) {
+  using H = std::conditional_t<ONE, T, float>;
+  const auto column = [&](int c) { return lo + (c * NT + (int)threadIdx.x) * 8; };
+  const bool tiny = CH == 1 && a.vocab < 8;  // which takes the smallest kernels
+  const auto plane = [&](const T *p, int c) {
+    if (!tiny) return load8_clamped(p, column(c), a.vocab);
+    Raw8<T> r;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) r.v[i] = i < a.vocab ? p[i] : (T)-INFINITY;
-      return r;
-    }
-  };
-  if constexpr (ONE) {
-    return plane(z);
-  } else {
-    Raw8<float> r;
-    for (int p = a.nc - 1; p >= 0; --p) {
-      const Raw8<T> u = plane(z + p * a.plane);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) r.v[i] = p == a.nc - 1 ? (float)u.v[i] : r.v[i] + (float)u.v[i];
-    }
+    for (int i = 0; i < 8; ++i) r.v[i] = column(c) + i < a.vocab ? p[column(c) + i] : (T)-INFINITY;
     return r;
+  };
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    if constexpr (ONE) {
+      v[c] = plane(z, c);
+    } else {
+      for (int p = a.nc - 1; p >= 0; --p) {
+        const Raw8<T> u = plane(z + p * a.plane, c);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[c].v[i] = p == a.nc - 1 ? (float)u.v[i] : v[c].v[i] + (float)u.v[i];
+      }
+    }
   }
+  if (tiny) return;
+#pragma unroll
+  for (int c = 0; c < CH; ++c)
+    if (lo + (c + 1) * (NT * 8) > a.vocab) load8_settle(v[c], (int64_t)(a.vocab - column(c)), (H)-INFINITY);
 }
 
 // The numbers of a row from its part; every thread has them.
@@ -429,21 +433,7 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
   int id = -1;
   if (!SPLIT && lane < a.given) id = a.ids[row * a.given + lane];
   Raw8<H> v[CH];
-  if (lo + (int64_t)(NT * CH * 8) <= a.vocab) {
-#pragma unroll
-    for (int c = 0; c < CH; ++c) v[c] = logits8<T, ONE, true>(a, z, lo + (c * NT + threadIdx.x) * 8);
-  } else {
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int64_t col = lo + (int64_t)(c * NT + (int)threadIdx.x) * 8;
-      if (col < a.vocab) {
-        v[c] = logits8<T, ONE>(a, z, col);
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[c].v[i] = (H)-INFINITY;
-      }
-    }
-  }
+  logits<T, ONE, NT>(a, z, lo, v);
   float given = 0.0f;
   if (id >= 0 && id < a.vocab) given = logit<T, ONE>(a, z, id);
   float own = -FLT_MAX;
@@ -564,38 +554,50 @@ __global__ __launch_bounds__(256) void logp_join_kernel(LogpArgs a) {
   if constexpr (TOP) select_keys<256>(sel, a.top, keys, n, held, [&](int i, uint64_t key) { put_top(a, row, r, i, key); });
 }
 
-// Chunks of a row: one while it fits, 32768 logits; rows of few, 4096 each.
-constexpr int FEW = 4096, LONG = 32768;
-int chunk_of(int64_t rows, int64_t vocab) {
-  if (rows < 256 && vocab > 2 * FEW) return FEW;
-  return vocab > LONG ? LONG : 0;
+// How a row is cut into chunks of `pieces` pieces of 8 logits for each of the threads.  A row is one workgroup's while
+// it fits 8 pieces of 512 threads, else it is cut into chunks alike; rows of a few are cut into chunks of 4096 logits.
+struct Cut {
+  int threads, pieces, chunks;
+};
+Cut cut_of(int64_t rows, int64_t vocab) {
+  const auto up = [](int64_t n, int64_t d) { return (int)((n + d - 1) / d); };
+  if (vocab > 8192 && rows < 256) return {256, 2, up(vocab, 4096)};
+  if (vocab <= 8192) return {256, vocab <= 2048 ? 1 : (vocab <= 4096 ? 2 : 4), 1};
+  const int chunks = up(vocab, 32768), pieces = up(up(vocab, chunks), 4096);
+  return {512, pieces <= 4 && chunks == 1 ? 4 : (pieces <= 6 ? 6 : 8), chunks};
 }
 
 template <typename T, bool ONE, bool TOP>
-hipError_t run_fwd(LogpArgs a, hipStream_t stream) {
-  const int chunk = chunk_of(a.rows, a.vocab);
+hipError_t run_fwd(LogpArgs a, const Cut &cut, hipStream_t stream) {
   const int64_t most = LAUNCH_MAX / a.chunks > 0 ? LAUNCH_MAX / a.chunks : 1;
   for (a.first = 0; a.first < a.rows; a.first += most) {
     const int64_t rows = a.rows - a.first < most ? a.rows - a.first : most;
     const unsigned grid = (unsigned)(rows * a.chunks);
     constexpr bool SHORT = ONE && sizeof(T) == 2;
 #define ROW(NT, CH, SPLIT, OCC) logp_kernel<T, ONE, NT, CH, TOP, SPLIT, OCC><<<grid, NT, 0, stream>>>(a)
-    if (chunk == FEW)
-      ROW(256, 2, true, 8);
-    else if (chunk == LONG)
-      ROW(512, 8, true, SHORT ? 8 : 4);
-    else if (a.vocab <= 2048)
-      ROW(256, 1, false, 8);
-    else if (a.vocab <= 4096)
-      ROW(256, 2, false, 8);
-    else if (a.vocab <= 8192)
-      ROW(256, 4, false, SHORT ? 8 : (TOP ? 5 : 6));
-    else if (a.vocab <= 16384)
+    if (a.chunks > 1) {
+      if (cut.threads == 256)
+        ROW(256, 2, true, 8);
+      else if (cut.pieces == 6)
+        ROW(512, 6, true, SHORT ? 8 : 4);
+      else
+        ROW(512, 8, true, SHORT ? 8 : 4);
+      logp_join_kernel<T, ONE, TOP><<<(unsigned)rows, 256, 0, stream>>>(a);
+    } else if (cut.threads == 256) {
+      if (cut.pieces == 1)
+        ROW(256, 1, false, 8);
+      else if (cut.pieces == 2)
+        ROW(256, 2, false, 8);
+      else
+        ROW(256, 4, false, SHORT ? 8 : (TOP ? 5 : 6));
+    } else if (cut.pieces == 4) {
       ROW(512, 4, false, SHORT ? 8 : 6);
-    else
+    } else if (cut.pieces == 6) {
+      ROW(512, 6, false, SHORT ? 8 : 4);
+    } else {
       ROW(512, 8, false, SHORT ? 8 : 4);
+    }
 #undef ROW
-    if (chunk) logp_join_kernel<T, ONE, TOP><<<(unsigned)rows, 256, 0, stream>>>(a);
   }
   return hipGetLastError();
 }
@@ -624,17 +626,8 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
   const float m = a.stats[3 * row], L = a.stats[3 * row + 1], B = a.stats[3 * row + 2];
   const float gh = a.gh ? a.gh[row] : 0.0f;
   Raw8<std::conditional_t<ONE, T, float>> v[CH];
+  logits<T, ONE, NT>(a, z, lo, v);
   const bool whole = lo + NT * CH * 8 <= a.vocab;
-  if (whole) {
-#pragma unroll
-    for (int c = 0; c < CH; ++c) v[c] = logits8<T, ONE, true>(a, z, lo + (c * NT + threadIdx.x) * 8);
-  } else {
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      const int64_t col = lo + (int64_t)(c * NT + (int)threadIdx.x) * 8;
-      if (col < a.vocab) v[c] = logits8<T, ONE>(a, z, col);
-    }
-  }
   if constexpr (NT > 64)
     __syncthreads();
   else
@@ -686,7 +679,7 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
 
 template <typename T, bool ONE>
 hipError_t run_bwd(LogpArgs a, hipStream_t stream) {
-  const bool small = a.vocab <= 512 && a.given <= 8;
+  const bool small = a.vocab <= 512;
   const int per = small ? 512 : 8192;
   a.chunks = (a.vocab + per - 1) / per;
   const int64_t most = LAUNCH_MAX / a.chunks > 0 ? LAUNCH_MAX / a.chunks : 1;
@@ -694,10 +687,12 @@ hipError_t run_bwd(LogpArgs a, hipStream_t stream) {
     const int64_t rows = a.rows - a.first < most ? a.rows - a.first : most;
     const unsigned grid = (unsigned)(rows * a.chunks);
     const int space = 8 * a.given;
-    if (a.given > 8)
-      logp_bwd_kernel<T, ONE, 256, 4, false><<<grid, 256, space, stream>>>(a);
+    if (small && a.given > 8)
+      logp_bwd_kernel<T, ONE, 64, 1, false><<<grid, 64, space, stream>>>(a);
     else if (small)
       logp_bwd_kernel<T, ONE, 64, 1, true><<<grid, 64, space, stream>>>(a);
+    else if (a.given > 8)
+      logp_bwd_kernel<T, ONE, 256, 4, false><<<grid, 256, space, stream>>>(a);
     else
       logp_bwd_kernel<T, ONE, 256, 4, true><<<grid, 256, space, stream>>>(a);
   }
@@ -727,9 +722,9 @@ int64_t parts_bytes(int64_t parts) { return (parts * (int64_t)sizeof(Part) + 15)
 }  // namespace
 
 int64_t logprobs_workspace_bytes(int64_t rows, int64_t vocab, int64_t top) {
-  const int chunk = chunk_of(rows, vocab);
-  if (!chunk) return 0;
-  const int64_t parts = rows * ((vocab + chunk - 1) / chunk);
+  const int chunks = cut_of(rows, vocab).chunks;
+  if (chunks == 1) return 0;
+  const int64_t parts = rows * chunks;
   return parts_bytes(parts) + parts * top * 8;
 }
 
@@ -737,8 +732,8 @@ hipError_t launch_logprobs_fwd(int dtype, int nc, int64_t rows, int64_t vocab, i
                                const void *ids, double temperature, void *ws, void *logp, void *entropy, void *top_ids,
                                void *top_logp, void *stats, hipStream_t stream) {
   LogpArgs a = args_of(nc, rows, vocab, given, z, ids, temperature);
-  const int chunk = chunk_of(rows, vocab);
-  a.chunks = chunk ? (int)((vocab + chunk - 1) / chunk) : 1;
+  const Cut cut = cut_of(rows, vocab);
+  a.chunks = cut.chunks;
   a.top = (int)top;
   a.parts = (Part *)ws;
   a.keys = (uint64_t *)((char *)ws + parts_bytes(rows * a.chunks));
@@ -749,8 +744,8 @@ hipError_t launch_logprobs_fwd(int dtype, int nc, int64_t rows, int64_t vocab, i
   a.stats_out = (float *)stats;
   const auto go = [&](auto zero) {
     using T = decltype(zero);
-    if (nc == 1) return top > 0 ? run_fwd<T, true, true>(a, stream) : run_fwd<T, true, false>(a, stream);
-    return top > 0 ? run_fwd<T, false, true>(a, stream) : run_fwd<T, false, false>(a, stream);
+    if (nc == 1) return top > 0 ? run_fwd<T, true, true>(a, cut, stream) : run_fwd<T, true, false>(a, cut, stream);
+    return top > 0 ? run_fwd<T, false, true>(a, cut, stream) : run_fwd<T, false, false>(a, cut, stream);
   };
   if (dtype == LM_F16) return go((_Float16)0.0f);
   if (dtype == LM_BF16) return go((__bf16)0.0f);

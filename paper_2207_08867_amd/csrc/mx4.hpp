@@ -59,20 +59,46 @@ __device__ inline Raw8<T> load8_tail(const T *p, int64_t left) {
   return r;
 }
 
-// Eight elements from column col < n of a row of n >= 8, those past n as `fill`.  The load itself has no other form
-// for the row's end, where it starts early and its elements move down: a second form between a wavefront's
-// loads makes it wait for each of them (a 4096 x 4096 bfloat16 norm 41 us, 27 so).  EVEN: n is a multiple of 8.
+// Eight elements from column col of a row of n >= 8, as many as are left of it last and then others in front of them;
+// load8_settle moves those down, where `left` are wanted, and fills up.  Apart, so that a wavefront's loads all go out
+// before the first of them is looked at: a second form of a load, or a move right behind it, makes the wavefront wait
+// there (a 4096 x 4096 bfloat16 norm 41 us, 27 so).
+template <typename T>
+__device__ inline Raw8<T> load8_clamped(const T *row, int64_t col, int64_t n) {
+  // rows have at most 2^30 elements: a 32-bit offset to the row's start
+  const uint32_t at = (uint32_t)(col < n - 8 ? col : n - 8) * (uint32_t)sizeof(T);
+  return load8(reinterpret_cast<const T *>(reinterpret_cast<const char *>(row) + at));
+}
+template <typename T>
+__device__ inline void load8_settle(Raw8<T> &r, int64_t left, T fill) {
+  if (!__any(left < 8)) return;  // a scalar branch: nothing of what follows elsewhere
+  constexpr int W = sizeof(r) / 4;
+  // whole words, so that 16-bit elements stay packed
+  uint32_t w[W], f;
+  __builtin_memcpy(w, &r, sizeof(r));
+  if constexpr (sizeof(T) == 2)
+    f = (uint32_t)__builtin_bit_cast(uint16_t, fill) * 0x10001u;
+  else
+    f = __builtin_bit_cast(uint32_t, fill);
+  const uint32_t over = left >= 8 ? 0u : (left > 0 ? (uint32_t)(8 - left) : 8u);
+#pragma unroll
+  for (int b = W; b; b >>= 1) {  // words
+    const bool go = over & (uint32_t)(b * 8 / W);
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = go ? (i + b < W ? w[i + b] : f) : w[i];
+  }
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = over & 1 ? __builtin_amdgcn_alignbit(i + 1 < W ? w[i + 1] : f, w[i], 16) : w[i];
+  }
+  __builtin_memcpy(&r, w, sizeof(r));
+}
+// Both.  EVEN: n is a multiple of 8 and col < n.
 template <bool EVEN, typename T>
 __device__ inline Raw8<T> load8_row(const T *row, int64_t col, int64_t n, T fill) {
   if constexpr (EVEN) return load8(row + col);
-  const int over = n - col < 8 ? (int)(col + 8 - n) : 0;
-  Raw8<T> r = load8(row + col - over);
-  if (over) {
-#pragma unroll
-    for (int b = 4; b; b >>= 1)
-#pragma unroll
-      for (int i = 0; i < 8; ++i) r.v[i] = over & b ? (i + b < 8 ? r.v[i + b] : fill) : r.v[i];
-  }
+  Raw8<T> r = load8_clamped(row, col, n);
+  load8_settle(r, n - col, fill);
   return r;
 }
 

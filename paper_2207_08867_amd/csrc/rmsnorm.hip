@@ -247,9 +247,16 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT, OCC) void norm16_kernel(NormAr
     const int col = column(c), left = n - col;
 #pragma unroll
     for (int i = 0; i < 8; ++i) hr[c].v[i] = (T)0.0f;
-    if (left <= 0) continue;
-    hr[c] = load8_row<EVEN>(h, col, n, (T)0.0f);
-    if (a.x) xr[c] = load8_row<EVEN>(x, col, n, (T)0.0f);
+    if (EVEN && left <= 0) continue;
+    hr[c] = EVEN ? load8(h + col) : load8_clamped(h, col, n);
+    if (a.x) xr[c] = EVEN ? load8(x + col) : load8_clamped(x, col, n);
+  }
+  if constexpr (!EVEN) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      load8_settle(hr[c], n - column(c), (T)0.0f);
+      if (a.x) load8_settle(xr[c], n - column(c), (T)0.0f);
+    }
   }
   // p of a piece; the weight is read again, from the first-level cache as a rule
   const auto weighed = [&](int c, float p[8]) {
@@ -632,7 +639,6 @@ __global__ __launch_bounds__(256) void norm_bwd_long_dw_kernel(NormBwdArgs a) {
   const int64_t col = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8;
   if (col >= a.n) return;
   double sum[8] = {0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0, 0.0};
-#pragma unroll 2
   for (int64_t row = blockIdx.y; row < a.rows; row += a.groups) {
     double v[8], d[8];
     planes8<END_ODD>(reinterpret_cast<const T *>(a.h) + row * a.n, a.plane, a.nc, col, a.n, v);

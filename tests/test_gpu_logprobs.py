@@ -252,7 +252,8 @@ def test_many_short_rows(mcf):
     dz = mcf.mc_logprobs_bwd(z, ids, stats)
     want = torch.log_softmax(z.double(), -1)
     assert bool(((logp[:, 0].double() - want.gather(1, ids.long())[:, 0]).abs() < 1e-5).all())
-    assert torch.equal(ti.long(), want.topk(2).indices)
+    # among millions of rows some have equal logits, whose order torch's topk leaves open
+    assert torch.equal(ti.long(), torch.sort(z, dim=-1, descending=True, stable=True).indices[:, :2])
     assert bool(((dz.double() + want.exp() - torch.nn.functional.one_hot(ids[:, 0].long(), V)).abs() < 1e-5).all())
 
 
