@@ -35,7 +35,7 @@ struct LogpArgs {
   float *logp, *entropy, *top_logp, *stats_out;
   int32_t *top_ids;
   Part *parts;     // [rows][chunks], where a row is several workgroups'
-  uint64_t *keys;  // [rows][chunks][top]
+  uint64_t *keys;  // [rows][top][chunks]: the chunks' largest keys first, which so fall to different threads
   const float *stats, *g, *gh;
   void *dz;
   int64_t rows, plane;
@@ -508,7 +508,7 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
   if constexpr (TOP) {
     select_logits<NT, CH>(sel, pool, a.top, v, own, lo, [&](int i, uint64_t key) {
       if constexpr (SPLIT)
-        a.keys[(row * a.chunks + chunk) * a.top + i] = key;
+        a.keys[(row * a.top + i) * a.chunks + chunk] = key;
       else
         put_top(a, row, result, i, key);
     });
@@ -555,13 +555,15 @@ __global__ __launch_bounds__(256) void logp_join_kernel(LogpArgs a) {
 }
 
 // How a row is cut into chunks of `pieces` pieces of 8 logits for each of the threads.  A row is one workgroup's while
-// it fits 8 pieces of 512 threads, else it is cut into chunks alike; rows of a few are cut into chunks of 4096 logits.
+// it fits 8 pieces of 512 threads, else it is cut into chunks alike, or, where there would be few of them, of 4096
+// logits.
+constexpr int MANY = 128;
 struct Cut {
   int threads, pieces, chunks;
 };
 Cut cut_of(int64_t rows, int64_t vocab) {
   const auto up = [](int64_t n, int64_t d) { return (int)((n + d - 1) / d); };
-  if (vocab > 8192 && rows < 256) return {256, 2, up(vocab, 4096)};
+  if (vocab > 32768 && rows * up(vocab, 32768) < MANY) return {256, 2, up(vocab, 4096)};
   if (vocab <= 8192) return {256, vocab <= 2048 ? 1 : (vocab <= 4096 ? 2 : 4), 1};
   const int chunks = up(vocab, 32768), pieces = up(up(vocab, chunks), 4096);
   return {512, pieces <= 4 && chunks == 1 ? 4 : (pieces <= 6 ? 6 : 8), chunks};
@@ -679,22 +681,28 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
 
 template <typename T, bool ONE>
 hipError_t run_bwd(LogpArgs a, hipStream_t stream) {
-  const bool small = a.vocab <= 512;
-  const int per = small ? 512 : 8192;
+  // threads and pieces by the row's length: lanes past its end load its end again
+  const bool small = a.vocab <= 512, middle = !small && a.vocab <= 2048;
+  const int per = small ? 512 : (middle ? 2048 : 8192);
   a.chunks = (a.vocab + per - 1) / per;
   const int64_t most = LAUNCH_MAX / a.chunks > 0 ? LAUNCH_MAX / a.chunks : 1;
   for (a.first = 0; a.first < a.rows; a.first += most) {
     const int64_t rows = a.rows - a.first < most ? a.rows - a.first : most;
     const unsigned grid = (unsigned)(rows * a.chunks);
     const int space = 8 * a.given;
-    if (small && a.given > 8)
-      logp_bwd_kernel<T, ONE, 64, 1, false><<<grid, 64, space, stream>>>(a);
-    else if (small)
-      logp_bwd_kernel<T, ONE, 64, 1, true><<<grid, 64, space, stream>>>(a);
-    else if (a.given > 8)
-      logp_bwd_kernel<T, ONE, 256, 4, false><<<grid, 256, space, stream>>>(a);
-    else
-      logp_bwd_kernel<T, ONE, 256, 4, true><<<grid, 256, space, stream>>>(a);
+#define ROW(NT, CH)                                                                     \
+  if (a.given > 8)                                                                      \
+    logp_bwd_kernel<T, ONE, NT, CH, false><<<grid, NT, space, stream>>>(a);             \
+  else                                                                                  \
+    logp_bwd_kernel<T, ONE, NT, CH, true><<<grid, NT, space, stream>>>(a)
+    if (small) {
+      ROW(64, 1);
+    } else if (middle) {
+      ROW(256, 1);
+    } else {
+      ROW(256, 4);
+    }
+#undef ROW
   }
   return hipGetLastError();
 }
