@@ -306,9 +306,10 @@ struct Pool {
 // thread's largest, own (at least -FLT_MAX); first: the index of thread 0's first.  A bound that at least k of 256
 // groups' largest logits reach bounds the k-th largest logit from below.  The threads with a logit that reaches it, k
 // and a few more as a rule, hand theirs to the workgroup, which looks through them and ranks those that reach it.
-template <int NT, int CH, typename H, typename Out>
+// again(c) reads the thread's piece c once more.
+template <int NT, int CH, typename H, typename Again, typename Out>
 __device__ inline void select_logits(Select &sh, Pool<CH, H> &pool, int k, const Raw8<H> (&v)[CH], float own,
-                                     uint32_t first, Out out) {
+                                     uint32_t first, Again again, Out out) {
   constexpr int PER = NT / GROUPS;
   static_assert(PER >= 1 && NT % GROUPS == 0 && GROUPS > LOGP_TOP, "a group has whole threads");
   const float big = lanes_max<PER>(own);
@@ -347,13 +348,14 @@ __device__ inline void select_logits(Select &sh, Pool<CH, H> &pool, int k, const
   int n = sh.n;
   if (slots > POOL || n > KEEP) {
     // Many equal logits at the bound, or a row whose order follows the threads'.  The k-th largest logit by
-    // bisection over all of them; the larger ones, fewer than k, and the first of those equal to it.
+    // bisection over all of them; the larger ones, fewer than k, and the first of those equal to it.  The row is read
+    // again, so that it need not stay in registers behind the rest.
     const uint32_t mine0 = first + threadIdx.x * 8;
     const auto count = [&](auto test) {
       int n = 0;
-#pragma unroll
+#pragma unroll 1
       for (int c = 0; c < CH; ++c) {
-        const Raw8<H> u = renewed(v[c]);
+        const Raw8<H> u = again(c);
 #pragma unroll
         for (int i = 0; i < 8; ++i) n += __popcll(__ballot(test((float)u.v[i])));
       }
@@ -367,27 +369,23 @@ __device__ inline void select_logits(Select &sh, Pool<CH, H> &pool, int k, const
     __syncthreads();
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
-    if (own > bound) {
+#pragma unroll 1
+    for (int c = 0; c < CH; ++c) {
+      const Raw8<H> u = again(c);
 #pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        const Raw8<H> u = renewed(v[c]);
-        uint32_t j = mine0 + c * NT * 8;
-        asm volatile("" : "+v"(j));
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if ((float)u.v[i] > bound) {
-            const int at = atomicAdd(&sh.n, 1);
-            if (at < KEEP) sh.kept[at] = key_of((float)u.v[i], j + i);
-          }
-      }
+      for (int i = 0; i < 8; ++i)
+        if ((float)u.v[i] > bound) {
+          const int at = atomicAdd(&sh.n, 1);
+          if (at < KEEP) sh.kept[at] = key_of((float)u.v[i], mine0 + c * NT * 8 + i);
+        }
     }
     __syncthreads();
     n = sh.n;
     if (n < k) {
       int need = k - n;
-#pragma unroll
+#pragma unroll 1
       for (int c = 0; c < CH; ++c) {
-        const Raw8<H> u = renewed(v[c]);
+        const Raw8<H> u = again(c);
         int mine = 0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) mine += (float)u.v[i] == bound;
@@ -402,7 +400,6 @@ __device__ inline void select_logits(Select &sh, Pool<CH, H> &pool, int k, const
         before -= mine;
         for (int w = 0; w < (int)(threadIdx.x >> 6); ++w) before += sh.wave[w];
         uint32_t j = mine0 + c * NT * 8;
-        asm volatile("" : "+v"(j));
 #pragma unroll
         for (int i = 0; i < 8; ++i, ++j)
           if ((float)u.v[i] == bound && before < need) sh.kept[k - need + before++] = key_of(bound, j);
@@ -506,7 +503,12 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
     }
   }
   if constexpr (TOP) {
-    select_logits<NT, CH>(sel, pool, a.top, v, own, lo, [&](int i, uint64_t key) {
+    const auto again = [&](int c) {
+      Raw8<H> u[1];
+      logits<T, ONE, NT>(a, z, lo + c * NT * 8, u);
+      return u[0];
+    };
+    select_logits<NT, CH>(sel, pool, a.top, v, own, lo, again, [&](int i, uint64_t key) {
       if constexpr (SPLIT)
         a.keys[(row * a.top + i) * a.chunks + chunk] = key;
       else
