@@ -74,8 +74,7 @@ __device__ inline int32_t key_index(uint64_t k) { return (int32_t)~(uint32_t)k; 
 
 constexpr int GROUPS = 256;  // of the threads, for the alternatives; above LOGP_TOP
 constexpr int KEEP = 1024;   // candidates
-
-constexpr int RANKS = 512;   // candidates whose ranks all wavefronts count together
+constexpr int RANKS = 256;   // candidates that are ranked, above LOGP_TOP + LOGP_TOP / 8
 
 struct Select {
   union {
@@ -123,36 +122,6 @@ __device__ inline U bound_of_groups(Select &sh, int k) {
   return (U)sh.bound;
 }
 
-// out(r, key) takes the r-th largest of the n <= KEEP kept keys, r < k, and 0 where there is none: ranks by
-// counting, each wavefront a part of the comparisons.
-template <int NT, typename Out>
-__device__ inline void rank_kept(Select &sh, int k, int n, Out out) {
-  constexpr int W = NT / 64;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (n <= RANKS) {
-    const int from = n * wave / W, to = n * (wave + 1) / W;
-    for (int i = lane; i < n; i += 64) {
-      const uint64_t mine = sh.kept[i];
-      int above = 0;
-#pragma unroll 4
-      for (int j = from; j < to; ++j) above += sh.kept[j] > mine;
-      atomicAdd(&sh.rank[i], above);
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += NT)
-      if (sh.rank[i] < k) out(sh.rank[i], sh.kept[i]);
-  } else {
-    for (int i = threadIdx.x; i < n; i += NT) {
-      const uint64_t mine = sh.kept[i];
-      int above = 0;
-#pragma unroll 8
-      for (int j = 0; j < n; ++j) above += sh.kept[j] > mine;
-      if (above < k) out(above, mine);
-    }
-  }
-  for (int r = n + (int)threadIdx.x; r < k; r += NT) out(r, (uint64_t)0);
-}
-
 // The sum of the workgroup's wavefronts' numbers.
 template <int NT>
 __device__ inline int waves_sum(Select &sh, int n) {
@@ -163,6 +132,46 @@ __device__ inline int waves_sum(Select &sh, int n) {
 #pragma unroll
   for (int w = 0; w < NT / 64; ++w) n += sh.wave[w];
   return n;
+}
+
+// out(r, key) takes the r-th largest of the n <= KEEP kept keys, r < k, and 0 where there is none: ranks by
+// counting, each wavefront a part of the comparisons.  They grow with n^2, so that many keys are cut down to little
+// more than k first (1000 candidates for 128 places, 8192 rows: 905 us ranked as they are, 91 us so).
+template <int NT, typename Out>
+__device__ inline void rank_kept(Select &sh, int k, int n, Out out) {
+  static_assert(RANKS >= LOGP_TOP + LOGP_TOP / 8 && KEEP % NT == 0, "what is cut down is ranked");
+  constexpr int W = NT / 64, PER = KEEP / NT;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (n > RANKS) {
+    uint64_t key[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) key[i] = (int)threadIdx.x + i * NT < n ? sh.kept[threadIdx.x + i * NT] : 0;
+    const uint64_t bound = bound_of<uint64_t>(k, k + k / 8, [&](uint64_t b) {
+      int c = 0;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) c += __popcll(__ballot(key[i] >= b));
+      return waves_sum<NT>(sh, c);
+    });
+    if (threadIdx.x == 0) sh.n = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      if (key[i] >= bound) sh.kept[atomicAdd(&sh.n, 1)] = key[i];
+    __syncthreads();
+    n = sh.n;
+  }
+  const int from = n * wave / W, to = n * (wave + 1) / W;
+  for (int i = lane; i < n; i += 64) {
+    const uint64_t mine = sh.kept[i];
+    int above = 0;
+#pragma unroll 4
+    for (int j = from; j < to; ++j) above += sh.kept[j] > mine;
+    atomicAdd(&sh.rank[i], above);
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += NT)
+    if (sh.rank[i] < k) out(sh.rank[i], sh.kept[i]);
+  for (int r = n + (int)threadIdx.x; r < k; r += NT) out(r, (uint64_t)0);
 }
 
 // The first keys of a thread, held in registers.
@@ -303,10 +312,11 @@ struct Pool {
 };
 
 // The k largest of the workgroup's logits by (logit, index), those of -inf apart, where they are held: v, and the
-// thread's largest, own (at least -FLT_MAX); first: the index of thread 0's first.  A bound that at least k of 256
+// thread's largest, own; first: the index of thread 0's first.  A bound that at least k of 256
 // groups' largest logits reach bounds the k-th largest logit from below.  The threads with a logit that reaches it, k
-// and a few more as a rule, hand theirs to the workgroup, which looks through them and ranks those that reach it.
-// again(c) reads the thread's piece c once more.
+// and a few more as a rule, hand theirs to the workgroup, which looks through them and ranks those that reach it.  Where
+// they are more than the pool takes, for about 100 alternatives and up, each reads its logits again and looks through
+// them by itself.  again(c) reads the thread's piece c once more.
 template <int NT, int CH, typename H, typename Again, typename Out>
 __device__ inline void select_logits(Select &sh, Pool<CH, H> &pool, int k, const Raw8<H> (&v)[CH], float own,
                                      uint32_t first, Again again, Out out) {
@@ -325,28 +335,31 @@ __device__ inline void select_logits(Select &sh, Pool<CH, H> &pool, int k, const
       for (int c = 0; c < CH; ++c) pool.piece[at][c] = v[c];
     }
   }
+  const auto keep = [&](const Raw8<H> &u, uint32_t j) {
+    uint32_t mask = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mask |= (float)u.v[e] >= bound ? 1u << e : 0u;
+    if (mask == 0) return;
+    int at = atomicAdd(&sh.n, __popc(mask));
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (mask >> e & 1) {
+        if (at < KEEP) sh.kept[at] = key_of((float)u.v[e], j + e);
+        ++at;
+      }
+  };
   __syncthreads();
   const int slots = sh.slots;
   if (slots <= POOL) {
-    for (int i = threadIdx.x; i < slots * CH; i += NT) {
-      const Raw8<H> u = pool.piece[0][i];
-      uint32_t mask = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) mask |= (float)u.v[e] >= bound ? 1u << e : 0u;
-      if (mask == 0) continue;
-      const uint32_t j = first + (i % CH * NT + pool.owner[i / CH]) * 8;
-      int at = atomicAdd(&sh.n, __popc(mask));
-#pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (mask >> e & 1) {
-          if (at < KEEP) sh.kept[at] = key_of((float)u.v[e], j + e);
-          ++at;
-        }
-    }
-    __syncthreads();
+    for (int i = threadIdx.x; i < slots * CH; i += NT)
+      keep(pool.piece[0][i], first + (i % CH * NT + pool.owner[i / CH]) * 8);
+  } else if (own >= bound) {
+#pragma unroll 1
+    for (int c = 0; c < CH; ++c) keep(again(c), first + (c * NT + threadIdx.x) * 8);
   }
+  __syncthreads();
   int n = sh.n;
-  if (slots > POOL || n > KEEP) {
+  if (n > KEEP) {
     // Many equal logits at the bound, or a row whose order follows the threads'.  The k-th largest logit by
     // bisection over all of them; the larger ones, fewer than k, and the first of those equal to it.  The row is read
     // again, so that it need not stay in registers behind the rest.
@@ -433,14 +446,14 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
   logits<T, ONE, NT>(a, z, lo, v);
   float given = 0.0f;
   if (id >= 0 && id < a.vocab) given = logit<T, ONE>(a, z, id);
-  float own = -FLT_MAX;
+  float own = -INFINITY;
 #pragma unroll
   for (int c = 0; c < CH; ++c)
 #pragma unroll
     for (int i = 0; i < 8; ++i) own = fmaxf(own, (float)v[c].v[i]);
   // Each wavefront's sums relative to its own largest logit, so that it works on its logits while the others'
   // are on their way.
-  const float mw = lanes_max(own);
+  const float mw = lanes_max(fmaxf(own, -FLT_MAX));
   float s = 0.0f, d1 = 0.0f;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
