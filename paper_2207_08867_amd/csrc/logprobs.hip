@@ -51,8 +51,10 @@ __device__ inline float expd(const LogpArgs &a, float d) {
 }
 
 __device__ inline Part join(const LogpArgs &a, const Part &x, const Part &y) {
+  // member by member: a reference to one or the other would put both into memory
   const bool first = x.m >= y.m;
-  const Part &hi = first ? x : y, &lo = first ? y : x;
+  const Part hi = {first ? x.m : y.m, first ? x.s : y.s, first ? x.a : y.a};
+  const Part lo = {first ? y.m : x.m, first ? y.s : x.s, first ? y.a : x.a};
   if (lo.s == -1.0f) return hi.s == -1.0f ? lo : hi;
   if (hi.s == -1.0f) return lo;
   const float d = hi.m - lo.m, f = expd(a, d), n = 1.0f + lo.s;
@@ -555,7 +557,9 @@ __global__ __launch_bounds__(256) void logp_join_kernel(LogpArgs a) {
   for (int d = 1; d < 64; d <<= 1) {
     const Part o = {__shfl_xor(p.m, d), __shfl_xor(p.s, d), __shfl_xor(p.a, d)};
     // both sides join in the lower lane's order, so the lanes agree
-    p = (threadIdx.x & d) ? join(a, o, p) : join(a, p, o);
+    const bool upper = threadIdx.x & d;
+    p = join(a, Part{upper ? o.m : p.m, upper ? o.s : p.s, upper ? o.a : p.a},
+             Part{upper ? p.m : o.m, upper ? p.s : o.s, upper ? p.a : o.a});
   }
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = p;
   __syncthreads();

@@ -371,7 +371,8 @@ hipError_t run_norm(NormArgs a, hipStream_t stream) {
   const int64_t width = INT8 ? a.pitch : a.n;
   const auto pick = [&](auto end) {
     constexpr End E = decltype(end)::value;
-    if constexpr (ONE && sizeof(T) == 2 && E != END_SHORT) {
+    constexpr bool PLAIN16 = ONE && sizeof(T) == 2 && E != END_SHORT;
+    if constexpr (PLAIN16) {
 #define ROW(NT, CH) return go(norm16_kernel<T, NT, CH, NORM, INT8, E == END_EVEN, 8>, NT)
       if (width <= 128) ROW(16, 1);
       if (width <= 512) ROW(64, 1);
@@ -383,13 +384,17 @@ hipError_t run_norm(NormArgs a, hipStream_t stream) {
 #undef ROW
     }
 #define ROW(NT, CH) return go(norm_kernel<T, ONE, NT, CH, NORM, INT8, E>, NT)
-    if (E == END_SHORT || width <= 128) ROW(16, 1);
-    if constexpr (E != END_SHORT) {
-      if (width <= 512) ROW(64, 1);
-      if (width <= 2048) ROW(256, 1);
-      if (width <= 4096) ROW(512, 1);
-      if (width <= 8192) ROW(1024, 1);
-      if (width <= 16384) ROW(1024, 2);
+    if constexpr (E == END_SHORT) {
+      ROW(16, 1);
+    } else {
+      if constexpr (!PLAIN16) {
+        if (width <= 128) ROW(16, 1);
+        if (width <= 512) ROW(64, 1);
+        if (width <= 2048) ROW(256, 1);
+        if (width <= 4096) ROW(512, 1);
+        if (width <= 8192) ROW(1024, 1);
+        if (width <= 16384) ROW(1024, 2);
+      }
       ROW(1024, 0);
     }
 #undef ROW
