@@ -358,6 +358,13 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT, OCC) void norm16_kernel(NormAr
   }
 }
 
+// Threads and pieces of 8 elements by the row's length and the types alone, so that a row's result is the same alone
+// and among others.  Two pieces: half the wavefronts to join and twice the loads on their way; one: less to wait for in a
+// row alone.  One and two pieces (us, in a graph, with x into 8 bits unless said):
+//   bfloat16, 16 x 4096 3.8 and 4.5; 8192 x 1024 14.2 and 14.7, without 8 bits 13.1 and 12.3; 4096 x 4099 45 and 41;
+//     4096 x 4096 28.5 and 29.3, quantisation alone 17.7 and 13.5; four pieces 45 and 16.6
+//   two binary16 planes, 4096 x 4096 59 and 49, 16 x 4096 5.2 and 6.0; three, 8192 x 1024 49 and 33
+//   binary32, 4096 x 4096 45 and 46, without 8 bits 49 and 53, quantisation alone 25 and 17.
 template <typename T, bool ONE, bool NORM, bool INT8>
 hipError_t run_norm(NormArgs a, hipStream_t stream) {
   const auto go = [&](auto kernel, int nt) {
@@ -372,30 +379,26 @@ hipError_t run_norm(NormArgs a, hipStream_t stream) {
   const auto pick = [&](auto end) {
     constexpr End E = decltype(end)::value;
     constexpr bool PLAIN16 = ONE && sizeof(T) == 2 && E != END_SHORT;
-    if constexpr (PLAIN16) {
-#define ROW(NT, CH) return go(norm16_kernel<T, NT, CH, NORM, INT8, E == END_EVEN, 8>, NT)
-      if (width <= 128) ROW(16, 1);
-      if (width <= 512) ROW(64, 1);
-      if (width <= 1024) ROW(64, 2);
-      if (width <= 2048) ROW(128, 2);
-      if (width <= 4096) ROW(256, 2);
-      if (width <= 8192) ROW(512, 2);
-      if (width <= 16384) ROW(1024, 2);
-#undef ROW
-    }
-#define ROW(NT, CH) return go(norm_kernel<T, ONE, NT, CH, NORM, INT8, E>, NT)
+#define ROW(NT, CH) \
+  if constexpr (PLAIN16) return go(norm16_kernel<T, NT, CH, NORM, INT8, E == END_EVEN, 8>, NT); \
+  else return go(norm_kernel<T, ONE, NT, CH, NORM, INT8, E>, NT)
     if constexpr (E == END_SHORT) {
-      ROW(16, 1);
+      return go(norm_kernel<T, ONE, 16, 1, NORM, INT8, E>, 16);
     } else {
-      if constexpr (!PLAIN16) {
-        if (width <= 128) ROW(16, 1);
-        if (width <= 512) ROW(64, 1);
-        if (width <= 2048) ROW(256, 1);
-        if (width <= 4096) ROW(512, 1);
-        if (width <= 8192) ROW(1024, 1);
-        if (width <= 16384) ROW(1024, 2);
+      if (width <= 128) { ROW(16, 1); }
+      if (width <= 512) { ROW(64, 1); }
+      if constexpr (ONE && sizeof(T) == 4 && NORM) {
+        if (width <= 2048) { ROW(256, 1); }
+        if (width <= 4096) { ROW(512, 1); }
+        if (width <= 8192) { ROW(1024, 1); }
+      } else {
+        if (width <= 1024) { ROW(64, 2); }
+        if (width <= 2048) { ROW(128, 2); }
+        if (width <= 4096) { ROW(256, 2); }
+        if (width <= 8192) { ROW(512, 2); }
       }
-      ROW(1024, 0);
+      if (width <= 16384) { ROW(1024, 2); }
+      return go(norm_kernel<T, ONE, 1024, 0, NORM, INT8, E>, 1024);
     }
 #undef ROW
   };
@@ -679,11 +682,13 @@ __global__ __launch_bounds__(1024) void norm_bwd_sum_kernel(NormBwdArgs a) {
 
 constexpr int64_t BWD_LONG = 16384;  // the longest row that stays in registers
 
-// Workgroups: two a CU of long rows, whose next rows are on their way, four of short ones; of rows that do not stay,
-// parts of the rows for dw.
+// Workgroups: as many as are resident, since a row's loads go out ahead of the row before: one a CU of rows that
+// take 1024 threads, two of 512, four of shorter rows.  With twice (half) as many (us; 4096 x 4096 bfloat16, with g) 46 (49)
+// in place of 40, 8192 x 1024 32 (33) in place of 26, 4096 x 8192 78 in place of 69.  Of rows that do not stay in
+// registers, parts of the rows for dw.
 int bwd_groups(int64_t rows, int64_t n) {
   if (n > BWD_LONG) return (int)(rows < 64 ? rows : 64);
-  const int64_t slots = n <= 128 ? 16 : (n <= 512 ? 4 : 1), most = n <= 2048 ? 1024 : 512, wanted = (rows + slots - 1) / slots;
+  const int64_t slots = n <= 128 ? 16 : (n <= 512 ? 4 : 1), most = n <= 2048 ? 1024 : (n <= 4096 ? 512 : 256), wanted = (rows + slots - 1) / slots;
   return (int)(wanted < most ? wanted : most);
 }
 
