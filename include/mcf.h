@@ -526,7 +526,8 @@ int64_t mc_int8_linear_fwd_workspace(int dtype, int64_t batch, int64_t in, int64
  * Without x, v is the sum of h's planes and h_out must be NULL.
  * h: [nc][rows][n] (a plain stream: nc = 1); x: [rows][n] or NULL; w: [n] or NULL for ones; h_out:
  * [nc][rows][n], may be h itself (in place); y: [rows][n].  Everything between the loads and the
- * roundings is binary64.  n >= 1, eps >= 0 and finite. */
+ * roundings is binary64, but that y of a plain 16-bit stream is rounded from a binary32 number
+ * within 2^-23 of v_i w_i r.  A row's result does not depend on the other rows.  A row of zeros with eps = 0 has r = inf and so NaN.  n >= 1, eps >= 0 and finite. */
 int mc_rmsnorm_fwd(int dtype, int nc, int64_t rows, int64_t n, const void *h, const void *x, const void *w, double eps,
                    void *h_out, void *y, void *stream);
 
@@ -565,8 +566,8 @@ int64_t mc_rmsnorm_bwd_workspace(int dtype, int64_t rows, int64_t n);
  *   binary32 [rows][top], 0 <= top <= 128.
  * stats: binary32 [rows][3] or NULL, for the gradient: the row's largest logit m, L = log sum_j
  *   exp((z_j - m) / T), and entropy - L.
- * Statistics and sums are binary32; the log probability of a token the row is sure of keeps its relative
- * accuracy.  No output may overlap an input or another output.  rows < 2^31,
+ * Statistics and sums are binary32, summed in an order that depends on rows and vocab alone; the log
+ * probability of a token the row is sure of keeps its relative accuracy.  No output may overlap an input or another output.  rows < 2^31,
  * 1 <= vocab <= 2^30.  Workspace as for the MXFP4 calls. */
 int mc_logprobs_fwd(int dtype, int nc, int64_t rows, int64_t vocab, int64_t given, int64_t top, const void *z,
                     const void *ids, double temperature, void *workspace, int64_t workspace_bytes, void *logp,
