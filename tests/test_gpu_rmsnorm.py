@@ -4,7 +4,8 @@ against plain binary64 forms.
 The stream behind the addition and the codes are fixed functions of the input and must come out exactly.
 Tolerances: everything else is binary64 until it is rounded to binary32 and from there to the format,
 so a value is within |v| (2^-24 + U) of its own, and sums of n terms in binary64 add n 2^-53 of the
-terms' magnitudes.  dw's sums of a workgroup's rows are kept in binary32 each: 2^-24 of the magnitudes."""
+terms' magnitudes.  (y of a plain 16-bit row is a binary32 product with a rounded factor first: 2^-23, where a
+hundredth of U is 2^-18 or more.)  dw's sums of a workgroup's rows are kept in binary32 each: 2^-24 of the magnitudes."""
 import numpy as np
 import pytest
 
@@ -224,6 +225,25 @@ def test_no_rows(mcf):
         h = torch.empty(0, n, device="cuda")
         dh, dw = mcf.mc_rmsnorm_bwd(h, None, h)
         assert dh.shape == (0, n) and dw.shape == (n,) and not dw.any()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("nc", [1, 2])
+@pytest.mark.parametrize("n", [5, 200, 1000, 1023, 4096, 5000, 20000])
+def test_a_row_alone(mcf, dtype, nc, n):
+    """A row's results have the same bits alone, among few and among many."""
+    import torch
+
+    h, x, w = (dev(t, dtype) for t in tensors(n, 300, n, nc, dtype, True))
+    (codes, scales), stream = mcf.mc_rmsnorm_int8(h, w, x=x, eps=EPS, h_mc=True)
+    y, _ = mcf.mc_rmsnorm_fwd(h, w, x=x, eps=EPS, h_mc=True)
+    dx, _ = mcf.mc_rmsnorm_bwd(stream, w, x, eps=EPS, h_mc=True)
+    for lo, hi in ((7, 8), (120, 137)):
+        a, b = h[:, lo:hi].contiguous(), x[lo:hi].contiguous()
+        (c, s), st = mcf.mc_rmsnorm_int8(a, w, x=b, eps=EPS, h_mc=True)
+        assert torch.equal(c, codes[lo:hi]) and torch.equal(s, scales[lo:hi]) and torch.equal(st, stream[:, lo:hi])
+        assert torch.equal(mcf.mc_rmsnorm_fwd(a, w, x=b, eps=EPS, h_mc=True)[0], y[lo:hi])
+        assert torch.equal(mcf.mc_rmsnorm_bwd(st, w, b, eps=EPS, h_mc=True)[0], dx[lo:hi])
 
 
 def test_many_short_rows(mcf):
