@@ -83,7 +83,7 @@ int mc_rmsnorm_int8(int dtype, int nc, int64_t rows, int64_t n, const void *h, c
 
 int64_t mc_rmsnorm_bwd_workspace(int dtype, int64_t rows, int64_t n) {
   const int st = norm_check(dtype, 1, rows, n, 0.0);
-  return st != MCF_OK ? st : mcf::rmsnorm_bwd_workspace_bytes(rows, n);
+  return st != MCF_OK ? st : mcf::rmsnorm_bwd_workspace_bytes(dtype, rows, n);
 }
 
 int mc_rmsnorm_bwd(int dtype, int nc, int64_t rows, int64_t n, const void *h, const void *w, const void *dy,
@@ -94,7 +94,7 @@ int mc_rmsnorm_bwd(int dtype, int nc, int64_t rows, int64_t n, const void *h, co
   if (rows == 0) dh = nullptr;
   if (!dh && !dw) return MCF_OK;
   if (rows > 0 && (!h || !dy)) return MCF_E_NULL;
-  const int64_t wb = dw ? mcf::rmsnorm_bwd_workspace_bytes(rows, n) : 0;
+  const int64_t wb = dw ? mcf::rmsnorm_bwd_workspace_bytes(dtype, rows, n) : 0;
   const int ws = workspace_check(workspace, workspace_bytes, wb);
   if (ws != MCF_OK) return ws;
   const int64_t es = elem_size(dtype), plane = rows * n * es;

@@ -85,7 +85,8 @@ constexpr int RANKS = 256;   // candidates that are ranked, above LOGP_TOP + LOG
 
 struct Select {
   union {
-    uint64_t group[GROUPS];
+    uint64_t group[GROUPS];      // of keys
+    uint32_t logit[2 * GROUPS];  // the threads' largest logits, of which threads GROUPS apart are a group
     int rank[RANKS];  // once the groups are done with
   };
   uint64_t kept[KEEP];
@@ -108,14 +109,22 @@ __device__ inline U bound_of(int k, int few, Count count) {
   return b;
 }
 
-// The same of the 256 groups' numbers in sh.group, by one wavefront, for all.
+// The same of the 256 groups' numbers, in sh.group or sh.logit, by one wavefront, for all.
 template <int NT, typename U>
 __device__ inline U bound_of_groups(Select &sh, int k) {
   __syncthreads();
   if (threadIdx.x < 64) {
     U g[GROUPS / 64];
 #pragma unroll
-    for (int i = 0; i < GROUPS / 64; ++i) g[i] = (U)sh.group[threadIdx.x + 64 * i];
+    for (int i = 0; i < GROUPS / 64; ++i) {
+      const int at = threadIdx.x + 64 * i;
+      if constexpr (sizeof(U) == 8) {
+        g[i] = sh.group[at];
+      } else {
+        g[i] = sh.logit[at];
+        if (NT > GROUPS) g[i] = sh.logit[at + GROUPS] > g[i] ? sh.logit[at + GROUPS] : g[i];
+      }
+    }
     const U b = bound_of<U>(k, k + k / 8, [&](U b) {
       int n = 0;
 #pragma unroll
@@ -327,10 +336,8 @@ struct Pool {
 template <int NT, int CH, typename H, typename Again, typename Out>
 __device__ inline void select_logits(Select &sh, Pool<CH, H> &pool, int k, const Raw8<H> (&v)[CH], float own,
                                      uint32_t first, Again again, Out out) {
-  constexpr int PER = NT / GROUPS;
-  static_assert(PER >= 1 && NT % GROUPS == 0 && GROUPS > LOGP_TOP, "a group has whole threads");
-  const float big = lanes_max<PER>(own);
-  if (threadIdx.x % PER == 0) sh.group[threadIdx.x / PER] = ordered(big);
+  static_assert((NT == GROUPS || NT == 2 * GROUPS) && GROUPS > LOGP_TOP, "a group has one or two threads");
+  sh.logit[threadIdx.x] = ordered(own);
   const uint32_t b = bound_of_groups<NT, uint32_t>(sh, k);
   const uint32_t lowest = ordered(-FLT_MAX);
   float bound = ordered_value(b < lowest ? lowest : b);
@@ -587,7 +594,8 @@ __global__ __launch_bounds__(256) void logp_join_kernel(LogpArgs a) {
 
 // How a row is cut into chunks of `pieces` pieces of 8 logits for each of the threads.  A row is one workgroup's while
 // it fits 8 pieces of 512 threads, else it is cut into chunks alike, or, where there would be few of them, of 4096
-// logits.  One workgroup and chunks of 4096 (us, in a graph): 1 x 32000 with 20 alternatives 12.0 and 15.3, 128 x
+// logits.  The pieces follow the length, as lanes past a row's end cost as much as others (8184 x 8200 binary32 with 64
+// alternatives in three pieces 97 us, in four 141).  One workgroup and chunks of 4096 (us, in a graph): 1 x 32000 with 20 alternatives 12.0 and 15.3, 128 x
 // 32768 8.1 and 11.0; chunks of 32768 and of 4096: 1 x 131072 11.5 and 9.0, 64 x 131072 the same within 3%.
 constexpr int MANY = 128;
 struct Cut {
@@ -596,9 +604,9 @@ struct Cut {
 Cut cut_of(int64_t rows, int64_t vocab) {
   const auto up = [](int64_t n, int64_t d) { return (int)((n + d - 1) / d); };
   if (vocab > 32768 && rows * up(vocab, 32768) < MANY) return {256, 2, up(vocab, 4096)};
-  if (vocab <= 8192) return {256, vocab <= 2048 ? 1 : (vocab <= 4096 ? 2 : 4), 1};
-  const int chunks = up(vocab, 32768), pieces = up(up(vocab, chunks), 4096);
-  return {512, pieces <= 4 && chunks == 1 ? 4 : (pieces <= 6 ? 6 : 8), chunks};
+  if (vocab <= 8192) return {256, up(vocab, 2048), 1};
+  const int chunks = up(vocab, 32768);
+  return {512, up(up(vocab, chunks), 4096), chunks};
 }
 
 template <typename T, bool ONE, bool TOP>
@@ -612,8 +620,12 @@ hipError_t run_fwd(LogpArgs a, const Cut &cut, hipStream_t stream) {
     if (a.chunks > 1) {
       if (cut.threads == 256)
         ROW(256, 2, true, 8);
+      else if (cut.pieces == 5)
+        ROW(512, 5, true, SHORT ? 8 : 4);
       else if (cut.pieces == 6)
         ROW(512, 6, true, SHORT ? 8 : 4);
+      else if (cut.pieces == 7)
+        ROW(512, 7, true, SHORT ? 8 : 4);
       else
         ROW(512, 8, true, SHORT ? 8 : 4);
       logp_join_kernel<T, ONE, TOP><<<(unsigned)rows, 256, 0, stream>>>(a);
@@ -622,12 +634,20 @@ hipError_t run_fwd(LogpArgs a, const Cut &cut, hipStream_t stream) {
         ROW(256, 1, false, 8);
       else if (cut.pieces == 2)
         ROW(256, 2, false, 8);
+      else if (cut.pieces == 3)
+        ROW(256, 3, false, SHORT ? 8 : 6);
       else
         ROW(256, 4, false, SHORT ? 8 : (TOP ? 5 : 6));
+    } else if (cut.pieces == 3) {
+      ROW(512, 3, false, SHORT ? 8 : 6);
     } else if (cut.pieces == 4) {
       ROW(512, 4, false, SHORT ? 8 : 6);
+    } else if (cut.pieces == 5) {
+      ROW(512, 5, false, SHORT ? 8 : 4);
     } else if (cut.pieces == 6) {
       ROW(512, 6, false, SHORT ? 8 : 4);
+    } else if (cut.pieces == 7) {
+      ROW(512, 7, false, SHORT ? 8 : 4);
     } else {
       ROW(512, 8, false, SHORT ? 8 : 4);
     }
@@ -714,11 +734,12 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
 
 template <typename T, bool ONE>
 hipError_t run_bwd(LogpArgs a, hipStream_t stream) {
-  // threads and pieces by the row's length: lanes past its end load its end again (8192 x 1000 bfloat16 with 256 threads
-  // of one piece 15.4 us, of four 21)
+  // threads and pieces by the row's length: lanes past its end load its end again (bfloat16, 8192 x 1000 with 256 threads
+  // of one piece 15.4 us, of four 21; 8184 x 8200 in two chunks of three pieces 82 us, of four 101)
   const bool small = a.vocab <= 512, middle = !small && a.vocab <= 2048;
-  const int per = small ? 512 : (middle ? 2048 : 8192);
-  a.chunks = (a.vocab + per - 1) / per;
+  const auto up = [](int n, int d) { return (n + d - 1) / d; };
+  const int pieces = up(up(a.vocab, up(a.vocab, 8192)), 2048);  // of the longer rows: chunks alike
+  a.chunks = small ? 1 : up(a.vocab, 2048 * pieces);
   const int64_t most = LAUNCH_MAX / a.chunks > 0 ? LAUNCH_MAX / a.chunks : 1;
   for (a.first = 0; a.first < a.rows; a.first += most) {
     const int64_t rows = a.rows - a.first < most ? a.rows - a.first : most;
@@ -733,6 +754,10 @@ hipError_t run_bwd(LogpArgs a, hipStream_t stream) {
       ROW(64, 1);
     } else if (middle) {
       ROW(256, 1);
+    } else if (pieces == 2) {
+      ROW(256, 2);
+    } else if (pieces == 3) {
+      ROW(256, 3);
     } else {
       ROW(256, 4);
     }

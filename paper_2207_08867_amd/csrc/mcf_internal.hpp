@@ -161,12 +161,12 @@ hipError_t launch_distill(int dtype, int nc, int64_t rows, int64_t vocab, int64_
 
 // RMS norm of a residual stream with a layer's output added, plain (y) or 8-bit (codes, scales) output,
 // and 8-bit quantisation (norm false); reading back; the norm's gradients (rmsnorm.hip).  dh and dw may
-// each be null; ws holds rmsnorm_bwd_workspace_bytes(rows, n) bytes with dw.
+// each be null; ws holds rmsnorm_bwd_workspace_bytes(dtype, rows, n) bytes with dw.
 hipError_t launch_rmsnorm(int dtype, int nc, int64_t rows, int64_t n, const void *h, const void *x, const void *w,
                           double eps, void *h_out, void *y, void *codes, void *scales, bool norm, hipStream_t stream);
 hipError_t launch_int8_dequantize(int dtype, int64_t rows, int64_t n, const void *codes, const void *scales, void *out,
                                   hipStream_t stream);
-int64_t rmsnorm_bwd_workspace_bytes(int64_t rows, int64_t n);
+int64_t rmsnorm_bwd_workspace_bytes(int dtype, int64_t rows, int64_t n);
 hipError_t launch_rmsnorm_bwd(int dtype, int nc, int64_t rows, int64_t n, const void *h, const void *w, const void *dy,
                               const void *g, double eps, void *dh, void *dw, void *ws, hipStream_t stream);
 

@@ -389,6 +389,7 @@ hipError_t run_norm(NormArgs a, hipStream_t stream) {
       return go(norm_kernel<T, ONE, 16, 1, NORM, INT8, E>, 16);
     } else {
       if (width <= 128) { ROW(16, 1); }
+      if (width <= 256) { ROW(32, 1); }
       if (width <= 512) { ROW(64, 1); }
       if constexpr (ONE && sizeof(T) == 4 && NORM) {
         if (width <= 2048) { ROW(256, 1); }
@@ -681,12 +682,15 @@ __global__ __launch_bounds__(1024) void norm_bwd_sum_kernel(NormBwdArgs a) {
 constexpr int64_t BWD_LONG = 16384;  // the longest row that stays in registers
 
 // Workgroups: as many as are resident, since a row's loads go out ahead of the row before: one a CU of rows that
-// take 1024 threads, two of 512, four of shorter rows.  With twice (half) as many (us; 4096 x 4096 bfloat16, with g) 46 (49)
+// take 1024 threads, two of 512, four of 256, eight of 128 (16-bit rows: 32263 x 520 62 us, with 256 threads 75; binary32
+// 71 and 67); four where a workgroup has several rows.  With twice (half) as many (us; 4096 x 4096 bfloat16, with g) 46 (49)
 // in place of 40, 8192 x 1024 32 (33) in place of 26, 4096 x 8192 78 in place of 69.  Of rows that do not stay in
 // registers, parts of the rows for dw.
-int bwd_groups(int64_t rows, int64_t n) {
+int bwd_groups(int dtype, int64_t rows, int64_t n) {
   if (n > BWD_LONG) return (int)(rows < 64 ? rows : 64);
-  const int64_t slots = n <= 128 ? 16 : (n <= 512 ? 4 : 1), most = n <= 2048 ? 1024 : (n <= 4096 ? 512 : 256);
+  const int64_t slots = n <= 128 ? 16 : (n <= 256 ? 8 : (n <= 512 ? 4 : 1));
+  const bool narrow = dtype != LM_F32 && n > 512 && n <= 1024;
+  const int64_t most = narrow ? 2048 : (n <= 2048 ? 1024 : (n <= 4096 ? 512 : 256));
   const int64_t wanted = (rows + slots - 1) / slots;
   return (int)(wanted < most ? wanted : most);
 }
@@ -708,7 +712,10 @@ hipError_t run_bwd(NormBwdArgs a, hipStream_t stream) {
 #define ROW(NT, CH) return norm_bwd_kernel<T, ONE, NT, CH, E><<<grid, NT <= 64 ? 256 : NT, 0, stream>>>(a)
       if (E == END_SHORT || a.n <= 128) ROW(16, 1);
       if constexpr (E != END_SHORT) {
+        if (a.n <= 256) ROW(32, 1);
         if (a.n <= 512) ROW(64, 1);
+        if constexpr (sizeof(T) == 2)
+          if (a.n <= 1024) ROW(128, 1);
         if (a.n <= 2048) ROW(256, 1);
         if (a.n <= 4096) ROW(512, 1);
         if (a.n <= 8192) ROW(1024, 1);
@@ -767,8 +774,8 @@ hipError_t launch_int8_dequantize(int dtype, int64_t rows, int64_t n, const void
   return read_back<float>(rows, n, codes, scales, out, stream);
 }
 
-int64_t rmsnorm_bwd_workspace_bytes(int64_t rows, int64_t n) {
-  return bwd_groups(rows, n) * n * 4 + (n > BWD_LONG ? rows * 8 + 8 : 0);
+int64_t rmsnorm_bwd_workspace_bytes(int dtype, int64_t rows, int64_t n) {
+  return bwd_groups(dtype, rows, n) * n * 4 + (n > BWD_LONG ? rows * 8 + 8 : 0);
 }
 
 hipError_t launch_rmsnorm_bwd(int dtype, int nc, int64_t rows, int64_t n, const void *h, const void *w, const void *dy,
@@ -787,7 +794,7 @@ hipError_t launch_rmsnorm_bwd(int dtype, int nc, int64_t rows, int64_t n, const 
   a.eps = eps;
   a.inv_n = n > 0 ? 1.0 / (double)n : 0.0;
   a.nc = nc;
-  a.groups = bwd_groups(rows, n);
+  a.groups = bwd_groups(dtype, rows, n);
   a.r = (double *)((char *)ws + (a.groups * n * 4 + 7) / 8 * 8);
   if (dtype == LM_F16) return run_bwd<_Float16>(a, stream);
   if (dtype == LM_BF16) return run_bwd<__bf16>(a, stream);

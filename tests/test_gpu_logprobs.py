@@ -111,7 +111,9 @@ def batch(seed, rows, V, given, dtype, nc=1):
                                                (3, 513, 1, 64), (4, 2049, 2, 20), (256, 4100, 1, 20), (2, 8192, 1, 32), (3, 8193, 1, 128),
                                                (2, 32768, 5, 64), (257, 9000, 1, 1), (256, 16390, 2, 7), (256, 32769, 1, 128),
                                                (257, 70000, 1, 20), (1, 131071, 1, 100), (3, 4100, 1024, 3), (2, 40, 0, 0),
-                                               (3, 1000, 12, 128), (2, 32768, 1, 128), (2, 1000, 65, 64), (2, 200, 9, 100)])
+                                               (3, 1000, 12, 128), (2, 32768, 1, 128), (2, 1000, 65, 64), (2, 200, 9, 100),
+                                               (66, 100000, 1, 128), (2, 5001, 2, 128), (2, 12001, 2, 64), (2, 20001, 10, 64), (2, 28001, 2, 128),
+                                               (130, 34003, 1, 30), (64, 42001, 1, 64), (64, 49999, 1, 64), (64, 65001, 1, 64)])
 def test_rows(mcf, dtype, T, rows, V, given, k):
     z, ids, g, gh = batch(rows + V, rows, V, given, dtype)
     check(mcf, z, ids, k, T, dtype, g, gh)

@@ -62,7 +62,7 @@ def check_int8(pair, p, r, n):
 
 
 SIZES = [(1, 1), (3, 7), (5, 8), (17, 16), (37, 100), (300, 128), (9, 129), (5, 500), (4, 513), (3, 1000), (2, 2048),
-         (3, 2049), (5, 4096), (2, 4100), (3, 8191), (2, 8200), (2, 16384), (2, 16400), (2, 40001)]
+         (3, 2049), (5, 4096), (2, 4100), (3, 8191), (2, 8200), (2, 16384), (2, 16400), (2, 40001), (41, 200), (40, 256)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
@@ -162,7 +162,8 @@ def test_quantize_and_read_back(mcf, dtype, n):
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("nc", [1, 2])
 @pytest.mark.parametrize("rows, n", [(1, 1), (3, 7), (700, 40), (513, 64), (9, 129), (5, 513), (1100, 1000), (3, 2049),
-                                     (4, 4100), (530, 4096), (3, 8200), (2, 16384), (5, 16400), (2, 40001)])
+                                     (4, 4100), (530, 4096), (3, 8200), (2, 16384), (5, 16400), (2, 40001), (9000, 200),
+                                     (2100, 600), (300, 5000)])
 def test_gradients(mcf, dtype, nc, rows, n):
     import torch
 
