@@ -413,26 +413,38 @@ hipError_t run_norm(NormArgs a, hipStream_t stream) {
   }
 }
 
-// code scale, 8 elements a thread.  HBM bounds it: 4096 x 8192 to bfloat16 20.8 us, 4.8 TB/s, where a large copy
-// reaches 5.1.  Two, four and eight pieces a thread, 256 pieces apart: 27.6, 28.7, 29.7; codes that the norm has just
-// written, still in a cache, take the same within 1% either way.
+// code scale, a thread READ pieces of 8 elements, 256 pieces apart.  HBM bounds it: 4096 x 8192 to bfloat16 21 us, 4.8
+// TB/s, where a large copy reaches 5.1.  Two, four and eight pieces a thread: 27.6, 28.7, 29.7; codes that the norm has just
+// written, still in a cache, take the same within 1% either way.  (Written without the arrays 25 us.)
+constexpr int READ = 1;
 template <typename T>
 __global__ __launch_bounds__(256) void int8_read_kernel(const uint64_t *codes, const float *scales, T *out, int64_t rows,
                                                         int64_t n, int64_t across, int64_t first) {
-  const int64_t id = (first + blockIdx.x) * 256 + threadIdx.x;
-  if (id >= rows * across) return;
-  const int64_t row = id <= 0xffffffffll ? (int64_t)((uint32_t)id / (uint32_t)across) : id / across, col = id - row * across;
-  const uint64_t w = codes[row * (int8_pitch(n) >> 3) + col];
-  const float s = scales[row];
-  Raw8<T> o;
+  const int64_t total = rows * across, pitch = int8_pitch(n) >> 3;
+  int64_t row[READ], col[READ];
+  uint64_t w[READ];
+  float s[READ];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) o.v[i] = (T)((float)(int8_t)(w >> (8 * i)) * s);
-  store8_tail(out + row * n + col * 8, o, n - col * 8);
+  for (int k = 0; k < READ; ++k) {
+    int64_t id = (first + blockIdx.x) * (256 * READ) + k * 256 + threadIdx.x;
+    if (id >= total) id = total - 1;  // again
+    row[k] = id <= 0xffffffffll ? (int64_t)((uint32_t)id / (uint32_t)across) : id / across;
+    col[k] = id - row[k] * across;
+    w[k] = codes[row[k] * pitch + col[k]];
+    s[k] = scales[row[k]];
+  }
+#pragma unroll
+  for (int k = 0; k < READ; ++k) {
+    Raw8<T> o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o.v[i] = (T)((float)(int8_t)(w[k] >> (8 * i)) * s[k]);
+    store8_tail(out + row[k] * n + col[k] * 8, o, n - col[k] * 8);
+  }
 }
 
 template <typename T>
 hipError_t read_back(int64_t rows, int64_t n, const void *codes, const void *scales, void *out, hipStream_t stream) {
-  const int64_t across = (n + 7) / 8, groups = (rows * across + 255) / 256;
+  const int64_t across = (n + 7) / 8, groups = (rows * across + 256 * READ - 1) / (256 * READ);
   for (int64_t first = 0; first < groups; first += LAUNCH_MAX)
     int8_read_kernel<T><<<(unsigned)(groups - first < LAUNCH_MAX ? groups - first : LAUNCH_MAX), 256, 0, stream>>>(
         (const uint64_t *)codes, (const float *)scales, (T *)out, rows, n, across, first);
