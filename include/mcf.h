@@ -561,7 +561,8 @@ int64_t mc_rmsnorm_bwd_workspace(int dtype, int64_t rows, int64_t n);
  * z: plain [rows][vocab], or (nc > 1) an MC value [nc][rows][vocab] whose planes are summed in
  *   binary32, the last one first; its gradient is plain, that of the sum (Section 2.1).
  * ids: int32 [rows][given], 0 <= given <= 1024, in any order, also equal ones.
- * temperature: positive and finite.
+ * temperature: finite and above 2^-127, as a binary32 number.  At a very small one the entropy has terms near binary32's
+ *   smallest numbers, and so an error of up to vocab 2^-149 / temperature beside that of its roundings.
  * logp: binary32 [rows][given]; entropy: binary32 [rows] or NULL; top_ids: int32 and top_logp:
  *   binary32 [rows][top], 0 <= top <= 128.
  * stats: binary32 [rows][3] or NULL, for the gradient: the row's largest logit m, L = log sum_j

@@ -10,7 +10,9 @@
 // The gradient, given g_i with respect to the log probability of token id_i and h with respect to H:
 //   dz_j = (sum of the g_i with id_i = j - q_j (sum of all g_i + h (log q_j + H))) / T.
 //
-// Sums are binary32, in an order that depends on the sizes (rows and vocabulary) alone.
+// Sums are binary32, in an order that depends on the sizes (rows and vocabulary) alone.  From a temperature of 2^64 up
+// differences are taken of logits times 2^-64, with T 2^-64 in T's place, so that neither a difference of the format's
+// whole range nor a row's sum of them passes binary32's range; what that rounds away is below 2^-126 of T.
 //
 // A row is read once, and the gradient reads it again and writes as much, so HBM bounds the large calls: 4096 rows of
 // 32768 bfloat16 logits (268 MB) 54 to 61 us, 4.4 to 5.0 TB/s, the gradient 108 us, 5.0 TB/s; binary32 97 and 195 us,
@@ -29,7 +31,7 @@ namespace mcf {
 namespace {
 
 // What a part of a row contributes: its largest logit, at least -FLT_MAX; s as above, or -1 where the
-// part has no logit above -inf; a = sum d exp(-d / T).
+// part has no logit above -inf; a = sum d exp(-d / T), of scaled differences.
 struct Part {
   float m, s, a;
 };
@@ -46,10 +48,15 @@ struct LogpArgs {
   int64_t rows, plane;
   int64_t first;  // the launch's first row
   int vocab, given, top, nc, chunks;
-  float temperature, inv_t, c_hi, c_lo;  // c_hi + c_lo = log2(e) / T
+  float temperature, scale;  // T; what differences are scaled by, 1 or 2^-64
+  float inv_t, c_hi, c_lo;   // 1 / (T scale); c_hi + c_lo = log2(e) / (T scale)
 };
 
-// exp(-d / T), d >= 0.  The factor's second term keeps the argument's error at one rounding; both are
+// The scaled difference of a larger logit m, given as m scale, and a smaller one; the scale is a power of two, so that
+// it is rounded once.
+__device__ inline float below(const LogpArgs &a, float m_scaled, float z) { return fmaf(-a.scale, z, m_scaled); }
+
+// exp(-d / T) of a scaled d >= 0.  The factor's second term keeps the argument's error at one rounding; both are
 // positive, so that an infinite d gives 0.
 __device__ inline float expd(const LogpArgs &a, float d) {
   return __builtin_amdgcn_exp2f(-fmaf(d, a.c_hi, d * a.c_lo));
@@ -62,7 +69,7 @@ __device__ inline Part join(const LogpArgs &a, const Part &x, const Part &y) {
   const Part lo = {first ? y.m : x.m, first ? y.s : x.s, first ? y.a : x.a};
   if (lo.s == -1.0f) return hi.s == -1.0f ? lo : hi;
   if (hi.s == -1.0f) return lo;
-  const float d = hi.m - lo.m, f = expd(a, d), n = 1.0f + lo.s;
+  const float d = below(a, hi.m * a.scale, lo.m), f = expd(a, d), n = 1.0f + lo.s;
   return Part{hi.m, hi.s + n * f, hi.a + (lo.a + (f == 0.0f ? 0.0f : d) * n) * f};
 }
 
@@ -440,6 +447,11 @@ __device__ inline void select_logits(Select &sh, Pool<CH, H> &pool, int k, const
   rank_kept<NT>(sh, k, n, out);
 }
 
+// A value that all lanes have, in a scalar register.
+__device__ inline float scalar(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
+}
+
 // A chunk of NT CH pieces of 8 logits of a row, in registers; SPLIT: of several, which the kernel below joins.
 // 16-bit logits stay in their format, so that four workgroups of 512 threads and 32768 logits share a CU and some
 // load while others sum or select; in binary32 they are half as many.
@@ -474,14 +486,14 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
     for (int i = 0; i < 8; ++i) own = fmaxf(own, (float)v[c].v[i]);
   // Each wavefront's sums relative to its own largest logit, so that it works on its logits while the others'
   // are on their way.
-  const float mw = lanes_max(fmaxf(own, -FLT_MAX));
+  const float mw = scalar(lanes_max(fmaxf(own, -FLT_MAX))), mws = mw * a.scale;
   float s = 0.0f, d1 = 0.0f;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const Raw8<H> u = renewed(v[c]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float d = mw - (float)u.v[i], e = expd(a, d);
+      const float d = below(a, mws, (float)u.v[i]), e = expd(a, d);
       s += e;
       d1 = fmaf(e, fminf(d, FLT_MAX), d1);
     }
@@ -499,6 +511,7 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
   // The first wavefront with the row's largest logit finishes.  It sums its others alone; one more largest logit
   // elsewhere makes the sum 1 or more, which then needs no such care.
   if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) == __builtin_amdgcn_readfirstlane(first)) {
+    const float ms = m * a.scale;
     float equal = 0.0f;
     s = 0.0f;
 #pragma unroll
@@ -508,7 +521,7 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
       for (int i = 0; i < 8; ++i) {
         const float x = (float)u.v[i];
         equal += x == m ? 1.0f : 0.0f;
-        s += x == m ? 0.0f : expd(a, m - x);
+        s += x == m ? 0.0f : expd(a, below(a, ms, x));
       }
       asm volatile("" : "+v"(s), "+v"(equal));
     }
@@ -520,7 +533,7 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const Part x = sums[w];
-      const float d = m - x.m, f = w == first ? 0.0f : expd(a, d);
+      const float d = below(a, ms, x.m), f = w == first ? 0.0f : expd(a, d);
       part.s += w == first ? 0.0f : x.s * f;
       part.a += w == first ? 0.0f : (x.a + (f == 0.0f ? 0.0f : d) * x.s) * f;
     }
@@ -679,7 +692,7 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
     g[i] = used ? (a.g ? a.g[row * a.given + i] : 1.0f) : 0.0f;
   }
   const float m = a.stats[3 * row], L = a.stats[3 * row + 1], B = a.stats[3 * row + 2];
-  const float gh = a.gh ? a.gh[row] : 0.0f;
+  float gh = a.gh ? a.gh[row] : 0.0f;
   Raw8<std::conditional_t<ONE, T, float>> v[CH];
   logits<T, ONE, NT>(a, z, lo, v);
   const bool whole = lo + NT * CH * 8 <= a.vocab;
@@ -690,16 +703,23 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
   float all = 0.0f;
   for (int i = 0; i < a.given; ++i) all += g[i];
   const bool none = m == -INFINITY;
-  const float inv_s = expf(-L) * a.inv_t;
+  // 1 / T goes to the weights below a temperature of 2^64 and to the upstream gradients from there up: neither
+  // then passes binary32's range before the result does
+  float inv_s = expf(-L);
+  if (a.scale == 1.0f)
+    inv_s *= a.inv_t;
+  else
+    all = all * a.inv_t * a.scale, gh = gh * a.inv_t * a.scale;
+  const float ms = m * a.scale;
   const auto grad = [&](float x) {
-    const float d = m - x, q = expd(a, d) * inv_s;
+    const float d = below(a, ms, x), q = expd(a, d) * inv_s;
     return q == 0.0f ? 0.0f : -q * (all + gh * (B - d * a.inv_t));
   };
   // what the given tokens add; equal ids add up
   const auto given = [&](int j) {
     float sum = 0.0f;
     for (int k = 0; k < a.given; ++k) sum += id[k] == j ? g[k] : 0.0f;
-    return sum * a.inv_t;
+    return sum * a.inv_t * a.scale;
   };
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -776,8 +796,10 @@ LogpArgs args_of(int nc, int64_t rows, int64_t vocab, int64_t given, const void 
   a.given = (int)given;
   a.nc = nc;
   a.temperature = (float)temperature;
-  a.inv_t = 1.0f / a.temperature;
-  const double c = 1.4426950408889634 / (double)a.temperature;
+  a.scale = a.temperature < 0x1p64f ? 1.0f : 0x1p-64f;
+  const float t = a.temperature * a.scale;
+  a.inv_t = 1.0f / t;
+  const double c = 1.4426950408889634 / (double)t;
   a.c_hi = (float)c;
   if ((double)a.c_hi > c) a.c_hi = nextafterf(a.c_hi, 0.0f);
   a.c_lo = fmaxf((float)(c - (double)a.c_hi), FLT_MIN);
