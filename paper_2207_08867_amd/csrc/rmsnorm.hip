@@ -459,6 +459,7 @@ struct NormBwdArgs {
   float *partial;              // [groups][n], with dw
   double *r;                   // [rows], of long rows
   int64_t rows, n, plane;
+  int64_t first;  // the first 64 columns of a launch of the sum
   double eps, inv_n;
   int nc, groups;
 };
@@ -672,12 +673,13 @@ __global__ __launch_bounds__(256) void norm_bwd_long_dw_kernel(NormBwdArgs a) {
     if (col + i < a.n) p[col + i] = (float)sum[i];
 }
 
-// The workgroups' sums: 64 columns by 16 parts of the workgroups, each in order, then the parts.
+// The workgroups' sums: 64 columns by 16 parts of the workgroups, each in order, then the parts.  Rows past 2^27
+// elements take several launches.
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_bwd_sum_kernel(NormBwdArgs a) {
   __shared__ double part[16][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+  const int64_t col = (a.first + blockIdx.x) * 64 + lane;
   const int from = a.groups * wave / 16, to = a.groups * (wave + 1) / 16;
   double s = 0.0;
   if (col < a.n)
@@ -742,7 +744,10 @@ hipError_t run_bwd(NormBwdArgs a, hipStream_t stream) {
       default: pick(std::integral_constant<End, END_SHORT>());
     }
   }
-  if (a.dw) norm_bwd_sum_kernel<T><<<(unsigned)((a.n + 63) / 64), 1024, 0, stream>>>(a);
+  if (!a.dw) return hipGetLastError();
+  const int64_t all = (a.n + 63) / 64;
+  for (; a.first < all; a.first += LAUNCH_MAX)
+    norm_bwd_sum_kernel<T><<<(unsigned)(all - a.first < LAUNCH_MAX ? all - a.first : LAUNCH_MAX), 1024, 0, stream>>>(a);
   return hipGetLastError();
 }
 
