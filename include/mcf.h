@@ -568,8 +568,9 @@ int64_t mc_rmsnorm_bwd_workspace(int dtype, int64_t rows, int64_t n);
  * stats: binary32 [rows][3] or NULL, for the gradient: the row's largest logit m, L = log sum_j
  *   exp((z_j - m) / T), and entropy - L.
  * Statistics and sums are binary32, summed in an order that depends on rows and vocab alone; the log
- * probability of a token the row is sure of keeps its relative accuracy.  No output may overlap an input or another output.  rows < 2^31,
- * 1 <= vocab <= 2^30.  Workspace as for the MXFP4 calls. */
+ * probability of a token the row is sure of, and the gradient there, keep their relative accuracy.
+ * No output may overlap an input or another output.  rows < 2^31, 1 <= vocab <= 2^30.  Workspace as
+ * for the MXFP4 calls. */
 int mc_logprobs_fwd(int dtype, int nc, int64_t rows, int64_t vocab, int64_t given, int64_t top, const void *z,
                     const void *ids, double temperature, void *workspace, int64_t workspace_bytes, void *logp,
                     void *entropy, void *top_ids, void *top_logp, void *stats, void *stream);

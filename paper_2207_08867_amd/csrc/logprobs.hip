@@ -692,7 +692,7 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
     g[i] = used ? (a.g ? a.g[row * a.given + i] : 1.0f) : 0.0f;
   }
   const float m = a.stats[3 * row], L = a.stats[3 * row + 1], B = a.stats[3 * row + 2];
-  float gh = a.gh ? a.gh[row] : 0.0f;
+  const float gh = a.gh ? a.gh[row] : 0.0f;
   Raw8<std::conditional_t<ONE, T, float>> v[CH];
   logits<T, ONE, NT>(a, z, lo, v);
   const bool whole = lo + NT * CH * 8 <= a.vocab;
@@ -706,20 +706,27 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
   // 1 / T goes to the weights below a temperature of 2^64 and to the upstream gradients from there up: neither
   // then passes binary32's range before the result does
   float inv_s = expf(-L);
+  float slope = gh;
   if (a.scale == 1.0f)
     inv_s *= a.inv_t;
   else
-    all = all * a.inv_t * a.scale, gh = gh * a.inv_t * a.scale;
+    all = all * a.inv_t * a.scale, slope = gh * a.inv_t * a.scale;
   const float ms = m * a.scale;
   const auto grad = [&](float x) {
     const float d = below(a, ms, x), q = expd(a, d) * inv_s;
-    return q == 0.0f ? 0.0f : -q * (all + gh * (B - d * a.inv_t));
+    return q == 0.0f ? 0.0f : -q * (all + slope * (B - d * a.inv_t));
   };
-  // what the given tokens add; equal ids add up
-  const auto given = [&](int j) {
-    float sum = 0.0f;
-    for (int k = 0; k < a.given; ++k) sum += id[k] == j ? g[k] : 0.0f;
-    return sum * a.inv_t * a.scale;
+  // The gradient at a given token j with logit x; equal ids add up.  G_j (1 - q_j) - q_j (the others' sum) in place of
+  // G_j - q_j (all of them), and 1 - q_j from log q_j: a token the row is sure of keeps its relative accuracy.
+  const auto token = [&](int j, float x) {
+    float own = 0.0f, others = 0.0f;
+    for (int k = 0; k < a.given; ++k) {
+      own += id[k] == j ? g[k] : 0.0f;
+      others += id[k] == j ? 0.0f : g[k];
+    }
+    const float d = below(a, ms, x), e = d * a.inv_t, q = expd(a, d) * expf(-L);
+    const float rest = q == 0.0f ? 0.0f : q * (others + gh * (B - e));
+    return (own * -expm1f(-e - L) - rest) * a.inv_t * a.scale;
   };
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -732,8 +739,17 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
       bool hit = false;
       for (int k = 0; k < a.given; ++k) hit = hit || (uint32_t)(id[k] - (int)col) < 8;
       if (hit && !none) {
+#pragma unroll 1
+        for (int k = 0; k < a.given; ++k) {
+          const int at = id[k] - (int)col;
+          if ((uint32_t)at >= 8) continue;
+          float x = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] += given((int)col + i);
+          for (int i = 0; i < 8; ++i) x = i == at ? (float)v[c].v[i] : x;
+          const float t = token(id[k], x);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) d[i] = i == at ? t : d[i];
+        }
       }
     }
     Raw8<T> o;
@@ -747,7 +763,7 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
     const int hi = lo + NT * CH * 8;
     for (int i = threadIdx.x; i < a.given; i += NT) {
       const int j = id[i];
-      if (j >= lo && j < hi) dz[j] = (T)(grad(logit<T, ONE>(a, z, j)) + given(j));
+      if (j >= lo && j < hi) dz[j] = (T)token(j, logit<T, ONE>(a, z, j));
     }
   }
 }
