@@ -12,7 +12,8 @@
 //
 // Sums are binary32, in an order that depends on the sizes (rows and vocabulary) alone.  From a temperature of 2^64 up
 // differences are taken of logits times 2^-64, with T 2^-64 in T's place, so that neither a difference of the format's
-// whole range nor a row's sum of them passes binary32's range; what that rounds away is below 2^-126 of T.
+// whole range nor a row's sum of them passes binary32's range; what that rounds away is below 2^-126 of T.  The kernels of MC
+// logits alone do so, and take plain rows then too, of one plane: in the others it cost bfloat16 rows 1 to 2% of a call.
 //
 // A row is read once, and the gradient reads it again and writes as much, so HBM bounds the large calls: 4096 rows of
 // 32768 bfloat16 logits (268 MB) 54 to 61 us, 4.4 to 5.0 TB/s, the gradient 108 us, 5.0 TB/s; binary32 97 and 195 us,
@@ -52,9 +53,16 @@ struct LogpArgs {
   float inv_t, c_hi, c_lo;   // 1 / (T scale); c_hi + c_lo = log2(e) / (T scale)
 };
 
-// The scaled difference of a larger logit m, given as m scale, and a smaller one; the scale is a power of two, so that
-// it is rounded once.
-__device__ inline float below(const LogpArgs &a, float m_scaled, float z) { return fmaf(-a.scale, z, m_scaled); }
+// The scaled difference of a larger logit m, given as `scaled`, and a smaller one; the scale is a power of two, so that
+// it is rounded once.  ONE: the scale is 1.
+template <bool ONE>
+__device__ inline float scaled(const LogpArgs &a, float v) {
+  return ONE ? v : v * a.scale;
+}
+template <bool ONE>
+__device__ inline float below(const LogpArgs &a, float m_scaled, float z) {
+  return ONE ? m_scaled - z : fmaf(-a.scale, z, m_scaled);
+}
 
 // exp(-d / T) of a scaled d >= 0.  The factor's second term keeps the argument's error at one rounding; both are
 // positive, so that an infinite d gives 0.
@@ -62,6 +70,7 @@ __device__ inline float expd(const LogpArgs &a, float d) {
   return __builtin_amdgcn_exp2f(-fmaf(d, a.c_hi, d * a.c_lo));
 }
 
+template <bool ONE>
 __device__ inline Part join(const LogpArgs &a, const Part &x, const Part &y) {
   // member by member: a reference to one or the other would put both into memory
   const bool first = x.m >= y.m;
@@ -69,7 +78,7 @@ __device__ inline Part join(const LogpArgs &a, const Part &x, const Part &y) {
   const Part lo = {first ? y.m : x.m, first ? y.s : x.s, first ? y.a : x.a};
   if (lo.s == -1.0f) return hi.s == -1.0f ? lo : hi;
   if (hi.s == -1.0f) return lo;
-  const float d = below(a, hi.m * a.scale, lo.m), f = expd(a, d), n = 1.0f + lo.s;
+  const float d = below<ONE>(a, scaled<ONE>(a, hi.m), lo.m), f = expd(a, d), n = 1.0f + lo.s;
   return Part{hi.m, hi.s + n * f, hi.a + (lo.a + (f == 0.0f ? 0.0f : d) * n) * f};
 }
 
@@ -447,7 +456,8 @@ __device__ inline void select_logits(Select &sh, Pool<CH, H> &pool, int k, const
   rank_kept<NT>(sh, k, n, out);
 }
 
-// A value that all lanes have, in a scalar register.
+// A value that all lanes have, in a scalar register: the scaled one takes the vector register (80 in place of 81 of MC rows
+// in eight pieces, which is a workgroup more on a CU: 2048 x 32000 of two binary16 planes 72 us, 76 without).
 __device__ inline float scalar(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
 }
@@ -486,14 +496,14 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
     for (int i = 0; i < 8; ++i) own = fmaxf(own, (float)v[c].v[i]);
   // Each wavefront's sums relative to its own largest logit, so that it works on its logits while the others'
   // are on their way.
-  const float mw = scalar(lanes_max(fmaxf(own, -FLT_MAX))), mws = mw * a.scale;
+  const float top = lanes_max(fmaxf(own, -FLT_MAX)), mw = ONE ? top : scalar(top), mws = scaled<ONE>(a, mw);
   float s = 0.0f, d1 = 0.0f;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     const Raw8<H> u = renewed(v[c]);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float d = below(a, mws, (float)u.v[i]), e = expd(a, d);
+      const float d = below<ONE>(a, mws, (float)u.v[i]), e = expd(a, d);
       s += e;
       d1 = fmaf(e, fminf(d, FLT_MAX), d1);
     }
@@ -511,7 +521,7 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
   // The first wavefront with the row's largest logit finishes.  It sums its others alone; one more largest logit
   // elsewhere makes the sum 1 or more, which then needs no such care.
   if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 6) == __builtin_amdgcn_readfirstlane(first)) {
-    const float ms = m * a.scale;
+    const float ms = scaled<ONE>(a, m);
     float equal = 0.0f;
     s = 0.0f;
 #pragma unroll
@@ -521,7 +531,7 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
       for (int i = 0; i < 8; ++i) {
         const float x = (float)u.v[i];
         equal += x == m ? 1.0f : 0.0f;
-        s += x == m ? 0.0f : expd(a, below(a, ms, x));
+        s += x == m ? 0.0f : expd(a, below<ONE>(a, ms, x));
       }
       asm volatile("" : "+v"(s), "+v"(equal));
     }
@@ -533,7 +543,7 @@ __global__ __launch_bounds__(NT, OCC) void logp_kernel(LogpArgs a) {
 #pragma unroll
     for (int w = 0; w < W; ++w) {
       const Part x = sums[w];
-      const float d = below(a, ms, x.m), f = w == first ? 0.0f : expd(a, d);
+      const float d = below<ONE>(a, ms, x.m), f = w == first ? 0.0f : expd(a, d);
       part.s += w == first ? 0.0f : x.s * f;
       part.a += w == first ? 0.0f : (x.a + (f == 0.0f ? 0.0f : d) * x.s) * f;
     }
@@ -582,7 +592,7 @@ __global__ __launch_bounds__(256) void logp_join_kernel(LogpArgs a) {
   int id = -1;
   if ((int)threadIdx.x < a.given) id = a.ids[row * a.given + threadIdx.x];
   Part p = {-FLT_MAX, -1.0f, 0.0f};
-  for (int c = threadIdx.x; c < a.chunks; c += 256) p = join(a, p, a.parts[row * a.chunks + c]);
+  for (int c = threadIdx.x; c < a.chunks; c += 256) p = join<ONE>(a, p, a.parts[row * a.chunks + c]);
   float given = 0.0f;
   if (id >= 0 && id < a.vocab) given = logit<T, ONE>(a, z, id);
 #pragma unroll
@@ -590,14 +600,14 @@ __global__ __launch_bounds__(256) void logp_join_kernel(LogpArgs a) {
     const Part o = {__shfl_xor(p.m, d), __shfl_xor(p.s, d), __shfl_xor(p.a, d)};
     // both sides join in the lower lane's order, so the lanes agree
     const bool upper = threadIdx.x & d;
-    p = join(a, Part{upper ? o.m : p.m, upper ? o.s : p.s, upper ? o.a : p.a},
+    p = join<ONE>(a, Part{upper ? o.m : p.m, upper ? o.s : p.s, upper ? o.a : p.a},
              Part{upper ? p.m : o.m, upper ? p.s : o.s, upper ? p.a : o.a});
   }
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = p;
   __syncthreads();
   p = sums[0];
 #pragma unroll
-  for (int w = 1; w < 4; ++w) p = join(a, p, sums[w]);
+  for (int w = 1; w < 4; ++w) p = join<ONE>(a, p, sums[w]);
   const Row r = row_of(a, p);
   if ((int)threadIdx.x < a.given)
     a.logp[row * a.given + threadIdx.x] = id >= 0 && id < a.vocab ? log_prob(a, r, given) : 0.0f;
@@ -672,15 +682,18 @@ hipError_t run_fwd(LogpArgs a, const Cut &cut, hipStream_t stream) {
 // --- the gradient ----------------------------------------------------------------------
 
 // The given tokens' ids and gradients, 8 bytes of LDS each.
-extern __shared__ float given_space[];
+struct Given {
+  int id;
+  float g;
+};
+extern __shared__ Given given_space[];
 
 // A workgroup takes 8 CH NT logits of a row.  FEW: few given tokens, for which every piece of 8 logits looks;
 // else they are written over what the pass left there.  HBM bounds it: 4096 x 32768 bfloat16 108 us, 5.0 TB/s, where a
 // large copy reaches 5.1.
 template <typename T, bool ONE, int NT, int CH, bool FEW>
 __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
-  int *const id = (int *)given_space;
-  float *const g = given_space + a.given;
+  Given *const given = given_space;
   const int64_t row = a.first + blockIdx.x / a.chunks;
   const int lo = (int)(blockIdx.x % a.chunks) * (NT * CH * 8);
   const T *z = reinterpret_cast<const T *>(a.z) + row * a.vocab;
@@ -688,8 +701,7 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
   for (int i = threadIdx.x; i < a.given; i += NT) {
     const int j = a.ids[row * a.given + i];
     const bool used = j >= 0 && j < a.vocab;
-    id[i] = used ? j : -1;
-    g[i] = used ? (a.g ? a.g[row * a.given + i] : 1.0f) : 0.0f;
+    given[i] = Given{used ? j : -1, used ? (a.g ? a.g[row * a.given + i] : 1.0f) : 0.0f};
   }
   const float m = a.stats[3 * row], L = a.stats[3 * row + 1], B = a.stats[3 * row + 2];
   const float gh = a.gh ? a.gh[row] : 0.0f;
@@ -701,32 +713,38 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
   else
     wave_sync();
   float all = 0.0f;
-  for (int i = 0; i < a.given; ++i) all += g[i];
+  for (int i = 0; i < a.given; ++i) all += given[i].g;
   const bool none = m == -INFINITY;
   // 1 / T goes to the weights below a temperature of 2^64 and to the upstream gradients from there up: neither
   // then passes binary32's range before the result does
   float inv_s = expf(-L);
   float slope = gh;
-  if (a.scale == 1.0f)
+  if (ONE || a.scale == 1.0f)
     inv_s *= a.inv_t;
   else
-    all = all * a.inv_t * a.scale, slope = gh * a.inv_t * a.scale;
-  const float ms = m * a.scale;
+    all = scaled<ONE>(a, all * a.inv_t), slope = scaled<ONE>(a, gh * a.inv_t);
+  const float ms = scaled<ONE>(a, m);
   const auto grad = [&](float x) {
-    const float d = below(a, ms, x), q = expd(a, d) * inv_s;
+    const float d = below<ONE>(a, ms, x), q = expd(a, d) * inv_s;
     return q == 0.0f ? 0.0f : -q * (all + slope * (B - d * a.inv_t));
   };
-  // The gradient at a given token j with logit x; equal ids add up.  G_j (1 - q_j) - q_j (the others' sum) in place of
-  // G_j - q_j (all of them), and 1 - q_j from log q_j: a token the row is sure of keeps its relative accuracy.
+  // The gradient at a given token j with logit x; equal ids add up.  A row is sure of one token at most: there it is
+  // G_j (1 - q_j) - q_j (the others' sum) in place of G_j - q_j (all of them), and 1 - q_j comes from log q_j, which
+  // keeps its relative accuracy.
   const auto token = [&](int j, float x) {
+    const float d = below<ONE>(a, ms, x), e = d * a.inv_t, q = expd(a, d) * expf(-L);
+    const bool sure = q > 0.5f;
     float own = 0.0f, others = 0.0f;
-    for (int k = 0; k < a.given; ++k) {
-      own += id[k] == j ? g[k] : 0.0f;
-      others += id[k] == j ? 0.0f : g[k];
-    }
-    const float d = below(a, ms, x), e = d * a.inv_t, q = expd(a, d) * expf(-L);
-    const float rest = q == 0.0f ? 0.0f : q * (others + gh * (B - e));
-    return (own * -expm1f(-e - L) - rest) * a.inv_t * a.scale;
+    if (__any(sure))
+      for (int k = 0; k < a.given; ++k) {
+        const Given t = given[k];
+        own += t.id == j ? t.g : 0.0f;
+        others += t.id == j ? 0.0f : t.g;
+      }
+    else
+      for (int k = 0; k < a.given; ++k) own += given[k].id == j ? given[k].g : 0.0f;
+    if (sure) return scaled<ONE>(a, (own * -expm1f(-e - L) - q * (others + gh * (B - e))) * a.inv_t);
+    return grad(x) + scaled<ONE>(a, own * a.inv_t);
   };
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
@@ -736,20 +754,23 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) d[i] = none ? 0.0f : grad((float)v[c].v[i]);
     if constexpr (FEW) {
-      bool hit = false;
-      for (int k = 0; k < a.given; ++k) hit = hit || (uint32_t)(id[k] - (int)col) < 8;
-      if (hit && !none) {
+      // The given tokens among the piece's, one by one, each lane its own (8192 x 1000 bfloat16 with 8 tokens 17 us;
+      // 26 where all tokens were looked through for each of the piece's logits).
+      uint32_t hits = 0;
+      for (int k = 0; k < a.given; ++k) {
+        const uint32_t at = (uint32_t)(given[k].id - (int)col);
+        hits |= at < 8 ? 1u << at : 0u;
+      }
+      if (none) hits = 0;
 #pragma unroll 1
-        for (int k = 0; k < a.given; ++k) {
-          const int at = id[k] - (int)col;
-          if ((uint32_t)at >= 8) continue;
-          float x = 0.0f;
+      for (; hits; hits &= hits - 1) {
+        const int at = __builtin_ctz(hits);
+        float x = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x = i == at ? (float)v[c].v[i] : x;
-          const float t = token(id[k], x);
+        for (int i = 0; i < 8; ++i) x = i == at ? (float)v[c].v[i] : x;
+        const float t = token((int)col + at, x);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) d[i] = i == at ? t : d[i];
-        }
+        for (int i = 0; i < 8; ++i) d[i] = i == at ? t : d[i];
       }
     }
     Raw8<T> o;
@@ -762,7 +783,7 @@ __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
     __syncthreads();  // the pass's stores come before the tokens'
     const int hi = lo + NT * CH * 8;
     for (int i = threadIdx.x; i < a.given; i += NT) {
-      const int j = id[i];
+      const int j = given[i].id;
       if (j >= lo && j < hi) dz[j] = (T)token(j, logit<T, ONE>(a, z, j));
     }
   }
@@ -849,7 +870,8 @@ hipError_t launch_logprobs_fwd(int dtype, int nc, int64_t rows, int64_t vocab, i
   a.stats_out = (float *)stats;
   const auto go = [&](auto zero) {
     using T = decltype(zero);
-    if (nc == 1) return top > 0 ? run_fwd<T, true, true>(a, cut, stream) : run_fwd<T, true, false>(a, cut, stream);
+    if (nc == 1 && a.scale == 1.0f)
+      return top > 0 ? run_fwd<T, true, true>(a, cut, stream) : run_fwd<T, true, false>(a, cut, stream);
     return top > 0 ? run_fwd<T, false, true>(a, cut, stream) : run_fwd<T, false, false>(a, cut, stream);
   };
   if (dtype == LM_F16) return go((_Float16)0.0f);
@@ -867,7 +889,7 @@ hipError_t launch_logprobs_bwd(int dtype, int nc, int64_t rows, int64_t vocab, i
   a.dz = dz;
   const auto go = [&](auto zero) {
     using T = decltype(zero);
-    return nc == 1 ? run_bwd<T, true>(a, stream) : run_bwd<T, false>(a, stream);
+    return nc == 1 && a.scale == 1.0f ? run_bwd<T, true>(a, stream) : run_bwd<T, false>(a, stream);
   };
   if (dtype == LM_F16) return go((_Float16)0.0f);
   if (dtype == LM_BF16) return go((__bf16)0.0f);

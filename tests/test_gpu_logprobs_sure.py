@@ -1,9 +1,10 @@
 """The gradient of the log probabilities at the token of a row that is sure of it: g (1 - q) with 1 - q far below
 binary32's step at one, to a relative bound.
 
-A row has its largest logit d above all V - 1 others, so L = log(1 + s), s = (V - 1) exp(-d).  With e = 2^-24: s has a relative error
-of (2 d + 106) e (test_gpu_logprobs.py counts it), L, 1 - q = 1 - exp(-L) and the entropy's part B = d s / (1 + s) 8 e beside it, a sum
-of n upstream gradients n e relative to their magnitudes, the products and the difference 8 e more, the format half a step."""
+A row has its largest logit d above all V - 1 others, so L = log(1 + s), s = (V - 1) exp(-d).  With e = 2^-24: s has a
+relative error of (2 d + 106) e (test_gpu_logprobs.py counts it), L, 1 - q = 1 - exp(-L) and the entropy's part
+B = d s / (1 + s) 8 e beside it, a sum of n upstream gradients n e relative to their magnitudes, the products and the
+difference 8 e more, the format half a step."""
 import numpy as np
 import pytest
 
@@ -25,7 +26,8 @@ def test_sure_token(mcf, dtype, V, ids):  # noqa: F811
     at = np.array([0, V - 1, V // 2, 7])  # of the sure token
     z = np.zeros((4, V)) - depth[:, None] * T
     z[np.arange(4), at] = 0.0
-    places = np.where(np.array(ids) == 0, at[:, None], np.where(np.array(ids) < 0, -1, (at[:, None] + np.array(ids)) % V)).astype(np.int32)
+    ids = np.array(ids)
+    places = np.where(ids == 0, at[:, None], np.where(ids < 0, -1, (at[:, None] + ids) % V)).astype(np.int32)
     up = g.uniform(0.5, 1.0, size=places.shape).astype(np.float32)
     uh = g.uniform(-1, 1, size=4).astype(np.float32)
     tz, tids = dev(z, dtype), dev(places)
