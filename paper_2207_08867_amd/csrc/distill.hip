@@ -35,12 +35,21 @@ struct DistillArgs {
   int64_t rows, plane;
   int64_t first;  // the launch's first row, where a workgroup takes one
   int vocab, k, nc, chunks;
-  float temperature, c_hi, c_lo;  // c_hi + c_lo = log2(e) / T
+  float temperature, scale;  // T; what differences are scaled by, 1 or 2^-64
+  float c_hi, c_lo;          // c_hi + c_lo = log2(e) / (T scale)
 };
 
 constexpr int CHUNK = 4096;  // elements of a row a workgroup takes where a row has several
 
-// exp((z - m) / T).  The second term of the factor keeps the argument's error at one rounding
+// The scaled difference z - m.  From a temperature of 2^64 up logits are taken times 2^-64, with T 2^-64 in T's place,
+// so that neither a difference of a format's whole range nor c_lo leaves binary32's.  The kernels of MC logits alone do
+// so, and take plain rows then too, of one plane.  ONE: the scale is 1.
+template <bool ONE>
+__device__ inline float above(const DistillArgs &a, float z, float m) {
+  return ONE ? z - m : fmaf(a.scale, z, -m * a.scale);
+}
+
+// exp((z - m) / T) of a scaled difference.  The second term of the factor keeps the argument's error at one rounding
 // where the result is binary32; it is positive, so that a difference of -inf stays -inf.
 template <typename T>
 __device__ inline float expz(const DistillArgs &a, float d) {
@@ -52,22 +61,22 @@ struct MaxSum {
   float m, s;
 };
 
-template <typename T>
+template <typename T, bool ONE>
 __device__ inline MaxSum join(const DistillArgs &a, MaxSum x, MaxSum y) {
   MaxSum r;
   r.m = fmaxf(x.m, y.m);
-  r.s = x.s * expz<T>(a, x.m - r.m) + y.s * expz<T>(a, y.m - r.m);
+  r.s = x.s * expz<T>(a, above<ONE>(a, x.m, r.m)) + y.s * expz<T>(a, above<ONE>(a, y.m, r.m));
   return r;
 }
 
-template <typename T>
+template <typename T, bool ONE>
 __device__ inline void add8(const DistillArgs &a, MaxSum &r, const float v[8]) {
   float m = r.m;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = fmaxf(m, v[i]);
-  float s = r.s * expz<T>(a, r.m - m);
+  float s = r.s * expz<T>(a, above<ONE>(a, r.m, m));
 #pragma unroll
-  for (int i = 0; i < 8; ++i) s += expz<T>(a, v[i] - m);
+  for (int i = 0; i < 8; ++i) s += expz<T>(a, above<ONE>(a, v[i], m));
   r.m = m;
   r.s = s;
 }
@@ -103,7 +112,7 @@ __device__ inline float logit(const DistillArgs &a, const T *z, int64_t col) {
 }
 
 // Joins over the workgroup in a fixed order; every thread gets the result.
-template <typename T, int NT>
+template <typename T, bool ONE, int NT>
 __device__ inline MaxSum block_join(const DistillArgs &a, MaxSum r, MaxSum *lds) {
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
@@ -111,13 +120,13 @@ __device__ inline MaxSum block_join(const DistillArgs &a, MaxSum r, MaxSum *lds)
     o.m = __shfl_xor(r.m, d);
     o.s = __shfl_xor(r.s, d);
     // both sides join in the lower lane's order, so the lanes agree
-    r = (threadIdx.x & d) ? join<T>(a, o, r) : join<T>(a, r, o);
+    r = (threadIdx.x & d) ? join<T, ONE>(a, o, r) : join<T, ONE>(a, r, o);
   }
   if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = r;
   __syncthreads();
   r = lds[0];
 #pragma unroll
-  for (int w = 1; w < NT / 64; ++w) r = join<T>(a, r, lds[w]);
+  for (int w = 1; w < NT / 64; ++w) r = join<T, ONE>(a, r, lds[w]);
   return r;
 }
 
@@ -200,7 +209,7 @@ __device__ inline void teacher(const DistillArgs &a, int64_t row, const T *z, co
     top = wave_max(top);
     double sum = 0.0;
     for (int i = threadIdx.x; i < a.k; i += 64) {
-      const float e = expz<float>(a, ee[i] - top);
+      const float e = expz<float>(a, above<ONE>(a, ee[i], top));
       ee[i] = e;
       sum += (double)e;
     }
@@ -251,23 +260,23 @@ __device__ inline void row_loss(const DistillArgs &a, int64_t row, const MaxSum 
 
 // The gradient at the teacher's entries of columns [lo, hi): written over what the pass over the row
 // left there.
-template <typename T, int NT>
+template <typename T, bool ONE, int NT>
 __device__ inline void entries(const DistillArgs &a, T *dz, const MaxSum &st, float inv_s, float inv_p, float coef, int lo,
                                int hi) {
   ENTRIES;
   for (int i = threadIdx.x; i < a.k; i += NT) {
     const int id = eid[i];
     if (id < lo || id >= hi) continue;
-    const float q = expz<T>(a, ez[i] - st.m) * inv_s;
+    const float q = expz<T>(a, above<ONE>(a, ez[i], st.m)) * inv_s;
     dz[id] = (T)(coef * (q - eall[i] * inv_p));
   }
 }
 
-template <typename T>
+template <typename T, bool ONE>
 __device__ inline Raw8<T> grad8(const DistillArgs &a, const float v[8], float m, float f) {
   Raw8<T> r;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) r.v[i] = (T)(expz<T>(a, v[i] - m) * f);
+  for (int i = 0; i < 8; ++i) r.v[i] = (T)(expz<T>(a, above<ONE>(a, v[i], m)) * f);
   return r;
 }
 
@@ -342,10 +351,10 @@ __global__ __launch_bounds__(NT, OCC) void distill_row_kernel(DistillArgs a) {
 #pragma unroll
         for (int u = 0; u < FLY; ++u) logits8<T, ONE>(a, z, col + u * NT * 8, v[u]);
 #pragma unroll
-        for (int u = 0; u < FLY; ++u) add8<T>(a, st, v[u]);
+        for (int u = 0; u < FLY; ++u) add8<T, ONE>(a, st, v[u]);
       }
     }
-    st = block_join<T, NT>(a, st, sh.join);
+    st = block_join<T, ONE, NT>(a, st, sh.join);
   }
   if constexpr (GRAD) {
     T *dz = reinterpret_cast<T *>(a.dz) + row * a.vocab;
@@ -362,7 +371,7 @@ __global__ __launch_bounds__(NT, OCC) void distill_row_kernel(DistillArgs a) {
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = (float)keep[c].v[i];
-            const Raw8<T> r = grad8<T>(a, v, st.m, coef * inv_s);
+            const Raw8<T> r = grad8<T, ONE>(a, v, st.m, coef * inv_s);
             __builtin_memcpy(dz + begin(c), &r, sizeof(r));
           }
       } else {
@@ -373,12 +382,12 @@ __global__ __launch_bounds__(NT, OCC) void distill_row_kernel(DistillArgs a) {
 #pragma unroll
           for (int u = 0; u < FLY; ++u) {
             const int64_t at = col + u * NT * 8;
-            store8_tail(dz + at, grad8<T>(a, v[u], st.m, coef * inv_s), a.vocab - at);
+            store8_tail(dz + at, grad8<T, ONE>(a, v[u], st.m, coef * inv_s), a.vocab - at);
           }
         }
       }
       __syncthreads();  // the pass's stores come before the entries'
-      entries<T, NT>(a, dz, st, inv_s, (float)(1.0 / sh.sum), coef, 0, a.vocab);
+      entries<T, ONE, NT>(a, dz, st, inv_s, (float)(1.0 / sh.sum), coef, 0, a.vocab);
     }
   }
   if (threadIdx.x < 64) {
@@ -398,9 +407,9 @@ __global__ __launch_bounds__(256) void distill_partial_kernel(DistillArgs a) {
   for (int c = 0; c < CHUNK / 2048; ++c) {
     float v[8];
     logits8<T, ONE>(a, z, lo + c * 2048 + threadIdx.x * 8, v);
-    add8<T>(a, st, v);
+    add8<T, ONE>(a, st, v);
   }
-  st = block_join<T, 256>(a, st, lds);
+  st = block_join<T, ONE, 256>(a, st, lds);
   if (threadIdx.x == 0) a.partial[row * a.chunks + blockIdx.x] = {st.m, st.s};
 }
 
@@ -420,9 +429,9 @@ __global__ __launch_bounds__(256) void distill_finish_kernel(DistillArgs a) {
   } else {
     for (int c = threadIdx.x; c < a.chunks; c += 256) {
       const f32x2 p = a.partial[row * a.chunks + c];
-      st = join<T>(a, st, MaxSum{p[0], p[1]});
+      st = join<T, ONE>(a, st, MaxSum{p[0], p[1]});
     }
-    st = block_join<T, 256>(a, st, sh.join);
+    st = block_join<T, ONE, 256>(a, st, sh.join);
   }
   if constexpr (GRAD) {
     T *dz = reinterpret_cast<T *>(a.dz) + row * a.vocab;
@@ -437,14 +446,14 @@ __global__ __launch_bounds__(256) void distill_finish_kernel(DistillArgs a) {
       if (!none) {
         float v[8];
         logits8<T, ONE>(a, z, col, v);
-        r = grad8<T>(a, v, st.m, coef * inv_s);
+        r = grad8<T, ONE>(a, v, st.m, coef * inv_s);
       }
       store8_tail(dz + col, r, a.vocab - col);
     }
     if (!none) {
       __syncthreads();
       const int64_t hi = lo + CHUNK < a.vocab ? lo + CHUNK : a.vocab;
-      entries<T, 256>(a, dz, st, inv_s, (float)(1.0 / sh.sum), coef, (int)lo, (int)hi);
+      entries<T, ONE, 256>(a, dz, st, inv_s, (float)(1.0 / sh.sum), coef, (int)lo, (int)hi);
     }
   }
   if (blockIdx.x == 0 && threadIdx.x < 64) {
@@ -534,13 +543,14 @@ hipError_t launch_distill(int dtype, int nc, int64_t rows, int64_t vocab, int64_
   a.nc = nc;
   a.chunks = (int)((vocab + CHUNK - 1) / CHUNK);
   a.temperature = (float)temperature;
-  const double c = 1.4426950408889634 / (double)a.temperature;
+  a.scale = a.temperature < 0x1p64f ? 1.0f : 0x1p-64f;
+  const double c = 1.4426950408889634 / (double)(a.temperature * a.scale);
   a.c_hi = (float)c;
   if ((double)a.c_hi > c) a.c_hi = nextafterf(a.c_hi, 0.0f);
   a.c_lo = fmaxf((float)(c - (double)a.c_hi), FLT_MIN);
   const auto go = [&](auto zero) {
     using T = decltype(zero);
-    if (nc == 1) return dz ? run<T, true, true>(a, stream) : run<T, true, false>(a, stream);
+    if (nc == 1 && a.scale == 1.0f) return dz ? run<T, true, true>(a, stream) : run<T, true, false>(a, stream);
     return dz ? run<T, false, true>(a, stream) : run<T, false, false>(a, stream);
   };
   if (dtype == LM_F16) return go((_Float16)0.0f);
