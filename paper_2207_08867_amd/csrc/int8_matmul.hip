@@ -35,10 +35,11 @@ __device__ inline void store4(const Int8Args &a, int64_t m, int64_t n, i32x4 v, 
 
 // Up to 16 MT rows of A.  A workgroup owns 16 rows of B and its NW wavefronts share the reduction by groups
 // of 128 bytes, two 16 x 16 x 64 products each; their sums are joined through LDS.  B is read once, straight into
-// registers, all of its groups asked for ahead of use where the row has 4096 elements or fewer; what bounds the small
-// sizes is the latency of a launch and of those loads (8 rows by 4096 x 4096: 6.9 us, 2.4 TB/s), the large ones the memory
-// (one row by 32768 x 4096: 26.5 us, 5.1 TB/s).  4, 8 and 16 wavefronts with 2 to 8 groups ahead measured the same
-// within 5%.
+// registers, U groups a wavefront asked for together, which are 4096 elements of a row (2048 past 16 rows of A); what
+// those leave of a row goes a group at a time, each waited for.  What bounds the small sizes is the latency of a launch
+// and of those loads (8 rows by 4096 x 1024, 2048, 4096, 5120 and 8192: 4.2, 5.0, 6.8, 7.2 and 10.4 us, 2.4 TB/s at
+// 4096), the large ones the memory (one row by 32768 x 4096: 26.5 us, 5.1 TB/s).  4, 8 and 16 wavefronts with 2 to 8
+// groups ahead measured the same within 5%.
 template <typename T, int MT, int NW, int U>
 __global__ __launch_bounds__(64 * NW) void int8_thin_kernel(Int8Args a) {
   __shared__ i32x4 part[NW][MT][64];
@@ -90,8 +91,7 @@ __global__ __launch_bounds__(64 * NW) void int8_thin_kernel(Int8Args a) {
 }
 
 // One or two rows of a plain x quantised on the way: the wavefronts ask for their first U groups of B, then all quantise
-// x (every workgroup the same) into LDS, from which the products take it.  One launch in place of two (us, in a graph; one
-// row by 4096 x 4096): 7.4 and 9.8; two rows 8.8 and 10.9, four 11.2 and 10.5.
+// x (every workgroup the same) into LDS, from which the products take it.
 constexpr int TOKEN_BYTES = 32768;
 template <typename T, int NW, int U>
 __global__ __launch_bounds__(64 * NW) void int8_token_kernel(Int8Args a, const T *x, int64_t K) {
@@ -174,9 +174,11 @@ __global__ __launch_bounds__(64 * NW) void int8_token_kernel(Int8Args a, const T
 }
 
 // Few rows read B straight into registers; tiles read it through LDS and do not read A again for every 16 rows of B,
-// which costs more the larger B is.  Straight and by tiles (us, launches in a graph; rows of A, B): 8, 14336 x 4096 16.0
-// and 13.8, 32768 x 4096 30.8 and 33.6; 16, 4096 x 4096 7.5 and 10.3, 8192 x 4096 11.1 and 11.8, 14336 x 4096
-// 18.2 and 14.1; 32, 4096 x 4096 9.6 and 11.3, 8192 x 4096 15.0 and 12.1, 32768 x 4096 55.9 and 33.7.
+// which costs more the larger B is.  Straight and by tiles (us, launches in a graph; rows of A, B): 4, 14336 x 4096 14.6
+// and 19.6, 32768 x 4096 28.2 and 34.5; 8, 8192 x 4096 9.9 and 11.5, 14336 x 4096 16.3 and 13.8, 4096 x 16384 18.1 and
+// 16.0, 24576 x 4096 24.3 and 29.2, 32768 x 4096 30.8 and 33.6, 131072 x 1024 31.4 and 37.4 (straight loses at 56 to 64
+// MiB alone); 16, 4096 x 4096 7.5 and 10.3, 8192 x 4096 11.1 and 11.8, 14336 x 4096 18.2 and 14.1; 32, 4096 x 4096
+// 9.6 and 11.3, 8192 x 4096 15.0 and 12.1, 32768 x 4096 55.9 and 33.7.
 bool thin(int64_t M, int64_t N, int64_t P) {
   const int64_t mib = N * P >> 20;
   return M <= 8 || (M <= 16 && mib < 48) || (M <= 32 && mib < 24);
@@ -210,7 +212,16 @@ hipError_t run(const Int8Args &a, void *ws, hipStream_t stream) {
 
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
-bool token(int64_t batch, int64_t in) { return batch <= 2 && in > 0 && batch * int8_pitch(in) <= TOKEN_BYTES; }
+// One launch, in which every workgroup quantises x, in place of two.  Past two workgroups a CU, 8192 outputs, their
+// quantisations follow one another; they pay where each has 64 KiB of weights or more to read beside it.  One launch
+// and two (us, in a graph, bfloat16; in -> out), one row: 4096 -> 4096 7.4 and 9.8, 1024 -> 8192 7.2 and 7.2, 1024 ->
+// 16384 12.6 and 9.4, 1024 -> 131072 85 and 29, 4096 -> 16384 16.0 and 17.6, 4096 -> 32768 29.7 and 31.1, 4096 -> 65536
+// 53.8 and 53.0, 32768 -> 1024 26.6 and 30.5; two rows: 1024 -> 4096 6.7 and 6.8, 1024 -> 8192 8.9 and 7.2, 4096 ->
+// 8192 11.8 and 12.7, 4096 -> 16384 19.5 and 17.9, 4096 -> 32768 38.2 and 30.9; four rows 4096 -> 4096 11.2 and 10.5.
+bool token(int64_t batch, int64_t in, int64_t out) {
+  if (batch > 2 || in == 0 || batch * int8_pitch(in) > TOKEN_BYTES) return false;
+  return out <= (in < 4096 ? 8192 / batch : (batch == 1 ? 32768 : 8192));
+}
 
 template <typename T>
 hipError_t run_token(const Int8Args &a, const void *x, int64_t K, hipStream_t stream) {
@@ -244,13 +255,13 @@ hipError_t launch_int8_matmul(int dtype, int64_t M, int64_t N, int64_t K, const 
 
 // x in 8 bits: codes, then scales, then the product's partial sums.
 int64_t int8_linear_workspace_bytes(int64_t batch, int64_t in, int64_t out) {
-  if (token(batch, in)) return 0;
+  if (token(batch, in, out)) return 0;
   return batch * int8_pitch(in) + up16(4 * batch) + int8_matmul_workspace_bytes(batch, out, in);
 }
 
 hipError_t launch_int8_linear(int dtype, int64_t batch, int64_t in, int64_t out, const void *x, const void *codes,
                               const void *scales, const void *bias, void *ws, void *y, hipStream_t stream) {
-  if (token(batch, in)) {
+  if (token(batch, in, out)) {
     Int8Args a = {};
     a.b = (const char *)codes;
     a.sb = (const float *)scales;
