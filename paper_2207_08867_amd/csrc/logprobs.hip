@@ -390,9 +390,10 @@ __device__ inline void select_logits(Select &sh, Pool<CH, H> &pool, int k, const
   __syncthreads();
   int n = sh.n;
   if (n > KEEP) {
-    // Many equal logits at the bound, or a row whose order follows the threads'.  The k-th largest logit by
-    // bisection over all of them; the larger ones, fewer than k, and the first of those equal to it.  The row is read
-    // again, so that it need not stay in registers behind the rest.
+    // Many equal logits at the bound, or a row whose order follows the threads'.  The k-th largest logit is the bound if
+    // fewer than k are larger, as a rule where many are equal, or comes of a bisection over all of them; then the
+    // larger ones, fewer than k, and the first of those equal to it.  The row is read again, up to 36 times, so
+    // that it need not stay in registers behind the rest.
     const uint32_t mine0 = first + threadIdx.x * 8;
     const auto count = [&](auto test) {
       int n = 0;
@@ -404,11 +405,13 @@ __device__ inline void select_logits(Select &sh, Pool<CH, H> &pool, int k, const
       }
       return n;
     };
-    const uint32_t e = bound_of<uint32_t>(k, k, [&](uint32_t b) {
-      const float least = ordered_value(b < lowest ? lowest : b);
-      return waves_sum<NT>(sh, count([&](float x) { return x >= least; }));
-    });
-    bound = ordered_value(e < lowest ? lowest : e);
+    if (waves_sum<NT>(sh, count([&](float x) { return x > bound; })) >= k) {
+      const uint32_t e = bound_of<uint32_t>(k, k, [&](uint32_t b) {
+        const float least = ordered_value(b < lowest ? lowest : b);
+        return waves_sum<NT>(sh, count([&](float x) { return x >= least; }));
+      });
+      bound = ordered_value(e < lowest ? lowest : e);
+    }
     __syncthreads();
     if (threadIdx.x == 0) sh.n = 0;
     __syncthreads();
