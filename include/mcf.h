@@ -456,7 +456,7 @@ int64_t mc_mx4_linear_bwd_workspace(int dtype, int nc, int64_t batch, int64_t in
  * z: plain [rows][vocab], or (nc > 1) an MC value [nc][rows][vocab] whose planes are summed
  *   in binary32, the last one first; its gradient is plain, that of the sum (Section 2.1).
  * ids: int32 [rows][k]; t: [rows][k] in z's format; 0 <= k <= 1024 (may be NULL for k = 0).
- * temperature: positive and finite.  loss: binary32 [rows].
+ * temperature: finite and above 2^-127, as a binary32 number.  loss: binary32 [rows], which has T^2.
  * stats: binary32 [rows][2], the row's largest logit m and sum_j exp((z_j - m) / T).
  * g: binary32 [rows], or NULL for ones.  dz: [rows][vocab] in z's format.
  * No output may overlap an input or another output.  rows < 2^31, 1 <= vocab <= 2^30. */
@@ -527,7 +527,9 @@ int64_t mc_int8_linear_fwd_workspace(int dtype, int64_t batch, int64_t in, int64
  * h: [nc][rows][n] (a plain stream: nc = 1); x: [rows][n] or NULL; w: [n] or NULL for ones; h_out:
  * [nc][rows][n], may be h itself (in place); y: [rows][n].  Everything between the loads and the
  * roundings is binary64, but that y of a plain 16-bit stream is rounded from a binary32 number
- * within 2^-23 of v_i w_i r.  A row's result does not depend on the other rows.  A row of zeros with eps = 0 has r = inf and so NaN.  n >= 1, eps >= 0 and finite. */
+ * within 2^-23 of v_i w_i r, relative to it, or within 2^-140 where v_i w_i is below 2^-126.  A row's
+ * result does not depend on the other rows.  A row of zeros with eps = 0 has r = inf and so NaN.
+ * n >= 1, eps >= 0 and finite. */
 int mc_rmsnorm_fwd(int dtype, int nc, int64_t rows, int64_t n, const void *h, const void *x, const void *w, double eps,
                    void *h_out, void *y, void *stream);
 
@@ -561,8 +563,9 @@ int64_t mc_rmsnorm_bwd_workspace(int dtype, int64_t rows, int64_t n);
  * z: plain [rows][vocab], or (nc > 1) an MC value [nc][rows][vocab] whose planes are summed in
  *   binary32, the last one first; its gradient is plain, that of the sum (Section 2.1).
  * ids: int32 [rows][given], 0 <= given <= 1024, in any order, also equal ones.
- * temperature: finite and above 2^-127, as a binary32 number.  At a very small one the entropy has terms near binary32's
- *   smallest numbers, and so an error of up to vocab 2^-149 / temperature beside that of its roundings.
+ * temperature: finite and above 2^-127, as a binary32 number.  At a very small one the entropy has
+ *   terms near binary32's smallest numbers, and so an error of up to vocab 2^-149 / temperature beside
+ *   that of its roundings.
  * logp: binary32 [rows][given]; entropy: binary32 [rows] or NULL; top_ids: int32 and top_logp:
  *   binary32 [rows][top], 0 <= top <= 128.
  * stats: binary32 [rows][3] or NULL, for the gradient: the row's largest logit m, L = log sum_j

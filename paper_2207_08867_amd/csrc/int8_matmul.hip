@@ -275,7 +275,8 @@ hipError_t launch_int8_linear(int dtype, int64_t batch, int64_t in, int64_t out,
     return run_token<float>(a, x, in, stream);
   }
   char *const xc = (char *)ws, *const xs = xc + batch * int8_pitch(in), *const rest = xs + up16(4 * batch);
-  const hipError_t e = launch_rmsnorm(dtype, 1, batch, in, x, nullptr, nullptr, 0.0, nullptr, nullptr, xc, xs, false, stream);
+  const hipError_t e =
+      launch_rmsnorm(dtype, 1, batch, in, x, nullptr, nullptr, 0.0, nullptr, nullptr, xc, xs, false, stream);
   if (e != hipSuccess) return e;
   return launch_int8_matmul(dtype, batch, out, in, xc, xs, codes, scales, bias, rest, y, stream);
 }

@@ -12,13 +12,16 @@
 //
 // Sums are binary32, in an order that depends on the sizes (rows and vocabulary) alone.  From a temperature of 2^64 up
 // differences are taken of logits times 2^-64, with T 2^-64 in T's place, so that neither a difference of the format's
-// whole range nor a row's sum of them passes binary32's range; what that rounds away is below 2^-126 of T.  The kernels of MC
-// logits alone do so, and take plain rows then too, of one plane: in the others it cost bfloat16 rows 1 to 2% of a call.
+// whole range nor a row's sum of them passes binary32's range; what that rounds away is below 2^-126 of T.  The kernels
+// of MC logits alone do so, and take plain rows then too, of one plane: in the others it cost bfloat16 rows 1 to 2% of
+// a call.
 //
 // A row is read once, and the gradient reads it again and writes as much, so HBM bounds the large calls: 4096 rows of
 // 32768 bfloat16 logits (268 MB) 54 to 61 us, 4.4 to 5.0 TB/s, the gradient 108 us, 5.0 TB/s; binary32 97 and 195 us,
 // 5.5 TB/s.  The alternatives are found where the row is held: 66 us with 20, 73 with 64, 123 with 128.
-// Calls of few rows are launches and waits: one row of 131071 binary32 logits 7.4 us, 13.8 with 20 alternatives.
+// Calls of few rows are launches and waits: one row of 131071 binary32 logits 7.4 us, 13.8 with 20 alternatives.  Two
+// planes: 2048 rows of 32768 binary16 70 us, 90 with 20 alternatives, the gradient 89, 4.5 TB/s; of binary32 98, 117
+// and 150.
 #include <float.h>
 #include <math.h>
 
@@ -258,8 +261,8 @@ __device__ inline float logit(const LogpArgs &a, const T *z, int64_t j) {
   return v;
 }
 
-// CH pieces of 8 logits of a row, piece c from column lo + 8 (c NT + t) of thread t, as they are held: plain ones in their
-// format.  Past the row they are -inf.
+// CH pieces of 8 logits of a row, piece c from column lo + 8 (c NT + t) of thread t, as they are held: plain ones in
+// their format.  Past the row they are -inf.
 template <typename T, bool ONE, int NT, int CH>
 __device__ inline void logits(const LogpArgs &a, const T *z, int lo, Raw8<std::conditional_t<ONE, T, float>> (&v)[CH]) {
   using H = std::conditional_t<ONE, T, float>;
@@ -459,8 +462,8 @@ __device__ inline void select_logits(Select &sh, Pool<CH, H> &pool, int k, const
   rank_kept<NT>(sh, k, n, out);
 }
 
-// A value that all lanes have, in a scalar register: the scaled one takes the vector register (80 in place of 81 of MC rows
-// in eight pieces, which is a workgroup more on a CU: 2048 x 32000 of two binary16 planes 72 us, 76 without).
+// A value that all lanes have, in a scalar register: the scaled one takes the vector register (80 in place of 81 of MC
+// rows in eight pieces, which is a workgroup more on a CU: 2048 x 32000 of two binary16 planes 72 us, 76 without).
 __device__ inline float scalar(float v) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, v)));
 }
@@ -615,14 +618,16 @@ __global__ __launch_bounds__(256) void logp_join_kernel(LogpArgs a) {
   if ((int)threadIdx.x < a.given)
     a.logp[row * a.given + threadIdx.x] = id >= 0 && id < a.vocab ? log_prob(a, r, given) : 0.0f;
   finish<T, ONE, 256>(a, row, r, z, 256, threadIdx.x);
-  if constexpr (TOP) select_keys<256>(sel, a.top, keys, n, held, [&](int i, uint64_t key) { put_top(a, row, r, i, key); });
+  if constexpr (TOP)
+    select_keys<256>(sel, a.top, keys, n, held, [&](int i, uint64_t key) { put_top(a, row, r, i, key); });
 }
 
 // How a row is cut into chunks of `pieces` pieces of 8 logits for each of the threads.  A row is one workgroup's while
 // it fits 8 pieces of 512 threads, else it is cut into chunks alike, or, where there would be few of them, of 4096
 // logits.  The pieces follow the length, as lanes past a row's end cost as much as others (8184 x 8200 binary32 with 64
-// alternatives in three pieces 97 us, in four 141).  One workgroup and chunks of 4096 (us, in a graph): 1 x 32000 with 20 alternatives 12.0 and 15.3, 128 x
-// 32768 8.1 and 11.0; chunks of 32768 and of 4096: 1 x 131072 11.5 and 9.0, 64 x 131072 the same within 3%.
+// alternatives in three pieces 97 us, in four 141).  One workgroup and chunks of 4096 (us, in a graph): 1 x 32000 with
+// 20 alternatives 12.0 and 15.3, 128 x 32768 8.1 and 11.0; chunks of 32768 and of 4096: 1 x 131072 11.5 and 9.0, 64 x
+// 131072 the same within 3%.
 constexpr int MANY = 128;
 struct Cut {
   int threads, pieces, chunks;
@@ -693,7 +698,8 @@ extern __shared__ Given given_space[];
 
 // A workgroup takes 8 CH NT logits of a row.  FEW: few given tokens, for which every piece of 8 logits looks;
 // else they are written over what the pass left there.  HBM bounds it: 4096 x 32768 bfloat16 108 us, 5.0 TB/s, where a
-// large copy reaches 5.1.
+// large copy reaches 5.1; from a few dozen tokens a row on, their search for equal ids, each through all: with 8 tokens
+// 111 us, 64 122, 256 211, 1024 2170 (8192 x 1000 17, 23, 99, 1128).
 template <typename T, bool ONE, int NT, int CH, bool FEW>
 __global__ __launch_bounds__(NT) void logp_bwd_kernel(LogpArgs a) {
   Given *const given = given_space;

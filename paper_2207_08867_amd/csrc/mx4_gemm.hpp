@@ -27,8 +27,8 @@
 // the clock at 1.7 to 2.0 GHz; under it a loop of the scaled instruction alone reaches 6.55 PFLOP/s.
 // 8192^3 FP4 262 to 272 us, 4.1 PFLOP/s; 4096^3 MIX 102 us, 1.34 PFLOP/s, where a library product of
 // plain bfloat16 takes 98; 4096^3 MIXH 107 us, 5 of them the pass over the scales.  I8: the power limit, 66% busy at
-// 1.8 GHz; 8192^3 438 to 450 us, 2.45 to 2.5 POP/s, as a library product of 8-bit integers (440 to 449), and 358 us on
-// zeros, 4096^3 62 us.  Grids of about 256
+// 1.8 GHz; 8192^3 438 to 479 us from card to card, 2.3 to 2.5 POP/s, 0 to 4% behind a library product of 8-bit integers
+// on the same card (440 to 451), and 358 us on zeros, 4096^3 62 to 64 us.  Grids of about 256
 // small tiles: a step takes 0.36 to 0.6 us whatever it multiplies, its loads' and reads' latency
 // (4096 x 4096 by 256 rows: MIX 22 us, FP4 12, where bytes and operations need 6 and 2).
 #pragma once

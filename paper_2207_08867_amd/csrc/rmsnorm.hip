@@ -126,7 +126,10 @@ __device__ inline void stream8(const NormArgs &a, int64_t at, int64_t col, doubl
   for (int c = (ONE ? 1 : 4) - 1; c >= 0; --c) {
     if (c >= nc) continue;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) total[i] = c == nc - 1 ? (double)(float)part[c].v[i] : total[i] + (double)(float)part[c].v[i];
+    for (int i = 0; i < 8; ++i) {
+      const double q = (double)(float)part[c].v[i];
+      total[i] = c == nc - 1 ? q : total[i] + q;
+    }
   }
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = total[i];
@@ -228,9 +231,11 @@ __global__ __launch_bounds__(NT <= 64 ? 256 : NT) void norm_kernel(NormArgs a) {
 
 // The same of plain 16-bit rows, with binary32 between the loads and the roundings where that is exact or enough: v
 // and, in its range, p = v w are exact there, and their squares are summed in binary64.  Rows whose m lies near the
-// ends of binary32's range, and outputs whose r or p do, take the binary64 forms.  All of a row's loads go out before
-// the first is looked at, eight wavefronts a SIMD.  HBM bounds it: 8192 x 4096 bfloat16 with x 50 us, 5.4 TB/s, into 8 bits
-// 49 us, 4.8, quantisation alone 23 us, 4.3 (binary64 between loads and roundings: 4096 x 4096 into 8 bits 45 us, 29 so).
+// ends of binary32's range, and outputs past it or whose r is far from one, take the binary64 forms; a p below binary32's
+// normal numbers is off by 2^-150, which r <= 2^10 leaves below 2^-140.  All of a row's loads go out before
+// the first is looked at, eight wavefronts a SIMD.  HBM bounds it: 8192 x 4096 bfloat16 with x 50 us, 5.4 TB/s, into 8
+// bits 49 us, 4.8, quantisation alone 23 us, 4.3 (binary64 between loads and roundings: 4096 x 4096 into 8 bits 45 us,
+// 29 so).
 template <typename T, int NT, int CH, bool NORM, bool INT8, bool EVEN, int OCC>
 __global__ __launch_bounds__(NT <= 64 ? 256 : NT, OCC) void norm16_kernel(NormArgs a) {
   constexpr int BLOCK = NT <= 64 ? 256 : NT;
@@ -413,9 +418,9 @@ hipError_t run_norm(NormArgs a, hipStream_t stream) {
   }
 }
 
-// code scale, a thread READ pieces of 8 elements, 256 pieces apart.  HBM bounds it: 4096 x 8192 to bfloat16 21 us, 4.8
-// TB/s, where a large copy reaches 5.1.  Two, four and eight pieces a thread: 27.6, 28.7, 29.7; codes that the norm has just
-// written, still in a cache, take the same within 1% either way.  (Written without the arrays 25 us.)
+// code scale, a thread READ pieces of 8 elements, 256 pieces apart.  HBM bounds it: 4096 x 8192 to bfloat16 20 to 21
+// us, 4.8 TB/s, where a large copy reaches 5.1.  Two, four and eight pieces a thread: 27.6, 28.7, 29.7; codes that the
+// norm has just written, still in a cache, take the same within 1% either way.  (Written without the arrays 25 us.)
 constexpr int READ = 1;
 template <typename T>
 __global__ __launch_bounds__(256) void int8_read_kernel(const uint64_t *codes, const float *scales, T *out, int64_t rows,
@@ -490,7 +495,10 @@ struct BwdRow {
 //
 // HBM and binary64 arithmetic bound it alike: 8192 x 4096 bfloat16 with g 60 us and 5 us for the sum over workgroups,
 // 4.0 TB/s; 43 vector instructions an element, 60% of the cycles; binary32 4096 x 4096
-// 56 us, 4.8 TB/s.  Without the next row's loads ahead 95 us, 67 so.
+// 56 us, 4.8 TB/s.  Without the next row's loads ahead 95 us, 67 so.  Two pieces a thread, rows past 8192 elements, hold
+// 20 to 56 registers too many and keep them in 52 to 168 bytes of scratch memory a lane, plain 16-bit rows of whole
+// pieces apart: 2048 x 16384 bfloat16 73 us (no scratch), binary32 147, 3.7 TB/s, two planes of either 109 and 188
+// without g, 2048 x 12001 97 and 148.
 template <typename T, bool ONE, int NT, int CH, End E>
 __global__ __launch_bounds__(NT <= 64 ? 256 : NT, 4) void norm_bwd_kernel(NormBwdArgs a) {
   constexpr int BLOCK = NT <= 64 ? 256 : NT, SLOTS = BLOCK / NT;
@@ -697,9 +705,9 @@ constexpr int64_t BWD_LONG = 16384;  // the longest row that stays in registers
 
 // Workgroups: as many as are resident, since a row's loads go out ahead of the row before: one a CU of rows that
 // take 1024 threads, two of 512, four of 256, eight of 128 (16-bit rows: 32263 x 520 62 us, with 256 threads 75; binary32
-// 71 and 67); four where a workgroup has several rows.  With twice (half) as many (us; 4096 x 4096 bfloat16, with g) 46 (49)
-// in place of 40, 8192 x 1024 32 (33) in place of 26, 4096 x 8192 78 in place of 69.  Of rows that do not stay in
-// registers, parts of the rows for dw.
+// 71 and 67); four where a workgroup has several rows.  With twice (half) as many (us; 4096 x 4096 bfloat16, with g)
+// 46 (49) in place of 40, 8192 x 1024 32 (33) in place of 26, 4096 x 8192 78 in place of 69.  Of rows that do not stay
+// in registers, parts of the rows for dw.
 int bwd_groups(int dtype, int64_t rows, int64_t n) {
   if (n > BWD_LONG) return (int)(rows < 64 ? rows : 64);
   const int64_t slots = n <= 128 ? 16 : (n <= 256 ? 8 : (n <= 512 ? 4 : 1));
