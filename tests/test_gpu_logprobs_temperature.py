@@ -26,10 +26,18 @@ def logits(seed, rows, V, T, dtype):
 @pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
 @pytest.mark.parametrize("T", [2.0 ** 63, 2.0 ** 64, 2.0 ** 65, 1e30, 1e33, 1e36, 1e37, 1e38, 3.4028e38])
 @pytest.mark.parametrize("rows, V, given, k", [(2, 3, 1, 3), (3, 300, 3, 9), (2, 1000, 12, 5), (2, 9000, 2, 20),
-                                               (3, 40001, 1, 20), (260, 33001, 9, 0)])
+                                               (3, 40001, 1, 20)])
 def test_large(mcf, dtype, T, rows, V, given, k):  # noqa: F811
-    if rows > 3 and T not in (2.0 ** 64, 1e38):
-        pytest.skip("large rows at two temperatures")
+    both(mcf, dtype, T, rows, V, given, k)
+
+
+@pytest.mark.parametrize("dtype", ["bfloat16", "float32"])
+@pytest.mark.parametrize("T", [2.0 ** 64, 1e38])
+def test_many_long_rows(mcf, dtype, T):  # noqa: F811
+    both(mcf, dtype, T, 260, 33001, 9, 0)
+
+
+def both(mcf, dtype, T, rows, V, given, k):  # noqa: F811
     T = float(np.float32(T))
     z, g = logits(rows + V, rows, V, T, dtype)
     ids = g.integers(0, V, size=(rows, given))
